@@ -280,6 +280,115 @@ int adacluster_quest_scores(int32_t H, int32_t Lq, int32_t Lk, int32_t d, int32_
                             const void* Q, const void* R_pos, const void* R_neg, float* S, void* stream);
 
 /*
+ * Attention over pages of keys: the sparse attention of this library with pages of consecutive positions in the place of
+ * clusters, scored by Eq. 1 (Sec. 3.2.3) on every page's per-dimension box, for language models and autoregressive video:
+ * shared heads of keys, causal order, ragged batches, a paged cache in 16, 32 or 4 bits, and gradients.
+ *
+ *   Positions   Sequence b has the queries cu_q[b] .. cu_q[b+1]-1 (rows of q) and n_b keys; its LAST query is at the position of
+ *               its LAST key (query i of nq is at n_b - nq + i), so a chunk of a prompt, a single new token and a whole
+ *               sequence are the same call.  A query at a position below 0 sees nothing.
+ *   Keys        paged (num_pages > 0): position t of sequence b lies in page page_table[b][t / page] of the pool, at t % page,
+ *               and n_b = seq_lens[b]; or packed (num_pages == 0): rows cu_k[b] .. cu_k[b+1]-1 of k and v.
+ *               Query head h reads the head h / (Hq / Hkv) of keys.
+ *   Blocks      `qblock` consecutive queries of a sequence (counted from its first query of the call) and the query heads of one
+ *               head of keys share a list of pages.  nb = ceil(max_q / qblock) records a sequence.
+ *   Lists       sel_idx [B][nb][Hkv][topk]: pages in ascending order, -1 behind the end.  An entry that names no page of the
+ *               sequence or is not above the entry before it counts as -1.  A block attends to the keys of its pages that
+ *               exist (below n_b) and, if causal, are not behind the query.  sel_idx NULL: all pages.
+ *   Empty rows  A query with no key of score above -inf has output 0 and lse -inf.  What lies in a page behind a sequence's last
+ *               key is not looked at.  Within what a block lists, a value that is an infinity or a NaN reaches the rows it is
+ *               masked for inside its own 32 keys.
+ *   Device data is not trusted for addresses: lengths are held to max_pages * page and to the buffers, a page_table entry
+ *               outside [0, num_pages) names no keys, cu_q and cu_k are held to [0, q_rows] and [0, k_rows].  Queries of a
+ *               sequence past max_q are left out.  Rows of o, lse, dq (dk, dv) that belong to no sequence are left as they were.
+ *   Layout      q, o, d_o, dq: row t, head h at t * stride[0] + h * stride[1] (elements), d contiguous; packed k, v, dk, dv
+ *               the same; the pool: page g, token t, head h at g * stride[0] + t * stride[1] + h * stride[2] (packed keys:
+ *               stride[0] is not used).  Bases and strides must be multiples of 16 bytes.  lse is fp32 [q_rows][Hq].
+ *   4 bits      (bits = 4; dtype stays that of q, o and new tokens.)  codes uint8 [num_pages][Hkv][page][d/2], dimension 2j in
+ *               the low half of byte j; meta [num_pages][Hkv][page][d/64] pairs of bfloat16 (step, lowest; step in the lower
+ *               half of the 32 bits).  A value is lowest + code * step; 64 dimensions share a pair: lowest = their minimum
+ *               rounded down, step = (maximum - lowest) * (1/15 as a float) rounded up, code = (x - lowest) / step rounded to nearest even.
+ *               A group with a NaN or an infinity, or whose span overflows, is held as NaN.
+ *   Boxes       [num_pages][Hkv][2][d] of a pool, [B][max_pages][Hkv][2][d] of packed keys, in dtype: maxima, then minima, over
+ *               the keys a page holds, as they were given (before 4 bits).  A NaN does not enter a box.
+ * All calls are asynchronous on `stream`, block no thread, allocate nothing and may be captured into a graph.  Unlike in the
+ * clustered calls the device that owns the tensors must be the current one, as for any launch.
+ */
+typedef struct adacluster_block_params {
+  int32_t B;                    /* sequences                                                     */
+  int32_t Hq, Hkv, d;           /* query heads, heads of keys (Hq % Hkv == 0), head width 64 or 128 */
+  int32_t dtype;                /* ADACLUSTER_F32 or ADACLUSTER_BF16                             */
+  int32_t bits;                 /* of cached keys and values: 0 as dtype, or 4                   */
+  int32_t page;                 /* tokens of a page: 16, 32, 64 or 128                           */
+  int32_t num_pages;            /* pages of the pool; 0: packed keys                             */
+  int32_t max_pages;            /* pages of a sequence at most; row length of page_table         */
+  int32_t max_q;                /* queries (new tokens) of a sequence at most                    */
+  int32_t qblock;               /* queries that share a list, 1 .. 1024                          */
+  int32_t causal;               /* 1: a query sees positions up to its own; 0: all               */
+  int32_t topk;                 /* entries of a list                                             */
+  int32_t keep_first;           /* pages from the start that every list holds                    */
+  int32_t q_rows, k_rows;       /* rows of q (new tokens), rows of packed k                      */
+  float   softmax_scale;        /* <= 0 means 1/sqrt(d)                                          */
+  int64_t q_stride[2], o_stride[2], k_stride[3], v_stride[3];
+  int64_t new_k_stride[2], new_v_stride[2];                           /* adacluster_cache_append */
+  int64_t do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2];     /* gradients               */
+} adacluster_block_params;
+
+#define ADACLUSTER_BLOCK_SELECT   0
+#define ADACLUSTER_BLOCK_ATTN     1
+#define ADACLUSTER_BLOCK_BACKWARD 2
+/* Bytes of workspace that one of these calls needs (host pointer out; may be 0, and ws NULL then). */
+int adacluster_block_workspace_bytes(const adacluster_block_params* p, int32_t call, size_t* bytes);
+
+/*
+ * New tokens into a cache: rows cu_new[b] .. cu_new[b+1]-1 of k and v [q_rows][Hkv][d] become positions seq_lens[b] .. of
+ * sequence b (seq_lens: tokens held BEFORE the call, which the caller then advances), and the boxes of the pages they go to take
+ * them in; a page that held none before starts its box anew.  Tokens past max_pages * page, or in a page that page_table
+ * does not name, are dropped.  A page that is written must belong to one sequence of the call (copy a shared one first).
+ */
+int adacluster_cache_append(const adacluster_block_params* p, const void* k, const void* v, const int32_t* cu_new,
+                            const int32_t* seq_lens, const int32_t* page_table, void* k_pool, void* v_pool,
+                            uint32_t* k_meta, uint32_t* v_meta, void* boxes, void* stream);
+
+/* The other way: positions first[b] .. first[b] + (cu_new[b+1] - cu_new[b]) - 1 of every sequence, as values in dtype, to rows
+ * cu_new[b] .. of k and v [q_rows][Hkv][d] (contiguous).  Tokens of a page that page_table does not name are zero; rows past
+ * max_pages * page are left as they were. */
+int adacluster_cache_read(const adacluster_block_params* p, const int32_t* cu_new, const int32_t* first, const int32_t* page_table,
+                          const void* k_pool, const void* v_pool, const uint32_t* k_meta, const uint32_t* v_meta,
+                          void* k, void* v, void* stream);
+
+/* Boxes of packed keys (num_pages == 0).  Pages past a sequence's last are zero. */
+int adacluster_block_boxes(const adacluster_block_params* p, const void* k, const int32_t* cu_k, void* boxes, void* stream);
+
+/*
+ * The pages of every block of queries.  With u_h the sum of the block's queries of head h,
+ *   S(h, p) = sum_d u_hd (u_hd >= 0 ? max_pd : min_pd)   (Eq. 1: the larger product; qblock 1: an upper bound on a page's logits),
+ * and a page's score is the largest over the query heads that share the keys.  Always listed: the pages of the block's own
+ * positions (causal) and the first keep_first ones; the others by score while there is room, a tie to the lower page.  If causal
+ * no page behind the block's last position is listed.  Scores are formed in fp64; one that is NaN counts as -inf.
+ * topk must hold keep_first + ceil((qblock - 1) / page) + 1 pages if causal, keep_first otherwise.
+ *   sel_idx [B][nb][Hkv][topk], sel_cnt [B][nb][Hkv] out, fully overwritten (blocks that have no query: count 0).
+ */
+int adacluster_block_select(const adacluster_block_params* p, const void* q, const int32_t* cu_q, const int32_t* cu_k,
+                            const int32_t* seq_lens, const int32_t* page_table, const void* boxes,
+                            int32_t* sel_idx, int32_t* sel_cnt, void* ws, size_t ws_bytes, void* stream);
+
+/* Attention over the listed pages (sel_idx NULL: all).  lse (natural logarithm of the sum of exponentials) may be NULL. */
+int adacluster_block_attn(const adacluster_block_params* p, const void* q, const int32_t* cu_q, const void* k, const void* v,
+                          const uint32_t* k_meta, const uint32_t* v_meta, const int32_t* cu_k, const int32_t* seq_lens,
+                          const int32_t* page_table, const int32_t* sel_idx, void* o, float* lse,
+                          void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Gradients of adacluster_block_attn over packed keys, with the lists it was given (they carry no gradient): dq of every query, dk
+ * and dv of every key of a sequence (zero where no list holds it), from its o and lse and the gradient d_o of o.  No atomics
+ * on sums: results repeat bit for bit.
+ */
+int adacluster_block_attn_backward(const adacluster_block_params* p, const void* q, const void* k, const void* v, const void* o,
+                                   const float* lse, const void* d_o, const int32_t* cu_q, const int32_t* cu_k,
+                                   const int32_t* sel_idx, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Stage timing for benchmarks.  adacluster_profile_enable(1) creates HIP events; while enabled,
  * adacluster_attn, adacluster_sparse_attn and adacluster_dense_attn record them on the call's
  * stream at their stage boundaries (adacluster_qcluster and adacluster_kcluster record their own).

@@ -50,6 +50,15 @@ class CHeadStats(ctypes.Structure):
                 ("reserved", ctypes.c_int32), ("executed_pairs", ctypes.c_int64), ("issued_pairs", ctypes.c_int64)]
 
 
+class CBlockParams(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_int32) for n in ("B", "Hq", "Hkv", "d", "dtype", "bits", "page", "num_pages", "max_pages", "max_q", "qblock",
+                                               "causal", "topk", "keep_first", "q_rows", "k_rows")]
+                + [("softmax_scale", ctypes.c_float)]
+                + [(n, ctypes.c_int64 * k) for n, k in (("q_stride", 2), ("o_stride", 2), ("k_stride", 3), ("v_stride", 3),
+                                                        ("new_k_stride", 2), ("new_v_stride", 2), ("do_stride", 2), ("dq_stride", 2),
+                                                        ("dk_stride", 2), ("dv_stride", 2))])
+
+
 @dataclass
 class Params:
     H: int
@@ -83,6 +92,41 @@ class Params:
         return self.k_max_clusters + self.k_m0
 
 
+@dataclass
+class BlockParams:
+    """adacluster_block_params without what follows from the tensors of a call (pages of the pool, rows, strides)."""
+    B: int
+    Hq: int
+    Hkv: int
+    d: int
+    dtype: int = BF16
+    bits: int = 0
+    page: int = 64
+    max_pages: int = 1
+    max_q: int = 1
+    qblock: int = 1
+    causal: int = 1
+    topk: int = 0
+    keep_first: int = 1
+    softmax_scale: float = 0.0
+
+    @property
+    def blocks(self) -> int:
+        return -(-self.max_q // self.qblock)
+
+
+@dataclass
+class BlockCache:
+    """Tensors of a paged cache: k, v [num_pages,Hkv,page,d] of the params dtype in any strides, or with bits=4 the codes,
+    uint8 [num_pages,Hkv,page,d/2], and k_meta, v_meta, bfloat16 [num_pages,Hkv,page,d/64,2], contiguous; boxes
+    [num_pages,Hkv,2,d]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_meta: torch.Tensor = None
+    v_meta: torch.Tensor = None
+    boxes: torch.Tensor = None
+
+
 _param_values = operator.attrgetter(*(name for name, _ in CParams._fields_))
 _lib = None
 
@@ -113,10 +157,19 @@ def load_library():
     lib.adacluster_mfma_probe.argtypes = [ctypes.c_int32, vp, sz, ctypes.POINTER(ctypes.c_double), vp]
     lib.adacluster_stats_fetch.argtypes = [P, vp, sz, ctypes.POINTER(CHeadStats), vp]
     lib.adacluster_quest_scores.argtypes = [ctypes.c_int32] * 7 + [vp] * 5
+    BP = ctypes.POINTER(CBlockParams)
+    lib.adacluster_block_workspace_bytes.argtypes = [BP, ctypes.c_int32, ctypes.POINTER(sz)]
+    lib.adacluster_cache_append.argtypes = [BP] + [vp] * 11
+    lib.adacluster_cache_read.argtypes = [BP] + [vp] * 10
+    lib.adacluster_block_boxes.argtypes = [BP] + [vp] * 4
+    lib.adacluster_block_select.argtypes = [BP] + [vp] * 9 + [sz, vp]
+    lib.adacluster_block_attn.argtypes = [BP] + [vp] * 13 + [sz, vp]
+    lib.adacluster_block_attn_backward.argtypes = [BP] + [vp] * 13 + [sz, vp]
     lib.adacluster_profile_enable.argtypes = [ctypes.c_int]
     lib.adacluster_profile_read.argtypes = [ctypes.POINTER(ctypes.c_float)]
     for n in ("profile_enable", "profile_read", "centroid_capacity", "workspace_bytes", "last_error", "qcluster", "kcluster", "select",
-              "sparse_attn", "attn", "dense_attn", "compactness", "compactness_noalloc", "quest_scores", "stats_fetch", "mfma_probe"):
+              "sparse_attn", "attn", "dense_attn", "compactness", "compactness_noalloc", "quest_scores", "stats_fetch", "mfma_probe",
+              "block_workspace_bytes", "cache_append", "cache_read", "block_boxes", "block_select", "block_attn", "block_attn_backward"):
         getattr(lib, "adacluster_" + n).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -126,6 +179,8 @@ EXPORTED = ["adacluster_centroid_capacity", "adacluster_workspace_bytes", "adacl
             "adacluster_qcluster", "adacluster_kcluster", "adacluster_select",
             "adacluster_sparse_attn", "adacluster_attn", "adacluster_dense_attn", "adacluster_compactness",
             "adacluster_compactness_noalloc", "adacluster_quest_scores", "adacluster_stats_fetch", "adacluster_mfma_probe",
+            "adacluster_block_workspace_bytes", "adacluster_cache_append", "adacluster_cache_read", "adacluster_block_boxes",
+            "adacluster_block_select", "adacluster_block_attn", "adacluster_block_attn_backward",
             "adacluster_profile_enable", "adacluster_profile_read"]
 
 STAGES = ["qcluster", "kcluster", "select", "permute", "plan", "attention", "kreduce"]
@@ -380,3 +435,247 @@ def adacluster_dense_attn(p: Params, Q, K, V, out=None, ws=None):
         ctypes.byref(cp), _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(ws), ws.numel(), _stream()),
         "adacluster_dense_attn")
     return O
+
+
+# ---- attention over pages of keys ---------------------------------------------------------------------------------------
+
+BLOCK_SELECT, BLOCK_ATTN, BLOCK_BACKWARD = 0, 1, 2
+_block_values = operator.attrgetter("B", "Hq", "Hkv", "d", "dtype", "bits", "page", "max_pages", "max_q", "qblock", "causal", "topk", "keep_first",
+                                    "softmax_scale")
+
+
+def _block_c(p: BlockParams, q_rows, k_rows=0, num_pages=0) -> CBlockParams:
+    B_, Hq, Hkv, d, dtype, bits, page, max_pages, max_q, qblock, causal, topk, keep_first, scale = _block_values(p)
+    return CBlockParams(B_, Hq, Hkv, d, dtype, bits, page, num_pages, max_pages, max_q, qblock, causal, topk, keep_first, q_rows, k_rows, scale)
+
+
+def _rows(name, t, dtype, heads, d, device):
+    """A [rows, heads, d] tensor with d contiguous; its strides of rows and heads."""
+    if t.dtype != dtype or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or not t.is_cuda or t.device != device:
+        raise ValueError(f"{name} must be a [rows, {heads}, {d}] tensor of {dtype} on {device}")
+    s = t.stride()
+    if s[2] != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return s[0], s[1]
+
+
+def _ints(name, t, shape, device):
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor {tuple(shape)} on {device}")
+
+
+def _pool(cp, p: BlockParams, cache: BlockCache, device, boxes):
+    """Checks a cache and writes its strides and number of pages into cp."""
+    n, Hkv, page, d = cache.k.shape[0], p.Hkv, p.page, p.d
+    if p.bits == 4:
+        for name, t, shape, dt in (("k", cache.k, (n, Hkv, page, d // 2), torch.uint8), ("v", cache.v, (n, Hkv, page, d // 2), torch.uint8),
+                                   ("k_meta", cache.k_meta, (n, Hkv, page, d // 64, 2), torch.bfloat16),
+                                   ("v_meta", cache.v_meta, (n, Hkv, page, d // 64, 2), torch.bfloat16)):
+            if t is None or t.shape != shape or t.dtype != dt or not t.is_contiguous() or t.device != device:
+                raise ValueError(f"cache.{name} must be a contiguous {dt} tensor {shape} on {device}")
+    else:
+        for name, t, to in (("k", cache.k, cp.k_stride), ("v", cache.v, cp.v_stride)):
+            if t.shape != (n, Hkv, page, d) or t.dtype != _tdtype(p) or t.stride(3) != 1 or t.device != device:
+                raise ValueError(f"cache.{name} must be a {_tdtype(p)} tensor {(n, Hkv, page, d)} on {device}, its last dimension contiguous")
+            s = t.stride()
+            to[0], to[1], to[2] = s[0], s[2], s[1]
+    if boxes:
+        _boxes(cache.boxes, (n, Hkv, 2, d), p, device)
+    cp.num_pages = n
+
+
+def _boxes(t, shape, p, device):
+    if t is None or t.shape != shape or t.dtype != _tdtype(p) or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"boxes must be a contiguous {_tdtype(p)} tensor {tuple(shape)} on {device}")
+
+
+def _block_ws(cp, call, device, ws):
+    n = ctypes.c_size_t(0)
+    _check(load_library().adacluster_block_workspace_bytes(ctypes.byref(cp), call, ctypes.byref(n)), "block_workspace_bytes")
+    if ws is None:
+        # a tensor of its own for every call: torch hands memory out by stream, and to a captured graph from that graph's pool
+        ws = torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+    return ws, 0 if ws is None else ws.numel()
+
+
+def _on(device):
+    """The device that owns the tensors made current for a launch, and its current stream."""
+    return torch.cuda.device(device)
+
+
+def alloc_cache(p: BlockParams, num_pages, device="cuda"):
+    """A BlockCache of num_pages empty pages."""
+    z = lambda *s, dt: torch.zeros(s, dtype=dt, device=device)  # noqa: E731
+    n, dt = num_pages, _tdtype(p)
+    boxes = z(n, p.Hkv, 2, p.d, dt=dt)
+    if p.bits == 4:
+        codes = lambda: z(n, p.Hkv, p.page, p.d // 2, dt=torch.uint8)  # noqa: E731
+        meta = lambda: z(n, p.Hkv, p.page, p.d // 64, 2, dt=torch.bfloat16)  # noqa: E731
+        return BlockCache(codes(), codes(), meta(), meta(), boxes)
+    return BlockCache(z(n, p.Hkv, p.page, p.d, dt=dt), z(n, p.Hkv, p.page, p.d, dt=dt), None, None, boxes)
+
+
+def adacluster_block_workspace_bytes(p: BlockParams, call, q_rows, k_rows=0, num_pages=0) -> int:
+    out = ctypes.c_size_t(0)
+    cp = _block_c(p, q_rows, k_rows, num_pages)
+    _check(load_library().adacluster_block_workspace_bytes(ctypes.byref(cp), call, ctypes.byref(out)), "block_workspace_bytes")
+    return out.value
+
+
+def adacluster_cache_append(p: BlockParams, k, v, cu_new, seq_lens, page_table, cache: BlockCache):
+    """Writes new tokens k, v [rows,Hkv,d] into the cache behind the seq_lens[b] tokens that sequence b holds."""
+    dev = k.device
+    cp = _block_c(p, k.shape[0])
+    cp.new_k_stride[:] = _rows("k", k, _tdtype(p), p.Hkv, p.d, dev)
+    cp.new_v_stride[:] = _rows("v", v, _tdtype(p), p.Hkv, p.d, dev)
+    if v.shape[0] != k.shape[0]:
+        raise ValueError("k and v must have the same rows")
+    _ints("cu_new", cu_new, (p.B + 1,), dev)
+    _ints("seq_lens", seq_lens, (p.B,), dev)
+    _ints("page_table", page_table, (p.B, p.max_pages), dev)
+    _pool(cp, p, cache, dev, True)
+    if k.shape[0] == 0:
+        return
+    with _on(dev):
+        _check(load_library().adacluster_cache_append(
+            ctypes.byref(cp), _ptr(k), _ptr(v), _ptr(cu_new), _ptr(seq_lens), _ptr(page_table), _ptr(cache.k), _ptr(cache.v),
+            _ptr(cache.k_meta), _ptr(cache.v_meta), _ptr(cache.boxes), _stream()), "adacluster_cache_append")
+
+
+def adacluster_cache_read(p: BlockParams, cache: BlockCache, cu_new, first, page_table, rows, out=None):
+    """Tokens of the cache as values -> k, v [rows,Hkv,d]: of sequence b those from position first[b] on, to its rows by cu_new."""
+    dev = cache.k.device
+    cp = _block_c(p, rows)
+    _ints("cu_new", cu_new, (p.B + 1,), dev)
+    _ints("first", first, (p.B,), dev)
+    _ints("page_table", page_table, (p.B, p.max_pages), dev)
+    _pool(cp, p, cache, dev, False)
+    if out is None:
+        out = tuple(torch.empty((rows, p.Hkv, p.d), dtype=_tdtype(p), device=dev) for _ in range(2))
+    for t in out:
+        if t.shape != (rows, p.Hkv, p.d) or t.dtype != _tdtype(p) or not t.is_contiguous() or t.device != dev:
+            raise ValueError(f"out must be two contiguous {_tdtype(p)} tensors {(rows, p.Hkv, p.d)} on {dev}")
+    if rows:
+        with _on(dev):
+            _check(load_library().adacluster_cache_read(
+                ctypes.byref(cp), _ptr(cu_new), _ptr(first), _ptr(page_table), _ptr(cache.k), _ptr(cache.v), _ptr(cache.k_meta),
+                _ptr(cache.v_meta), _ptr(out[0]), _ptr(out[1]), _stream()), "adacluster_cache_read")
+    return out
+
+
+def adacluster_block_boxes(p: BlockParams, k, cu_k, out=None):
+    """Boxes of packed keys [rows,Hkv,d] -> [B,max_pages,Hkv,2,d]."""
+    dev = k.device
+    cp = _block_c(p, 1, k.shape[0])
+    cp.k_stride[1:] = _rows("k", k, _tdtype(p), p.Hkv, p.d, dev)
+    _ints("cu_k", cu_k, (p.B + 1,), dev)
+    shape = (p.B, p.max_pages, p.Hkv, 2, p.d)
+    boxes = torch.empty(shape, dtype=_tdtype(p), device=dev) if out is None else out
+    _boxes(boxes, shape, p, dev)
+    with _on(dev):
+        _check(load_library().adacluster_block_boxes(ctypes.byref(cp), _ptr(k), _ptr(cu_k), _ptr(boxes), _stream()), "adacluster_block_boxes")
+    return boxes
+
+
+def _keys_of(p, cu_k, seq_lens, page_table, dev, paged):
+    if paged:
+        if seq_lens is None or page_table is None:
+            raise ValueError("a paged cache needs seq_lens and page_table")
+        _ints("seq_lens", seq_lens, (p.B,), dev)
+        _ints("page_table", page_table, (p.B, p.max_pages), dev)
+    else:
+        if cu_k is None:
+            raise ValueError("packed keys need cu_k")
+        _ints("cu_k", cu_k, (p.B + 1,), dev)
+
+
+def adacluster_block_select(p: BlockParams, q, cu_q, boxes, cu_k=None, seq_lens=None, page_table=None, k_rows=None, ws=None):
+    """Pages of every block of queries -> sel_idx [B,blocks,Hkv,topk], sel_cnt [B,blocks,Hkv].  cu_k: packed keys (k_rows: rows of
+    the key tensor, where it has fewer than cu_k says); seq_lens and page_table: a paged cache."""
+    dev = q.device
+    paged = cu_k is None
+    cp = _block_c(p, q.shape[0], 0 if paged else (2 ** 31 - 1 if k_rows is None else k_rows), boxes.shape[0] if paged else 0)
+    cp.q_stride[:] = _rows("q", q, _tdtype(p), p.Hq, p.d, dev)
+    _ints("cu_q", cu_q, (p.B + 1,), dev)
+    _keys_of(p, cu_k, seq_lens, page_table, dev, paged)
+    _boxes(boxes, (boxes.shape[0], p.Hkv, 2, p.d) if paged else (p.B, p.max_pages, p.Hkv, 2, p.d), p, dev)
+    idx = torch.empty((p.B, p.blocks, p.Hkv, p.topk), dtype=torch.int32, device=dev)
+    cnt = torch.empty((p.B, p.blocks, p.Hkv), dtype=torch.int32, device=dev)
+    with _on(dev):
+        ws, n = _block_ws(cp, BLOCK_SELECT, dev, ws)
+        _check(load_library().adacluster_block_select(
+            ctypes.byref(cp), _ptr(q), _ptr(cu_q), _ptr(cu_k), _ptr(seq_lens), _ptr(page_table), _ptr(boxes), _ptr(idx), _ptr(cnt),
+            _ptr(ws), n, _stream()), "adacluster_block_select")
+    return idx, cnt
+
+
+def adacluster_block_attn(p: BlockParams, q, cu_q, k=None, v=None, cu_k=None, cache: BlockCache = None, seq_lens=None, page_table=None,
+                          sel_idx=None, out=None, lse=None, ws=None):
+    """Attention of q [rows,Hq,d] over packed k, v [rows,Hkv,d] with cu_k, or over a cache with seq_lens and page_table; over the
+    pages of sel_idx, or all -> o like q, lse float32 [rows,Hq]."""
+    dev = q.device
+    cp = _block_c(p, q.shape[0])
+    cp.q_stride[:] = _rows("q", q, _tdtype(p), p.Hq, p.d, dev)
+    _ints("cu_q", cu_q, (p.B + 1,), dev)
+    _keys_of(p, cu_k, seq_lens, page_table, dev, cache is not None)
+    meta = (None, None)
+    if cache is not None:
+        _pool(cp, p, cache, dev, False)
+        k, v, meta, cu_k = cache.k, cache.v, (cache.k_meta, cache.v_meta), None
+    else:
+        cp.k_rows = _kv(cp, p, k, v, dev)
+    if sel_idx is not None:
+        _ints("sel_idx", sel_idx, (p.B, p.blocks, p.Hkv, p.topk), dev)
+    o = torch.empty_like(q) if out is None else out
+    cp.o_stride[:] = _rows("out", o, _tdtype(p), p.Hq, p.d, dev)
+    lse = torch.empty((q.shape[0], p.Hq), dtype=torch.float32, device=dev) if lse is None else lse
+    _lse(lse, q, p, dev)
+    if o.shape[0] != q.shape[0]:
+        raise ValueError("out must have the rows of q")
+    with _on(dev):
+        ws, n = _block_ws(cp, BLOCK_ATTN, dev, ws)
+        _check(load_library().adacluster_block_attn(
+            ctypes.byref(cp), _ptr(q), _ptr(cu_q), _ptr(k), _ptr(v), _ptr(meta[0]), _ptr(meta[1]), _ptr(cu_k), _ptr(seq_lens),
+            _ptr(page_table), _ptr(sel_idx), _ptr(o), _ptr(lse), _ptr(ws), n, _stream()), "adacluster_block_attn")
+    return o, lse
+
+
+def _kv(cp, p, k, v, dev):
+    if k is None or v is None or k.shape[0] != v.shape[0]:
+        raise ValueError("k and v must be given, with the same rows")
+    cp.k_stride[1:] = _rows("k", k, _tdtype(p), p.Hkv, p.d, dev)
+    cp.v_stride[1:] = _rows("v", v, _tdtype(p), p.Hkv, p.d, dev)
+    return k.shape[0]
+
+
+def _lse(lse, q, p, dev):
+    if lse.shape != (q.shape[0], p.Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != dev:
+        raise ValueError(f"lse must be a contiguous float32 tensor {(q.shape[0], p.Hq)} on {dev}")
+
+
+def adacluster_block_attn_backward(p: BlockParams, q, k, v, o, lse, d_o, cu_q, cu_k, sel_idx=None, outs=None, ws=None):
+    """Gradients of adacluster_block_attn over packed keys -> dq, dk, dv (like q, k, v).  Without `outs`, rows that belong to no
+    sequence are zero."""
+    dev = q.device
+    cp = _block_c(p, q.shape[0])
+    cp.q_stride[:] = _rows("q", q, _tdtype(p), p.Hq, p.d, dev)
+    cp.k_rows = _kv(cp, p, k, v, dev)
+    cp.o_stride[:] = _rows("o", o, _tdtype(p), p.Hq, p.d, dev)
+    cp.do_stride[:] = _rows("d_o", d_o, _tdtype(p), p.Hq, p.d, dev)
+    _lse(lse, q, p, dev)
+    _ints("cu_q", cu_q, (p.B + 1,), dev)
+    _ints("cu_k", cu_k, (p.B + 1,), dev)
+    if sel_idx is not None:
+        _ints("sel_idx", sel_idx, (p.B, p.blocks, p.Hkv, p.topk), dev)
+    dq, dk, dv = (torch.zeros_like(t) for t in (q, k, v)) if outs is None else outs
+    cp.dq_stride[:] = _rows("dq", dq, _tdtype(p), p.Hq, p.d, dev)
+    cp.dk_stride[:] = _rows("dk", dk, _tdtype(p), p.Hkv, p.d, dev)
+    cp.dv_stride[:] = _rows("dv", dv, _tdtype(p), p.Hkv, p.d, dev)
+    if not (o.shape[0] == d_o.shape[0] == dq.shape[0] == q.shape[0] and dk.shape[0] == dv.shape[0] == k.shape[0]):
+        raise ValueError("o, d_o and dq must have the rows of q, dk and dv those of k")
+    with _on(dev):
+        ws, n = _block_ws(cp, BLOCK_BACKWARD, dev, ws)
+        _check(load_library().adacluster_block_attn_backward(
+            ctypes.byref(cp), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(cu_q), _ptr(cu_k), _ptr(sel_idx),
+            _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), n, _stream()), "adacluster_block_attn_backward")
+    return dq, dk, dv

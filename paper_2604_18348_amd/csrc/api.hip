@@ -21,8 +21,19 @@ constexpr size_t STATIC_SCRATCH_DOUBLES = 65536;                 // 512 KiB
 static __device__ __align__(256) double scratch[STATIC_SCRATCH_DOUBLES];
 
 namespace {
-
 thread_local char g_err[256] = "";
+}
+
+int adac::fail(int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(g_err, sizeof(g_err), fmt, ap);
+  va_end(ap);
+  return code;
+}
+
+namespace {
+
 
 // Optional stage timing: hipEvents recorded at the stage boundaries of a call.  A stage is timed
 // from the event in from[] (default: the previous recorded stage boundary); the fused call runs
@@ -111,8 +122,6 @@ AuxStream* aux_stream() {
   return &a;
 }
 
-int fail(int code, const char* fmt, ...);
-
 // Device address of `scratch` on the current device, looked up once per device.
 std::mutex g_scratch_mu;
 double* g_scratch_ptr[64] = {};
@@ -126,14 +135,6 @@ double* static_scratch() {
     g_scratch_ptr[dev] = (double*)ptr;
   }
   return g_scratch_ptr[dev];
-}
-
-int fail(int code, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_err, sizeof(g_err), fmt, ap);
-  va_end(ap);
-  return code;
 }
 
 int check_params(const adacluster_params* p) {

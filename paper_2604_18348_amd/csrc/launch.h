@@ -186,4 +186,7 @@ int launch_attention(hipStream_t s, int dtype, int d, int H, int N, int Cq, int 
                      const int32_t* rng_pre, const int32_t* rng_cnt, int maxr, const int32_t* perm_k /* NULL: identity */,
                      int segs /* 0: dealt by their number */, int32_t* deal);
 
+// Leaves a message for adacluster_last_error (of the calling thread) and returns `code`.
+int fail(int code, const char* fmt, ...);
+
 }  // namespace adac
