@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_lib")
 LIB_PATH = os.path.join(OUT_DIR, "libadacluster.so")
-SOURCES = ["sort.hip", "cluster.hip", "select.hip", "quest.hip", "attn.hip", "block_cache.hip", "block_attn.hip", "block_grad.hip",
+SOURCES = ["sort.hip", "cluster.hip", "select.hip", "quest.hip", "attn.hip", "block_cache.hip", "block_attn.hip", "block_wide.hip", "block_grad.hip",
            "block_api.hip", "api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fgpu-rdc" if False else "-fno-gpu-rdc",

@@ -177,6 +177,8 @@ struct BlockAttnArgs {
 };
 size_t block_attn_bytes(const BlockDims& m, int dtype, int bits, int d, bool listed);
 int launch_block_attn(hipStream_t s, int dtype, int bits, int d, BlockAttnArgs a, void* ws);
+bool block_wide_takes(const BlockAttnArgs& a, int dtype, int bits);      // (block_wide.hip)
+int launch_block_attn_wide(hipStream_t s, int d, const BlockAttnArgs& a);
 
 struct BlockGradArgs {
   BlockDims m;

@@ -379,6 +379,7 @@ size_t block_attn_bytes(const BlockDims& m, int dtype, int bits, int d, bool lis
 }
 
 int launch_block_attn(hipStream_t s, int dtype, int bits, int d, BlockAttnArgs a, void* ws) {
+  if (block_wide_takes(a, dtype, bits)) return launch_block_attn_wide(s, d, a);
   const Shape sh = shape_of(a.m, dtype, a.sel != nullptr);
   if (!grid_fits(sh.items * (sh.nsplit > sh.R ? sh.nsplit : sh.R))) return ADACLUSTER_E_UNSUPPORTED;
   a.nsplit = sh.nsplit;

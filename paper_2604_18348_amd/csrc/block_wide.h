@@ -1,0 +1,89 @@
+// What the bf16 kernels for many rows share: tiles of 64 rows staged in LDS by direct loads, read by all waves (internal).
+//
+// 32x32x16 products (v_mfma_f32_32x32x16_bf16): half the LDS reads a product of the 16x16 tiles.  A result holds in lane l column
+// l % 32 and, in value v, row 8 (v / 4) + 4 (l / 32) + v % 4; eight consecutive values are the operand of the next product, whose
+// other operand is read column-wise (two transposing reads: rows 4 (l / 32) .. + 3 and 8 further) to match.
+#pragma once
+
+#include "block.h"
+
+namespace adac {
+
+typedef __attribute__((address_space(3))) void lds_void_t;
+
+constexpr int TILE = 64;               // rows of a tile, staged as four sixteenths of pages
+constexpr int LIST = 512;              // pages of a list held in LDS at a time
+
+// Rows of D bf16 in LDS, unpadded.  Piece q (16 bytes) of row r sits in slot q ^ swz(r): in ROWS order for reads of one piece of 32
+// rows, in COLS order for transposing reads, both free of bank conflicts; a tile that is read both ways keeps the ROWS order,
+// whose transposing reads meet two rows a bank at most.
+template <int D> __device__ __forceinline__ int swz_rows(int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); }
+template <int D> __device__ __forceinline__ int swz_cols(int r) { return D == 128 ? ((r & 3) << 2) : (((r >> 1) & 1) << 2); }
+
+__device__ __forceinline__ bf16x8_t join_tr(s16x4_tr lo, s16x4_tr hi) {
+  union { s16x4_tr h[2]; bf16x8_t v; } u{{lo, hi}};
+  return u.v;
+}
+__device__ __forceinline__ s16x4_tr read_tr(const char* p) { return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_t*)p); }
+
+// Eight values of a result (8 s2 .. + 7) as the operand of the next product.
+__device__ __forceinline__ bf16x8_t pack8(const f32x16_t& x, int s2) {
+  union { uint32_t w[4]; bf16x8_t v; } u;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) u.w[j] = pack_bf16x2(x[8 * s2 + 2 * j], x[8 * s2 + 2 * j + 1]);
+  return u.v;
+}
+// ... and their sum, of the rounded values
+__device__ __forceinline__ float sum8(const bf16x8_t& v, float c) {
+  const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
+  union { bf16x8_t v; bf16x2_t w[4]; } u{v};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_fdot2_f32_bf16(u.w[j], one, c, false);
+  return c;
+}
+
+__device__ __forceinline__ f32x16_t mfma32(const bf16x8_t& a, const bf16x8_t& b, const f32x16_t& c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16_t zero16() {
+  f32x16_t z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+
+// a value that all lanes share, where the compiler keeps it in a vector register (divisions are made there)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t v = (uint64_t)p;
+  return (const char*)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+
+// Pages e0 .. e0 + LIST - 1 of a list that name keys below `pages`, in order: {page, place in the pool}.  Returns how many.
+template <int NT>
+__device__ __forceinline__ int fill_list(const BlockDims& m, int b, const int32_t* list, int e0, int e1, int pages, int2* out, int32_t* counts) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int n = 0;
+  for (int base = e0; base < min(e1, e0 + LIST); base += NT) {
+    const int e = base + tid;
+    int pg = e < min(e1, e0 + LIST) ? list_page(list, e, pages) : -1, phys = 0;
+    if (pg >= 0 && m.num_pages) { phys = pool_page(m, b, pg); if (phys < 0) pg = -1; }
+    const uint64_t some = __ballot(pg >= 0);
+    if (lane == 0) counts[wave] = __popcll(some);
+    __syncthreads();
+    int at = n + __popcll(some & ((1ull << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) { if (w < wave) at += counts[w]; n += counts[w]; }
+    if (pg >= 0) out[at] = int2{pg, phys};
+    __syncthreads();
+  }
+  return __builtin_amdgcn_readfirstlane(n);
+}
+
+// A launch's workgroups go to the 8 XCDs in turn: runs of GROUP neighbours (blocks of a sequence, whose lists are alike) share one.
+constexpr int XCD_RUN = 16;
+__device__ __forceinline__ int xcd_item(int id) {
+  const int run = id / (8 * XCD_RUN);
+  return (run * 8 + id % 8) * XCD_RUN + id / 8 % XCD_RUN;
+}
+static inline long long xcd_grid(long long items) { return (items + 8 * XCD_RUN - 1) / (8 * XCD_RUN) * (8 * XCD_RUN); }
+
+}  // namespace adac

@@ -1,0 +1,273 @@
+// Attention of blocks of many rows over listed pages, bf16: the walk of block_attn with tiles of 64 keys staged once for all waves.
+#include "block_wide.h"
+
+namespace adac {
+
+namespace {
+
+// NW waves of 32 rows each.  A tile's keys and values go global -> LDS directly, 16 bytes a lane, one tile ahead of
+// the products.  Rows past a sequence's end are read from the last row there is in
+// their sixteenth (or the page's first) and masked: nothing behind the end is touched.
+struct Part { int pg, phys, sub; };          // a sixteenth of a page
+__device__ __forceinline__ int pick(int i, int a, int b, int c, int d) { return i < 2 ? i == 0 ? a : b : i == 2 ? c : d; }
+
+template <int D, int NW>
+__global__ __launch_bounds__(NW * 64) void block_attn_wide(BlockAttnArgs a, int rts, int items) {
+  constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
+  constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB, NBUF = 2, VM_STEP = 2 * PT;
+  constexpr int STRIDE = 2 * KS / VM_STEP, J0 = 2 * KS - 1 - (VM_STEP - 1) * STRIDE < 3 ? 2 * KS - 1 - (VM_STEP - 1) * STRIDE : 3;
+  static_assert(STRIDE >= 1 && J0 >= 0, "every request finds a product to go behind");
+  __shared__ __align__(16) char lds[2 * NBUF * TILEB];
+  __shared__ int2 pages_l[LIST];
+  __shared__ int32_t counts[NW];
+  const BlockDims& m = a.m;
+  int id = xcd_item(blockIdx.x);
+  if (id >= items) return;
+  const int rt = uniform(id % rts); id /= rts;
+  const int i = uniform(id % m.nb); id /= m.nb;
+  const int hk = uniform(id % m.Hkv), b = uniform(id / m.Hkv);
+  const BlockSeq s = block_seq(m, b);
+  const int t0 = i * m.qblock, rows = min(m.qblock, s.nq - t0) * m.G, base_row = rt * NT / 2;
+  if (t0 >= s.nq || base_row >= rows) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
+
+  const int row = base_row + wave * 32 + c, tok = t0 + row / m.G, head = hk * m.G + row % m.G;
+  const bool there = row < rows;
+  bf16x8_t qf[KS];
+  {
+    const bf16raw* const p = (const bf16raw*)a.q + (long long)(s.q0 + tok) * a.qs.token + (long long)head * a.qs.head + hb * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const u32x4_t w = there ? *(const u32x4_t*)(p + ks * 16) : u32x4_t{0, 0, 0, 0};
+      qf[ks] = *(const bf16x8_t*)&w;
+    }
+  }
+  const int lim = there ? (m.causal ? min(s.n, s.first + tok + 1) : s.n) : INT32_MAX;      // (a row that is not there needs no mask)
+  const int wave_first = base_row + wave * 32, wave_last = min(wave_first + 32, rows) - 1;
+  const bool wave_has_rows = wave_first < rows;
+  const int minlim = m.causal ? min(s.n, s.first + t0 + wave_first / m.G + 1) : s.n;       // keys below: seen by all rows of the wave
+  const int last = min(base_row + NT / 2, rows) - 1;
+  const int maxlim = m.causal ? min(s.n, s.first + t0 + last / m.G + 1) : s.n;
+  const int pages = maxlim > 0 ? (maxlim + m.page - 1) >> m.lpage : 0;
+  const int32_t* const list = a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
+  const int entries = list ? m.topk : pages;
+  (void)wave_last;
+
+  f32x16_t oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) oacc[db] = zero16();
+  // The weights are taken relative to a reference that moves only when a tile's sum leaves its range (see below); the lowest
+  // value that is finite when scaled too, so that tiles a row sees nothing of leave sum and accumulator at zero.
+  const float sc = a.scale_log2e, lowest = -3.402823466e38f / fmaxf(sc, 1.f);
+  float mref = lowest, lrun = 0.f;
+
+  int lrow[PT], piece_k[PT], piece_v[PT];            // this thread's pieces of a tile
+#pragma unroll
+  for (int x = 0; x < PT; ++x) {
+    const int item = tid + x * NT;
+    lrow[x] = item / CH;
+    piece_k[x] = ((item % CH) ^ swz_rows<D>(lrow[x])) * 16;
+    piece_v[x] = ((item % CH) ^ swz_cols<D>(lrow[x])) * 16;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t*)lds;
+  const int lsub = m.lpage - 4, ktok = (int)(a.ks.token * 2), vtok = (int)(a.vs.token * 2);
+  int kaddr[KS], vaddr[DB];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) kaddr[ks] = c * ROWB + (((ks * 2 + hb) ^ swz_rows<D>(c)) * 16);
+  {
+    const int i16 = lane & 15, vrow = 4 * hb + (i16 >> 2), gl = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) vaddr[db] = NBUF * TILEB + vrow * ROWB + (((db * 4 + gl) ^ swz_cols<D>(vrow)) * 16) + 8 * (i16 & 1);
+  }
+
+  for (int e0 = 0; e0 < entries; e0 += LIST) {
+    const int n = fill_list<NT>(m, b, list, e0, entries, pages, pages_l, counts);
+    const int parts = n << lsub, tiles = (parts + 3) >> 2;
+    if (!tiles) continue;
+    // the four sixteenths of tile t (past the end: the last one again)
+    Part next[4];
+    auto look = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int part = min(t * 4 + x, parts - 1);
+        const int2 pp = pages_l[part >> lsub];
+        next[x] = Part{__builtin_amdgcn_readfirstlane(pp.x), __builtin_amdgcn_readfirstlane(pp.y), part & ((1 << lsub) - 1)};
+      }
+    };
+    // request `op` of the tile looked up last: even keys, odd values; a wave's request lies inside one sixteenth
+    auto issue = [&](int stage, int op) __attribute__((always_inline)) {
+      const int x = op >> 1, at = ((wave * 64 + x * NT) / CH) >> 4;
+      const Part p{pick(at, next[0].pg, next[1].pg, next[2].pg, next[3].pg), pick(at, next[0].phys, next[1].phys, next[2].phys, next[3].phys), pick(at, next[0].sub, next[1].sub, next[2].sub, next[3].sub)};
+      int sub = p.sub, have = s.n - ((p.pg << m.lpage) + sub * 16);      // rows of the sixteenth that exist
+      if (have <= 0) { sub = 0; have = 1; }
+      const int r = min(lrow[x] & 15, have - 1);
+      const uint32_t dst = lds0 + stage * TILEB + (wave * 64 + x * NT) * 16;
+      if ((op & 1) == 0) dma_b128(dst, (uint32_t)(r * ktok + piece_k[x]), uniform((const char*)a.k + row_at(m, s, a.ks, p.phys, p.pg, sub, hk) * 2));
+      else dma_b128(dst + NBUF * TILEB, (uint32_t)(r * vtok + piece_v[x]), uniform((const char*)a.v + row_at(m, s, a.vs, p.phys, p.pg, sub, hk) * 2));
+    };
+    int key0[4];                                    // of the tile being worked on
+    bool whole;
+    auto turn = [&](int t) __attribute__((always_inline)) {      // the tile looked up last, number t, is worked on next
+      whole = true;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        key0[x] = t * 4 + x < parts ? (next[x].pg << m.lpage) + next[x].sub * 16 : INT32_MAX - 64;
+        whole = whole && key0[x] + 16 <= minlim;
+      }
+    };
+    auto compute = [&](int stage, int t, auto&& request) __attribute__((always_inline)) {
+      const char* const base = lds + stage * TILEB;
+      f32x16_t sacc[2];
+      bf16x8_t ka[2][KS];
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) ka[kb][ks] = *(const bf16x8_t*)(base + kb * 32 * ROWB + kaddr[ks]);
+      compiler_fence();
+      look(t + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          sacc[kb] = mfma32(ka[kb][ks], qf[ks], ks == 0 ? zero16() : sacc[kb]);
+          const int j = kb * KS + ks;
+          if (j >= J0 && (j - J0) % STRIDE == 0 && (j - J0) / STRIDE < VM_STEP) {
+            __builtin_amdgcn_sched_barrier(0);
+            request((j - J0) / STRIDE);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      compiler_fence();
+      if (!whole) {
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if (key0[kb * 2 + (v >> 3)] + 8 * ((v >> 2) & 1) + 4 * hb + (v & 3) >= lim) sacc[kb][v] = -INFINITY;
+      }
+      // p = 2^((s - reference) scale): any reference gives the same result as long as nothing overflows, or vanishes against a row
+      // that has had no larger score.  The tile's row sum tells: past its limit, or the reference still the lowest.
+      bf16x8_t pf[2][2];
+      float rsum;
+      auto weights = [&]() __attribute__((always_inline)) {
+        const float off = mref * sc;
+        float part[4];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int s2 = 0; s2 < 2; ++s2) {
+            f32x16_t& x = sacc[kb];
+            union { uint32_t w[4]; bf16x8_t v; } u;
+            part[2 * kb + s2] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float p0 = __builtin_amdgcn_exp2f(fmaf(x[8 * s2 + 2 * j], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(x[8 * s2 + 2 * j + 1], sc, -off));
+              u.w[j] = pack_bf16x2(p0, p1);
+              part[2 * kb + s2] += p0;              // (not the rounded ones: the sum's logarithm is an output)
+              part[2 * kb + s2] += p1;
+            }
+            pf[kb][s2] = u.v;
+          }
+        rsum = (part[0] + part[1]) + (part[2] + part[3]);
+      };
+      weights();
+      if (__any(!(rsum <= 65536.f))) {
+        float top = sacc[0][0];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) top = fmaxf(top, sacc[kb][v]);
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float next = fmaxf(mref, top), alpha = __builtin_amdgcn_exp2f((mref - next) * sc);
+        mref = next;
+        lrun *= alpha;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+        weights();
+      }
+      lrun += rsum;
+      compiler_fence();
+      bf16x8_t va[DB][2][2];
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int s2 = 0; s2 < 2; ++s2) {
+            const char* const p = base + (kb * 32 + 16 * s2) * ROWB + vaddr[db];
+            va[db][kb][s2] = join_tr(read_tr(p), read_tr(p + 8 * ROWB));
+          }
+      compiler_fence();
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int s2 = 0; s2 < 2; ++s2) oacc[db] = mfma32(va[db][kb][s2], pf[kb][s2], oacc[db]);
+    };
+    look(0);
+#pragma unroll
+    for (int op = 0; op < VM_STEP; ++op) issue(0, op);
+    turn(0);
+    wait_vmcnt<0>();
+    lds_barrier();
+    auto step = [&](auto stage, int t) __attribute__((always_inline)) {      // (loads past the end too: one more tile, never read)
+      constexpr int U = decltype(stage)::value;
+      auto request = [&](int op) __attribute__((always_inline)) { issue(1 - U, op); };
+      if (wave_has_rows) compute(U, t, request);
+      else {
+        look(t + 1);
+#pragma unroll
+        for (int op = 0; op < VM_STEP; ++op) request(op);
+      }
+      turn(t + 1);
+      wait_vmcnt<0>();
+      lds_barrier();
+    };
+    for (int t = 0; t < tiles; t += 2) {
+      step(std::integral_constant<int, 0>{}, t);
+      if (t + 1 < tiles) step(std::integral_constant<int, 1>{}, t + 1);
+    }
+    lds_barrier();                                  // before the list is filled again
+  }
+
+  if (!there) return;
+  const float all = lrun + __shfl_xor(lrun, 32), inv = all == 0.f ? 0.f : 1.f / all;
+  bf16raw* const out = (bf16raw*)a.o + (long long)(s.q0 + tok) * a.os.token + (long long)head * a.os.head + 4 * hb;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *(uint2*)(out + db * 32 + 8 * x) = uint2{pack_bf16x2(oacc[db][4 * x] * inv, oacc[db][4 * x + 1] * inv), pack_bf16x2(oacc[db][4 * x + 2] * inv, oacc[db][4 * x + 3] * inv)};
+  if (hb == 0 && a.lse) a.lse[(long long)(s.q0 + tok) * m.Hq + head] = all == 0.f ? -INFINITY : fmaf(mref, sc, __builtin_amdgcn_logf(all)) * LN2;
+}
+
+}  // namespace
+
+// Whether the kernel for many rows takes a call: bf16 keys, at least 48 rows a block and a workgroup a CU (below, the list has to be
+// split), offsets inside a sixteenth that 32 bits hold.
+bool block_wide_takes(const BlockAttnArgs& a, int dtype, int bits) {
+  const int rows = a.m.qblock * a.m.G;
+  if (dtype != ADACLUSTER_BF16 || bits || rows < 48) return false;
+  const int rt = rows <= 64 ? 64 : 128;
+  const long long items = (long long)((rows + rt - 1) / rt) * a.m.nb * a.m.Hkv * a.m.B;
+  return items >= 256 && a.ks.token < (1 << 25) && a.vs.token < (1 << 25);
+}
+
+int launch_block_attn_wide(hipStream_t s, int d, const BlockAttnArgs& a) {
+  const int rows = a.m.qblock * a.m.G, rt = rows <= 64 ? 64 : 128, rts = (rows + rt - 1) / rt;
+  const long long items = (long long)rts * a.m.nb * a.m.Hkv * a.m.B, grid = xcd_grid(items);
+  if (!grid_fits(grid)) return ADACLUSTER_E_UNSUPPORTED;
+  if (rt == 64) {
+    if (d == 64) block_attn_wide<64, 2><<<(int)grid, 128, 0, s>>>(a, rts, (int)items);
+    else block_attn_wide<128, 2><<<(int)grid, 128, 0, s>>>(a, rts, (int)items);
+  } else {
+    if (d == 64) block_attn_wide<64, 4><<<(int)grid, 256, 0, s>>>(a, rts, (int)items);
+    else block_attn_wide<128, 4><<<(int)grid, 256, 0, s>>>(a, rts, (int)items);
+  }
+  return launched();
+}
+
+}  // namespace adac

@@ -138,6 +138,15 @@ LAYOUTS = [  # d, page, Hq, Hkv, lens, news, qblock, topk, keep_first
     (128, 32, 2, 2, [90, 40], [20, 60], 64, 5, 1),           # more queries than positions
     (64, 16, 1, 1, [1000, 3], [1, 1], 1, 20, 1),
 ]
+# blocks of many rows and launches large enough for the kernel that stages tiles for all waves
+LAYOUTS_WIDE = [
+    (128, 16, 16, 4, [700, 333], [650, 333], 16, 9, 1),      # 64 rows a block
+    (64, 32, 24, 8, [400, 97], [400, 20], 17, 7, 2),         # 51 rows
+    (128, 64, 36, 4, [390, 64, 1], [390, 64, 1], 13, 4, 0),  # 117 rows
+    (64, 128, 32, 8, [515], [515], 100, 3, 1),               # 400 rows: four workgroups a block, the last ragged
+    (128, 128, 40, 40, [300], [300], 64, 4, 1),
+    (64, 16, 64, 1, [1300], [300], 1, 600, 0),               # a list longer than what is held at a time
+]
 
 
 @pytest.mark.parametrize("causal", [1, 0])
@@ -145,6 +154,17 @@ LAYOUTS = [  # d, page, Hq, Hkv, lens, news, qblock, topk, keep_first
 @pytest.mark.parametrize("dtype,bits", [(BF, 0), (F, 0), (BF, 4), (F, 4)])
 @pytest.mark.parametrize("layout", LAYOUTS)
 def test_attention_over_a_cache(layout, dtype, bits, listed, causal):
+    _attention_over_a_cache(layout, dtype, bits, listed, causal)
+
+
+@pytest.mark.parametrize("causal", [1, 0])
+@pytest.mark.parametrize("listed", [False, True])
+@pytest.mark.parametrize("layout", LAYOUTS_WIDE)
+def test_attention_of_many_rows(layout, listed, causal):
+    _attention_over_a_cache(layout, BF, 0, listed, causal)
+
+
+def _attention_over_a_cache(layout, dtype, bits, listed, causal):
     d, page, Hq, Hkv, lens, news, qblock, topk, first = layout
     x = Batch(dtype, bits, d, page, Hq, Hkv, lens, news, 5)
     p = x.params(qblock=qblock, topk=topk, keep_first=first, causal=causal)
@@ -220,6 +240,11 @@ def test_selection_with_infinities_and_nan():
 
 
 TRAIN = [  # d, page, Hq, Hkv, lens, qblock, topk, causal
+    (128, 64, 16, 4, [700, 130], 32, 3, 1),                  # (from here: launches of the kernels for many rows, in 16 bits)
+    (64, 128, 64, 32, [530], 64, 2, 0),
+    (64, 64, 15, 5, [260, 333, 7], 16, 6, 1),
+    (128, 32, 32, 16, [300], 64, 5, 1),
+    (128, 128, 8, 8, [1100], 128, 3, 1),                     # (to here)
     (64, 16, 2, 1, [50, 1], 4, 4, 1),
     (128, 32, 6, 2, [100, 33, 0], 16, 3, 1),
     (64, 64, 3, 3, [200, 65], 64, 2, 0),
