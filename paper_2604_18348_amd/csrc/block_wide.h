@@ -14,11 +14,19 @@ typedef __attribute__((address_space(3))) void lds_void_t;
 constexpr int TILE = 64;               // rows of a tile, staged as four sixteenths of pages
 constexpr int LIST = 512;              // pages of a list held in LDS at a time
 
-// Rows of D bf16 in LDS, unpadded.  Piece q (16 bytes) of row r sits in slot q ^ swz(r): in ROWS order for reads of one piece of 32
-// rows, in COLS order for transposing reads, both free of bank conflicts; a tile that is read both ways keeps the ROWS order,
-// whose transposing reads meet two rows a bank at most.
-template <int D> __device__ __forceinline__ int swz_rows(int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); }
-template <int D> __device__ __forceinline__ int swz_cols(int r) { return D == 128 ? ((r & 3) << 2) : (((r >> 1) & 1) << 2); }
+// Rows of D bf16 in LDS, unpadded.  Piece q (16 bytes) of row r sits in slot q ^ swz(r).  Sixteen rows that are read at one piece
+// (operands that are rows) lie in sixteen different slots, and the four rows of a transposing read (operands that are columns: 64
+// bytes of rows 4 i .. + 3) in four different 64-byte groups: neither read meets a bank twice.
+template <int D> __device__ __forceinline__ int swz(int r) {
+  return D == 128 ? ((r & 3) << 2 | ((r >> 2) & 3)) : (((r >> 1) & 1) << 2 | ((r >> 2) & 3));
+}
+// Byte addresses of a lane inside a tile: its row operand (row l % 32, dimensions 16 ks + 8 (l / 32) ..) and, for column block db, the
+// first of its two transposing reads (rows 4 (l / 32) .. + 3 of sixteen; the second is 8 rows on, whose slots are other ones).
+template <int D> __device__ __forceinline__ int row_operand(int lane, int ks) { const int c = lane & 31; return c * D * 2 + (((ks * 2 + (lane >> 5)) ^ swz<D>(c)) * 16); }
+template <int D> __device__ __forceinline__ int col_operand(int lane, int db, int second) {
+  const int i16 = lane & 15, r = 4 * (lane >> 5) + (i16 >> 2) + 8 * second, q = db * 4 + 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
+  return r * D * 2 + ((q ^ swz<D>(r)) * 16) + 8 * (i16 & 1);
+}
 
 __device__ __forceinline__ bf16x8_t join_tr(s16x4_tr lo, s16x4_tr hi) {
   union { s16x4_tr h[2]; bf16x8_t v; } u{{lo, hi}};

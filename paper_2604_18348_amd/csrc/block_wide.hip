@@ -61,24 +61,22 @@ __global__ __launch_bounds__(NW * 64) void block_attn_wide(BlockAttnArgs a, int 
   const float sc = a.scale_log2e, lowest = -3.402823466e38f / fmaxf(sc, 1.f);
   float mref = lowest, lrun = 0.f;
 
-  int lrow[PT], piece_k[PT], piece_v[PT];            // this thread's pieces of a tile
+  int lrow[PT], piece[PT];                         // this thread's pieces of a tile
 #pragma unroll
   for (int x = 0; x < PT; ++x) {
     const int item = tid + x * NT;
     lrow[x] = item / CH;
-    piece_k[x] = ((item % CH) ^ swz_rows<D>(lrow[x])) * 16;
-    piece_v[x] = ((item % CH) ^ swz_cols<D>(lrow[x])) * 16;
+    piece[x] = ((item % CH) ^ swz<D>(lrow[x])) * 16;
   }
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t*)lds;
   const int lsub = m.lpage - 4, ktok = (int)(a.ks.token * 2), vtok = (int)(a.vs.token * 2);
-  int kaddr[KS], vaddr[DB];
+  int kaddr[KS], vaddr[DB][2];
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) kaddr[ks] = c * ROWB + (((ks * 2 + hb) ^ swz_rows<D>(c)) * 16);
-  {
-    const int i16 = lane & 15, vrow = 4 * hb + (i16 >> 2), gl = 2 * ((lane >> 4) & 1) + ((i16 & 3) >> 1);
+  for (int ks = 0; ks < KS; ++ks) kaddr[ks] = row_operand<D>(lane, ks);
 #pragma unroll
-    for (int db = 0; db < DB; ++db) vaddr[db] = NBUF * TILEB + vrow * ROWB + (((db * 4 + gl) ^ swz_cols<D>(vrow)) * 16) + 8 * (i16 & 1);
-  }
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) vaddr[db][x] = NBUF * TILEB + col_operand<D>(lane, db, x);
 
   for (int e0 = 0; e0 < entries; e0 += LIST) {
     const int n = fill_list<NT>(m, b, list, e0, entries, pages, pages_l, counts);
@@ -102,8 +100,8 @@ __global__ __launch_bounds__(NW * 64) void block_attn_wide(BlockAttnArgs a, int 
       if (have <= 0) { sub = 0; have = 1; }
       const int r = min(lrow[x] & 15, have - 1);
       const uint32_t dst = lds0 + stage * TILEB + (wave * 64 + x * NT) * 16;
-      if ((op & 1) == 0) dma_b128(dst, (uint32_t)(r * ktok + piece_k[x]), uniform((const char*)a.k + row_at(m, s, a.ks, p.phys, p.pg, sub, hk) * 2));
-      else dma_b128(dst + NBUF * TILEB, (uint32_t)(r * vtok + piece_v[x]), uniform((const char*)a.v + row_at(m, s, a.vs, p.phys, p.pg, sub, hk) * 2));
+      if ((op & 1) == 0) dma_b128(dst, (uint32_t)(r * ktok + piece[x]), uniform((const char*)a.k + row_at(m, s, a.ks, p.phys, p.pg, sub, hk) * 2));
+      else dma_b128(dst + NBUF * TILEB, (uint32_t)(r * vtok + piece[x]), uniform((const char*)a.v + row_at(m, s, a.vs, p.phys, p.pg, sub, hk) * 2));
     };
     int key0[4];                                    // of the tile being worked on
     bool whole;
@@ -195,8 +193,8 @@ __global__ __launch_bounds__(NW * 64) void block_attn_wide(BlockAttnArgs a, int 
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
           for (int s2 = 0; s2 < 2; ++s2) {
-            const char* const p = base + (kb * 32 + 16 * s2) * ROWB + vaddr[db];
-            va[db][kb][s2] = join_tr(read_tr(p), read_tr(p + 8 * ROWB));
+            const char* const p = base + (kb * 32 + 16 * s2) * ROWB;
+            va[db][kb][s2] = join_tr(read_tr(p + vaddr[db][0]), read_tr(p + vaddr[db][1]));
           }
       compiler_fence();
       __builtin_amdgcn_sched_barrier(0);
