@@ -201,12 +201,185 @@ __device__ __forceinline__ Seen block_seen(const BlockDims& m, const BlockSeq& s
   return {first >> m.lpage, (last >> m.lpage) + 1, (last >> m.lpage) + 1};
 }
 
-// Scores of a block of queries against the boxes of pages: S(h, p) = sum_d max(u_d max_pd, u_d min_pd), u the sum of the
-// block's queries of head h, and the largest over the heads that share the keys.  In 64 bits: products of the sums with
-// bfloat16 boxes and their sums are then exact but for terms 2^-50 of the largest, and the list does not hang on the order
-// of a sum.  A lane holds VEC dimensions of u for every head of its group (up to SCORE_HEADS at a time) and reads VEC
-// of either side of a box.  A score that is NaN counts as minus infinity.
+// Scores of a block of queries against the boxes of pages: S(h, p) = sum_d u_d (u_d >= 0 ? max_pd : min_pd), u the sum of the block's
+// queries of head h, and the largest over the heads that share the keys.  In 64 bits: products of the sums with bfloat16 boxes
+// and their sums are then exact but for terms 2^-50 of the largest, and the list does not hang on the order of a sum.  A
+// lane holds VEC dimensions of u for up to SCORE_HEADS heads and reads VEC of either side of a box; LPR lanes a page.
+// A score that is NaN counts as minus infinity.
 constexpr int SCORE_HEADS = 4;
+template <typename T, int D>
+__device__ __forceinline__ void load_box(const BlockDims& m, int b, int hk, int p, const T* __restrict__ boxes, int col, float* mx, float* mn, bool* there) {
+  const int row = m.num_pages ? pool_page(m, b, p) : b * m.max_pages + p;
+  *there = row >= 0;
+  const T* const box = boxes + ((long long)max(row, 0) * m.Hkv + hk) * 2 * D + col;
+  unpack16<T>(*(const u32x4_t*)box, mx);
+  unpack16<T>(*(const u32x4_t*)(box + D), mn);
+}
+template <int VEC, int LPR>
+__device__ __forceinline__ double box_score(const double (*u)[VEC], int H, const float* mx, const float* mn) {
+  double best = -INFINITY;
+#pragma unroll
+  for (int h = 0; h < SCORE_HEADS; ++h) {
+    if (h >= H) break;
+    double c = 0.0;
+#pragma unroll
+    for (int x = 0; x < VEC; ++x) c = fma(u[h][x], (double)(u[h][x] >= 0.0 ? mx[x] : mn[x]), c);
+#pragma unroll
+    for (int o = 1; o < LPR; o <<= 1) c += __shfl_xor(c, o);
+    if (c > best) best = c;
+  }
+  return best + 0.0;                              // (-0 + 0 = 0: equal to it in the order below)
+}
+
+// The larger score has the larger key.
+__device__ __forceinline__ uint64_t order_key(double v) {
+  const uint64_t u = (uint64_t)__double_as_longlong(v + 0.0);
+  return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+
+// The list of one block of queries and head of keys from its scores: its own pages and the first ones, and of the others those of the
+// largest scores, ties to the lowest page, in ascending order.  The border is found digit by digit (8 bits) from the top.
+template <int NT>
+__device__ __forceinline__ void choose(const BlockDims& m, const Seen& see, const double* sc, int32_t* __restrict__ idx, int32_t* __restrict__ cnt) {
+  constexpr int NW = NT / 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int c1 = m.causal ? see.lo : see.seen, c0 = min(m.keep_first, c1);       // pages [c0, c1) are chosen from
+  const int need = m.topk - (see.seen - (c1 - c0));                            // (not below 0: the host has seen to it)
+  __shared__ int32_t s_hist[256], s_wave[NW];
+  __shared__ int32_t s_digit, s_left, s_in;
+  uint64_t prefix = 0, mask = 0;
+  int left = need;                                   // of those that agree with the prefix
+  if (need <= 0) prefix = mask = ~0ull;              // no score reaches it
+  for (int shift = 56; shift >= 0 && need > 0; shift -= 8) {
+    if (tid < 256) s_hist[tid] = 0;
+    __syncthreads();
+    for (int p = c0 + tid; p < c1; p += NT) {
+      const uint64_t key = order_key(sc[p]);
+      if ((key & mask) == prefix) atomicAdd(&s_hist[key >> shift & 255], 1);
+    }
+    __syncthreads();
+    // counts from the top: thread t takes digit 255 - t
+    const int n = tid < 256 ? s_hist[255 - tid] : 0;
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int u = __shfl_up(incl, o); if (lane >= o) incl += u; }
+    if (lane == 63) s_wave[wave] = incl;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) incl += s_wave[w];
+    if (tid < 256 && incl >= left && incl - n < left) { s_digit = 255 - tid; s_left = left - (incl - n); s_in = n; }
+    __syncthreads();
+    prefix |= (uint64_t)s_digit << shift;
+    mask |= 255ull << shift;
+    left = s_left;
+    const bool all = s_left == s_in;                 // the whole digit is taken: the order inside it does not matter
+    __syncthreads();
+    if (all) break;
+  }
+  int written = 0, equal = 0;
+  for (int base = 0; base < see.seen; base += NT) {
+    const int p = base + tid;
+    bool take = p < see.seen && (p < c0 || p >= c1), tie = false;
+    if (p < see.seen && !take) {
+      const uint64_t key = order_key(sc[p]) & mask;
+      take = key > prefix;
+      tie = key == prefix;
+    }
+    const uint64_t ties = __ballot(tie);
+    if (lane == 0) s_wave[wave] = __popcll(ties);
+    __syncthreads();
+    int before = equal + __popcll(ties & ((1ull << lane) - 1));
+    for (int w = 0; w < NW; ++w) { if (w < wave) before += s_wave[w]; equal += s_wave[w]; }
+    take = take || (tie && before < left);
+    __syncthreads();
+    const uint64_t takes = __ballot(take);
+    if (lane == 0) s_wave[wave] = __popcll(takes);
+    __syncthreads();
+    int at = written + __popcll(takes & ((1ull << lane) - 1));
+    for (int w = 0; w < NW; ++w) { if (w < wave) at += s_wave[w]; written += s_wave[w]; }
+    if (take) idx[at] = p;
+    __syncthreads();
+  }
+  if (tid == 0) *cnt = m.topk;
+}
+
+// All pages that can be listed fit: no score is asked.
+template <int NT>
+__device__ __forceinline__ void list_all(const BlockDims& m, const Seen& see, int32_t* __restrict__ idx, int32_t* __restrict__ cnt) {
+  for (int j = threadIdx.x; j < m.topk; j += NT) idx[j] = j < see.seen ? j : -1;
+  if (threadIdx.x == 0) *cnt = see.seen;
+}
+
+// A workgroup a record: sums of the block's queries, scores and list in one launch, u and the scores in LDS.
+constexpr int PICK_PAGES = 4096, PICK_HEADS = 16, PICK_NT = 512;
+template <typename T, int D>
+__global__ __launch_bounds__(PICK_NT) void block_pick(BlockDims m, const T* __restrict__ q, KeyStride qs, const T* __restrict__ boxes,
+                                                      int32_t* __restrict__ sel_idx, int32_t* __restrict__ sel_cnt) {
+  constexpr int VEC = Vec<T>::N, LPR = D / VEC, RPI = PICK_NT / LPR, AHEAD = 4;
+  extern __shared__ __align__(16) double lds[];      // [G][D] sums, then [max_pages] scores; before them the parts of the sums
+  const int hk = blockIdx.x % m.Hkv, i = blockIdx.x / m.Hkv % m.nb, b = blockIdx.x / m.Hkv / m.nb;
+  const BlockSeq s = block_seq(m, b);
+  const Seen see = block_seen(m, s, i);
+  const long long rec = ((long long)b * m.nb + i) * m.Hkv + hk;
+  int32_t* const idx = sel_idx + rec * m.topk;
+  if (see.seen <= m.topk) { list_all<PICK_NT>(m, see, idx, sel_cnt + rec); return; }
+  const int tid = threadIdx.x, col = tid % LPR * VEC;
+  const int t0 = i * m.qblock, t1 = min(t0 + m.qblock, s.nq);
+  double* const u_l = lds;
+  double* const sc = lds + m.G * D;
+  {
+    // vectors of VEC dimensions; where there are fewer than threads, the tokens go to groups of threads whose sums are added in order
+    const int vecs = m.G * LPR, groups = max(1, min(PICK_NT / vecs, t1 - t0)), g = tid / vecs;
+    for (int v = tid % vecs; v < vecs && g < groups; v += PICK_NT) {       // (vecs > threads: one group, several vectors)
+      const int h = v / LPR, c = v % LPR * VEC;
+      double sum[VEC];
+#pragma unroll
+      for (int x = 0; x < VEC; ++x) sum[x] = 0.0;
+      for (int t = t0 + g; t < t1; t += groups) {
+        float w[VEC];
+        unpack16<T>(*(const u32x4_t*)(q + (long long)(s.q0 + t) * qs.token + (hk * m.G + h) * qs.head + c), w);
+#pragma unroll
+        for (int x = 0; x < VEC; ++x) sum[x] += (double)w[x];
+      }
+#pragma unroll
+      for (int x = 0; x < VEC; ++x) (groups > 1 ? sc + g * m.G * D : u_l)[h * D + c + x] = sum[x];
+    }
+    __syncthreads();
+    if (groups > 1) {
+      for (int x = tid; x < m.G * D; x += PICK_NT) {
+        double sum = sc[x];
+        for (int y = 1; y < groups; ++y) sum += sc[y * m.G * D + x];
+        u_l[x] = sum;
+      }
+      __syncthreads();
+    }
+  }
+  const int p1 = m.causal ? see.lo : see.seen;       // own pages need no score
+  for (int h0 = 0; h0 < m.G; h0 += SCORE_HEADS) {
+    double u[SCORE_HEADS][VEC];
+    const int H = min(SCORE_HEADS, m.G - h0);
+#pragma unroll
+    for (int h = 0; h < SCORE_HEADS; ++h)
+#pragma unroll
+      for (int x = 0; x < VEC; ++x) u[h][x] = h < H ? u_l[(h0 + h) * D + col + x] : 0.0;
+    for (int p = tid / LPR; p < p1; p += RPI * AHEAD) {
+      float mx[AHEAD][VEC], mn[AHEAD][VEC];
+      bool there[AHEAD];
+#pragma unroll
+      for (int y = 0; y < AHEAD; ++y) load_box<T, D>(m, b, hk, min(p + y * RPI, p1 - 1), boxes, col, mx[y], mn[y], &there[y]);
+#pragma unroll
+      for (int y = 0; y < AHEAD; ++y) {
+        const int at = p + y * RPI;
+        double best = box_score<VEC, LPR>(u, H, mx[y], mn[y]);
+        if (!there[y]) best = -INFINITY;
+        if (col == 0 && at < p1) sc[at] = h0 ? fmax(sc[at], best) : best;
+      }
+    }
+  }
+  __syncthreads();
+  choose<PICK_NT>(m, see, sc, idx, sel_cnt + rec);
+}
+
+// Few records over long contexts: scores by many workgroups, to memory, and the lists from there.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void block_scores(BlockDims m, const T* __restrict__ q, KeyStride qs, const T* __restrict__ boxes,
                                                     double* __restrict__ scores, int pieces, int per) {
@@ -235,106 +408,23 @@ __global__ __launch_bounds__(256) void block_scores(BlockDims m, const T* __rest
         }
     }
     for (int p = p0 + tid / LPR; p < p1; p += RPI) {
-      const int row = m.num_pages ? pool_page(m, b, p) : b * m.max_pages + p;
-      double best = -INFINITY;
-      if (row >= 0) {
-        const T* const box = boxes + ((long long)row * m.Hkv + hk) * 2 * D + col;
-        float mx[VEC], mn[VEC];
-        unpack16<T>(*(const u32x4_t*)box, mx);
-        unpack16<T>(*(const u32x4_t*)(box + D), mn);
-#pragma unroll
-        for (int h = 0; h < SCORE_HEADS; ++h) {
-          double c = 0.0;
-#pragma unroll
-          for (int x = 0; x < VEC; ++x) c = fma(u[h][x], (double)(u[h][x] >= 0.0 ? mx[x] : mn[x]), c);
-#pragma unroll
-          for (int o = 1; o < LPR; o <<= 1) c += __shfl_xor(c, o);
-          if (h < H && c > best) best = c;
-        }
-      }
-      if (col == 0) out[p] = h0 ? fmax(out[p], best) : best + 0.0;      // (-0 + 0 = 0: equal to it in the order below)
+      float mx[VEC], mn[VEC];
+      bool there;
+      load_box<T, D>(m, b, hk, p, boxes, col, mx, mn, &there);
+      double best = box_score<VEC, LPR>(u, H, mx, mn);
+      if (!there) best = -INFINITY;
+      if (col == 0) out[p] = h0 ? fmax(out[p], best) : best;
     }
   }
 }
 
-// The larger score has the larger key.
-__device__ __forceinline__ uint64_t order_key(double v) {
-  const uint64_t u = (uint64_t)__double_as_longlong(v + 0.0);
-  return u >> 63 ? ~u : u | 0x8000000000000000ull;
-}
-
-// Pages of one block of queries and head of keys: its own pages and the first ones, and of the others those of the largest
-// scores, ties to the lowest page, in ascending order.  The border is found digit by digit (8 bits) from the top.
 __global__ __launch_bounds__(256) void block_topk(BlockDims m, const double* __restrict__ scores, int32_t* __restrict__ sel_idx, int32_t* __restrict__ sel_cnt) {
   const int hk = blockIdx.x % m.Hkv, i = blockIdx.x / m.Hkv % m.nb, b = blockIdx.x / m.Hkv / m.nb;
   const BlockSeq s = block_seq(m, b);
   const Seen see = block_seen(m, s, i);
   const long long rec = ((long long)b * m.nb + i) * m.Hkv + hk;
-  int32_t* const idx = sel_idx + rec * m.topk;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  if (see.seen <= m.topk) {
-    for (int j = tid; j < m.topk; j += 256) idx[j] = j < see.seen ? j : -1;
-    if (tid == 0) sel_cnt[rec] = see.seen;
-    return;
-  }
-  const double* const sc = scores + rec * m.max_pages;
-  const int c0 = min(m.keep_first, m.causal ? see.lo : see.seen), c1 = m.causal ? see.lo : see.seen;       // pages [c0, c1) are chosen from
-  const int need = m.topk - (see.seen - (c1 - c0));                                                       // (not below 0: the host has seen to it)
-  __shared__ int32_t s_hist[256], s_wave[4];
-  __shared__ int32_t s_digit, s_left, s_in;
-  uint64_t prefix = 0, mask = 0;
-  int left = need;                                   // of those that agree with the prefix
-  if (need <= 0) prefix = mask = ~0ull;              // no score reaches it
-  for (int shift = 56; shift >= 0 && need > 0; shift -= 8) {
-    s_hist[tid] = 0;
-    __syncthreads();
-    for (int p = c0 + tid; p < c1; p += 256) {
-      const uint64_t key = order_key(sc[p]);
-      if ((key & mask) == prefix) atomicAdd(&s_hist[key >> shift & 255], 1);
-    }
-    __syncthreads();
-    // counts from the top: thread t takes digit 255 - t
-    const int n = s_hist[255 - tid];
-    int incl = n;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) { const int u = __shfl_up(incl, o); if (lane >= o) incl += u; }
-    if (lane == 63) s_wave[wave] = incl;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) incl += s_wave[w];
-    if (incl >= left && incl - n < left) { s_digit = 255 - tid; s_left = left - (incl - n); s_in = n; }
-    __syncthreads();
-    prefix |= (uint64_t)s_digit << shift;
-    mask |= 255ull << shift;
-    left = s_left;
-    const bool all = s_left == s_in;                 // the whole digit is taken: the order inside it does not matter
-    __syncthreads();
-    if (all) break;
-  }
-  int written = 0, equal = 0;
-  for (int base = 0; base < see.seen; base += 256) {
-    const int p = base + tid;
-    bool take = p < see.seen && (p < c0 || p >= c1), tie = false;
-    if (p < see.seen && !take) {
-      const uint64_t key = order_key(sc[p]) & mask;
-      take = key > prefix;
-      tie = key == prefix;
-    }
-    const uint64_t ties = __ballot(tie);
-    if (lane == 0) s_wave[wave] = __popcll(ties);
-    __syncthreads();
-    int before = equal + __popcll(ties & ((1ull << lane) - 1));
-    for (int w = 0; w < 4; ++w) { if (w < wave) before += s_wave[w]; equal += s_wave[w]; }
-    take = take || (tie && before < left);
-    __syncthreads();
-    const uint64_t takes = __ballot(take);
-    if (lane == 0) s_wave[wave] = __popcll(takes);
-    __syncthreads();
-    int at = written + __popcll(takes & ((1ull << lane) - 1));
-    for (int w = 0; w < 4; ++w) { if (w < wave) at += s_wave[w]; written += s_wave[w]; }
-    if (take) idx[at] = p;
-    __syncthreads();
-  }
-  if (tid == 0) sel_cnt[rec] = m.topk;
+  if (see.seen <= m.topk) list_all<256>(m, see, sel_idx + rec * m.topk, sel_cnt + rec);
+  else choose<256>(m, see, scores + rec * m.max_pages, sel_idx + rec * m.topk, sel_cnt + rec);
 }
 
 }  // namespace
@@ -372,13 +462,28 @@ int launch_block_boxes(hipStream_t s, int dtype, int d, const BlockDims& m, cons
   return launched();
 }
 
-size_t block_select_bytes(const BlockDims& m) { return (size_t)m.B * m.nb * m.Hkv * m.max_pages * sizeof(double); }
+// Whether a workgroup a record does (its u and scores in LDS): there are enough records to fill the chip, or few pages.
+static bool picks(const BlockDims& m) {
+  const long long recs = (long long)m.B * m.nb * m.Hkv;
+  return m.max_pages <= PICK_PAGES && m.G <= PICK_HEADS && (recs >= 128 || m.max_pages <= 1024);
+}
+
+size_t block_select_bytes(const BlockDims& m) { return picks(m) ? 0 : (size_t)m.B * m.nb * m.Hkv * m.max_pages * sizeof(double); }
 
 int launch_block_select(hipStream_t s, int dtype, int d, const BlockDims& m, const void* q, KeyStride qs, const void* boxes,
                         int32_t* sel_idx, int32_t* sel_cnt, void* ws) {
   const long long recs = (long long)m.B * m.nb * m.Hkv;
   const int per = 256, pieces = (m.max_pages + per - 1) / per;
-  if (!grid_fits(recs * pieces)) return ADACLUSTER_E_UNSUPPORTED;
+  if (!grid_fits(recs * (picks(m) ? PICK_NT / 256 : pieces))) return ADACLUSTER_E_UNSUPPORTED;
+  if (picks(m)) {
+    // sums, then scores or the parts of the sums (PICK_NT vectors of 16 bytes' elements at most)
+    const int vec = dtype == ADACLUSTER_BF16 ? 8 : 4, parts = PICK_NT * vec;
+    const size_t lds = ((size_t)m.G * d + (m.max_pages > parts ? m.max_pages : parts)) * sizeof(double);
+#define CALL(T, D) block_pick<T, D><<<(int)recs, PICK_NT, lds, s>>>(m, (const T*)q, qs, (const T*)boxes, sel_idx, sel_cnt)
+    BY_TYPE(dtype, d, CALL)
+#undef CALL
+    return launched();
+  }
   if (m.max_pages > m.topk) {
 #define CALL(T, D) block_scores<T, D><<<(int)(recs * pieces), 256, 0, s>>>(m, (const T*)q, qs, (const T*)boxes, (double*)ws, pieces, per)
     BY_TYPE(dtype, d, CALL)

@@ -8,16 +8,11 @@ namespace {
 // NW waves of 32 rows each.  A tile's keys and values go global -> LDS directly, 16 bytes a lane, one tile ahead of
 // the products.  Rows past a sequence's end are read from the last row there is in
 // their sixteenth (or the page's first) and masked: nothing behind the end is touched.
-struct Part { int pg, phys, sub; };          // a sixteenth of a page
-__device__ __forceinline__ int pick(int i, int a, int b, int c, int d) { return i < 2 ? i == 0 ? a : b : i == 2 ? c : d; }
-
 template <int D, int NW>
-__global__ __launch_bounds__(NW * 64) void block_attn_wide(BlockAttnArgs a, int rts, int items) {
+__global__ __launch_bounds__(NW * 64, 8 / NW) void block_attn_wide(BlockAttnArgs a, int rts, int items) {
   constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
-  constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB, NBUF = 2, VM_STEP = 2 * PT;
-  constexpr int STRIDE = 2 * KS / VM_STEP, J0 = 2 * KS - 1 - (VM_STEP - 1) * STRIDE < 3 ? 2 * KS - 1 - (VM_STEP - 1) * STRIDE : 3;
-  static_assert(STRIDE >= 1 && J0 >= 0, "every request finds a product to go behind");
-  __shared__ __align__(16) char lds[2 * NBUF * TILEB];
+  constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB;
+  __shared__ __align__(16) char lds[4 * TILEB];
   __shared__ int2 pages_l[LIST];
   __shared__ int32_t counts[NW];
   const BlockDims& m = a.m;
@@ -43,7 +38,7 @@ __global__ __launch_bounds__(NW * 64) void block_attn_wide(BlockAttnArgs a, int 
     }
   }
   const int lim = there ? (m.causal ? min(s.n, s.first + tok + 1) : s.n) : INT32_MAX;      // (a row that is not there needs no mask)
-  const int wave_first = base_row + wave * 32, wave_last = min(wave_first + 32, rows) - 1;
+  const int wave_first = base_row + wave * 32;
   const bool wave_has_rows = wave_first < rows;
   const int minlim = m.causal ? min(s.n, s.first + t0 + wave_first / m.G + 1) : s.n;       // keys below: seen by all rows of the wave
   const int last = min(base_row + NT / 2, rows) - 1;
@@ -51,7 +46,6 @@ __global__ __launch_bounds__(NW * 64) void block_attn_wide(BlockAttnArgs a, int 
   const int pages = maxlim > 0 ? (maxlim + m.page - 1) >> m.lpage : 0;
   const int32_t* const list = a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
   const int entries = list ? m.topk : pages;
-  (void)wave_last;
 
   f32x16_t oacc[DB];
 #pragma unroll
@@ -76,157 +70,109 @@ __global__ __launch_bounds__(NW * 64) void block_attn_wide(BlockAttnArgs a, int 
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int x = 0; x < 2; ++x) vaddr[db][x] = NBUF * TILEB + col_operand<D>(lane, db, x);
+    for (int x = 0; x < 2; ++x) vaddr[db][x] = col_operand<D>(lane, db, x);
 
   for (int e0 = 0; e0 < entries; e0 += LIST) {
     const int n = fill_list<NT>(m, b, list, e0, entries, pages, pages_l, counts);
     const int parts = n << lsub, tiles = (parts + 3) >> 2;
     if (!tiles) continue;
-    // the four sixteenths of tile t (past the end: the last one again)
-    Part next[4];
-    auto look = [&](int t) __attribute__((always_inline)) {
+    auto issue = [&](int stage, int t) __attribute__((always_inline)) {
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int part = min(t * 4 + x, parts - 1);
+      for (int x = 0; x < PT; ++x) {                // a wave's request lies inside one sixteenth of a page
+        const int part = min(t * 4 + (((wave * 64 + x * NT) / CH) >> 4), parts - 1);
         const int2 pp = pages_l[part >> lsub];
-        next[x] = Part{__builtin_amdgcn_readfirstlane(pp.x), __builtin_amdgcn_readfirstlane(pp.y), part & ((1 << lsub) - 1)};
+        const int pg = uniform(pp.x), phys = uniform(pp.y);
+        int sub = part & ((1 << lsub) - 1), have = s.n - ((pg << m.lpage) + sub * 16);      // rows of it that exist
+        if (have <= 0) { sub = 0; have = 1; }
+        const int r = min(lrow[x] & 15, have - 1);
+        const uint32_t dst = lds0 + stage * 2 * TILEB + (wave * 64 + x * NT) * 16;
+        dma_b128(dst, (uint32_t)(r * ktok + piece[x]), uniform((const char*)a.k + row_at(m, s, a.ks, phys, pg, sub, hk) * 2));
+        dma_b128(dst + TILEB, (uint32_t)(r * vtok + piece[x]), uniform((const char*)a.v + row_at(m, s, a.vs, phys, pg, sub, hk) * 2));
       }
     };
-    // request `op` of the tile looked up last: even keys, odd values; a wave's request lies inside one sixteenth
-    auto issue = [&](int stage, int op) __attribute__((always_inline)) {
-      const int x = op >> 1, at = ((wave * 64 + x * NT) / CH) >> 4;
-      const Part p{pick(at, next[0].pg, next[1].pg, next[2].pg, next[3].pg), pick(at, next[0].phys, next[1].phys, next[2].phys, next[3].phys), pick(at, next[0].sub, next[1].sub, next[2].sub, next[3].sub)};
-      int sub = p.sub, have = s.n - ((p.pg << m.lpage) + sub * 16);      // rows of the sixteenth that exist
-      if (have <= 0) { sub = 0; have = 1; }
-      const int r = min(lrow[x] & 15, have - 1);
-      const uint32_t dst = lds0 + stage * TILEB + (wave * 64 + x * NT) * 16;
-      if ((op & 1) == 0) dma_b128(dst, (uint32_t)(r * ktok + piece[x]), uniform((const char*)a.k + row_at(m, s, a.ks, p.phys, p.pg, sub, hk) * 2));
-      else dma_b128(dst + NBUF * TILEB, (uint32_t)(r * vtok + piece[x]), uniform((const char*)a.v + row_at(m, s, a.vs, p.phys, p.pg, sub, hk) * 2));
-    };
-    int key0[4];                                    // of the tile being worked on
-    bool whole;
-    auto turn = [&](int t) __attribute__((always_inline)) {      // the tile looked up last, number t, is worked on next
-      whole = true;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        key0[x] = t * 4 + x < parts ? (next[x].pg << m.lpage) + next[x].sub * 16 : INT32_MAX - 64;
-        whole = whole && key0[x] + 16 <= minlim;
-      }
-    };
-    auto compute = [&](int stage, int t, auto&& request) __attribute__((always_inline)) {
-      const char* const base = lds + stage * TILEB;
-      f32x16_t sacc[2];
-      bf16x8_t ka[2][KS];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) ka[kb][ks] = *(const bf16x8_t*)(base + kb * 32 * ROWB + kaddr[ks]);
-      compiler_fence();
-      look(t + 1);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          sacc[kb] = mfma32(ka[kb][ks], qf[ks], ks == 0 ? zero16() : sacc[kb]);
-          const int j = kb * KS + ks;
-          if (j >= J0 && (j - J0) % STRIDE == 0 && (j - J0) / STRIDE < VM_STEP) {
-            __builtin_amdgcn_sched_barrier(0);
-            request((j - J0) / STRIDE);
-            __builtin_amdgcn_sched_barrier(0);
-          }
-        }
-      compiler_fence();
-      if (!whole) {
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int v = 0; v < 16; ++v)
-            if (key0[kb * 2 + (v >> 3)] + 8 * ((v >> 2) & 1) + 4 * hb + (v & 3) >= lim) sacc[kb][v] = -INFINITY;
-      }
-      // p = 2^((s - reference) scale): any reference gives the same result as long as nothing overflows, or vanishes against a row
-      // that has had no larger score.  The tile's row sum tells: past its limit, or the reference still the lowest.
-      bf16x8_t pf[2][2];
-      float rsum;
-      auto weights = [&]() __attribute__((always_inline)) {
-        const float off = mref * sc;
-        float part[4];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int s2 = 0; s2 < 2; ++s2) {
-            f32x16_t& x = sacc[kb];
-            union { uint32_t w[4]; bf16x8_t v; } u;
-            part[2 * kb + s2] = 0.f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float p0 = __builtin_amdgcn_exp2f(fmaf(x[8 * s2 + 2 * j], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(x[8 * s2 + 2 * j + 1], sc, -off));
-              u.w[j] = pack_bf16x2(p0, p1);
-              part[2 * kb + s2] += p0;              // (not the rounded ones: the sum's logarithm is an output)
-              part[2 * kb + s2] += p1;
-            }
-            pf[kb][s2] = u.v;
-          }
-        rsum = (part[0] + part[1]) + (part[2] + part[3]);
-      };
-      weights();
-      if (__any(!(rsum <= 65536.f))) {
-        float top = sacc[0][0];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) top = fmaxf(top, sacc[kb][v]);
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float next = fmaxf(mref, top), alpha = __builtin_amdgcn_exp2f((mref - next) * sc);
-        mref = next;
-        lrun *= alpha;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
-        weights();
-      }
-      lrun += rsum;
-      compiler_fence();
-      bf16x8_t va[DB][2][2];
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int s2 = 0; s2 < 2; ++s2) {
-            const char* const p = base + (kb * 32 + 16 * s2) * ROWB;
-            va[db][kb][s2] = join_tr(read_tr(p + vaddr[db][0]), read_tr(p + vaddr[db][1]));
-          }
-      compiler_fence();
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int s2 = 0; s2 < 2; ++s2) oacc[db] = mfma32(va[db][kb][s2], pf[kb][s2], oacc[db]);
-    };
-    look(0);
-#pragma unroll
-    for (int op = 0; op < VM_STEP; ++op) issue(0, op);
-    turn(0);
+    issue(0, 0);
     wait_vmcnt<0>();
     lds_barrier();
-    auto step = [&](auto stage, int t) __attribute__((always_inline)) {      // (loads past the end too: one more tile, never read)
-      constexpr int U = decltype(stage)::value;
-      auto request = [&](int op) __attribute__((always_inline)) { issue(1 - U, op); };
-      if (wave_has_rows) compute(U, t, request);
-      else {
-        look(t + 1);
+    for (int t = 0; t < tiles; ++t) {
+      if (t + 1 < tiles) issue((t + 1) & 1, t + 1);
+      if (wave_has_rows) {
+        const char* const kt = lds + (t & 1) * 2 * TILEB;
+        const char* const vt = kt + TILEB;
+        f32x16_t sacc[2];
 #pragma unroll
-        for (int op = 0; op < VM_STEP; ++op) request(op);
+        for (int kb = 0; kb < 2; ++kb) {
+          sacc[kb] = zero16();
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) sacc[kb] = mfma32(*(const bf16x8_t*)(kt + kb * 32 * ROWB + kaddr[ks]), qf[ks], sacc[kb]);
+        }
+        int key0[4];
+        bool whole = true;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int part = t * 4 + x, pg = uniform(pages_l[min(part, parts - 1) >> lsub].x);
+          key0[x] = part < parts ? (pg << m.lpage) + (part & ((1 << lsub) - 1)) * 16 : INT32_MAX - 64;
+          whole = whole && key0[x] + 16 <= minlim;
+        }
+        if (!whole) {
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v)
+              if (key0[kb * 2 + (v >> 3)] + 8 * ((v >> 2) & 1) + 4 * hb + (v & 3) >= lim) sacc[kb][v] = -INFINITY;
+        }
+        // p = 2^((s - reference) scale): any reference gives the same result as long as nothing overflows.  The row sum of the tile
+        // tells (on the first tile with a score above -inf it is infinite): only then is the tile's maximum taken, the reference
+        // moved up to it and the accumulator scaled.
+        bf16x8_t pf[2][2];
+        float rsum;
+        auto weights = [&]() __attribute__((always_inline)) {
+          const float off = mref * sc;
+          float part[4];
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int s2 = 0; s2 < 2; ++s2) {
+              const f32x16_t& x = sacc[kb];
+              union { uint32_t w[4]; bf16x8_t v; } u;
+              part[2 * kb + s2] = 0.f;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float p0 = __builtin_amdgcn_exp2f(fmaf(x[8 * s2 + 2 * j], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(x[8 * s2 + 2 * j + 1], sc, -off));
+                u.w[j] = pack_bf16x2(p0, p1);
+                part[2 * kb + s2] += p0;            // (not the rounded ones: the sum's logarithm is an output)
+                part[2 * kb + s2] += p1;
+              }
+              pf[kb][s2] = u.v;
+            }
+          rsum = (part[0] + part[1]) + (part[2] + part[3]);
+        };
+        weights();
+        if (__any(!(rsum <= 65536.f))) {
+          float top = sacc[0][0];
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) top = fmaxf(top, sacc[kb][v]);
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float next = fmaxf(mref, top), alpha = __builtin_amdgcn_exp2f((mref - next) * sc);
+          mref = next;
+          lrun *= alpha;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+          weights();
+        }
+        lrun += rsum;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int s2 = 0; s2 < 2; ++s2) {
+            const char* const p = vt + (kb * 32 + 16 * s2) * ROWB;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) oacc[db] = mfma32(join_tr(read_tr(p + vaddr[db][0]), read_tr(p + vaddr[db][1])), pf[kb][s2], oacc[db]);
+          }
       }
-      turn(t + 1);
       wait_vmcnt<0>();
       lds_barrier();
-    };
-    for (int t = 0; t < tiles; t += 2) {
-      step(std::integral_constant<int, 0>{}, t);
-      if (t + 1 < tiles) step(std::integral_constant<int, 1>{}, t + 1);
     }
     lds_barrier();                                  // before the list is filled again
   }

@@ -204,6 +204,10 @@ def _check_selection(x, p, sel, cnt):
     (F, 64, 16, 6, 1, [4097], [1], 1, 100, 0),
     (BF, 64, 32, 9, 1, [3000, 700], [100, 33], 16, 20, 2),
     (BF, 128, 16, 4, 2, [9000], [40], 8, 2, 0),              # room for the own pages alone (causal), or little more
+    (BF, 64, 16, 2, 1, [17000], [1], 1, 50, 1),              # few records of many pages: scores in memory
+    (F, 128, 16, 5, 1, [20000, 90], [6, 6], 3, 30, 1),
+    (BF, 64, 128, 40, 2, [700], [9], 9, 3, 1),               # more heads than a workgroup holds sums of
+    (F, 128, 16, 16, 1, [1000], [200], 64, 9, 1),
 ])
 def test_selection_of_long_contexts(dtype, d, page, Hq, Hkv, lens, news, qblock, topk, first, causal):
     x = Batch(dtype, 0, d, page, Hq, Hkv, lens, news, 11)
