@@ -8,8 +8,10 @@ and there is no fallback: a missing library or a failing call raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 import operator
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -157,7 +159,7 @@ def load_library():
     lib.adacluster_mfma_probe.argtypes = [ctypes.c_int32, vp, sz, ctypes.POINTER(ctypes.c_double), vp]
     lib.adacluster_stats_fetch.argtypes = [P, vp, sz, ctypes.POINTER(CHeadStats), vp]
     lib.adacluster_quest_scores.argtypes = [ctypes.c_int32] * 7 + [vp] * 5
-    BP = ctypes.POINTER(CBlockParams)
+    BP = vp                                            # (the bytes of a CBlockParams, or a pointer to one)
     lib.adacluster_block_workspace_bytes.argtypes = [BP, ctypes.c_int32, ctypes.POINTER(sz)]
     lib.adacluster_cache_append.argtypes = [BP] + [vp] * 11
     lib.adacluster_cache_read.argtypes = [BP] + [vp] * 10
@@ -440,48 +442,62 @@ def adacluster_dense_attn(p: Params, Q, K, V, out=None, ws=None):
 # ---- attention over pages of keys ---------------------------------------------------------------------------------------
 
 BLOCK_SELECT, BLOCK_ATTN, BLOCK_BACKWARD = 0, 1, 2
-_block_values = operator.attrgetter("B", "Hq", "Hkv", "d", "dtype", "bits", "page", "max_pages", "max_q", "qblock", "causal", "topk", "keep_first",
-                                    "softmax_scale")
+_block_values = operator.attrgetter("B", "Hq", "Hkv", "d", "dtype", "bits", "page")
+_block_more = operator.attrgetter("max_pages", "max_q", "qblock", "causal", "topk", "keep_first")
+_block_pack = struct.Struct("@16if22q").pack      # CBlockParams; a token's step of generation is a few calls of 20 us, of which ctypes.Structure would be 5
+_NO2, _NO3 = (0, 0), (0, 0, 0)
 
 
-def _block_c(p: BlockParams, q_rows, k_rows=0, num_pages=0) -> CBlockParams:
-    B_, Hq, Hkv, d, dtype, bits, page, max_pages, max_q, qblock, causal, topk, keep_first, scale = _block_values(p)
-    return CBlockParams(B_, Hq, Hkv, d, dtype, bits, page, num_pages, max_pages, max_q, qblock, causal, topk, keep_first, q_rows, k_rows, scale)
+def _block_c(p: BlockParams, q_rows, k_rows=0, num_pages=0, q=_NO2, o=_NO2, k=_NO3, v=_NO3, new_k=_NO2, new_v=_NO2, d_o=_NO2, dq=_NO2, dk=_NO2,
+             dv=_NO2) -> bytes:
+    """adacluster_block_params as bytes; the rest are the strides."""
+    return _block_pack(*_block_values(p), num_pages, *_block_more(p), q_rows, k_rows, p.softmax_scale, *q, *o, *k, *v, *new_k, *new_v, *d_o, *dq,
+                       *dk, *dv)
 
 
 def _rows(name, t, dtype, heads, d, device):
     """A [rows, heads, d] tensor with d contiguous; its strides of rows and heads."""
-    if t.dtype != dtype or t.dim() != 3 or t.shape[1] != heads or t.shape[2] != d or not t.is_cuda or t.device != device:
+    s = t.shape
+    if len(s) != 3 or s[1] != heads or s[2] != d or t.dtype != dtype or t.device != device:
         raise ValueError(f"{name} must be a [rows, {heads}, {d}] tensor of {dtype} on {device}")
-    s = t.stride()
-    if s[2] != 1:
+    a, b, c = t.stride()
+    if c != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
-    return s[0], s[1]
+    return a, b
+
+
+def _gpu(t):
+    if not t.is_cuda:
+        raise ValueError("tensors must be on a GPU: %s must be a CUDA tensor" % type(t).__name__)
+    return t.device
 
 
 def _ints(name, t, shape, device):
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or t.device != device:
+    if t.shape != shape or t.dtype != torch.int32 or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 tensor {tuple(shape)} on {device}")
 
 
-def _pool(cp, p: BlockParams, cache: BlockCache, device, boxes):
-    """Checks a cache and writes its strides and number of pages into cp."""
-    n, Hkv, page, d = cache.k.shape[0], p.Hkv, p.page, p.d
+def _pool(p: BlockParams, cache: BlockCache, device, boxes):
+    """Checks a cache; its number of pages and the strides of k and v (page, token, head)."""
+    ck, cv, Hkv, page, d = cache.k, cache.v, p.Hkv, p.page, p.d
+    n = ck.shape[0]
+    if boxes:
+        _boxes(cache.boxes, (n, Hkv, 2, d), p, device)
     if p.bits == 4:
-        for name, t, shape, dt in (("k", cache.k, (n, Hkv, page, d // 2), torch.uint8), ("v", cache.v, (n, Hkv, page, d // 2), torch.uint8),
+        for name, t, shape, dt in (("k", ck, (n, Hkv, page, d // 2), torch.uint8), ("v", cv, (n, Hkv, page, d // 2), torch.uint8),
                                    ("k_meta", cache.k_meta, (n, Hkv, page, d // 64, 2), torch.bfloat16),
                                    ("v_meta", cache.v_meta, (n, Hkv, page, d // 64, 2), torch.bfloat16)):
             if t is None or t.shape != shape or t.dtype != dt or not t.is_contiguous() or t.device != device:
                 raise ValueError(f"cache.{name} must be a contiguous {dt} tensor {shape} on {device}")
-    else:
-        for name, t, to in (("k", cache.k, cp.k_stride), ("v", cache.v, cp.v_stride)):
-            if t.shape != (n, Hkv, page, d) or t.dtype != _tdtype(p) or t.stride(3) != 1 or t.device != device:
-                raise ValueError(f"cache.{name} must be a {_tdtype(p)} tensor {(n, Hkv, page, d)} on {device}, its last dimension contiguous")
-            s = t.stride()
-            to[0], to[1], to[2] = s[0], s[2], s[1]
-    if boxes:
-        _boxes(cache.boxes, (n, Hkv, 2, d), p, device)
-    cp.num_pages = n
+        return n, _NO3, _NO3
+    shape, dt = (n, Hkv, page, d), _tdtype(p)
+    out = [n]
+    for name, t in (("k", ck), ("v", cv)):
+        a, b, c, e = t.stride() if t.dim() == 4 else (0, 0, 0, 0)
+        if t.shape != shape or t.dtype != dt or e != 1 or t.device != device:
+            raise ValueError(f"cache.{name} must be a {dt} tensor {shape} on {device}, its last dimension contiguous")
+        out.append((a, c, b))
+    return out
 
 
 def _boxes(t, shape, p, device):
@@ -489,18 +505,38 @@ def _boxes(t, shape, p, device):
         raise ValueError(f"boxes must be a contiguous {_tdtype(p)} tensor {tuple(shape)} on {device}")
 
 
-def _block_ws(cp, call, device, ws):
+@functools.lru_cache(maxsize=1024)
+def _block_bytes(cp: bytes, call):
+    """Workspace of a call: it follows from the parameters alone."""
     n = ctypes.c_size_t(0)
-    _check(load_library().adacluster_block_workspace_bytes(ctypes.byref(cp), call, ctypes.byref(n)), "block_workspace_bytes")
+    _check(load_library().adacluster_block_workspace_bytes(cp, call, ctypes.byref(n)), "block_workspace_bytes")
+    return n.value
+
+
+def _block_ws(cp, call, device, ws):
     if ws is None:
         # a tensor of its own for every call: torch hands memory out by stream, and to a captured graph from that graph's pool
-        ws = torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
-    return ws, 0 if ws is None else ws.numel()
+        n = _block_bytes(cp, call)
+        return (torch.empty(n, dtype=torch.uint8, device=device), n) if n else (None, 0)
+    if ws.dtype != torch.uint8 or not ws.is_contiguous() or ws.device != device:
+        raise ValueError(f"ws must be a contiguous uint8 tensor on {device}")
+    return ws, ws.numel()
 
 
-def _on(device):
-    """The device that owns the tensors made current for a launch, and its current stream."""
-    return torch.cuda.device(device)
+def _on(device, name, *args):
+    """Calls an entry point on the current stream of the device that owns the tensors, which has to be the current one for a launch."""
+    i = device.index
+    fn = getattr(load_library(), name)
+    if i == torch.cuda.current_device():
+        rc = fn(*args, _raw_stream(i))
+    else:
+        with torch.cuda.device(device):
+            rc = fn(*args, _raw_stream(i))
+    if rc:
+        _check(rc, name)
+
+
+_raw_stream = torch._C._cuda_getCurrentRawStream      # (torch.cuda.current_stream(i).cuda_stream makes an object on the way: 2 us)
 
 
 def alloc_cache(p: BlockParams, num_pages, device="cuda"):
@@ -516,64 +552,54 @@ def alloc_cache(p: BlockParams, num_pages, device="cuda"):
 
 
 def adacluster_block_workspace_bytes(p: BlockParams, call, q_rows, k_rows=0, num_pages=0) -> int:
-    out = ctypes.c_size_t(0)
-    cp = _block_c(p, q_rows, k_rows, num_pages)
-    _check(load_library().adacluster_block_workspace_bytes(ctypes.byref(cp), call, ctypes.byref(out)), "block_workspace_bytes")
-    return out.value
+    return _block_bytes(_block_c(p, q_rows, k_rows, num_pages), call)
 
 
 def adacluster_cache_append(p: BlockParams, k, v, cu_new, seq_lens, page_table, cache: BlockCache):
     """Writes new tokens k, v [rows,Hkv,d] into the cache behind the seq_lens[b] tokens that sequence b holds."""
-    dev = k.device
-    cp = _block_c(p, k.shape[0])
-    cp.new_k_stride[:] = _rows("k", k, _tdtype(p), p.Hkv, p.d, dev)
-    cp.new_v_stride[:] = _rows("v", v, _tdtype(p), p.Hkv, p.d, dev)
-    if v.shape[0] != k.shape[0]:
+    dev, dt = _gpu(k), _tdtype(p)
+    rows = k.shape[0]
+    if v.shape[0] != rows:
         raise ValueError("k and v must have the same rows")
     _ints("cu_new", cu_new, (p.B + 1,), dev)
     _ints("seq_lens", seq_lens, (p.B,), dev)
     _ints("page_table", page_table, (p.B, p.max_pages), dev)
-    _pool(cp, p, cache, dev, True)
-    if k.shape[0] == 0:
-        return
-    with _on(dev):
-        _check(load_library().adacluster_cache_append(
-            ctypes.byref(cp), _ptr(k), _ptr(v), _ptr(cu_new), _ptr(seq_lens), _ptr(page_table), _ptr(cache.k), _ptr(cache.v),
-            _ptr(cache.k_meta), _ptr(cache.v_meta), _ptr(cache.boxes), _stream()), "adacluster_cache_append")
+    n, ks, vs = _pool(p, cache, dev, True)
+    cp = _block_c(p, rows, 0, n, k=ks, v=vs, new_k=_rows("k", k, dt, p.Hkv, p.d, dev), new_v=_rows("v", v, dt, p.Hkv, p.d, dev))
+    if rows:
+        _on(dev, "adacluster_cache_append", cp, k.data_ptr(), v.data_ptr(), cu_new.data_ptr(), seq_lens.data_ptr(), page_table.data_ptr(),
+            cache.k.data_ptr(), cache.v.data_ptr(), _ptr(cache.k_meta), _ptr(cache.v_meta), cache.boxes.data_ptr())
 
 
 def adacluster_cache_read(p: BlockParams, cache: BlockCache, cu_new, first, page_table, rows, out=None):
     """Tokens of the cache as values -> k, v [rows,Hkv,d]: of sequence b those from position first[b] on, to its rows by cu_new."""
-    dev = cache.k.device
-    cp = _block_c(p, rows)
+    dev, dt = _gpu(cache.k), _tdtype(p)
     _ints("cu_new", cu_new, (p.B + 1,), dev)
     _ints("first", first, (p.B,), dev)
     _ints("page_table", page_table, (p.B, p.max_pages), dev)
-    _pool(cp, p, cache, dev, False)
+    n, ks, vs = _pool(p, cache, dev, False)
+    shape = (rows, p.Hkv, p.d)
     if out is None:
-        out = tuple(torch.empty((rows, p.Hkv, p.d), dtype=_tdtype(p), device=dev) for _ in range(2))
-    for t in out:
-        if t.shape != (rows, p.Hkv, p.d) or t.dtype != _tdtype(p) or not t.is_contiguous() or t.device != dev:
-            raise ValueError(f"out must be two contiguous {_tdtype(p)} tensors {(rows, p.Hkv, p.d)} on {dev}")
+        out = torch.empty(shape, dtype=dt, device=dev), torch.empty(shape, dtype=dt, device=dev)
+    else:
+        for t in out:
+            if t.shape != shape or t.dtype != dt or not t.is_contiguous() or t.device != dev:
+                raise ValueError(f"out must be two contiguous {dt} tensors {shape} on {dev}")
     if rows:
-        with _on(dev):
-            _check(load_library().adacluster_cache_read(
-                ctypes.byref(cp), _ptr(cu_new), _ptr(first), _ptr(page_table), _ptr(cache.k), _ptr(cache.v), _ptr(cache.k_meta),
-                _ptr(cache.v_meta), _ptr(out[0]), _ptr(out[1]), _stream()), "adacluster_cache_read")
+        _on(dev, "adacluster_cache_read", _block_c(p, rows, 0, n, k=ks, v=vs), cu_new.data_ptr(), first.data_ptr(), page_table.data_ptr(),
+            cache.k.data_ptr(), cache.v.data_ptr(), _ptr(cache.k_meta), _ptr(cache.v_meta), out[0].data_ptr(), out[1].data_ptr())
     return out
 
 
 def adacluster_block_boxes(p: BlockParams, k, cu_k, out=None):
     """Boxes of packed keys [rows,Hkv,d] -> [B,max_pages,Hkv,2,d]."""
-    dev = k.device
-    cp = _block_c(p, 1, k.shape[0])
-    cp.k_stride[1:] = _rows("k", k, _tdtype(p), p.Hkv, p.d, dev)
+    dev, dt = _gpu(k), _tdtype(p)
     _ints("cu_k", cu_k, (p.B + 1,), dev)
     shape = (p.B, p.max_pages, p.Hkv, 2, p.d)
-    boxes = torch.empty(shape, dtype=_tdtype(p), device=dev) if out is None else out
+    boxes = torch.empty(shape, dtype=dt, device=dev) if out is None else out
     _boxes(boxes, shape, p, dev)
-    with _on(dev):
-        _check(load_library().adacluster_block_boxes(ctypes.byref(cp), _ptr(k), _ptr(cu_k), _ptr(boxes), _stream()), "adacluster_block_boxes")
+    _on(dev, "adacluster_block_boxes", _block_c(p, 1, k.shape[0], k=(0, *_rows("k", k, dt, p.Hkv, p.d, dev))), k.data_ptr(), cu_k.data_ptr(),
+        boxes.data_ptr())
     return boxes
 
 
@@ -592,20 +618,19 @@ def _keys_of(p, cu_k, seq_lens, page_table, dev, paged):
 def adacluster_block_select(p: BlockParams, q, cu_q, boxes, cu_k=None, seq_lens=None, page_table=None, k_rows=None, ws=None):
     """Pages of every block of queries -> sel_idx [B,blocks,Hkv,topk], sel_cnt [B,blocks,Hkv].  cu_k: packed keys (k_rows: rows of
     the key tensor, where it has fewer than cu_k says); seq_lens and page_table: a paged cache."""
-    dev = q.device
+    dev = _gpu(q)
     paged = cu_k is None
-    cp = _block_c(p, q.shape[0], 0 if paged else (2 ** 31 - 1 if k_rows is None else k_rows), boxes.shape[0] if paged else 0)
-    cp.q_stride[:] = _rows("q", q, _tdtype(p), p.Hq, p.d, dev)
+    n = boxes.shape[0]
+    cp = _block_c(p, q.shape[0], 0 if paged else (2 ** 31 - 1 if k_rows is None else k_rows), n if paged else 0,
+                  q=_rows("q", q, _tdtype(p), p.Hq, p.d, dev))
     _ints("cu_q", cu_q, (p.B + 1,), dev)
     _keys_of(p, cu_k, seq_lens, page_table, dev, paged)
-    _boxes(boxes, (boxes.shape[0], p.Hkv, 2, p.d) if paged else (p.B, p.max_pages, p.Hkv, 2, p.d), p, dev)
+    _boxes(boxes, (n, p.Hkv, 2, p.d) if paged else (p.B, p.max_pages, p.Hkv, 2, p.d), p, dev)
     idx = torch.empty((p.B, p.blocks, p.Hkv, p.topk), dtype=torch.int32, device=dev)
     cnt = torch.empty((p.B, p.blocks, p.Hkv), dtype=torch.int32, device=dev)
-    with _on(dev):
-        ws, n = _block_ws(cp, BLOCK_SELECT, dev, ws)
-        _check(load_library().adacluster_block_select(
-            ctypes.byref(cp), _ptr(q), _ptr(cu_q), _ptr(cu_k), _ptr(seq_lens), _ptr(page_table), _ptr(boxes), _ptr(idx), _ptr(cnt),
-            _ptr(ws), n, _stream()), "adacluster_block_select")
+    ws, size = _block_ws(cp, BLOCK_SELECT, dev, ws)
+    _on(dev, "adacluster_block_select", cp, q.data_ptr(), cu_q.data_ptr(), _ptr(cu_k), _ptr(seq_lens), _ptr(page_table), boxes.data_ptr(),
+        idx.data_ptr(), cnt.data_ptr(), _ptr(ws), size)
     return idx, cnt
 
 
@@ -613,69 +638,63 @@ def adacluster_block_attn(p: BlockParams, q, cu_q, k=None, v=None, cu_k=None, ca
                           sel_idx=None, out=None, lse=None, ws=None):
     """Attention of q [rows,Hq,d] over packed k, v [rows,Hkv,d] with cu_k, or over a cache with seq_lens and page_table; over the
     pages of sel_idx, or all -> o like q, lse float32 [rows,Hq]."""
-    dev = q.device
-    cp = _block_c(p, q.shape[0])
-    cp.q_stride[:] = _rows("q", q, _tdtype(p), p.Hq, p.d, dev)
+    dev, dt = _gpu(q), _tdtype(p)
+    rows = q.shape[0]
     _ints("cu_q", cu_q, (p.B + 1,), dev)
     _keys_of(p, cu_k, seq_lens, page_table, dev, cache is not None)
-    meta = (None, None)
+    km = vm = None
+    n = k_rows = 0
     if cache is not None:
-        _pool(cp, p, cache, dev, False)
-        k, v, meta, cu_k = cache.k, cache.v, (cache.k_meta, cache.v_meta), None
+        n, ks, vs = _pool(p, cache, dev, False)
+        k, v, km, vm, cu_k = cache.k, cache.v, cache.k_meta, cache.v_meta, None
     else:
-        cp.k_rows = _kv(cp, p, k, v, dev)
+        k_rows, ks, vs = _kv(p, k, v, dev)
     if sel_idx is not None:
         _ints("sel_idx", sel_idx, (p.B, p.blocks, p.Hkv, p.topk), dev)
     o = torch.empty_like(q) if out is None else out
-    cp.o_stride[:] = _rows("out", o, _tdtype(p), p.Hq, p.d, dev)
-    lse = torch.empty((q.shape[0], p.Hq), dtype=torch.float32, device=dev) if lse is None else lse
-    _lse(lse, q, p, dev)
-    if o.shape[0] != q.shape[0]:
+    if lse is None:
+        lse = torch.empty((rows, p.Hq), dtype=torch.float32, device=dev)
+    else:
+        _lse(lse, rows, p, dev)
+    if o.shape[0] != rows:
         raise ValueError("out must have the rows of q")
-    with _on(dev):
-        ws, n = _block_ws(cp, BLOCK_ATTN, dev, ws)
-        _check(load_library().adacluster_block_attn(
-            ctypes.byref(cp), _ptr(q), _ptr(cu_q), _ptr(k), _ptr(v), _ptr(meta[0]), _ptr(meta[1]), _ptr(cu_k), _ptr(seq_lens),
-            _ptr(page_table), _ptr(sel_idx), _ptr(o), _ptr(lse), _ptr(ws), n, _stream()), "adacluster_block_attn")
+    cp = _block_c(p, rows, k_rows, n, q=_rows("q", q, dt, p.Hq, p.d, dev), o=_rows("out", o, dt, p.Hq, p.d, dev), k=ks, v=vs)
+    ws, size = _block_ws(cp, BLOCK_ATTN, dev, ws)
+    _on(dev, "adacluster_block_attn", cp, q.data_ptr(), cu_q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(km), _ptr(vm), _ptr(cu_k), _ptr(seq_lens),
+        _ptr(page_table), _ptr(sel_idx), o.data_ptr(), lse.data_ptr(), _ptr(ws), size)
     return o, lse
 
 
-def _kv(cp, p, k, v, dev):
+def _kv(p, k, v, dev):
     if k is None or v is None or k.shape[0] != v.shape[0]:
         raise ValueError("k and v must be given, with the same rows")
-    cp.k_stride[1:] = _rows("k", k, _tdtype(p), p.Hkv, p.d, dev)
-    cp.v_stride[1:] = _rows("v", v, _tdtype(p), p.Hkv, p.d, dev)
-    return k.shape[0]
+    dt = _tdtype(p)
+    return k.shape[0], (0, *_rows("k", k, dt, p.Hkv, p.d, dev)), (0, *_rows("v", v, dt, p.Hkv, p.d, dev))
 
 
-def _lse(lse, q, p, dev):
-    if lse.shape != (q.shape[0], p.Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != dev:
-        raise ValueError(f"lse must be a contiguous float32 tensor {(q.shape[0], p.Hq)} on {dev}")
+def _lse(lse, rows, p, dev):
+    if lse.shape != (rows, p.Hq) or lse.dtype != torch.float32 or not lse.is_contiguous() or lse.device != dev:
+        raise ValueError(f"lse must be a contiguous float32 tensor {(rows, p.Hq)} on {dev}")
 
 
 def adacluster_block_attn_backward(p: BlockParams, q, k, v, o, lse, d_o, cu_q, cu_k, sel_idx=None, outs=None, ws=None):
     """Gradients of adacluster_block_attn over packed keys -> dq, dk, dv (like q, k, v).  Without `outs`, rows that belong to no
     sequence are zero."""
-    dev = q.device
-    cp = _block_c(p, q.shape[0])
-    cp.q_stride[:] = _rows("q", q, _tdtype(p), p.Hq, p.d, dev)
-    cp.k_rows = _kv(cp, p, k, v, dev)
-    cp.o_stride[:] = _rows("o", o, _tdtype(p), p.Hq, p.d, dev)
-    cp.do_stride[:] = _rows("d_o", d_o, _tdtype(p), p.Hq, p.d, dev)
-    _lse(lse, q, p, dev)
+    dev, dt = _gpu(q), _tdtype(p)
+    rows = q.shape[0]
+    k_rows, ks, vs = _kv(p, k, v, dev)
+    _lse(lse, rows, p, dev)
     _ints("cu_q", cu_q, (p.B + 1,), dev)
     _ints("cu_k", cu_k, (p.B + 1,), dev)
     if sel_idx is not None:
         _ints("sel_idx", sel_idx, (p.B, p.blocks, p.Hkv, p.topk), dev)
     dq, dk, dv = (torch.zeros_like(t) for t in (q, k, v)) if outs is None else outs
-    cp.dq_stride[:] = _rows("dq", dq, _tdtype(p), p.Hq, p.d, dev)
-    cp.dk_stride[:] = _rows("dk", dk, _tdtype(p), p.Hkv, p.d, dev)
-    cp.dv_stride[:] = _rows("dv", dv, _tdtype(p), p.Hkv, p.d, dev)
-    if not (o.shape[0] == d_o.shape[0] == dq.shape[0] == q.shape[0] and dk.shape[0] == dv.shape[0] == k.shape[0]):
+    if not (o.shape[0] == d_o.shape[0] == dq.shape[0] == rows and dk.shape[0] == dv.shape[0] == k_rows):
         raise ValueError("o, d_o and dq must have the rows of q, dk and dv those of k")
-    with _on(dev):
-        ws, n = _block_ws(cp, BLOCK_BACKWARD, dev, ws)
-        _check(load_library().adacluster_block_attn_backward(
-            ctypes.byref(cp), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(lse), _ptr(d_o), _ptr(cu_q), _ptr(cu_k), _ptr(sel_idx),
-            _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ws), n, _stream()), "adacluster_block_attn_backward")
+    at = lambda name, t, heads: _rows(name, t, dt, heads, p.d, dev)  # noqa: E731
+    cp = _block_c(p, rows, k_rows, 0, q=at("q", q, p.Hq), o=at("o", o, p.Hq), k=ks, v=vs, d_o=at("d_o", d_o, p.Hq), dq=at("dq", dq, p.Hq),
+                  dk=at("dk", dk, p.Hkv), dv=at("dv", dv, p.Hkv))
+    ws, size = _block_ws(cp, BLOCK_BACKWARD, dev, ws)
+    _on(dev, "adacluster_block_attn_backward", cp, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), d_o.data_ptr(),
+        cu_q.data_ptr(), cu_k.data_ptr(), _ptr(sel_idx), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(ws), size)
     return dq, dk, dv

@@ -99,13 +99,17 @@ __device__ __forceinline__ f32x4_t mma(float, const u32x4_t& a, const u32x4_t& b
 // acc[16 columns of X from d0][.] += X^T W over 32 rows of X in LDS (row-major, lds_piece); w0, w1: what the lane holds of W's
 // rows 4 quarter .. + 3 of either half, as a result tile leaves it.
 template <int D>
-__device__ __forceinline__ f32x4_t mma_cols(bf16raw, const char* lds, int d0, int lane, const f32x4_t& w0, const f32x4_t& w1, f32x4_t acc) {
+__device__ __forceinline__ f32x4_t mma_cols(const char* lds, int d0, int lane, const bf16x8_t& w, f32x4_t acc) {
   const int r = 4 * (lane >> 4) + ((lane >> 2) & 3), u = d0 / 8 + ((lane >> 1) & 1), in = (lane & 1) * 8;
   const s16x4_tr lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_t*)(lds + lds_piece<bf16raw, D>(r, u) + in));
   const s16x4_tr hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_t*)(lds + lds_piece<bf16raw, D>(r + 16, u) + in));
   union { struct { s16x4_tr lo, hi; } s; bf16x8_t v; } a{{lo, hi}};
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, w, acc, 0, 0, 0);
+}
+template <int D>
+__device__ __forceinline__ f32x4_t mma_cols(bf16raw, const char* lds, int d0, int lane, const f32x4_t& w0, const f32x4_t& w1, f32x4_t acc) {
   union { uint32_t w[4]; bf16x8_t v; } b{{pack_bf16x2(w0[0], w0[1]), pack_bf16x2(w0[2], w0[3]), pack_bf16x2(w1[0], w1[1]), pack_bf16x2(w1[2], w1[3])}};
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, acc, 0, 0, 0);
+  return mma_cols<D>(lds, d0, lane, b.v, acc);
 }
 template <int D>
 __device__ __forceinline__ f32x4_t mma_cols(float, const char* lds, int d0, int lane, const f32x4_t& w0, const f32x4_t& w1, f32x4_t acc) {

@@ -92,7 +92,7 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
   for (int r = 0; r < R; ++r) {
     const int row = base_row + r * 16 + n16, t = t0 + row / m.G;
     const bool there = row < rows;
-    lim[r] = there ? (m.causal ? min(s.n, s.first + t + 1) : s.n) : 0;
+    lim[r] = there ? (m.causal ? min(s.n, s.first + t + 1) : s.n) : INT32_MAX;      // (a row that is not there needs no mask)
     const T* const p = (const T*)a.q + (long long)(s.q0 + t) * a.qs.token + (long long)(hk * m.G + row % m.G) * a.qs.head;
 #pragma unroll
     for (int f = 0; f < NF; ++f) q[r].p[f] = there ? *(const u32x4_t*)(p + piece_at<T, BITS>(f, quarter) * Vec<T>::N) : u32x4_t{0, 0, 0, 0};
@@ -108,21 +108,25 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
           // dimensions 0..7 -> 0 4 1 5 2 6 3 7
           w = u32x4_t{(w[0] & 0xFFFFu) | w[2] << 16, w[0] >> 16 | (w[2] & 0xFFFF0000u), (w[1] & 0xFFFFu) | w[3] << 16, w[1] >> 16 | (w[3] & 0xFFFF0000u)};
         }
-        qsum[r][g] = quarters_sum(sum);
+        qsum[r][g] = quarters_sum(sum);                  // (of 64 dimensions)
       }
     }
   }
   const int last = min(base_row + R * 16, rows) - 1;
   const int maxlim = m.causal ? min(s.n, s.first + t0 + last / m.G + 1) : s.n;      // (no row sees further)
+  const int minlim = m.causal ? min(s.n, s.first + t0 + base_row / m.G + 1) : s.n;      // keys below: seen by all rows
   const int pages = maxlim > 0 ? (maxlim + m.page - 1) >> m.lpage : 0;
   const int32_t* const list = a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
   const int lsub = m.lpage - 4, halves = (list ? m.topk : pages) << lsub, turns = (halves + 1) >> 1;
 
-  float mx[R], sum[R], corr[R][NG];
+  // The weights are taken relative to a reference that moves only when a turn's sum leaves its range (see below); the lowest
+  // value that is finite when scaled too, so that turns a row sees nothing of leave sum and accumulator at zero.
+  const float scale = a.scale_log2e;
+  float ref[R], sum[R], corr[R][NG];
   f32x4_t acc[R][ND];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    mx[r] = -INFINITY; sum[r] = 0.f;
+    ref[r] = -3.402823466e38f / fmaxf(scale, 1.f); sum[r] = 0.f;
 #pragma unroll
     for (int g = 0; g < NG; ++g) corr[r][g] = 0.f;
 #pragma unroll
@@ -133,7 +137,7 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
   for (int turn = split * 4 + wave; turn < turns; turn += a.nsplit * 4) {
     int key0[2];
     RowFrag<T, D> k[2];
-    uint32_t kp[2][4][MW], vp[2][4][MW];              // CODES: (step, lowest) of keys 4 * quarter + i
+    uint32_t kp[2][4][MW], vp[2][4][MW];              // CODES: (step, lowest) of keys 4 * quarter + j
     bool any = false;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -150,19 +154,26 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
         const long long at = ((long long)phys * m.Hkv + hk) * m.page + sub * 16;
         load_raw<T, BITS, D>(kr, a.k, (at + n16) * (D / 2), quarter, there);
         load_raw<T, BITS, D>(vr, a.v, (at + n16) * (D / 2), quarter, there);
+        const int own = CODES ? 4 * quarter : n16;
         if (pg >= 0) {
+          const uint32_t* const km = a.km + (at + own) * MW;
+          const uint32_t* const vm = a.vm + (at + own) * MW;
 #pragma unroll
           for (int x = 0; x < MW; ++x) {
             if constexpr (CODES) {
 #pragma unroll
-              for (int j = 0; j < 4; ++j) { kp[h][j][x] = a.km[(at + 4 * quarter + j) * MW + x]; vp[h][j][x] = a.vm[(at + 4 * quarter + j) * MW + x]; }
-            } else { kn[x] = a.km[(at + n16) * MW + x]; vn[x] = a.vm[(at + n16) * MW + x]; }
+              for (int j = 0; j < 4; ++j) { kp[h][j][x] = km[j * MW + x]; vp[h][j][x] = vm[j * MW + x]; }
+            } else { kn[x] = km[x]; vn[x] = vm[x]; }
           }
-        } else if constexpr (CODES) {
+        }
+        if constexpr (CODES) {
+          if (pg < 0 || key0[h] + 16 > s.n) {            // behind the end lies anything: its weight of 0 must meet a number
 #pragma unroll
-          for (int x = 0; x < MW; ++x)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) kp[h][j][x] = vp[h][j][x] = 0;
+              for (int x = 0; x < MW; ++x)
+                if (pg < 0 || key0[h] + own + j >= s.n) kp[h][j][x] = vp[h][j][x] = 0;
+          }
         }
       } else {
         load_raw<T, BITS, D>(kr, a.k, row_at(m, s, a.ks, phys, pg, sub, hk) + n16 * a.ks.token, quarter, there);
@@ -180,64 +191,85 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
 
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      f32x4_t p[2];
-      float top = -INFINITY;
+      f32x4_t sc[2], p[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        f32x4_t sc{0.f, 0.f, 0.f, 0.f};
+        sc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
         if constexpr (CODES) {
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
-            f32x4_t x{0.f, 0.f, 0.f, 0.f};
+            const float start = -128.f * qsum[r][g];     // what the 128 of every code adds to a product
+            f32x4_t x{start, start, start, start};
             x = mma(T{}, k[h].p[2 * g], q[r].p[2 * g], x);
             x = mma(T{}, k[h].p[2 * g + 1], q[r].p[2 * g + 1], x);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float step = __uint_as_float(kp[h][j][g] << 16), low = __uint_as_float(kp[h][j][g] & 0xFFFF0000u);
-              sc[j] += fmaf(step, x[j], fmaf(-128.f, step, low) * qsum[r][g]);
-            }
+            for (int j = 0; j < 4; ++j)
+              sc[h][j] = fmaf(__uint_as_float(kp[h][j][g] << 16), x[j], fmaf(__uint_as_float(kp[h][j][g] & 0xFFFF0000u), qsum[r][g], sc[h][j]));
           }
         } else {
 #pragma unroll
-          for (int f = 0; f < NF; ++f) sc = mma(T{}, k[h].p[f], q[r].p[f], sc);
+          for (int f = 0; f < NF; ++f) sc[h] = mma(T{}, k[h].p[f], q[r].p[f], sc[h]);
         }
+        if (key0[h] + 16 > minlim) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          p[h][j] = key0[h] + 4 * quarter + j < lim[r] ? sc[j] * a.scale_log2e : -INFINITY;
-          top = fmaxf(top, p[h][j]);
+          for (int j = 0; j < 4; ++j) sc[h][j] = key0[h] + 4 * quarter + j < lim[r] ? sc[h][j] : -INFINITY;
         }
       }
-      top = fmaxf(quarters_max(top), mx[r]);
-      const float ref = top == -INFINITY ? 0.f : top, alpha = __builtin_amdgcn_exp2f(mx[r] - ref);
-      mx[r] = top;
-      sum[r] *= alpha;
+      // p = 2^((s - reference) scale): any reference gives the same result as long as nothing overflows.  The turn's sum tells (it
+      // is infinite at a row's first score above -inf): only then is the maximum taken, the reference moved up to it and what
+      // has been summed scaled.
+      float rsum;
+      auto weights = [&]() __attribute__((always_inline)) {
+        const float off = ref[r] * scale;
+        rsum = 0.f;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) { p[h][j] = __builtin_amdgcn_exp2f(p[h][j] - ref); sum[r] += p[h][j]; }
+          for (int j = 0; j < 4; ++j) { p[h][j] = __builtin_amdgcn_exp2f(fmaf(sc[h][j], scale, -off)); rsum += p[h][j]; }
+      };
+      weights();
+      if (__any(!(rsum <= 65536.f))) {
+        float top = ref[r];
 #pragma unroll
-      for (int x = 0; x < ND; ++x) acc[r][x] *= alpha;
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[h][j]);
+        top = quarters_max(top);
+        const float alpha = __builtin_amdgcn_exp2f((ref[r] - top) * scale);
+        ref[r] = top;
+        sum[r] *= alpha;
+#pragma unroll
+        for (int g = 0; g < NG; ++g) corr[r][g] *= alpha;
+#pragma unroll
+        for (int x = 0; x < ND; ++x) acc[r][x] *= alpha;
+        weights();
+      }
+      sum[r] += rsum;
       if constexpr (CODES) {
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          f32x4_t w[2];
-          float c = corr[r][g] * alpha;
+          // weights times steps, rounded here: what is taken off for the 128 has to be what the product adds.  8 more are taken off
+          // and come back unrounded: the rounding then weighs codes about their middle, not from 0 up.
+          const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
+          union { uint32_t w[4]; bf16x2_t b[4]; bf16x8_t v; } u;
+          float c = 0.f, back = corr[r][g];
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
+          for (int x = 0; x < 4; ++x) {
+            const int h = x >> 1, j = 2 * (x & 1);
+            const float s0 = __uint_as_float(vp[h][j][g] << 16), s1 = __uint_as_float(vp[h][j + 1][g] << 16);
+            u.w[x] = pack_bf16x2(p[h][j] * s0, p[h][j + 1] * s1);
+            c = __builtin_amdgcn_fdot2_f32_bf16(u.b[x], one, c, false);
+            back = fmaf(p[h][j], fmaf(8.f, s0, __uint_as_float(vp[h][j][g] & 0xFFFF0000u)), back);
+            back = fmaf(p[h][j + 1], fmaf(8.f, s1, __uint_as_float(vp[h][j + 1][g] & 0xFFFF0000u)), back);
+          }
+          corr[r][g] = fmaf(-136.f, c, back);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const bool sees = key0[h] + 4 * quarter + j < lim[r];
-              const float step = __uint_as_float(vp[h][j][g] << 16), low = __uint_as_float(vp[h][j][g] & 0xFFFF0000u);
-              // rounded here, so that what is taken off for the 128 is what the product adds.  8 more are taken off and come back
-              // unrounded: the rounding then weighs codes about their middle, not from 0 up
-              w[h][j] = sees ? __uint_as_float((uint32_t)f32_to_bf16(p[h][j] * step) << 16) : 0.f;
-              c = fmaf(-136.f, w[h][j], c);
-              c = sees ? fmaf(p[h][j], fmaf(8.f, step, low), c) : c;
-            }
-          corr[r][g] = c;
-#pragma unroll
-          for (int x = 0; x < 4; ++x) acc[r][4 * g + x] = mma_cols<D>(T{}, vl, 64 * g + 16 * x, lane, w[0], w[1], acc[r][4 * g + x]);
+          for (int x = 0; x < 4; ++x) acc[r][4 * g + x] = mma_cols<D>(vl, 64 * g + 16 * x, lane, u.v, acc[r][4 * g + x]);
         }
+      } else if constexpr (sizeof(T) == 2) {
+        union { uint32_t w[4]; bf16x8_t v; } u{{pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3])}};
+#pragma unroll
+        for (int x = 0; x < ND; ++x) acc[r][x] = mma_cols<D>(vl, 16 * x, lane, u.v, acc[r][x]);
       } else {
 #pragma unroll
         for (int x = 0; x < ND; ++x) acc[r][x] = mma_cols<D>(T{}, vl, 16 * x, lane, p[0], p[1], acc[r][x]);
@@ -264,7 +296,7 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
         const int dim = CODES ? (at & ~7) + code_order(at & 7) : at;
         jo[(wave * 16 + n16) * D + dim] = acc[r][x][j] + c[CODES ? x / 4 : 0];
       }
-    if (quarter == 0) { jm[(wave * 16 + n16) * 2] = mx[r]; jm[(wave * 16 + n16) * 2 + 1] = tot; }
+    if (quarter == 0) { jm[(wave * 16 + n16) * 2] = ref[r] * scale; jm[(wave * 16 + n16) * 2 + 1] = tot; }
     __syncthreads();
     const int jr = tid >> 4, row = base_row + r * 16 + jr, d0 = (tid & 15) * (D / 16);
     float top = -INFINITY, all = 0.f, o[D / 16];

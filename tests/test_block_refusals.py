@@ -2,6 +2,7 @@
 import ctypes
 import os
 import re
+import struct
 
 import pytest
 
@@ -22,7 +23,7 @@ def lib():
 def params(num_pages=8, q_rows=4, k_rows=0, strides=True, **kw):
     base = dict(B=2, Hq=4, Hkv=2, d=64, page=16, max_pages=8, max_q=2, topk=4)
     base.update(kw)
-    c = B._block_c(B.BlockParams(**base), q_rows, k_rows, num_pages)
+    c = B.CBlockParams.from_buffer_copy(B._block_c(B.BlockParams(**base), q_rows, k_rows, num_pages))
     if strides:
         for name, n in B.CBlockParams._fields_[17:]:
             for i in range(n._length_):
@@ -48,6 +49,10 @@ def test_struct_matches_the_header():
     names = [n.strip() for f in re.findall(r"\b(?:int32_t|int64_t|float)\s+([^;]+);", body) for n in f.split(",")]
     mine = [n if not hasattr(t, "_length_") else "%s[%d]" % (n, t._length_) for n, t in B.CBlockParams._fields_]
     assert names == mine
+    assert struct.calcsize("@16if22q") == ctypes.sizeof(B.CBlockParams)
+    c = B.CBlockParams.from_buffer_copy(B._block_c(B.BlockParams(B=3, Hq=8, Hkv=4, d=64, topk=9, softmax_scale=0.5), 5, 6, 7, q=(1, 2), dv=(3, 4)))
+    assert (c.B, c.Hq, c.num_pages, c.topk, c.q_rows, c.k_rows, c.softmax_scale) == (3, 8, 7, 9, 5, 6, 0.5)
+    assert list(c.q_stride) == [1, 2] and list(c.dv_stride) == [3, 4] and list(c.dk_stride) == [0, 0]
 
 
 @pytest.mark.parametrize("kw,code", [
