@@ -64,6 +64,37 @@ __device__ __forceinline__ int list_page(const int32_t* __restrict__ list, int e
   return v >= 0 && v > before && v < pages ? v : -1;
 }
 
+// a value that all lanes share, where the compiler keeps it in a vector register (divisions are made there)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint64_t v = (uint64_t)p;
+  return (const char*)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
+}
+
+// Entries e0, e0 + every, .. below e1 of a list, LIST at most, that name keys of pages below `pages`, in order: {page, place in the
+// pool}.  Returns how many.  A list is looked up once by all threads, so that no load of a key waits for an entry and its page.
+constexpr int LIST = 512;
+template <int NT>
+__device__ __forceinline__ int fill_list(const BlockDims& m, int b, const int32_t* list, int e0, int every, int e1, int pages, int2* out, int32_t* counts) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int n = 0;
+  const int end = (int)min((long long)e1, e0 + (long long)every * LIST);
+  for (int base = e0; base < end; base += NT * every) {
+    const int e = base + tid * every;
+    int pg = e < end ? list_page(list, e, pages) : -1, phys = 0;
+    if (pg >= 0 && m.num_pages) { phys = pool_page(m, b, pg); if (phys < 0) pg = -1; }
+    const uint64_t some = __ballot(pg >= 0);
+    if (lane == 0) counts[wave] = __popcll(some);
+    __syncthreads();
+    int at = n + __popcll(some & ((1ull << lane) - 1));
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) { if (w < wave) at += counts[w]; n += counts[w]; }
+    if (pg >= 0) out[at] = int2{pg, phys};
+    __syncthreads();
+  }
+  return __builtin_amdgcn_readfirstlane(n);
+}
+
 // Where the 16 keys of a sixteenth `sub` of page pg start, in elements from the tensor's base: keys of one head.
 struct Rows { long long at; int key0; };         // key0: position of the first; INT_MAX: there are none
 struct KeyStride { long long page, token, head; };

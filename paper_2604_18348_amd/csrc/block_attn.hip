@@ -72,6 +72,9 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
   constexpr int VBYTES = 32 * D * sizeof(T);
   constexpr int JBYTES = 4 * 16 * D * 4 + 4 * 16 * 2 * 4;
   __shared__ __align__(16) char lds[4 * VBYTES > JBYTES ? 4 * VBYTES : JBYTES];
+  __shared__ __align__(16) uint32_t meta[CODES ? 4 : 1][CODES ? 32 : 1][2 * MW];      // (step, lowest) of a wave's 32 keys and values
+  __shared__ int2 pages_l[LIST];
+  __shared__ int32_t counts[4];
   const BlockDims& m = a.m;
   int id = blockIdx.x;
   const int split = id % a.nsplit; id /= a.nsplit;
@@ -117,7 +120,7 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
   const int minlim = m.causal ? min(s.n, s.first + t0 + base_row / m.G + 1) : s.n;      // keys below: seen by all rows
   const int pages = maxlim > 0 ? (maxlim + m.page - 1) >> m.lpage : 0;
   const int32_t* const list = a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
-  const int lsub = m.lpage - 4, halves = (list ? m.topk : pages) << lsub, turns = (halves + 1) >> 1;
+  const int lsub = m.lpage - 4, entries = list ? m.topk : pages;
 
   // The weights are taken relative to a reference that moves only when a turn's sum leaves its range (see below); the lowest
   // value that is finite when scaled too, so that turns a row sees nothing of leave sum and accumulator at zero.
@@ -134,60 +137,72 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
   }
   char* const vl = lds + wave * VBYTES;
 
-  for (int turn = split * 4 + wave; turn < turns; turn += a.nsplit * 4) {
+  // What a turn reads, in registers one turn ahead (R > 1: in its own turn, the registers hold rows instead).
+  struct Fetch {
+    int key0[2];                                      // INT32_MAX - 64: no keys
+    Raw<T, BITS, D> k[2], v[2];
+    uint32_t pk[2][MW], pv[2][MW];                    // 4 bits: (step, lowest) of the lane's row
+  };
+  for (int e0 = split; e0 < entries; e0 += a.nsplit * LIST) {
+  const int halves = fill_list<256>(m, b, list, e0, a.nsplit, entries, pages, pages_l, counts) << lsub, turns = (halves + 1) >> 1;
+  auto fetch = [&](Fetch& f, int turn) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int half = 2 * turn + h, sub = half & ((1 << lsub) - 1);
+      const bool some = half < halves;
+      const int2 pp = pages_l[some ? half >> lsub : 0];
+      const int pg = uniform(pp.x), phys = uniform(pp.y);
+      f.key0[h] = some ? (pg << m.lpage) + sub * 16 : INT32_MAX - 64;
+      const bool there = f.key0[h] + n16 < s.n;
+      if constexpr (BITS == 4) {
+        const long long at = ((long long)phys * m.Hkv + hk) * m.page + sub * 16 + n16;
+        load_raw<T, BITS, D>(f.k[h], a.k, at * (D / 2), quarter, there);
+        load_raw<T, BITS, D>(f.v[h], a.v, at * (D / 2), quarter, there);
+#pragma unroll
+        for (int x = 0; x < MW; ++x) {                  // (behind the end lies anything: its weight of 0 must meet a number)
+          f.pk[h][x] = there ? a.km[at * MW + x] : 0;
+          f.pv[h][x] = there ? a.vm[at * MW + x] : 0;
+        }
+      } else {
+        load_raw<T, BITS, D>(f.k[h], a.k, row_at(m, s, a.ks, phys, pg, sub, hk) + n16 * a.ks.token, quarter, there);
+        load_raw<T, BITS, D>(f.v[h], a.v, row_at(m, s, a.vs, phys, pg, sub, hk) + n16 * a.vs.token, quarter, there);
+      }
+    }
+  };
+  Fetch next;
+  if (R == 1 && wave < turns) fetch(next, wave);
+  for (int turn = wave; turn < turns; turn += 4) {
+    if (R > 1) fetch(next, turn);
     int key0[2];
     RowFrag<T, D> k[2];
     uint32_t kp[2][4][MW], vp[2][4][MW];              // CODES: (step, lowest) of keys 4 * quarter + j
-    bool any = false;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int half = 2 * turn + h, e = half >> lsub, sub = half & ((1 << lsub) - 1);
-      int pg = half < halves ? list_page(list, e, pages) : -1, phys = 0;
-      if (pg >= 0 && m.num_pages) { phys = pool_page(m, b, pg); if (phys < 0) pg = -1; }
-      key0[h] = pg < 0 ? INT32_MAX - 64 : (pg << m.lpage) + sub * 16;
-      if (key0[h] >= maxlim) pg = -1;
-      any = any || pg >= 0;
-      const bool there = pg >= 0 && key0[h] + n16 < s.n;
-      Raw<T, BITS, D> kr, vr;
-      uint32_t kn[MW] = {}, vn[MW] = {};               // fp32 from codes: of the lane's row
-      if constexpr (BITS == 4) {
-        const long long at = ((long long)phys * m.Hkv + hk) * m.page + sub * 16;
-        load_raw<T, BITS, D>(kr, a.k, (at + n16) * (D / 2), quarter, there);
-        load_raw<T, BITS, D>(vr, a.v, (at + n16) * (D / 2), quarter, there);
-        const int own = CODES ? 4 * quarter : n16;
-        if (pg >= 0) {
-          const uint32_t* const km = a.km + (at + own) * MW;
-          const uint32_t* const vm = a.vm + (at + own) * MW;
-#pragma unroll
-          for (int x = 0; x < MW; ++x) {
-            if constexpr (CODES) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) { kp[h][j][x] = km[j * MW + x]; vp[h][j][x] = vm[j * MW + x]; }
-            } else { kn[x] = km[x]; vn[x] = vm[x]; }
-          }
-        }
-        if constexpr (CODES) {
-          if (pg < 0 || key0[h] + 16 > s.n) {            // behind the end lies anything: its weight of 0 must meet a number
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-              for (int x = 0; x < MW; ++x)
-                if (pg < 0 || key0[h] + own + j >= s.n) kp[h][j][x] = vp[h][j][x] = 0;
-          }
-        }
-      } else {
-        load_raw<T, BITS, D>(kr, a.k, row_at(m, s, a.ks, phys, pg, sub, hk) + n16 * a.ks.token, quarter, there);
-        load_raw<T, BITS, D>(vr, a.v, row_at(m, s, a.vs, phys, pg, sub, hk) + n16 * a.vs.token, quarter, there);
-      }
-      expand<T, BITS, D>(k[h], kr, kn, there);
+      key0[h] = next.key0[h];
+      const bool there = key0[h] + n16 < s.n;
+      expand<T, BITS, D>(k[h], next.k[h], next.pk[h], there);
       RowFrag<T, D> v;
-      expand<T, BITS, D>(v, vr, vn, there);
+      expand<T, BITS, D>(v, next.v[h], next.pv[h], there);
       compiler_fence();
 #pragma unroll
       for (int f = 0; f < NF; ++f) *(u32x4_t*)(vl + lds_piece<T, D>(16 * h + n16, piece_at<T, BITS>(f, quarter))) = v.p[f];
+      if constexpr (CODES) {
+        if (quarter == 0) {
+#pragma unroll
+          for (int x = 0; x < MW; ++x) { meta[wave][16 * h + n16][x] = next.pk[h][x]; meta[wave][16 * h + n16][MW + x] = next.pv[h][x]; }
+        }
+      }
     }
     compiler_fence();
-    if (!any) continue;
+    if constexpr (CODES) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+          for (int x = 0; x < MW; ++x) { kp[h][j][x] = meta[wave][16 * h + 4 * quarter + j][x]; vp[h][j][x] = meta[wave][16 * h + 4 * quarter + j][MW + x]; }
+    }
+    if (R == 1 && turn + 4 < turns) fetch(next, turn + 4);
 
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -276,6 +291,8 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
       }
     }
     compiler_fence();
+  }
+  __syncthreads();                                    // before the list is filled again
   }
 
   // join the four waves, 16 rows at a time: [wave][row][d], [wave][row] x {maximum, sum}

@@ -352,7 +352,7 @@ __global__ __launch_bounds__(NW * 64) void grad_q_wide(BlockGradArgs a, int rts,
     for (int x = 0; x < 2; ++x) ca[db][x] = col_operand<D>(lane, db, x);
 
   for (int e0 = 0; e0 < entries; e0 += LIST) {
-    const int n = fill_list<NT>(m, b, list, e0, entries, pages, pages_l, counts);
+    const int n = fill_list<NT>(m, b, list, e0, 1, entries, pages, pages_l, counts);
     const int parts = n << lsub, tiles = (parts + 3) >> 2;
     if (!tiles) continue;
     auto issue = [&](int stage, int t) __attribute__((always_inline)) {

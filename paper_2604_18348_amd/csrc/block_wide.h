@@ -12,7 +12,6 @@ namespace adac {
 typedef __attribute__((address_space(3))) void lds_void_t;
 
 constexpr int TILE = 64;               // rows of a tile, staged as four sixteenths of pages
-constexpr int LIST = 512;              // pages of a list held in LDS at a time
 
 // Rows of D bf16 in LDS, unpadded.  Piece q (16 bytes) of row r sits in slot q ^ swz(r).  Sixteen rows that are read at one piece
 // (operands that are rows) lie in sixteen different slots, and the four rows of a transposing read (operands that are columns: 64
@@ -56,34 +55,6 @@ __device__ __forceinline__ f32x16_t zero16() {
 #pragma unroll
   for (int i = 0; i < 16; ++i) z[i] = 0.f;
   return z;
-}
-
-// a value that all lanes share, where the compiler keeps it in a vector register (divisions are made there)
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ const char* uniform(const char* p) {
-  const uint64_t v = (uint64_t)p;
-  return (const char*)((uint64_t)(uint32_t)uniform((int)(v >> 32)) << 32 | (uint32_t)uniform((int)v));
-}
-
-// Pages e0 .. e0 + LIST - 1 of a list that name keys below `pages`, in order: {page, place in the pool}.  Returns how many.
-template <int NT>
-__device__ __forceinline__ int fill_list(const BlockDims& m, int b, const int32_t* list, int e0, int e1, int pages, int2* out, int32_t* counts) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int n = 0;
-  for (int base = e0; base < min(e1, e0 + LIST); base += NT) {
-    const int e = base + tid;
-    int pg = e < min(e1, e0 + LIST) ? list_page(list, e, pages) : -1, phys = 0;
-    if (pg >= 0 && m.num_pages) { phys = pool_page(m, b, pg); if (phys < 0) pg = -1; }
-    const uint64_t some = __ballot(pg >= 0);
-    if (lane == 0) counts[wave] = __popcll(some);
-    __syncthreads();
-    int at = n + __popcll(some & ((1ull << lane) - 1));
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) { if (w < wave) at += counts[w]; n += counts[w]; }
-    if (pg >= 0) out[at] = int2{pg, phys};
-    __syncthreads();
-  }
-  return __builtin_amdgcn_readfirstlane(n);
 }
 
 // A launch's workgroups go to the 8 XCDs in turn: runs of GROUP neighbours (blocks of a sequence, whose lists are alike) share one.

@@ -73,7 +73,7 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void block_attn_wide(BlockAttnArgs
     for (int x = 0; x < 2; ++x) vaddr[db][x] = col_operand<D>(lane, db, x);
 
   for (int e0 = 0; e0 < entries; e0 += LIST) {
-    const int n = fill_list<NT>(m, b, list, e0, entries, pages, pages_l, counts);
+    const int n = fill_list<NT>(m, b, list, e0, 1, entries, pages, pages_l, counts);
     const int parts = n << lsub, tiles = (parts + 3) >> 2;
     if (!tiles) continue;
     auto issue = [&](int stage, int t) __attribute__((always_inline)) {
