@@ -194,7 +194,7 @@ struct CacheArgs {
 int launch_cache_append(hipStream_t s, int dtype, int bits, int d, const CacheArgs& a);
 int launch_cache_read(hipStream_t s, int dtype, int bits, int d, const CacheArgs& a);
 int launch_block_boxes(hipStream_t s, int dtype, int d, const BlockDims& m, const void* k, KeyStride ks, void* boxes);
-size_t block_select_bytes(const BlockDims& m);
+size_t block_select_bytes(const BlockDims& m, int dtype);
 int launch_block_select(hipStream_t s, int dtype, int d, const BlockDims& m, const void* q, KeyStride qs, const void* boxes,
                         int32_t* sel_idx, int32_t* sel_cnt, void* ws);
 

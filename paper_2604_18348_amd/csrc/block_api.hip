@@ -111,7 +111,7 @@ int adacluster_block_workspace_bytes(const adacluster_block_params* p, int32_t c
   BlockDims m;
   if (int rc = check(p, &m)) return rc;
   if (!bytes) return fail(ADACLUSTER_E_BADARG, "bytes is NULL");
-  if (call == ADACLUSTER_BLOCK_SELECT) *bytes = block_select_bytes(m);
+  if (call == ADACLUSTER_BLOCK_SELECT) *bytes = block_select_bytes(m, p->dtype);
   else if (call == ADACLUSTER_BLOCK_ATTN) {
     const size_t x = block_attn_bytes(m, p->dtype, p->bits, p->d, true), y = block_attn_bytes(m, p->dtype, p->bits, p->d, false);
     *bytes = p->topk > 0 && x > y ? x : y;
@@ -175,7 +175,7 @@ int adacluster_block_select(const adacluster_block_params* p, const void* q, con
   m.cu_q = cu_q;
   const KeyStride qs = two(p->q_stride);
   if (int rc = check_rows("q", q, p->dtype, qs)) return rc;
-  if (int rc = check_ws(ws, ws_bytes, block_select_bytes(m))) return rc;
+  if (int rc = check_ws(ws, ws_bytes, block_select_bytes(m, p->dtype))) return rc;
   return done(launch_block_select((hipStream_t)stream, p->dtype, p->d, m, q, qs, boxes, sel_idx, sel_cnt, ws));
 }
 

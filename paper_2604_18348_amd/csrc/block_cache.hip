@@ -309,51 +309,43 @@ __device__ __forceinline__ void list_all(const BlockDims& m, const Seen& see, in
   if (threadIdx.x == 0) *cnt = see.seen;
 }
 
-// A workgroup a record: sums of the block's queries, scores and list in one launch, u and the scores in LDS.
-constexpr int PICK_PAGES = 4096, PICK_HEADS = 16, PICK_NT = 512;
-template <typename T, int D>
-__global__ __launch_bounds__(PICK_NT) void block_pick(BlockDims m, const T* __restrict__ q, KeyStride qs, const T* __restrict__ boxes,
-                                                      int32_t* __restrict__ sel_idx, int32_t* __restrict__ sel_cnt) {
-  constexpr int VEC = Vec<T>::N, LPR = D / VEC, RPI = PICK_NT / LPR, AHEAD = 4;
-  extern __shared__ __align__(16) double lds[];      // [G][D] sums, then [max_pages] scores; before them the parts of the sums
-  const int hk = blockIdx.x % m.Hkv, i = blockIdx.x / m.Hkv % m.nb, b = blockIdx.x / m.Hkv / m.nb;
-  const BlockSeq s = block_seq(m, b);
-  const Seen see = block_seen(m, s, i);
-  const long long rec = ((long long)b * m.nb + i) * m.Hkv + hk;
-  int32_t* const idx = sel_idx + rec * m.topk;
-  if (see.seen <= m.topk) { list_all<PICK_NT>(m, see, idx, sel_cnt + rec); return; }
-  const int tid = threadIdx.x, col = tid % LPR * VEC;
-  const int t0 = i * m.qblock, t1 = min(t0 + m.qblock, s.nq);
-  double* const u_l = lds;
-  double* const sc = lds + m.G * D;
-  {
-    // vectors of VEC dimensions; where there are fewer than threads, the tokens go to groups of threads whose sums are added in order
-    const int vecs = m.G * LPR, groups = max(1, min(PICK_NT / vecs, t1 - t0)), g = tid / vecs;
-    for (int v = tid % vecs; v < vecs && g < groups; v += PICK_NT) {       // (vecs > threads: one group, several vectors)
-      const int h = v / LPR, c = v % LPR * VEC;
-      double sum[VEC];
+// u of a record: sums of the block's queries of every head, in 64 bits, to u_l [G][D] (parts: NT * VEC doubles of scratch).
+template <typename T, int D, int NT>
+__device__ __forceinline__ void block_sums(const BlockDims& m, const BlockSeq& s, int i, int hk, const T* __restrict__ q, const KeyStride& qs, double* u_l, double* parts) {
+  constexpr int VEC = Vec<T>::N, LPR = D / VEC;
+  const int tid = threadIdx.x, t0 = i * m.qblock, t1 = min(t0 + m.qblock, s.nq);
+  // vectors of VEC dimensions; where there are fewer than threads, the tokens go to groups of threads whose sums are added in order
+  const int vecs = m.G * LPR, groups = max(1, min(NT / vecs, t1 - t0)), g = tid / vecs;
+  for (int v = tid % vecs; v < vecs && g < groups; v += NT) {              // (vecs > threads: one group, several vectors)
+    const int h = v / LPR, c = v % LPR * VEC;
+    double sum[VEC];
 #pragma unroll
-      for (int x = 0; x < VEC; ++x) sum[x] = 0.0;
-      for (int t = t0 + g; t < t1; t += groups) {
-        float w[VEC];
-        unpack16<T>(*(const u32x4_t*)(q + (long long)(s.q0 + t) * qs.token + (hk * m.G + h) * qs.head + c), w);
+    for (int x = 0; x < VEC; ++x) sum[x] = 0.0;
+    for (int t = t0 + g; t < t1; t += groups) {
+      float w[VEC];
+      unpack16<T>(*(const u32x4_t*)(q + (long long)(s.q0 + t) * qs.token + (hk * m.G + h) * qs.head + c), w);
 #pragma unroll
-        for (int x = 0; x < VEC; ++x) sum[x] += (double)w[x];
-      }
+      for (int x = 0; x < VEC; ++x) sum[x] += (double)w[x];
+    }
 #pragma unroll
-      for (int x = 0; x < VEC; ++x) (groups > 1 ? sc + g * m.G * D : u_l)[h * D + c + x] = sum[x];
+    for (int x = 0; x < VEC; ++x) (groups > 1 ? parts + g * m.G * D : u_l)[h * D + c + x] = sum[x];
+  }
+  __syncthreads();
+  if (groups > 1) {
+    for (int x = tid; x < m.G * D; x += NT) {
+      double sum = parts[x];
+      for (int y = 1; y < groups; ++y) sum += parts[y * m.G * D + x];
+      u_l[x] = sum;
     }
     __syncthreads();
-    if (groups > 1) {
-      for (int x = tid; x < m.G * D; x += PICK_NT) {
-        double sum = sc[x];
-        for (int y = 1; y < groups; ++y) sum += sc[y * m.G * D + x];
-        u_l[x] = sum;
-      }
-      __syncthreads();
-    }
   }
-  const int p1 = m.causal ? see.lo : see.seen;       // own pages need no score
+}
+
+// Scores of pages [p0, p1) from u in LDS to sc, in 64 bits: LPR lanes a page.  list: the pages, or NULL: p0 .. in order.
+template <typename T, int D, int NT>
+__device__ __forceinline__ void exact_scores(const BlockDims& m, int b, int hk, const T* __restrict__ boxes, const double* u_l, int p0, int p1, const int32_t* list, double* sc) {
+  constexpr int VEC = Vec<T>::N, LPR = D / VEC, RPI = NT / LPR, AHEAD = 2;
+  const int tid = threadIdx.x, col = tid % LPR * VEC;
   for (int h0 = 0; h0 < m.G; h0 += SCORE_HEADS) {
     double u[SCORE_HEADS][VEC];
     const int H = min(SCORE_HEADS, m.G - h0);
@@ -361,11 +353,14 @@ __global__ __launch_bounds__(PICK_NT) void block_pick(BlockDims m, const T* __re
     for (int h = 0; h < SCORE_HEADS; ++h)
 #pragma unroll
       for (int x = 0; x < VEC; ++x) u[h][x] = h < H ? u_l[(h0 + h) * D + col + x] : 0.0;
-    for (int p = tid / LPR; p < p1; p += RPI * AHEAD) {
+    for (int p = p0 + tid / LPR; p < p1; p += RPI * AHEAD) {
       float mx[AHEAD][VEC], mn[AHEAD][VEC];
       bool there[AHEAD];
 #pragma unroll
-      for (int y = 0; y < AHEAD; ++y) load_box<T, D>(m, b, hk, min(p + y * RPI, p1 - 1), boxes, col, mx[y], mn[y], &there[y]);
+      for (int y = 0; y < AHEAD; ++y) {
+        const int at = min(p + y * RPI, p1 - 1);
+        load_box<T, D>(m, b, hk, list ? list[at] : at, boxes, col, mx[y], mn[y], &there[y]);
+      }
 #pragma unroll
       for (int y = 0; y < AHEAD; ++y) {
         const int at = p + y * RPI;
@@ -376,7 +371,222 @@ __global__ __launch_bounds__(PICK_NT) void block_pick(BlockDims m, const T* __re
     }
   }
   __syncthreads();
+}
+
+// A workgroup a record: sums of the block's queries, scores and list in one launch, u and the scores in LDS.
+constexpr int PICK_PAGES = 4096, PICK_HEADS = 16, PICK_NT = 512;
+template <typename T, int D>
+__global__ __launch_bounds__(PICK_NT) void block_pick(BlockDims m, const T* __restrict__ q, KeyStride qs, const T* __restrict__ boxes,
+                                                      int32_t* __restrict__ sel_idx, int32_t* __restrict__ sel_cnt) {
+  extern __shared__ __align__(16) double lds[];      // [G][D] sums, then [max_pages] scores; before them the parts of the sums
+  const int hk = blockIdx.x % m.Hkv, i = blockIdx.x / m.Hkv % m.nb, b = blockIdx.x / m.Hkv / m.nb;
+  const BlockSeq s = block_seq(m, b);
+  const Seen see = block_seen(m, s, i);
+  const long long rec = ((long long)b * m.nb + i) * m.Hkv + hk;
+  int32_t* const idx = sel_idx + rec * m.topk;
+  if (see.seen <= m.topk) { list_all<PICK_NT>(m, see, idx, sel_cnt + rec); return; }
+  double* const sc = lds + m.G * D;
+  block_sums<T, D, PICK_NT>(m, s, i, hk, q, qs, lds, sc);
+  exact_scores<T, D, PICK_NT>(m, b, hk, boxes, lds, 0, m.causal ? see.lo : see.seen, nullptr, sc);      // (own pages need no score)
   choose<PICK_NT>(m, see, sc, idx, sel_cnt + rec);
+}
+
+// Largest value over the 16 lanes that share lane / 16.
+__device__ __forceinline__ float row16_max(float v) {
+  v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0xB1, 0xF, 0xF, false)));       // lanes 1 apart
+  v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x4E, 0xF, 0xF, false)));       // 2 apart
+  v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x141, 0xF, 0xF, false)));      // the other four of eight
+  return fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x140, 0xF, 0xF, false)));   // the other eight
+}
+__device__ __forceinline__ uint32_t order_key32(float v) {
+  const uint32_t u = __float_as_uint(v + 0.f);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+// block_pick for bfloat16, with the scores bounded on the matrix cores first and formed in 64 bits only where the border of the list
+// runs.  S = u+ max + u- min (u+, u-: u where it is >= 0, < 0), u as one or two bfloat16 (LO: sums of several queries; what is left out is
+// below 2^-16 |u|), 16 pages x 16 heads a tile, and with the same products of absolute values the sum A of what was added.  S is off
+// by at most 2^-12 A + 2^-70: at most 4 D products of exact factors added in fp32, each addition by 2^-22 of what it has, and
+// products or factors below 2^-126 taken for 0 (u is held to 2^-60 .. 2^40 here; a record outside is scored in 64 bits throughout).
+// With lo = S - e, hi = S + e (infinite where they are no numbers): a page whose hi is below the need-th largest lo is not
+// taken, one whose lo is above the (need + 1)-th largest hi is, and the others, a handful, are scored in 64 bits.  Bound by the
+// boxes it reads: 32 x 8 records of 1 640 pages on average (0.2 GB), %s; in 64 bits throughout 108.
+constexpr int PICK_BORDER = 512;
+template <int D, bool LO>
+__global__ __launch_bounds__(PICK_NT) void block_pick_bounds(BlockDims m, const bf16raw* __restrict__ q, KeyStride qs, const bf16raw* __restrict__ boxes,
+                                                             int32_t* __restrict__ sel_idx, int32_t* __restrict__ sel_cnt) {
+  constexpr int NF = D / 32, NW = PICK_NT / 64, PER = PICK_PAGES / PICK_NT;
+  extern __shared__ __align__(16) double lds[];      // [G][D] sums, then [max_pages] pairs of bounds; before them the parts of the sums
+  __shared__ double border_sc[PICK_BORDER];
+  __shared__ int32_t border_l[PICK_BORDER];
+  __shared__ unsigned long long taken[PICK_PAGES / 64];
+  __shared__ int32_t first_at[PICK_PAGES / 64], counts[2][NW][6], s_border, s_in, s_odd;
+  const int hk = blockIdx.x % m.Hkv, i = blockIdx.x / m.Hkv % m.nb, b = blockIdx.x / m.Hkv / m.nb;
+  const BlockSeq s = block_seq(m, b);
+  const Seen see = block_seen(m, s, i);
+  const long long rec = ((long long)b * m.nb + i) * m.Hkv + hk;
+  int32_t* const idx = sel_idx + rec * m.topk;
+  if (see.seen <= m.topk) { list_all<PICK_NT>(m, see, idx, sel_cnt + rec); return; }
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, quarter = lane >> 4;
+  double* const u_l = lds;
+  float2* const bound = (float2*)(lds + m.G * D);
+  if (tid == 0) s_border = s_in = s_odd = 0;
+  block_sums<bf16raw, D, PICK_NT>(m, s, i, hk, q, qs, u_l, lds + m.G * D);
+  {
+    bool odd = false;
+    for (int x = tid; x < m.G * D; x += PICK_NT) { const double v = fabs(u_l[x]); odd = odd || !(v == 0.0 || (v >= 0x1p-60 && v <= 0x1p40)); }
+    if (odd) s_odd = 1;
+  }
+  __syncthreads();
+  const int c1 = m.causal ? see.lo : see.seen, c0 = min(m.keep_first, c1), need = m.topk - (see.seen - (c1 - c0));
+  const auto exact = [&]() {
+    __syncthreads();
+    exact_scores<bf16raw, D, PICK_NT>(m, b, hk, boxes, u_l, 0, c1, nullptr, (double*)bound);
+    choose<PICK_NT>(m, see, (const double*)bound, idx, sel_cnt + rec);
+  };
+  if (s_odd) { exact(); return; }
+  if (need > 0) {
+    // operands: column n16 is head n16
+    RowFrag<bf16raw, D> ph, pl, nh, nl, pa, na;      // u+ and u-: upper and lower parts, and bounds of |u|
+#pragma unroll
+    for (int f = 0; f < NF; ++f)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        uint32_t o[6] = {0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const double v = n16 < m.G ? u_l[n16 * D + 32 * f + 8 * quarter + 2 * w + x] : 0.0;
+          const float vf = (float)v;
+          const uint32_t h = f32_to_bf16(vf), l = LO ? f32_to_bf16((float)(v - (double)__uint_as_float(h << 16))) : 0, a = (h & 0x7FFF) + (vf != 0.f);
+          const bool neg = vf < 0.f;
+          o[neg ? 2 : 0] |= h << (16 * x);
+          o[neg ? 3 : 1] |= l << (16 * x);
+          o[neg ? 5 : 4] |= a << (16 * x);
+        }
+        ph.p[f][w] = o[0]; pl.p[f][w] = o[1]; nh.p[f][w] = o[2]; nl.p[f][w] = o[3]; pa.p[f][w] = o[4]; na.p[f][w] = o[5];
+      }
+    const int tiles = (c1 + 15) >> 4;
+    auto row_of = [&](int t) __attribute__((always_inline)) {      // of the lane's page; -1: none
+      const int p = min(t * 16 + n16, c1 - 1);
+      return m.num_pages ? pool_page(m, b, p) : b * m.max_pages + p;
+    };
+    auto load = [&](RowFrag<bf16raw, D>& x, RowFrag<bf16raw, D>& y, int row) __attribute__((always_inline)) {
+      const bf16raw* const box = boxes + ((long long)max(row, 0) * m.Hkv + hk) * 2 * D;
+      load_frag(x, box, quarter, true);
+      load_frag(y, box + D, quarter, true);
+    };
+    RowFrag<bf16raw, D> mx, mn;
+    int row = wave < tiles ? row_of(wave) : -1, row1 = wave + NW < tiles ? row_of(wave + NW) : -1;
+    if (wave < tiles) load(mx, mn, row);
+    for (int t = wave; t < tiles; t += NW) {
+      f32x4_t sc{0.f, 0.f, 0.f, 0.f}, ab = sc;
+#pragma unroll
+      for (int f = 0; f < NF; ++f) {
+        sc = mma(bf16raw{}, mx.p[f], ph.p[f], sc);
+        sc = mma(bf16raw{}, mn.p[f], nh.p[f], sc);
+        if constexpr (LO) { sc = mma(bf16raw{}, mx.p[f], pl.p[f], sc); sc = mma(bf16raw{}, mn.p[f], nl.p[f], sc); }
+        ab = mma(bf16raw{}, mx.p[f] & 0x7FFF7FFFu, pa.p[f], ab);
+        ab = mma(bf16raw{}, mn.p[f] & 0x7FFF7FFFu, na.p[f], ab);
+      }
+      const bool none = row < 0;
+      const int row2 = t + 2 * NW < tiles ? row_of(t + 2 * NW) : -1;
+      if (t + NW < tiles) load(mx, mn, row1);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float e = fmaf(0x1p-12f, ab[j], 0x1p-70f);
+        float lo = sc[j] - e, hi = sc[j] + e;
+        if (!(finite(lo) && finite(hi))) { lo = -INFINITY; hi = INFINITY; }
+        if (n16 >= m.G) lo = hi = -INFINITY;
+        if (__shfl((int)none, 4 * quarter + j)) lo = hi = -INFINITY;      // (the page's row is looked up by lane page % 16)
+        lo = row16_max(lo);
+        hi = row16_max(hi);
+        const int p = t * 16 + 4 * quarter + j;
+        if (n16 == 0 && p < c1) bound[p] = float2{lo, hi};
+      }
+      row = row1; row1 = row2;
+    }
+  }
+  __syncthreads();
+  // the need-th largest lo and the (need + 1)-th largest hi, two bits a turn, by counting what is not below three values in between
+  uint32_t kl[PER], kh[PER];
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    const int p = c0 + tid + x * PICK_NT;
+    kl[x] = kh[x] = 0;                               // (below all keys)
+    if (need > 0 && p < c1) { const float2 v = bound[p]; kl[x] = order_key32(v.x); kh[x] = order_key32(v.y); }
+  }
+  uint32_t lth = 0, hth = 0;
+  if (need > 0) {
+    const int mine = (c1 - c0 + PICK_NT - 1) / PICK_NT;
+    for (int shift = 30; shift >= 0; shift -= 2) {
+      int n[6] = {0, 0, 0, 0, 0, 0};
+#pragma unroll
+      for (int x = 0; x < PER; ++x) {
+        if (x >= mine) break;
+#pragma unroll
+        for (int y = 0; y < 3; ++y) {
+          n[y] += __popcll(__ballot(kl[x] >= (lth | (uint32_t)(y + 1) << shift)));
+          n[3 + y] += __popcll(__ballot(kh[x] >= (hth | (uint32_t)(y + 1) << shift)));
+        }
+      }
+      const int turn = (shift >> 1) & 1;             // (a slot is read before the barrier that the next writer of it passes)
+      if (lane < 6) counts[turn][wave][lane] = lane == 0 ? n[0] : lane == 1 ? n[1] : lane == 2 ? n[2] : lane == 3 ? n[3] : lane == 4 ? n[4] : n[5];
+      __syncthreads();
+      int sum = 0;
+      if (lane < 6) {
+#pragma unroll
+        for (int w = 0; w < NW; ++w) sum += counts[turn][w][lane];
+      }
+      const unsigned long long up = __ballot(lane < 3 ? sum >= need : lane < 6 && sum >= need + 1);
+      lth |= (uint32_t)__popcll(up & 7) << shift;
+      hth |= (uint32_t)__popcll(up & 56) << shift;
+    }
+  }
+  // what is taken for certain, and the border
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    const int p = tid + x * PICK_NT;
+    if (x * PICK_NT >= see.seen) break;
+    bool in = false, edge = false;
+    if (need > 0 && p >= c0 && p < c1) {
+      const float2 v = bound[p];
+      in = order_key32(v.x) > hth;
+      edge = !in && order_key32(v.y) >= lth;
+    }
+    const unsigned long long sure = __ballot(in), w = sure | __ballot(p < see.seen && (p < c0 || p >= c1));
+    if (lane == 0) { taken[p >> 6] = w; if (sure) atomicAdd(&s_in, __popcll(sure)); }
+    if (edge) { const int at = atomicAdd(&s_border, 1); if (at < PICK_BORDER) border_l[at] = p; }      // (in any order: pages decide ties)
+  }
+  __syncthreads();
+  const int nb = s_border, left = need - s_in;
+  if (nb > PICK_BORDER) { exact(); return; }
+  if (nb == left) {
+    for (int x = tid; x < nb; x += PICK_NT) atomicOr(&taken[border_l[x] >> 6], 1ull << (border_l[x] & 63));
+  } else if (left > 0) {
+    exact_scores<bf16raw, D, PICK_NT>(m, b, hk, boxes, u_l, 0, nb, border_l, border_sc);
+    for (int x = tid; x < nb; x += PICK_NT) {
+      const uint64_t key = order_key(border_sc[x]);
+      const int p = border_l[x];
+      int before = 0;
+      for (int y = 0; y < nb; ++y) { const uint64_t other = order_key(border_sc[y]); before += other > key || (other == key && border_l[y] < p); }
+      if (before < left) atomicOr(&taken[p >> 6], 1ull << (p & 63));
+    }
+  }
+  __syncthreads();
+  const int words = (see.seen + 63) >> 6;
+  if (wave == 0) {
+    const int n = lane < words ? __popcll(taken[lane]) : 0;
+    int incl = n;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(incl, o); if (lane >= o) incl += v; }
+    first_at[lane] = incl - n;
+  }
+  __syncthreads();
+  for (int p = tid; p < see.seen; p += PICK_NT) {
+    const unsigned long long w = taken[p >> 6], bit = 1ull << (p & 63);
+    if (w & bit) idx[first_at[p >> 6] + __popcll(w & (bit - 1))] = p;
+  }
+  if (tid == 0) sel_cnt[rec] = m.topk;
 }
 
 // Few records over long contexts: scores by many workgroups, to memory, and the lists from there.
@@ -462,25 +672,32 @@ int launch_block_boxes(hipStream_t s, int dtype, int d, const BlockDims& m, cons
   return launched();
 }
 
-// Whether a workgroup a record does (its u and scores in LDS): there are enough records to fill the chip, or few pages.
-static bool picks(const BlockDims& m) {
+// Whether a workgroup a record does (its u and scores in LDS): bfloat16 scores are bounds first; in 64 bits there have to be enough
+// records to fill the chip, or few pages.
+static bool picks(const BlockDims& m, int dtype) {
   const long long recs = (long long)m.B * m.nb * m.Hkv;
-  return m.max_pages <= PICK_PAGES && m.G <= PICK_HEADS && (recs >= 128 || m.max_pages <= 1024);
+  return m.max_pages <= PICK_PAGES && m.G <= PICK_HEADS && (dtype == ADACLUSTER_BF16 || recs >= 128 || m.max_pages <= 1024);
 }
 
-size_t block_select_bytes(const BlockDims& m) { return picks(m) ? 0 : (size_t)m.B * m.nb * m.Hkv * m.max_pages * sizeof(double); }
+size_t block_select_bytes(const BlockDims& m, int dtype) { return picks(m, dtype) ? 0 : (size_t)m.B * m.nb * m.Hkv * m.max_pages * sizeof(double); }
 
 int launch_block_select(hipStream_t s, int dtype, int d, const BlockDims& m, const void* q, KeyStride qs, const void* boxes,
                         int32_t* sel_idx, int32_t* sel_cnt, void* ws) {
   const long long recs = (long long)m.B * m.nb * m.Hkv;
   const int per = 256, pieces = (m.max_pages + per - 1) / per;
-  if (!grid_fits(recs * (picks(m) ? PICK_NT / 256 : pieces))) return ADACLUSTER_E_UNSUPPORTED;
-  if (picks(m)) {
+  if (!grid_fits(recs * (picks(m, dtype) ? PICK_NT / 256 : pieces))) return ADACLUSTER_E_UNSUPPORTED;
+  if (picks(m, dtype)) {
     // sums, then scores or the parts of the sums (PICK_NT vectors of 16 bytes' elements at most)
     const int vec = dtype == ADACLUSTER_BF16 ? 8 : 4, parts = PICK_NT * vec;
     const size_t lds = ((size_t)m.G * d + (m.max_pages > parts ? m.max_pages : parts)) * sizeof(double);
-#define CALL(T, D) block_pick<T, D><<<(int)recs, PICK_NT, lds, s>>>(m, (const T*)q, qs, (const T*)boxes, sel_idx, sel_cnt)
-    BY_TYPE(dtype, d, CALL)
+#define CALL(D, LO) block_pick_bounds<D, LO><<<(int)recs, PICK_NT, lds, s>>>(m, (const bf16raw*)q, qs, (const bf16raw*)boxes, sel_idx, sel_cnt)
+    if (dtype == ADACLUSTER_BF16) {
+      if (m.qblock == 1) { if (d == 64) CALL(64, false); else CALL(128, false); }
+      else { if (d == 64) CALL(64, true); else CALL(128, true); }
+    }
+#undef CALL
+#define CALL(D) block_pick<float, D><<<(int)recs, PICK_NT, lds, s>>>(m, (const float*)q, qs, (const float*)boxes, sel_idx, sel_cnt)
+    else if (d == 64) CALL(64); else CALL(128);
 #undef CALL
     return launched();
   }

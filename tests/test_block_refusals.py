@@ -72,8 +72,8 @@ def test_workspace_sizes(lib):
     assert size(lib, params(), 3)[0] == -1
     assert lib.adacluster_block_workspace_bytes(None, 0, ctypes.byref(ctypes.c_size_t())) == -1
     assert lib.adacluster_block_workspace_bytes(ctypes.byref(params()), 0, None) == -1
-    big = params(B=1, max_pages=4096, max_q=1)                                     # few records, many pages: scores in memory
-    assert size(lib, big, B.BLOCK_SELECT)[1] >= 2 * 4096 * 8
+    big = params(B=1, max_pages=8192, max_q=1)                                     # few records, many pages: scores in memory
+    assert size(lib, big, B.BLOCK_SELECT)[1] >= 2 * 8192 * 8
 
 
 def append(lib, c, **kw):
@@ -134,7 +134,7 @@ def test_select(lib):
     assert "own positions" in message(lib)
     assert select(lib, params(topk=1, causal=0, keep_first=2)) == -1
     assert select(lib, params(), boxes=ctypes.c_void_p(258)) == -1
-    big = params(B=1, max_pages=4096, max_q=1)
+    big = params(B=1, max_pages=8192, max_q=1)
     assert select(lib, big, ws=Z) == -4
     assert select(lib, big, ws=ctypes.c_void_p(272)) == -4
     assert select(lib, big, n=8) == -4 and "too small" in message(lib)

@@ -206,6 +206,9 @@ def _check_selection(x, p, sel, cnt):
     (BF, 128, 16, 4, 2, [9000], [40], 8, 2, 0),              # room for the own pages alone (causal), or little more
     (BF, 64, 16, 2, 1, [17000], [1], 1, 50, 1),              # few records of many pages: scores in memory
     (F, 128, 16, 5, 1, [20000, 90], [6, 6], 3, 30, 1),
+    (BF, 128, 16, 32, 2, [40000, 30000], [1, 3], 1, 64, 1),  # sixteen heads, 2 500 pages
+    (BF, 128, 16, 8, 4, [3000], [700], 32, 12, 1),
+    (BF, 64, 32, 30, 3, [20000], [64], 16, 30, 0),
     (BF, 64, 128, 40, 2, [700], [9], 9, 3, 1),               # more heads than a workgroup holds sums of
     (F, 128, 16, 16, 1, [1000], [200], 64, 9, 1),
 ])
@@ -232,8 +235,42 @@ def test_selection_ties_go_to_the_lowest_page():
     _check_selection(x, p, *B.adacluster_block_select(p, x.q.cuda(), x.cu_q.cuda(), x.cache.boxes, **x.where()))
 
 
-def test_selection_with_infinities_and_nan():
-    x = Batch(F, 0, 64, 16, 4, 2, [1600], [1], 8)
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_selection_of_scores_a_rounding_apart(dtype):
+    """Boxes that differ in their last bits, so that 32-bit sums cannot order the pages; sums of queries that cancel."""
+    x = Batch(dtype, 0, 64, 16, 4, 2, [16 * 900], [4], 12)
+    g = torch.Generator().manual_seed(6)
+    base = 1 + torch.rand((1, 2, 1, 64), generator=g)
+    steps = torch.randint(-2, 3, (x.boxes.shape[0], 2, 1, 64), generator=g) * 2.0 ** -7
+    x.boxes = torch.cat([base + steps, -base + steps], 2).to(dtype)
+    if dtype == F:
+        x.boxes += torch.randint(-3, 4, x.boxes.shape, generator=g) * 2.0 ** -22
+    x.cache.boxes = x.boxes.cuda()
+    for qblock in (1, 2, 4):
+        x.q = torch.randn(x.q.shape, generator=g).to(dtype)
+        x.q[1] = -x.q[0]
+        x.q[1, :, :5] += 2.0 ** -6
+        p = x.params(qblock=qblock, topk=333)
+        _check_selection(x, p, *B.adacluster_block_select(p, x.q.cuda(), x.cu_q.cuda(), x.cache.boxes, **x.where()))
+
+
+@pytest.mark.parametrize("size", [1e-38, 1e-30, 1e30, 1e38])
+def test_selection_of_tiny_and_huge_values(size):
+    """Queries and boxes at the ends of the range: what a product in 32 bits would lose or overflow."""
+    x = Batch(BF, 0, 64, 16, 4, 2, [16 * 300], [1], 12)
+    for q, k in ((size, 1.0), (1.0, size), (size, 1 / size)):
+        y = torch.randn(x.q.shape, generator=torch.Generator().manual_seed(1)) * q
+        z = x.boxes.float() * k
+        y[:, :, ::7] /= q                                     # mixed
+        x2 = Batch(BF, 0, 64, 16, 4, 2, [16 * 300], [1], 12)
+        x2.q, x2.boxes = y.to(BF), z.to(BF)
+        p = x2.params(topk=40)
+        _check_selection(x2, p, *B.adacluster_block_select(p, x2.q.cuda(), x2.cu_q.cuda(), x2.boxes.cuda(), **x2.where()))
+
+
+@pytest.mark.parametrize("dtype", [F, BF])
+def test_selection_with_infinities_and_nan(dtype):
+    x = Batch(dtype, 0, 64, 16, 4, 2, [1600], [1], 8)
     x.boxes[3, 0, 0, 5] = math.inf
     x.boxes[9, 1, 1, 7] = -math.inf
     x.boxes[17, 0, 0, 1] = math.nan
