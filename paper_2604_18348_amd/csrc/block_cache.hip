@@ -215,20 +215,35 @@ __device__ __forceinline__ void load_box(const BlockDims& m, int b, int hk, int 
   unpack16<T>(*(const u32x4_t*)box, mx);
   unpack16<T>(*(const u32x4_t*)(box + D), mn);
 }
+template <int CTRL> __device__ __forceinline__ double add_lane(double v) {      // + the value of the lane that CTRL names (DPP)
+  const uint64_t u = (uint64_t)__double_as_longlong(v);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, 0xF, 0xF, false), hi = __builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, 0xF, 0xF, false);
+  return v + __longlong_as_double((long long)((uint64_t)hi << 32 | lo));
+}
 template <int VEC, int LPR>
 __device__ __forceinline__ double box_score(const double (*u)[VEC], int H, const float* mx, const float* mn) {
-  double best = -INFINITY;
+  double best = -INFINITY, c[SCORE_HEADS];
 #pragma unroll
-  for (int h = 0; h < SCORE_HEADS; ++h) {
-    if (h >= H) break;
-    double c = 0.0;
+  for (int h = 0; h < SCORE_HEADS; ++h) {            // (all of them, whatever H: no branch between the sums, which then overlap)
+    c[h] = 0.0;
 #pragma unroll
-    for (int x = 0; x < VEC; ++x) c = fma(u[h][x], (double)(u[h][x] >= 0.0 ? mx[x] : mn[x]), c);
-#pragma unroll
-    for (int o = 1; o < LPR; o <<= 1) c += __shfl_xor(c, o);
-    if (c > best) best = c;
+    for (int x = 0; x < VEC; ++x) c[h] = fma(u[h][x], (double)(u[h][x] >= 0.0 ? mx[x] : mn[x]), c[h]);
   }
-  return best + 0.0;                              // (-0 + 0 = 0: equal to it in the order below)
+#pragma unroll
+  for (int h = 0; h < SCORE_HEADS; ++h) c[h] = add_lane<0xB1>(c[h]);          // lanes 1 apart
+#pragma unroll
+  for (int h = 0; h < SCORE_HEADS; ++h) c[h] = add_lane<0x4E>(c[h]);          // 2 apart
+#pragma unroll
+  for (int h = 0; h < SCORE_HEADS; ++h) c[h] = add_lane<0x141>(c[h]);         // the other four of eight
+  if constexpr (LPR >= 16)
+#pragma unroll
+    for (int h = 0; h < SCORE_HEADS; ++h) c[h] = add_lane<0x140>(c[h]);       // the other eight of sixteen
+  if constexpr (LPR >= 32)
+#pragma unroll
+    for (int h = 0; h < SCORE_HEADS; ++h) c[h] += __shfl_xor(c[h], 16);
+#pragma unroll
+  for (int h = 0; h < SCORE_HEADS; ++h) if (h < H && c[h] > best) best = c[h];
+  return best + 0.0;                                 // (-0 + 0 = 0: equal to it in the order below)
 }
 
 // The larger score has the larger key.
@@ -250,7 +265,8 @@ __device__ __forceinline__ void choose(const BlockDims& m, const Seen& see, cons
   uint64_t prefix = 0, mask = 0;
   int left = need;                                   // of those that agree with the prefix
   if (need <= 0) prefix = mask = ~0ull;              // no score reaches it
-  for (int shift = 56; shift >= 0 && need > 0; shift -= 8) {
+  const bool few = c1 - c0 <= NT;                    // a page a thread: those before it are counted
+  for (int shift = 56; shift >= 0 && need > 0 && !few; shift -= 8) {
     if (tid < 256) s_hist[tid] = 0;
     __syncthreads();
     for (int p = c0 + tid; p < c1; p += NT) {
@@ -274,6 +290,48 @@ __device__ __forceinline__ void choose(const BlockDims& m, const Seen& see, cons
     const bool all = s_left == s_in;                 // the whole digit is taken: the order inside it does not matter
     __syncthreads();
     if (all) break;
+  }
+  if (few) {
+    __shared__ uint64_t s_take[NW], s_tie[NW];
+    const int p = c0 + tid;
+    const bool from = p < c1 && need > 0;
+    const uint64_t key = order_key(sc[min(p, max(c1 - 1, 0))]);
+    int above = 0;
+    __shared__ uint64_t s_key[NT];
+    s_key[tid] = p < c1 ? key : 0;                   // (0: above nothing)
+    __syncthreads();
+    if (__any(from))
+      for (int x0 = 0; x0 < c1 - c0; x0 += 8) {      // (eight reads on their way at a time; NT is a multiple of it)
+        uint64_t v[8];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) v[y] = s_key[x0 + y];
+#pragma unroll
+        for (int y = 0; y < 8; ++y) above += v[y] > key;
+      }
+    // taken: those with fewer than `need` above them, and of the last ones that tie as many as there is room for, in order
+    const uint64_t w = __ballot(from && above < need);
+    if (lane == 0) s_take[wave] = w;
+    if (tid == 0) { s_left = 0; s_in = 0; }
+    __syncthreads();
+    int all = 0;
+    for (int x = 0; x < NW; ++x) all += __popcll(s_take[x]);
+    if (all > need && from && above < need) atomicMax(&s_left, above);           // the tie: the largest count
+    __syncthreads();
+    const bool tie = all > need && from && above == s_left, sure = from && above < need && !tie;
+    const uint64_t ws = __ballot(sure), wt = __ballot(tie);
+    __syncthreads();
+    if (lane == 0) { s_take[wave] = ws; s_tie[wave] = wt; }
+    __syncthreads();
+    int room = need, at = c0, before = 0;            // (the first c0 pages are all taken)
+    for (int x = 0; x < NW; ++x) room -= __popcll(s_take[x]);
+    for (int x = 0; x < wave; ++x) { at += __popcll(s_take[x]); before += __popcll(s_tie[x]); }
+    at += __popcll(ws & ((1ull << lane) - 1));
+    before += __popcll(wt & ((1ull << lane) - 1));
+    if (sure || (tie && before < room)) idx[at + min(before, room)] = p;
+    for (int x = tid; x < c0; x += NT) idx[x] = x;
+    for (int x = c1 + tid; x < see.seen; x += NT) idx[m.topk - see.seen + x] = x;
+    if (tid == 0) *cnt = m.topk;
+    return;
   }
   int written = 0, equal = 0;
   for (int base = 0; base < see.seen; base += NT) {
@@ -321,11 +379,18 @@ __device__ __forceinline__ void block_sums(const BlockDims& m, const BlockSeq& s
     double sum[VEC];
 #pragma unroll
     for (int x = 0; x < VEC; ++x) sum[x] = 0.0;
-    for (int t = t0 + g; t < t1; t += groups) {
-      float w[VEC];
-      unpack16<T>(*(const u32x4_t*)(q + (long long)(s.q0 + t) * qs.token + (hk * m.G + h) * qs.head + c), w);
+    const T* const at = q + (long long)s.q0 * qs.token + (hk * m.G + h) * qs.head + c;
+    for (int t = t0 + g; t < t1; t += 4 * groups) {                        // (four loads on their way at a time)
+      u32x4_t w[4];
 #pragma unroll
-      for (int x = 0; x < VEC; ++x) sum[x] += (double)w[x];
+      for (int y = 0; y < 4; ++y) w[y] = *(const u32x4_t*)(at + (long long)min(t + y * groups, t1 - 1) * qs.token);
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        float f[VEC];
+        unpack16<T>(w[y], f);
+#pragma unroll
+        for (int x = 0; x < VEC; ++x) sum[x] += t + y * groups < t1 ? (double)f[x] : 0.0;
+      }
     }
 #pragma unroll
     for (int x = 0; x < VEC; ++x) (groups > 1 ? parts + g * m.G * D : u_l)[h * D + c + x] = sum[x];
@@ -374,8 +439,8 @@ __device__ __forceinline__ void exact_scores(const BlockDims& m, int b, int hk, 
 }
 
 // A workgroup a record: sums of the block's queries, scores and list in one launch, u and the scores in LDS.
-constexpr int PICK_PAGES = 4096, PICK_HEADS = 16, PICK_NT = 512;
-template <typename T, int D>
+constexpr int PICK_PAGES = 4096, PICK_HEADS = 16;
+template <typename T, int D, int PICK_NT>
 __global__ __launch_bounds__(PICK_NT) void block_pick(BlockDims m, const T* __restrict__ q, KeyStride qs, const T* __restrict__ boxes,
                                                       int32_t* __restrict__ sel_idx, int32_t* __restrict__ sel_cnt) {
   extern __shared__ __align__(16) double lds[];      // [G][D] sums, then [max_pages] scores; before them the parts of the sums
@@ -410,12 +475,12 @@ __device__ __forceinline__ uint32_t order_key32(float v) {
 // products or factors below 2^-126 taken for 0 (u is held to 2^-60 .. 2^40 here; a record outside is scored in 64 bits throughout).
 // With lo = S - e, hi = S + e (infinite where they are no numbers): a page whose hi is below the need-th largest lo is not
 // taken, one whose lo is above the (need + 1)-th largest hi is, and the others, a handful, are scored in 64 bits.  Bound by the
-// boxes it reads: 32 x 8 records of 1 640 pages on average (0.2 GB), %s; in 64 bits throughout 108.
+// boxes it reads: 32 x 8 records of 1 640 pages on average (0.2 GB), 62 us; in 64 bits throughout 108.
 constexpr int PICK_BORDER = 512;
-template <int D, bool LO>
-__global__ __launch_bounds__(PICK_NT) void block_pick_bounds(BlockDims m, const bf16raw* __restrict__ q, KeyStride qs, const bf16raw* __restrict__ boxes,
+template <int D, bool LO, int PICK_NT>
+__global__ __launch_bounds__(PICK_NT, LO && D == 128 ? 3 : 4) void block_pick_bounds(BlockDims m, const bf16raw* __restrict__ q, KeyStride qs, const bf16raw* __restrict__ boxes,
                                                              int32_t* __restrict__ sel_idx, int32_t* __restrict__ sel_cnt) {
-  constexpr int NF = D / 32, NW = PICK_NT / 64, PER = PICK_PAGES / PICK_NT;
+  constexpr int NF = D / 32, NW = PICK_NT / 64, PER = 8;
   extern __shared__ __align__(16) double lds[];      // [G][D] sums, then [max_pages] pairs of bounds; before them the parts of the sums
   __shared__ double border_sc[PICK_BORDER];
   __shared__ int32_t border_l[PICK_BORDER];
@@ -507,6 +572,12 @@ __global__ __launch_bounds__(PICK_NT) void block_pick_bounds(BlockDims m, const 
     }
   }
   __syncthreads();
+  // what is taken for certain, and the border
+  const auto settle = [&](int p, bool in, bool edge) {            // (all lanes of a wave, pages of 64 aligned to 64)
+    const unsigned long long sure = __ballot(in), w = sure | __ballot(p < see.seen && (p < c0 || p >= c1));
+    if (lane == 0) { taken[p >> 6] = w; if (sure) atomicAdd(&s_in, __popcll(sure)); }
+    if (edge) { const int at = atomicAdd(&s_border, 1); if (at < PICK_BORDER) border_l[at] = p; }      // (in any order: pages decide ties)
+  };
   // the need-th largest lo and the (need + 1)-th largest hi, two bits a turn, by counting what is not below three values in between
   uint32_t kl[PER], kh[PER];
 #pragma unroll
@@ -542,7 +613,6 @@ __global__ __launch_bounds__(PICK_NT) void block_pick_bounds(BlockDims m, const 
       hth |= (uint32_t)__popcll(up & 56) << shift;
     }
   }
-  // what is taken for certain, and the border
 #pragma unroll
   for (int x = 0; x < PER; ++x) {
     const int p = tid + x * PICK_NT;
@@ -553,9 +623,7 @@ __global__ __launch_bounds__(PICK_NT) void block_pick_bounds(BlockDims m, const 
       in = order_key32(v.x) > hth;
       edge = !in && order_key32(v.y) >= lth;
     }
-    const unsigned long long sure = __ballot(in), w = sure | __ballot(p < see.seen && (p < c0 || p >= c1));
-    if (lane == 0) { taken[p >> 6] = w; if (sure) atomicAdd(&s_in, __popcll(sure)); }
-    if (edge) { const int at = atomicAdd(&s_border, 1); if (at < PICK_BORDER) border_l[at] = p; }      // (in any order: pages decide ties)
+    settle(p, in, edge);
   }
   __syncthreads();
   const int nb = s_border, left = need - s_in;
@@ -685,20 +753,32 @@ int launch_block_select(hipStream_t s, int dtype, int d, const BlockDims& m, con
                         int32_t* sel_idx, int32_t* sel_cnt, void* ws) {
   const long long recs = (long long)m.B * m.nb * m.Hkv;
   const int per = 256, pieces = (m.max_pages + per - 1) / per;
-  if (!grid_fits(recs * (picks(m, dtype) ? PICK_NT / 256 : pieces))) return ADACLUSTER_E_UNSUPPORTED;
+  if (!grid_fits(recs * (picks(m, dtype) ? 2 : pieces))) return ADACLUSTER_E_UNSUPPORTED;
   if (picks(m, dtype)) {
-    // sums, then scores or the parts of the sums (PICK_NT vectors of 16 bytes' elements at most)
-    const int vec = dtype == ADACLUSTER_BF16 ? 8 : 4, parts = PICK_NT * vec;
+    // Threads: 512 where a launch has few records, so that a CU has loads on their way (256 records of 2 048 pages 62 us, with 256
+    // threads 76), 256 (more records a CU) else (512 records 116, with 512 threads 136).  Bounds pay from some 600 pages on (records of
+    // 512 pages: 35 us in 64 bits, 42 with bounds; of 750: 31 and 29; of 2 048: 108 and 62).
+    const bool wide = recs <= 256 || m.max_pages > 2048, bounds = dtype == ADACLUSTER_BF16 && m.max_pages > 512;
+    const int nt = wide ? 512 : 256, parts = nt * (dtype == ADACLUSTER_BF16 ? 8 : 4);      // sums, then scores or the parts of the sums
     const size_t lds = ((size_t)m.G * d + (m.max_pages > parts ? m.max_pages : parts)) * sizeof(double);
-#define CALL(D, LO) block_pick_bounds<D, LO><<<(int)recs, PICK_NT, lds, s>>>(m, (const bf16raw*)q, qs, (const bf16raw*)boxes, sel_idx, sel_cnt)
-    if (dtype == ADACLUSTER_BF16) {
-      if (m.qblock == 1) { if (d == 64) CALL(64, false); else CALL(128, false); }
-      else { if (d == 64) CALL(64, true); else CALL(128, true); }
+#define CALL(T, D)                                                                                                                              \
+  {                                                                                                                                             \
+    if (wide) block_pick<T, D, 512><<<(int)recs, 512, lds, s>>>(m, (const T*)q, qs, (const T*)boxes, sel_idx, sel_cnt);                       \
+    else block_pick<T, D, 256><<<(int)recs, 256, lds, s>>>(m, (const T*)q, qs, (const T*)boxes, sel_idx, sel_cnt);                            \
+  }
+#define BOUNDS(D, LO)                                                                                                                           \
+  {                                                                                                                                             \
+    if (wide) block_pick_bounds<D, LO, 512><<<(int)recs, 512, lds, s>>>(m, (const bf16raw*)q, qs, (const bf16raw*)boxes, sel_idx, sel_cnt);   \
+    else block_pick_bounds<D, LO, 256><<<(int)recs, 256, lds, s>>>(m, (const bf16raw*)q, qs, (const bf16raw*)boxes, sel_idx, sel_cnt);        \
+  }
+    if (bounds) {
+      if (m.qblock == 1) { if (d == 64) BOUNDS(64, false) else BOUNDS(128, false) }
+      else { if (d == 64) BOUNDS(64, true) else BOUNDS(128, true) }
+    } else {
+      BY_TYPE(dtype, d, CALL)
     }
 #undef CALL
-#define CALL(D) block_pick<float, D><<<(int)recs, PICK_NT, lds, s>>>(m, (const float*)q, qs, (const float*)boxes, sel_idx, sel_cnt)
-    else if (d == 64) CALL(64); else CALL(128);
-#undef CALL
+#undef BOUNDS
     return launched();
   }
   if (m.max_pages > m.topk) {
