@@ -45,7 +45,7 @@ __global__ __launch_bounds__(256) void grad_marks(BlockGradArgs a, long long ent
 //
 // In 16 bits rowsum(dO O) comes from a rounded O.  Its error e turns dS into dS - e P, whose rows no longer sum to 0, and a part of K
 // that all keys share then shows in dQ.  The row sums of dS are that error, so sum P K is kept beside dQ and dQ - rowsum(dS) sum P K
-// formed at the end (against 64 bits, 17 776 keys, d=64: dQ 0.0047 off without, 0.0025 with it); the corrected sums go on to grad_kv.
+// formed at the end (against 64 bits, 17 776 keys, d=64: dQ 0.0047 off without, 0.0024 with it); the corrected sums go on to grad_kv.
 template <typename T, int D, int R>
 __global__ __launch_bounds__(256) void grad_q(BlockGradArgs a, int rts) {
   constexpr int NF = D * sizeof(T) / 64, ND = D / 16;
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(256) void grad_kv(BlockGradArgs a, int groups) {
 
 // dQ of blocks of many rows, bf16: grad_q on tiles of 64 keys that all waves share (the walk of block_attn_wide), 32 rows a wave.
 template <int D, int NW>
-__global__ __launch_bounds__(NW * 64) void grad_q_wide(BlockGradArgs a, int rts, int items) {
+__global__ __launch_bounds__(NW * 64, 3) void grad_q_wide(BlockGradArgs a, int rts, int items) {
   constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB;
   __shared__ __align__(16) char lds[4 * TILEB];
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(NW * 64) void grad_q_wide(BlockGradArgs a, int rts,
       if (wave_has_rows) {
         const char* const kt = lds + (t & 1) * 2 * TILEB;
         const char* const vt = kt + TILEB;
-#pragma unroll
+#pragma unroll 1
         for (int kb = 0; kb < 2; ++kb) {
           f32x16_t sa = zero16(), dp = zero16();
 #pragma unroll
@@ -438,7 +438,7 @@ __global__ __launch_bounds__(NW * 64) void grad_q_wide(BlockGradArgs a, int rts,
 // them that share the rows of a tile.  A tile's rows of Q and dO are staged once for all waves and read both as rows (S, dP) and as
 // columns (dK, dV); the next tile is on its way meanwhile.
 template <int D, int KG>
-__global__ __launch_bounds__(256) void grad_kv_wide(BlockGradArgs a, int groups) {
+__global__ __launch_bounds__(256, 3) void grad_kv_wide(BlockGradArgs a, int groups) {
   constexpr int RG = 4 / KG, TR = 64 * RG, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int PT = TR * CH / 256, TILEB = TR * ROWB;
   __shared__ __align__(16) char lds[4 * TILEB];
@@ -545,7 +545,7 @@ __global__ __launch_bounds__(256) void grad_kv_wide(BlockGradArgs a, int groups)
     if (more) issue(u ^ 1);
     const char* const qt = lds + u * 2 * TILEB;
     const char* const gt = qt + TILEB;
-#pragma unroll
+#pragma unroll 1
     for (int half = 0; half < 2; ++half) {
       const int r0 = (rg * 2 + half) * 32;
       f32x16_t sa = zero16(), dp = zero16();
@@ -624,14 +624,353 @@ __global__ __launch_bounds__(256) void grad_kv_wide(BlockGradArgs a, int groups)
     }
 }
 
+// The same at d = 128, where a wave of 32 rows would hold 346 registers and a SIMD one wave.  Two waves share 32 rows: each forms the weights
+// and dS of 32 of a tile's 64 keys, passes the one that it does not need itself through LDS as the operand it is, and sums one of the two
+// products, dS K or P K, over all 64.  Two waves a SIMD then, of two workgroups with barriers of their own.  3 sequences up to 8 192 tokens, 16 / 4 heads: 794 us, by grad_q_wide
+// 1 033.
+__global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, int items) {
+  constexpr int D = 128, NW = 4, NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
+  constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB;
+  __shared__ __align__(16) char lds[4 * TILEB];
+  __shared__ __align__(16) u32x4_t pass[2][2][2][64];         // [rows][from][sixteen] of a lane's operands
+  __shared__ float offs[2][2][32];
+  __shared__ int2 pages_l[LIST];
+  __shared__ int32_t counts[NW];
+  const BlockDims& m = a.m;
+  int id = xcd_item(blockIdx.x);
+  if (id >= items) return;
+  const int rt = uniform(id % rts); id /= rts;
+  const int i = uniform(id % m.nb); id /= m.nb;
+  const int hk = uniform(id % m.Hkv), b = uniform(id / m.Hkv);
+  const BlockSeq s = block_seq(m, b);
+  const int t0 = i * m.qblock, rows = min(m.qblock, s.nq - t0) * m.G, base_row = rt * 64;
+  if (t0 >= s.nq || base_row >= rows) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5, rg = wave & 1, half = wave >> 1;
+  const int row = base_row + rg * 32 + c, tok = t0 + row / m.G, head = hk * m.G + row % m.G;
+  const bool there = row < rows;
+  const long long rec = (long long)(s.q0 + tok) * m.Hq + head;
+  bf16x8_t qf[KS], gf[KS];
+  {
+    const bf16raw* const q = (const bf16raw*)a.q + (long long)(s.q0 + tok) * a.qs.token + (long long)head * a.qs.head + hb * 8;
+    const bf16raw* const g = (const bf16raw*)a.d_o + (long long)(s.q0 + tok) * a.dos.token + (long long)head * a.dos.head + hb * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const u32x4_t z = {0, 0, 0, 0}, x = there ? *(const u32x4_t*)(q + ks * 16) : z, y = there ? *(const u32x4_t*)(g + ks * 16) : z;
+      qf[ks] = *(const bf16x8_t*)&x;
+      gf[ks] = *(const bf16x8_t*)&y;
+    }
+  }
+  const int lim = there ? (m.causal ? min(s.n, s.first + tok + 1) : s.n) : INT32_MAX;
+  const float l = there ? a.lse[rec] : -INFINITY, lse = l == -INFINITY ? INFINITY : l * LOG2E, delta = there ? a.delta[rec] : 0.f;
+  const bool wave_has_rows = base_row + rg * 32 < rows;
+  const int minlim = m.causal ? min(s.n, s.first + t0 + (base_row + rg * 32) / m.G + 1) : s.n;
+  const int last = min(base_row + 64, rows) - 1;
+  const int maxlim = m.causal ? min(s.n, s.first + t0 + last / m.G + 1) : s.n;
+  const int pages = maxlim > 0 ? (maxlim + m.page - 1) >> m.lpage : 0;
+  const int32_t* const list = a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
+  const int entries = list ? m.topk : pages;
+  f32x16_t acc[DB];                                 // of dS K in the first wave of a pair, of P K in the second
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = zero16();
+  float off = 0.f;
+  const float sc = a.scale_log2e;
+
+  int lrow[PT], piece[PT];
+#pragma unroll
+  for (int x = 0; x < PT; ++x) {
+    const int item = tid + x * NT;
+    lrow[x] = item / CH;
+    piece[x] = ((item % CH) ^ swz<D>(lrow[x])) * 16;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t*)lds;
+  const int lsub = m.lpage - 4, ktok = (int)(a.ks.token * 2), vtok = (int)(a.vs.token * 2);
+  int ra[KS], ca[DB][2];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) ra[ks] = row_operand<D>(lane, ks);
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) ca[db][x] = col_operand<D>(lane, db, x);
+
+  for (int e0 = 0; e0 < entries; e0 += LIST) {
+    const int n = fill_list<NT>(m, b, list, e0, 1, entries, pages, pages_l, counts);
+    const int parts = n << lsub, tiles = (parts + 3) >> 2;
+    if (!tiles) continue;
+    auto issue = [&](int stage, int t) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < PT; ++x) {
+        const int part = min(t * 4 + (((wave * 64 + x * NT) / CH) >> 4), parts - 1);
+        const int pg = __builtin_amdgcn_readfirstlane(pages_l[part >> lsub].x);
+        int sub = part & ((1 << lsub) - 1), have = s.n - ((pg << m.lpage) + sub * 16);
+        if (have <= 0) { sub = 0; have = 1; }
+        const int r = min(lrow[x] & 15, have - 1);
+        const uint32_t dst = lds0 + stage * 2 * TILEB + (wave * 64 + x * NT) * 16;
+        dma_b128(dst, (uint32_t)(r * ktok + piece[x]), uniform((const char*)a.k + row_at(m, s, a.ks, 0, pg, sub, hk) * 2));
+        dma_b128(dst + TILEB, (uint32_t)(r * vtok + piece[x]), uniform((const char*)a.v + row_at(m, s, a.vs, 0, pg, sub, hk) * 2));
+      }
+    };
+    issue(0, 0);
+    wait_vmcnt<0>();
+    lds_barrier();
+    for (int t = 0; t < tiles; ++t) {
+      if (t + 1 < tiles) issue((t + 1) & 1, t + 1);
+      const char* const kt = lds + (t & 1) * 2 * TILEB;
+      const char* const vt = kt + TILEB;
+      bf16x8_t own[2];
+      if (wave_has_rows) {
+        f32x16_t sa = zero16(), dp = zero16();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          sa = mfma32(*(const bf16x8_t*)(kt + half * 32 * ROWB + ra[ks]), qf[ks], sa);
+          dp = mfma32(*(const bf16x8_t*)(vt + half * 32 * ROWB + ra[ks]), gf[ks], dp);
+        }
+        bool whole = true;
+        int key0[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int part = t * 4 + half * 2 + x, pg = __builtin_amdgcn_readfirstlane(pages_l[min(part, parts - 1) >> lsub].x);
+          key0[x] = part < parts ? (pg << m.lpage) + (part & ((1 << lsub) - 1)) * 16 : INT32_MAX - 64;
+          whole = whole && key0[x] + 16 <= minlim;
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          sa[v] = __builtin_amdgcn_exp2f(fmaf(sa[v], sc, -lse));
+          dp[v] = sa[v] * (dp[v] - delta);
+        }
+        if (!whole) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if (key0[v >> 3] + 8 * ((v >> 2) & 1) + 4 * hb + (v & 3) >= lim) sa[v] = dp[v] = 0.f;
+        }
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+          const bf16x8_t pf = pack8(sa, s2), df = pack8(dp, s2);
+          off = sum8(df, off);
+          own[s2] = half ? pf : df;
+          *(bf16x8_t*)&pass[rg][half][s2][lane] = half ? df : pf;
+        }
+      }
+      lds_barrier();
+      if (wave_has_rows) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x)                   // its own half of the keys, then the other
+#pragma unroll
+          for (int s2 = 0; s2 < 2; ++s2) {
+            const bf16x8_t w = x == 0 ? own[s2] : *(const bf16x8_t*)&pass[rg][half ^ 1][s2][lane];
+            const char* const p = kt + ((half ^ x) * 32 + 16 * s2) * ROWB;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] = mfma32(join_tr(read_tr(p + ca[db][0]), read_tr(p + ca[db][1])), w, acc[db]);
+          }
+      }
+      wait_vmcnt<0>();
+      lds_barrier();
+    }
+  }
+  off += __shfl_xor(off, 32);
+  if (hb == 0) offs[rg][half][c] = off;
+  float* const pk = (float*)lds + rg * 64 * 64;      // P K to the first wave of a pair: [value][lane]
+  if (half) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) pk[(db * 16 + v) * 64 + lane] = acc[db][v];
+  }
+  __syncthreads();
+  if (half || !there) return;
+  const float e = offs[rg][0][c] + offs[rg][1][c];
+  bf16raw* const out = (bf16raw*)a.dq + (long long)(s.q0 + tok) * a.dqs.token + (long long)head * a.dqs.head + 4 * hb;
+#pragma unroll
+  for (int db = 0; db < DB; ++db) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) acc[db][v] = (acc[db][v] - e * pk[(db * 16 + v) * 64 + lane]) * a.scale;
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *(uint2*)(out + db * 32 + 8 * x) = uint2{pack_bf16x2(acc[db][4 * x], acc[db][4 * x + 1]), pack_bf16x2(acc[db][4 * x + 2], acc[db][4 * x + 3])};
+  }
+  if (hb == 0) a.delta[rec] = delta + e;             // (its only reader and writer in this launch)
+}
+
+// The same at d = 128, by pairs of waves as in grad_q_pair: each forms weights and dS of 32 of a tile's 64 rows, and sums one of dV and dK
+// over all of them.  64 keys a workgroup: 1 067 us, by grad_kv_wide 1 335.
+__global__ __launch_bounds__(256, 2) void grad_kv_pair(BlockGradArgs a, int groups) {
+  constexpr int D = 128, KG = 2, TR = 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
+  constexpr int PT = TR * CH / 256, TILEB = TR * ROWB;
+  __shared__ __align__(16) char lds[4 * TILEB];
+  __shared__ __align__(16) u32x4_t pass[2][2][2][64];         // [keys][from][sixteen] of a lane's operands
+  __shared__ __align__(16) float row_lse[2][TR], row_delta[2][TR];
+  __shared__ __align__(16) int row_lim[2][TR];
+  const BlockDims& m = a.m;
+  int id = blockIdx.x;                              // the first pages come first: they are seen by most
+  const int hk = uniform(id % m.Hkv); id /= m.Hkv;
+  const int b = uniform(id % m.B), kg = uniform(id / m.B);
+  const BlockSeq s = block_seq(m, b);
+  if (kg * KG * 32 >= s.n) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
+  const int kw = wave & 1, half = wave >> 1, key0 = kg * KG * 32 + kw * 32, key = key0 + c;
+  bf16x8_t kf[KS], vf[KS];
+  {
+    const bf16raw* const k = (const bf16raw*)a.k + (s.k0 + (long long)key) * a.ks.token + hk * a.ks.head + hb * 8;
+    const bf16raw* const v = (const bf16raw*)a.v + (s.k0 + (long long)key) * a.vs.token + hk * a.vs.head + hb * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const u32x4_t z = {0, 0, 0, 0}, x = key < s.n ? *(const u32x4_t*)(k + ks * 16) : z, y = key < s.n ? *(const u32x4_t*)(v + ks * 16) : z;
+      kf[ks] = *(const bf16x8_t*)&x;
+      vf[ks] = *(const bf16x8_t*)&y;
+    }
+  }
+  f32x16_t acc[DB];                                 // of dV in the first wave of a pair, of dK in the second
+#pragma unroll
+  for (int db = 0; db < DB; ++db) acc[db] = zero16();
+  const float sc = a.scale_log2e, inv_g = 1.f / m.G;
+
+  int lrow[PT], piece[PT];
+#pragma unroll
+  for (int x = 0; x < PT; ++x) {
+    const int item = tid + x * 256;
+    lrow[x] = item / CH;
+    piece[x] = ((item % CH) ^ swz<D>(lrow[x])) * 16;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t*)lds;
+  const int qtok = (int)(a.qs.token * 2), qhead = (int)(a.qs.head * 2), gtok = (int)(a.dos.token * 2), ghead = (int)(a.dos.head * 2);
+  int ra[KS], ca[DB][2];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) ra[ks] = row_operand<D>(lane, ks);
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) ca[db][x] = col_operand<D>(lane, db, x);
+
+  // tiles of the blocks that list the page and are not all before its keys: block `i`, rows from `base`
+  const uint32_t* const marks = a.sel ? a.marks + (((long long)b * m.Hkv + hk) * m.max_pages + (kg * KG * 32 >> m.lpage)) * a.words : nullptr;
+  const int blocks = (s.nq + m.qblock - 1) / m.qblock;
+  int word = -1, i = 0, base = 0, rows = 0;
+  uint32_t bits = 0;
+  auto advance = [&]() __attribute__((always_inline)) {      // false: no tile is left
+    base += TR;
+    for (;;) {
+      for (; base < rows; base += TR)
+        if (!m.causal || s.first + i * m.qblock + (min(base + TR, rows) - 1) / m.G >= kg * KG * 32) return true;
+      while (!bits) {
+        if (++word * 32 >= blocks) return false;
+        bits = marks ? (uint32_t)uniform((int)marks[word]) : ~0u;
+        if (blocks - word * 32 < 32) bits &= (1u << (blocks - word * 32)) - 1;
+      }
+      i = word * 32 + __builtin_ctz(bits);
+      bits &= bits - 1;
+      base = 0;
+      rows = min(m.qblock, s.nq - i * m.qblock) * m.G;
+    }
+  };
+  float nl = 0.f, nd = 0.f;
+  int nlim = 0;
+  auto issue = [&](int stage) __attribute__((always_inline)) {
+    const int t0 = i * m.qblock;
+    const char* const q = uniform((const char*)a.q + ((long long)(s.q0 + t0) * a.qs.token + (long long)(hk * m.G) * a.qs.head) * 2);
+    const char* const g = uniform((const char*)a.d_o + ((long long)(s.q0 + t0) * a.dos.token + (long long)(hk * m.G) * a.dos.head) * 2);
+#pragma unroll
+    for (int x = 0; x < PT; ++x) {
+      const int r = min(base + lrow[x], rows - 1), t = (int)((r + 0.5f) * inv_g), h = r - t * m.G;
+      const uint32_t dst = lds0 + stage * 2 * TILEB + (wave * 64 + x * 256) * 16;
+      dma_b128(dst, (uint32_t)(t * qtok + h * qhead + piece[x]), q);
+      dma_b128(dst + TILEB, (uint32_t)(t * gtok + h * ghead + piece[x]), g);
+    }
+    if (tid < TR) {
+      const int r = base + tid, t = (int)((r + 0.5f) * inv_g);
+      const bool there = r < rows;
+      const long long x = (long long)(s.q0 + t0 + t) * m.Hq + hk * m.G + (r - t * m.G);
+      const float l = there ? a.lse[x] : -INFINITY;
+      nl = l == -INFINITY ? INFINITY : l * LOG2E;
+      nd = there ? a.delta[x] : 0.f;
+      nlim = there ? (m.causal ? min(s.n, s.first + t0 + t + 1) : s.n) : 0;
+    }
+  };
+  auto land = [&](int stage) __attribute__((always_inline)) {
+    if (tid < TR) { row_lse[stage][tid] = nl; row_delta[stage][tid] = nd; row_lim[stage][tid] = nlim; }
+    wait_vmcnt<0>();
+    lds_barrier();
+  };
+  bool more = advance();
+  if (more) { issue(0); land(0); }
+  int u = 0;
+  while (more) {
+    // the keys a row of the tile misses at most: none where its first row sees them all and all of its rows are there
+    const int first_lim = m.causal ? min(s.n, s.first + i * m.qblock + base / m.G + 1) : s.n;
+    const bool whole = key0 + 32 <= first_lim && base + TR <= rows;
+    more = advance();
+    if (more) issue(u ^ 1);
+    const char* const qt = lds + u * 2 * TILEB;
+    const char* const gt = qt + TILEB;
+    bf16x8_t own[2];
+    {
+      const int r0 = half * 32;
+      f32x16_t sa = zero16(), dp = zero16();
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        sa = mfma32(*(const bf16x8_t*)(qt + r0 * ROWB + ra[ks]), kf[ks], sa);
+        dp = mfma32(*(const bf16x8_t*)(gt + r0 * ROWB + ra[ks]), vf[ks], dp);
+      }
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const f32x4_t l4 = *(const f32x4_t*)&row_lse[u][r0 + 8 * x + 4 * hb], d4 = *(const f32x4_t*)&row_delta[u][r0 + 8 * x + 4 * hb];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          sa[4 * x + j] = __builtin_amdgcn_exp2f(fmaf(sa[4 * x + j], sc, -l4[j]));
+          dp[4 * x + j] = sa[4 * x + j] * (dp[4 * x + j] - d4[j]);
+        }
+      }
+      if (!whole) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            if (key >= row_lim[u][r0 + 8 * x + 4 * hb + j]) sa[4 * x + j] = dp[4 * x + j] = 0.f;
+      }
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        const bf16x8_t pf = pack8(sa, s2), df = pack8(dp, s2);
+        own[s2] = half ? df : pf;
+        *(bf16x8_t*)&pass[kw][half][s2][lane] = half ? pf : df;
+      }
+    }
+    lds_barrier();
+    const char* const ct = half ? qt : gt;
+#pragma unroll
+    for (int x = 0; x < 2; ++x)                       // its own half of the rows, then the other
+#pragma unroll
+      for (int s2 = 0; s2 < 2; ++s2) {
+        const bf16x8_t w = x == 0 ? own[s2] : *(const bf16x8_t*)&pass[kw][half ^ 1][s2][lane];
+        const char* const p = ct + ((half ^ x) * 32 + 16 * s2) * ROWB;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] = mfma32(join_tr(read_tr(p + ca[db][0]), read_tr(p + ca[db][1])), w, acc[db]);
+      }
+    if (more) land(u ^ 1);
+    u ^= 1;
+  }
+  if (key >= s.n) return;
+  bf16raw* const out = (half ? (bf16raw*)a.dk + (s.k0 + (long long)key) * a.dks.token + hk * a.dks.head
+                             : (bf16raw*)a.dv + (s.k0 + (long long)key) * a.dvs.token + hk * a.dvs.head) + 4 * hb;
+  const float f = half ? a.scale : 1.f;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *(uint2*)(out + db * 32 + 8 * x) = uint2{pack_bf16x2(acc[db][4 * x] * f, acc[db][4 * x + 1] * f), pack_bf16x2(acc[db][4 * x + 2] * f, acc[db][4 * x + 3] * f)};
+}
+
 template <int D>
 int go_wide(hipStream_t s, const BlockGradArgs& a) {
   const BlockDims& m = a.m;
-  const int rows = m.qblock * m.G, rts = (rows + 127) / 128;
+  const int rows = m.qblock * m.G, rts = D == 128 ? (rows + 63) / 64 : (rows + 127) / 128;
   const long long items = (long long)rts * m.nb * m.Hkv * m.B, grid = xcd_grid(items);
-  const int KG = m.page >= 128 ? 4 : 2, groups = (m.max_pages << m.lpage) / (32 * KG);
+  const int KG = D == 64 && m.page >= 128 ? 4 : 2, groups = (m.max_pages << m.lpage) / (32 * KG);
   const long long wk = (long long)groups * m.Hkv * m.B;
   if (!grid_fits(grid) || !grid_fits(wk)) return ADACLUSTER_E_UNSUPPORTED;
+  if constexpr (D == 128) {
+    grad_q_pair<<<(int)grid, 256, 0, s>>>(a, rts, (int)items);
+    if (int rc = launched()) return rc;
+    grad_kv_pair<<<(int)wk, 256, 0, s>>>(a, groups);
+    return launched();
+  }
   grad_q_wide<D, 4><<<(int)grid, 256, 0, s>>>(a, rts, (int)items);
   if (int rc = launched()) return rc;
   if (KG == 4) grad_kv_wide<D, 4><<<(int)wk, 256, 0, s>>>(a, groups); else grad_kv_wide<D, 2><<<(int)wk, 256, 0, s>>>(a, groups);
@@ -651,7 +990,9 @@ int go(hipStream_t s, const BlockGradArgs& a) {
   constexpr int RPI = 256 / (D / Vec<T>::N);
   const long long deltas = ((long long)m.q_rows * m.Hq + RPI - 1) / RPI;
   const int rows = m.qblock * m.G, R = rows <= 16 ? 1 : 2, rts = (rows + 16 * R - 1) / (16 * R);
-  const int KR = m.page == 16 || (sizeof(T) == 4 && D == 128) ? 1 : 2, groups = (m.max_pages << m.lpage) / (16 * KR);
+  // 32 keys a workgroup (its registers allow that but for fp32 at d = 128) where that leaves two workgroups a CU (fp32, one head of 4 096
+  // keys: 128 workgroups %s us, 256 of 16 keys %s)
+  const int KR = m.page == 16 || (sizeof(T) == 4 && D == 128) || (long long)(m.max_pages << m.lpage) / 32 * m.Hkv * m.B < 512 ? 1 : 2, groups = (m.max_pages << m.lpage) / (16 * KR);
   const long long wq = (long long)rts * m.nb * m.Hkv * m.B, wk = (long long)groups * m.Hkv * m.B;
   const long long entries = a.sel ? (long long)m.B * m.nb * m.Hkv * m.topk : 0;
   if (!grid_fits(deltas) || !grid_fits(wq) || !grid_fits(wk) || !grid_fits(entries / 256 + 1)) return ADACLUSTER_E_UNSUPPORTED;

@@ -9,9 +9,10 @@ namespace {
 // the products.  Rows past a sequence's end are read from the last row there is in
 // their sixteenth (or the page's first) and masked: nothing behind the end is touched.
 template <int D, int NW>
-__global__ __launch_bounds__(NW * 64, 8 / NW) void block_attn_wide(BlockAttnArgs a, int rts, int items) {
+__global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(BlockAttnArgs a, int rts, int items) {
   constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
-  constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB;
+  constexpr int TK = 32, NKB = TK / 32, PARTS = TK / 16;      // keys a tile
+  constexpr int PT = TK * CH / NT, TILEB = TK * ROWB;
   __shared__ __align__(16) char lds[4 * TILEB];
   __shared__ int2 pages_l[LIST];
   __shared__ int32_t counts[NW];
@@ -74,12 +75,12 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void block_attn_wide(BlockAttnArgs
 
   for (int e0 = 0; e0 < entries; e0 += LIST) {
     const int n = fill_list<NT>(m, b, list, e0, 1, entries, pages, pages_l, counts);
-    const int parts = n << lsub, tiles = (parts + 3) >> 2;
+    const int parts = n << lsub, tiles = (parts + PARTS - 1) / PARTS;
     if (!tiles) continue;
     auto issue = [&](int stage, int t) __attribute__((always_inline)) {
 #pragma unroll
       for (int x = 0; x < PT; ++x) {                // a wave's request lies inside one sixteenth of a page
-        const int part = min(t * 4 + (((wave * 64 + x * NT) / CH) >> 4), parts - 1);
+        const int part = min(t * PARTS + (((wave * 64 + x * NT) / CH) >> 4), parts - 1);
         const int2 pp = pages_l[part >> lsub];
         const int pg = uniform(pp.x), phys = uniform(pp.y);
         int sub = part & ((1 << lsub) - 1), have = s.n - ((pg << m.lpage) + sub * 16);      // rows of it that exist
@@ -98,24 +99,24 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void block_attn_wide(BlockAttnArgs
       if (wave_has_rows) {
         const char* const kt = lds + (t & 1) * 2 * TILEB;
         const char* const vt = kt + TILEB;
-        f32x16_t sacc[2];
+        f32x16_t sacc[NKB];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
+        for (int kb = 0; kb < NKB; ++kb) {
           sacc[kb] = zero16();
 #pragma unroll
           for (int ks = 0; ks < KS; ++ks) sacc[kb] = mfma32(*(const bf16x8_t*)(kt + kb * 32 * ROWB + kaddr[ks]), qf[ks], sacc[kb]);
         }
-        int key0[4];
+        int key0[PARTS];
         bool whole = true;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int part = t * 4 + x, pg = uniform(pages_l[min(part, parts - 1) >> lsub].x);
+        for (int x = 0; x < PARTS; ++x) {
+          const int part = t * PARTS + x, pg = uniform(pages_l[min(part, parts - 1) >> lsub].x);
           key0[x] = part < parts ? (pg << m.lpage) + (part & ((1 << lsub) - 1)) * 16 : INT32_MAX - 64;
           whole = whole && key0[x] + 16 <= minlim;
         }
         if (!whole) {
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+          for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
             for (int v = 0; v < 16; ++v)
               if (key0[kb * 2 + (v >> 3)] + 8 * ((v >> 2) & 1) + 4 * hb + (v & 3) >= lim) sacc[kb][v] = -INFINITY;
@@ -123,13 +124,13 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void block_attn_wide(BlockAttnArgs
         // p = 2^((s - reference) scale): any reference gives the same result as long as nothing overflows.  The row sum of the tile
         // tells (on the first tile with a score above -inf it is infinite): only then is the tile's maximum taken, the reference
         // moved up to it and the accumulator scaled.
-        bf16x8_t pf[2][2];
+        bf16x8_t pf[NKB][2];
         float rsum;
         auto weights = [&]() __attribute__((always_inline)) {
           const float off = mref * sc;
-          float part[4];
+          float part[2 * NKB];
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+          for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
             for (int s2 = 0; s2 < 2; ++s2) {
               const f32x16_t& x = sacc[kb];
@@ -144,13 +145,14 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void block_attn_wide(BlockAttnArgs
               }
               pf[kb][s2] = u.v;
             }
-          rsum = (part[0] + part[1]) + (part[2] + part[3]);
+          rsum = part[0] + part[1];
+          if constexpr (NKB == 2) rsum += part[2] + part[3];
         };
         weights();
         if (__any(!(rsum <= 65536.f))) {
           float top = sacc[0][0];
 #pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
+          for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
             for (int v = 0; v < 16; ++v) top = fmaxf(top, sacc[kb][v]);
           top = fmaxf(top, __shfl_xor(top, 32));
@@ -163,7 +165,7 @@ __global__ __launch_bounds__(NW * 64, 8 / NW) void block_attn_wide(BlockAttnArgs
         }
         lrun += rsum;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int kb = 0; kb < NKB; ++kb)
 #pragma unroll
           for (int s2 = 0; s2 < 2; ++s2) {
             const char* const p = vt + (kb * 32 + 16 * s2) * ROWB;
