@@ -115,7 +115,7 @@ int adacluster_block_workspace_bytes(const adacluster_block_params* p, int32_t c
   else if (call == ADACLUSTER_BLOCK_ATTN) {
     const size_t x = block_attn_bytes(m, p->dtype, p->bits, p->d, true), y = block_attn_bytes(m, p->dtype, p->bits, p->d, false);
     *bytes = p->topk > 0 && x > y ? x : y;
-  } else if (call == ADACLUSTER_BLOCK_BACKWARD) *bytes = block_grad_bytes(m, true);
+  } else if (call == ADACLUSTER_BLOCK_BACKWARD) *bytes = block_grad_bytes(m, p->dtype, p->d, true);
   else return fail(ADACLUSTER_E_BADARG, "unknown call %d", call);
   return 0;
 }
@@ -213,7 +213,7 @@ int adacluster_block_attn_backward(const adacluster_block_params* p, const void*
   const struct { const char* name; const void* p; const KeyStride* s; } rows[] = {{"q", q, &a.qs}, {"k", k, &a.ks}, {"v", v, &a.vs}, {"o", o, &a.os},
       {"d_o", d_o, &a.dos}, {"dq", dq, &a.dqs}, {"dk", dk, &a.dks}, {"dv", dv, &a.dvs}};
   for (const auto& r : rows) if (int rc = check_rows(r.name, r.p, p->dtype, *r.s)) return rc;
-  if (int rc = check_ws(ws, ws_bytes, block_grad_bytes(a.m, sel_idx != nullptr))) return rc;
+  if (int rc = check_ws(ws, ws_bytes, block_grad_bytes(a.m, p->dtype, p->d, sel_idx != nullptr))) return rc;
   a.q = q; a.k = k; a.v = v; a.o = o; a.lse = lse; a.d_o = d_o; a.sel = sel_idx; a.dq = dq; a.dk = dk; a.dv = dv;
   a.scale = scale_of(p);
   a.scale_log2e = a.scale * LOG2E;

@@ -287,20 +287,40 @@ __global__ __launch_bounds__(256) void grad_kv(BlockGradArgs a, int groups) {
     }
 }
 
+// A page that far more blocks list than others (the first one, say) would be the launch's critical path.  Where a launch has few
+// workgroups, the blocks of such a page are dealt to up to `np` workgroups, each a run of the page's marks; their sums go to
+// memory (a wave's 64 values a lane as they are) and grad_kv_join adds them in order.
+struct Share { int first, count, parts; };
+__device__ __forceinline__ Share page_share(const BlockGradArgs& a, const uint32_t* marks, int blocks, int part) {
+  if (a.np == 1) return {0, blocks, 1};
+  int n = 0;
+  for (int w = 0; w * 32 < blocks; ++w) n += __popc((uint32_t)uniform((int)marks[w]));      // (no mark lies past the last block)
+  const int parts = min(a.np, max(1, (n + a.limit - 1) / a.limit));
+  const int first = (int)((long long)n * part / parts);
+  return {first, (int)((long long)n * (part + 1) / parts) - first, parts};
+}
+__device__ __forceinline__ float* share_slot(const BlockGradArgs& a, int group, int part, int wave, int lane) {
+  return a.sums + (((long long)group * a.np + part) * 4 + wave) * 4096 + lane;
+}
+template <int DB> __device__ __forceinline__ void store_rows(bf16raw* out, const f32x16_t* x, float f) {
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+      *(uint2*)(out + db * 32 + 8 * y) = uint2{pack_bf16x2(x[db][4 * y] * f, x[db][4 * y + 1] * f), pack_bf16x2(x[db][4 * y + 2] * f, x[db][4 * y + 3] * f)};
+}
+
 // dQ of blocks of many rows, bf16: grad_q on tiles of 64 keys that all waves share (the walk of block_attn_wide), 32 rows a wave.
-template <int D, int NW>
-__global__ __launch_bounds__(NW * 64, 3) void grad_q_wide(BlockGradArgs a, int rts, int items) {
-  constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
+__global__ __launch_bounds__(256, 3) void grad_q_wide(BlockGradArgs a, int rts, int split) {
+  constexpr int D = 64, NW = 4, NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB;
   __shared__ __align__(16) char lds[4 * TILEB];
   __shared__ int2 pages_l[LIST];
   __shared__ int32_t counts[NW];
   const BlockDims& m = a.m;
-  int id = xcd_item(blockIdx.x);
-  if (id >= items) return;
-  const int rt = uniform(id % rts); id /= rts;
-  const int i = uniform(id % m.nb); id /= m.nb;
-  const int hk = uniform(id % m.Hkv), b = uniform(id / m.Hkv);
+  const HeadItem it = xcd_item(blockIdx.x, m.B * m.Hkv, m.nb * rts, split);
+  if (it.head < 0) return;
+  const int rt = it.item % rts, i = it.item / rts, hk = it.head % m.Hkv, b = it.head / m.Hkv;
   const BlockSeq s = block_seq(m, b);
   const int t0 = i * m.qblock, rows = min(m.qblock, s.nq - t0) * m.G, base_row = rt * NT / 2;
   if (t0 >= s.nq || base_row >= rows) return;
@@ -437,19 +457,26 @@ __global__ __launch_bounds__(NW * 64, 3) void grad_q_wide(BlockGradArgs a, int r
 // dK and dV of 32 KG keys (a page, or a part of one), bf16, from blocks of many rows: KG waves of 32 keys side by side, and 4 / KG groups of
 // them that share the rows of a tile.  A tile's rows of Q and dO are staged once for all waves and read both as rows (S, dP) and as
 // columns (dK, dV); the next tile is on its way meanwhile.
-template <int D, int KG>
-__global__ __launch_bounds__(256, 3) void grad_kv_wide(BlockGradArgs a, int groups) {
-  constexpr int RG = 4 / KG, TR = 64 * RG, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
+template <int KG>
+__global__ __launch_bounds__(256, 3) void grad_kv_wide(BlockGradArgs a, int split) {
+  constexpr int D = 64, RG = 4 / KG, TR = 64 * RG, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int PT = TR * CH / 256, TILEB = TR * ROWB;
   __shared__ __align__(16) char lds[4 * TILEB];
   __shared__ __align__(16) float row_lse[2][TR], row_delta[2][TR];
   __shared__ __align__(16) int row_lim[2][TR];
   const BlockDims& m = a.m;
-  int id = blockIdx.x;                              // the first pages come first: they are seen by most
-  const int hk = uniform(id % m.Hkv); id /= m.Hkv;
-  const int b = uniform(id % m.B), kg = uniform(id / m.B);
+  // The first pages come first, those of all heads side by side: they are seen by most.  A head stays on the same XCDs (as in xcd_item).
+  // Shares behind the first come last.
+  const int heads = m.B * m.Hkv, units = heads * split, per = (a.groups + split - 1) / split * units;
+  const int part = uniform((int)(blockIdx.x / (unsigned)per)), at = uniform((int)(blockIdx.x % (unsigned)per)), unit = at % units;
+  const int head = unit / split, kg = at / units * split + unit % split, group = kg * heads + head, hk = head % m.Hkv, b = head / m.Hkv;
+  if (kg >= a.groups) return;
   const BlockSeq s = block_seq(m, b);
   if (kg * KG * 32 >= s.n) return;
+  const uint32_t* const marks = a.sel ? a.marks + (((long long)b * m.Hkv + hk) * m.max_pages + (kg * KG * 32 >> m.lpage)) * a.words : nullptr;
+  const int blocks = (s.nq + m.qblock - 1) / m.qblock;
+  const Share share = page_share(a, marks, blocks, part);
+  if (part >= share.parts) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
   const int rg = wave / KG, key0 = kg * KG * 32 + (wave % KG) * 32, key = key0 + c;
   bf16x8_t kf[KS], vf[KS];
@@ -486,9 +513,7 @@ __global__ __launch_bounds__(256, 3) void grad_kv_wide(BlockGradArgs a, int grou
     for (int x = 0; x < 2; ++x) ca[db][x] = col_operand<D>(lane, db, x);
 
   // tiles of the blocks that list the page and are not all before its keys: block `i`, rows from `base`
-  const uint32_t* const marks = a.sel ? a.marks + (((long long)b * m.Hkv + hk) * m.max_pages + (kg * KG * 32 >> m.lpage)) * a.words : nullptr;
-  const int blocks = (s.nq + m.qblock - 1) / m.qblock;
-  int word = -1, i = 0, base = 0, rows = 0;
+  int word = -1, i = 0, base = 0, rows = 0, skip = share.first, left = share.count;
   uint32_t bits = 0;
   auto advance = [&]() __attribute__((always_inline)) {      // false: no tile is left
     base += TR;
@@ -500,8 +525,11 @@ __global__ __launch_bounds__(256, 3) void grad_kv_wide(BlockGradArgs a, int grou
         bits = marks ? (uint32_t)uniform((int)marks[word]) : ~0u;
         if (blocks - word * 32 < 32) bits &= (1u << (blocks - word * 32)) - 1;
       }
+      if (!left) return false;
       i = word * 32 + __builtin_ctz(bits);
       bits &= bits - 1;
+      if (skip) { --skip; continue; }
+      --left;
       base = 0;
       rows = min(m.qblock, s.nq - i * m.qblock) * m.G;
     }
@@ -611,24 +639,24 @@ __global__ __launch_bounds__(256, 3) void grad_kv_wide(BlockGradArgs a, int grou
       }
     if (rg) return;
   }
+  if (share.parts > 1) {
+    float* const to = share_slot(a, group, part, wave, lane);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) { to[(db * 16 + v) * 64] = dk[db][v]; to[((DB + db) * 16 + v) * 64] = dv[db][v]; }
+    return;
+  }
   if (key >= s.n) return;
-  bf16raw* const ok = (bf16raw*)a.dk + (s.k0 + (long long)key) * a.dks.token + hk * a.dks.head + 4 * hb;
-  bf16raw* const ov = (bf16raw*)a.dv + (s.k0 + (long long)key) * a.dvs.token + hk * a.dvs.head + 4 * hb;
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const float f = a.scale;
-      *(uint2*)(ok + db * 32 + 8 * x) = uint2{pack_bf16x2(dk[db][4 * x] * f, dk[db][4 * x + 1] * f), pack_bf16x2(dk[db][4 * x + 2] * f, dk[db][4 * x + 3] * f)};
-      *(uint2*)(ov + db * 32 + 8 * x) = uint2{pack_bf16x2(dv[db][4 * x], dv[db][4 * x + 1]), pack_bf16x2(dv[db][4 * x + 2], dv[db][4 * x + 3])};
-    }
+  store_rows<DB>((bf16raw*)a.dk + (s.k0 + (long long)key) * a.dks.token + hk * a.dks.head + 4 * hb, dk, a.scale);
+  store_rows<DB>((bf16raw*)a.dv + (s.k0 + (long long)key) * a.dvs.token + hk * a.dvs.head + 4 * hb, dv, 1.f);
 }
 
 // The same at d = 128, where a wave of 32 rows would hold 346 registers and a SIMD one wave.  Two waves share 32 rows: each forms the weights
 // and dS of 32 of a tile's 64 keys, passes the one that it does not need itself through LDS as the operand it is, and sums one of the two
 // products, dS K or P K, over all 64.  Two waves a SIMD then, of two workgroups with barriers of their own.  3 sequences up to 8 192 tokens, 16 / 4 heads: 794 us, by grad_q_wide
 // 1 033.
-__global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, int items) {
+__global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, int split) {
   constexpr int D = 128, NW = 4, NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB;
   __shared__ __align__(16) char lds[4 * TILEB];
@@ -637,11 +665,9 @@ __global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, 
   __shared__ int2 pages_l[LIST];
   __shared__ int32_t counts[NW];
   const BlockDims& m = a.m;
-  int id = xcd_item(blockIdx.x);
-  if (id >= items) return;
-  const int rt = uniform(id % rts); id /= rts;
-  const int i = uniform(id % m.nb); id /= m.nb;
-  const int hk = uniform(id % m.Hkv), b = uniform(id / m.Hkv);
+  const HeadItem it = xcd_item(blockIdx.x, m.B * m.Hkv, m.nb * rts, split);
+  if (it.head < 0) return;
+  const int rt = it.item % rts, i = it.item / rts, hk = it.head % m.Hkv, b = it.head / m.Hkv;
   const BlockSeq s = block_seq(m, b);
   const int t0 = i * m.qblock, rows = min(m.qblock, s.nq - t0) * m.G, base_row = rt * 64;
   if (t0 >= s.nq || base_row >= rows) return;
@@ -792,7 +818,7 @@ __global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, 
 
 // The same at d = 128, by pairs of waves as in grad_q_pair: each forms weights and dS of 32 of a tile's 64 rows, and sums one of dV and dK
 // over all of them.  64 keys a workgroup: 1 067 us, by grad_kv_wide 1 335.
-__global__ __launch_bounds__(256, 2) void grad_kv_pair(BlockGradArgs a, int groups) {
+__global__ __launch_bounds__(256, 2) void grad_kv_pair(BlockGradArgs a, int split) {
   constexpr int D = 128, KG = 2, TR = 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int PT = TR * CH / 256, TILEB = TR * ROWB;
   __shared__ __align__(16) char lds[4 * TILEB];
@@ -800,11 +826,18 @@ __global__ __launch_bounds__(256, 2) void grad_kv_pair(BlockGradArgs a, int grou
   __shared__ __align__(16) float row_lse[2][TR], row_delta[2][TR];
   __shared__ __align__(16) int row_lim[2][TR];
   const BlockDims& m = a.m;
-  int id = blockIdx.x;                              // the first pages come first: they are seen by most
-  const int hk = uniform(id % m.Hkv); id /= m.Hkv;
-  const int b = uniform(id % m.B), kg = uniform(id / m.B);
+  // The first pages come first, those of all heads side by side: they are seen by most.  A head stays on the same XCDs (as in xcd_item).
+  // Shares behind the first come last.
+  const int heads = m.B * m.Hkv, units = heads * split, per = (a.groups + split - 1) / split * units;
+  const int part = uniform((int)(blockIdx.x / (unsigned)per)), at = uniform((int)(blockIdx.x % (unsigned)per)), unit = at % units;
+  const int head = unit / split, kg = at / units * split + unit % split, group = kg * heads + head, hk = head % m.Hkv, b = head / m.Hkv;
+  if (kg >= a.groups) return;
   const BlockSeq s = block_seq(m, b);
   if (kg * KG * 32 >= s.n) return;
+  const uint32_t* const marks = a.sel ? a.marks + (((long long)b * m.Hkv + hk) * m.max_pages + (kg * KG * 32 >> m.lpage)) * a.words : nullptr;
+  const int blocks = (s.nq + m.qblock - 1) / m.qblock;
+  const Share share = page_share(a, marks, blocks, part);
+  if (part >= share.parts) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
   const int kw = wave & 1, half = wave >> 1, key0 = kg * KG * 32 + kw * 32, key = key0 + c;
   bf16x8_t kf[KS], vf[KS];
@@ -841,9 +874,7 @@ __global__ __launch_bounds__(256, 2) void grad_kv_pair(BlockGradArgs a, int grou
     for (int x = 0; x < 2; ++x) ca[db][x] = col_operand<D>(lane, db, x);
 
   // tiles of the blocks that list the page and are not all before its keys: block `i`, rows from `base`
-  const uint32_t* const marks = a.sel ? a.marks + (((long long)b * m.Hkv + hk) * m.max_pages + (kg * KG * 32 >> m.lpage)) * a.words : nullptr;
-  const int blocks = (s.nq + m.qblock - 1) / m.qblock;
-  int word = -1, i = 0, base = 0, rows = 0;
+  int word = -1, i = 0, base = 0, rows = 0, skip = share.first, left = share.count;
   uint32_t bits = 0;
   auto advance = [&]() __attribute__((always_inline)) {      // false: no tile is left
     base += TR;
@@ -855,8 +886,11 @@ __global__ __launch_bounds__(256, 2) void grad_kv_pair(BlockGradArgs a, int grou
         bits = marks ? (uint32_t)uniform((int)marks[word]) : ~0u;
         if (blocks - word * 32 < 32) bits &= (1u << (blocks - word * 32)) - 1;
       }
+      if (!left) return false;
       i = word * 32 + __builtin_ctz(bits);
       bits &= bits - 1;
+      if (skip) { --skip; continue; }
+      --left;
       base = 0;
       rows = min(m.qblock, s.nq - i * m.qblock) * m.G;
     }
@@ -946,42 +980,93 @@ __global__ __launch_bounds__(256, 2) void grad_kv_pair(BlockGradArgs a, int grou
     if (more) land(u ^ 1);
     u ^= 1;
   }
+  if (share.parts > 1) {
+    float* const to = share_slot(a, group, part, wave, lane);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) to[(db * 16 + v) * 64] = acc[db][v];
+    return;
+  }
   if (key >= s.n) return;
-  bf16raw* const out = (half ? (bf16raw*)a.dk + (s.k0 + (long long)key) * a.dks.token + hk * a.dks.head
-                             : (bf16raw*)a.dv + (s.k0 + (long long)key) * a.dvs.token + hk * a.dvs.head) + 4 * hb;
-  const float f = half ? a.scale : 1.f;
+  store_rows<DB>((half ? (bf16raw*)a.dk + (s.k0 + (long long)key) * a.dks.token + hk * a.dks.head
+                       : (bf16raw*)a.dv + (s.k0 + (long long)key) * a.dvs.token + hk * a.dvs.head) + 4 * hb, acc, half ? a.scale : 1.f);
+}
+
+// The sums of pages whose blocks were dealt to several workgroups.  A wave's lane holds what it held there: d = 64 both gradients of a key
+// (wave: 32 keys, or with two of them the first two waves), d = 128 one of them (waves 0, 1: dV; 2, 3: dK).
+template <int D, int KG>
+__global__ __launch_bounds__(256) void grad_kv_join(BlockGradArgs a) {
+  constexpr int DB = D / 32;
+  const BlockDims& m = a.m;
+  const int group = blockIdx.x, hk = group % m.Hkv, b = group / m.Hkv % m.B, kg = group / m.Hkv / m.B;
+  const BlockSeq s = block_seq(m, b);
+  if (kg * KG * 32 >= s.n) return;
+  const uint32_t* const marks = a.marks + (((long long)b * m.Hkv + hk) * m.max_pages + (kg * KG * 32 >> m.lpage)) * a.words;
+  const Share share = page_share(a, marks, (s.nq + m.qblock - 1) / m.qblock, 0);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (share.parts < 2 || (D == 64 && wave >= KG)) return;
+  f32x16_t x[4];                                     // 64 values
 #pragma unroll
-  for (int db = 0; db < DB; ++db)
+  for (int y = 0; y < 4; ++y) x[y] = zero16();
+  for (int part = 0; part < share.parts; ++part) {
+    const float* const from = share_slot(a, group, part, wave, lane);
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-      *(uint2*)(out + db * 32 + 8 * x) = uint2{pack_bf16x2(acc[db][4 * x] * f, acc[db][4 * x + 1] * f), pack_bf16x2(acc[db][4 * x + 2] * f, acc[db][4 * x + 3] * f)};
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) x[y][v] += from[(y * 16 + v) * 64];
+  }
+  const int key = kg * KG * 32 + (D == 64 ? wave : wave & 1) * 32 + (lane & 31), hb = lane >> 5;
+  if (key >= s.n) return;
+  bf16raw* const ok = (bf16raw*)a.dk + (s.k0 + (long long)key) * a.dks.token + hk * a.dks.head + 4 * hb;
+  bf16raw* const ov = (bf16raw*)a.dv + (s.k0 + (long long)key) * a.dvs.token + hk * a.dvs.head + 4 * hb;
+  if constexpr (D == 64) { store_rows<DB>(ok, x, a.scale); store_rows<DB>(ov, x + DB, 1.f); }
+  else store_rows<DB>(wave >> 1 ? ok : ov, x, wave >> 1 ? a.scale : 1.f);
+}
+
+// Workgroups that a page's blocks go to at most, where there are lists and a launch has fewer than 4 096 workgroups (eight rounds of two a CU,
+// and 268 MB of sums at most); and the blocks from which on: a quarter more than a page has on average.  A training pass of one
+// sequence of 8 192 tokens, lists of 32 pages: 4 / 1 heads, d = 128 1 226 -> 541 us, 16 / 4 heads 1 575 -> 1 031, 8 / 2 heads, d = 64 734 -> 392;
+// three sequences, 1 536 workgroups: 3 % of the launch.
+struct Deal { int KG, groups, np, limit; long long wg; };
+Deal deal_of(const BlockDims& m, int d, bool listed) {
+  Deal x;
+  x.KG = d == 64 && m.page >= 128 ? 4 : 2;
+  x.groups = (m.max_pages << m.lpage) / (32 * x.KG);
+  x.wg = (long long)x.groups * m.Hkv * m.B;
+  x.np = listed && x.wg < 4096 ? (int)(x.wg < 512 ? 8 : 4096 / x.wg) : 1;
+  const long long mean = (long long)m.nb * m.topk / m.max_pages;
+  x.limit = (int)(mean + mean / 4 > 4 ? mean + mean / 4 : 4);
+  return x;
 }
 
 template <int D>
-int go_wide(hipStream_t s, const BlockGradArgs& a) {
+int go_wide(hipStream_t s, const BlockGradArgs& a, const Deal& x) {
   const BlockDims& m = a.m;
-  const int rows = m.qblock * m.G, rts = D == 128 ? (rows + 63) / 64 : (rows + 127) / 128;
-  const long long items = (long long)rts * m.nb * m.Hkv * m.B, grid = xcd_grid(items);
-  const int KG = D == 64 && m.page >= 128 ? 4 : 2, groups = (m.max_pages << m.lpage) / (32 * KG);
-  const long long wk = (long long)groups * m.Hkv * m.B;
+  const int rows = m.qblock * m.G, per = D == 128 ? 64 : 128, rts = (rows + per - 1) / per;
+  const long long heads = (long long)m.Hkv * m.B, grid = xcd_grid(heads, (long long)rts * m.nb), wk = xcd_grid(heads, x.groups) * x.np;
+  const int split = xcd_split(heads);
   if (!grid_fits(grid) || !grid_fits(wk)) return ADACLUSTER_E_UNSUPPORTED;
-  if constexpr (D == 128) {
-    grad_q_pair<<<(int)grid, 256, 0, s>>>(a, rts, (int)items);
-    if (int rc = launched()) return rc;
-    grad_kv_pair<<<(int)wk, 256, 0, s>>>(a, groups);
-    return launched();
-  }
-  grad_q_wide<D, 4><<<(int)grid, 256, 0, s>>>(a, rts, (int)items);
+  if constexpr (D == 128) grad_q_pair<<<(int)grid, 256, 0, s>>>(a, rts, split); else grad_q_wide<<<(int)grid, 256, 0, s>>>(a, rts, split);
   if (int rc = launched()) return rc;
-  if (KG == 4) grad_kv_wide<D, 4><<<(int)wk, 256, 0, s>>>(a, groups); else grad_kv_wide<D, 2><<<(int)wk, 256, 0, s>>>(a, groups);
+  if constexpr (D == 128) grad_kv_pair<<<(int)wk, 256, 0, s>>>(a, split);
+  else if (x.KG == 4) grad_kv_wide<4><<<(int)wk, 256, 0, s>>>(a, split);
+  else grad_kv_wide<2><<<(int)wk, 256, 0, s>>>(a, split);
+  if (x.np > 1) {
+    if (int rc = launched()) return rc;
+    if constexpr (D == 128) grad_kv_join<128, 2><<<(int)x.wg, 256, 0, s>>>(a);
+    else if (x.KG == 4) grad_kv_join<64, 4><<<(int)x.wg, 256, 0, s>>>(a);
+    else grad_kv_join<64, 2><<<(int)x.wg, 256, 0, s>>>(a);
+  }
   return launched();
 }
 
 // Blocks of at least 48 rows over pages of 64 keys or more, bf16, with offsets inside a block or a sixteenth that 32 bits hold.
+bool rows_wide(const BlockDims& m) { return m.qblock * m.G >= 48 && m.qblock * m.G <= (1 << 20) && m.page >= 64; }
 bool wide_takes(const BlockGradArgs& a) {
   const BlockDims& m = a.m;
   const auto block = [&](const KeyStride& st) { return m.qblock * st.token + m.G * st.head < (1 << 30); };
-  return m.qblock * m.G >= 48 && m.qblock * m.G <= (1 << 20) && m.page >= 64 && a.ks.token < (1 << 25) && a.vs.token < (1 << 25) && block(a.qs) && block(a.dos);
+  return rows_wide(m) && a.ks.token < (1 << 25) && a.vs.token < (1 << 25) && block(a.qs) && block(a.dos);
 }
 
 template <typename T, int D>
@@ -1003,7 +1088,7 @@ int go(hipStream_t s, const BlockGradArgs& a) {
   }
   grad_delta<T, D><<<(int)deltas, 256, 0, s>>>(a);
   if (int rc = launched()) return rc;
-  if constexpr (sizeof(T) == 2) if (wide_takes(a)) return go_wide<D>(s, a);
+  if constexpr (sizeof(T) == 2) if (wide_takes(a)) return go_wide<D>(s, a, deal_of(m, D, a.sel != nullptr));
   if (R == 1) grad_q<T, D, 1><<<(int)wq, 256, 0, s>>>(a, rts); else grad_q<T, D, 2><<<(int)wq, 256, 0, s>>>(a, rts);
   if (int rc = launched()) return rc;
   if (KR == 1) grad_kv<T, D, 1><<<(int)wk, 256, 0, s>>>(a, groups);
@@ -1011,18 +1096,29 @@ int go(hipStream_t s, const BlockGradArgs& a) {
   return launched();
 }
 
+size_t marks_bytes(const BlockDims& m) { return align_up((size_t)m.B * m.Hkv * m.max_pages * ((m.nb + 31) / 32) * 4, 256); }
 size_t delta_bytes(const BlockDims& m) { return align_up((size_t)m.q_rows * m.Hq * 4, 256); }
 
 }  // namespace
 
-size_t block_grad_bytes(const BlockDims& m, bool listed) {
-  return delta_bytes(m) + (listed ? (size_t)m.B * m.Hkv * m.max_pages * ((m.nb + 31) / 32) * 4 : 0);
+size_t block_grad_bytes(const BlockDims& m, int dtype, int d, bool listed) {
+  size_t n = delta_bytes(m) + (listed ? marks_bytes(m) : 0);
+  if (dtype == ADACLUSTER_BF16 && rows_wide(m)) {
+    const Deal x = deal_of(m, d, listed);
+    if (x.np > 1) n += (size_t)x.wg * x.np * 4 * 4096 * sizeof(float);
+  }
+  return n;
 }
 
 int launch_block_attn_backward(hipStream_t s, int dtype, int d, BlockGradArgs a, void* ws) {
+  const Deal x = deal_of(a.m, d, a.sel != nullptr);
   a.delta = (float*)ws;
   a.marks = (uint32_t*)((char*)ws + delta_bytes(a.m));
+  a.sums = (float*)((char*)a.marks + marks_bytes(a.m));
   a.words = (a.m.nb + 31) / 32;
+  a.np = x.np;
+  a.groups = x.groups;
+  a.limit = x.limit;
   if (dtype == ADACLUSTER_BF16) return d == 64 ? go<bf16raw, 64>(s, a) : go<bf16raw, 128>(s, a);
   return d == 64 ? go<float, 64>(s, a) : go<float, 128>(s, a);
 }

@@ -57,12 +57,15 @@ __device__ __forceinline__ f32x16_t zero16() {
   return z;
 }
 
-// A launch's workgroups go to the 8 XCDs in turn: runs of GROUP neighbours (blocks of a sequence, whose lists are alike) share one.
-constexpr int XCD_RUN = 16;
-__device__ __forceinline__ int xcd_item(int id) {
-  const int run = id / (8 * XCD_RUN);
-  return (run * 8 + id % 8) * XCD_RUN + id / 8 % XCD_RUN;
+// A launch's workgroups go to the 8 XCDs in turn, and each XCD has an L2 of its own, which the keys (or the rows) of about one head of a
+// sequence fill.  So a head's workgroups stay on one XCD, one head after the other; where the heads of all sequences are no
+// multiple of 8, each goes to `split` XCDs, every split-th workgroup to each.
+struct HeadItem { int head, item; };                 // head < 0: none
+__device__ __forceinline__ HeadItem xcd_item(int id, int heads, int items, int split) {
+  const int per = (items + split - 1) / split, unit = (id & 7) + 8 * ((id >> 3) / per), item = (id >> 3) % per * split + unit % split;
+  return {item < items ? uniform(unit / split) : -1, uniform(item)};
 }
-static inline long long xcd_grid(long long items) { return (items + 8 * XCD_RUN - 1) / (8 * XCD_RUN) * (8 * XCD_RUN); }
+static inline int xcd_split(long long heads) { return heads % 8 == 0 ? 1 : heads % 4 == 0 ? 2 : heads % 2 == 0 ? 4 : 8; }
+static inline long long xcd_grid(long long heads, long long items) { const int s = xcd_split(heads); return heads * s * ((items + s - 1) / s); }
 
 }  // namespace adac

@@ -9,7 +9,7 @@ namespace {
 // the products.  Rows past a sequence's end are read from the last row there is in
 // their sixteenth (or the page's first) and masked: nothing behind the end is touched.
 template <int D, int NW>
-__global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(BlockAttnArgs a, int rts, int items) {
+__global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(BlockAttnArgs a, int rts, int split) {
   constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int TK = 32, NKB = TK / 32, PARTS = TK / 16;      // keys a tile
   constexpr int PT = TK * CH / NT, TILEB = TK * ROWB;
@@ -17,11 +17,9 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
   __shared__ int2 pages_l[LIST];
   __shared__ int32_t counts[NW];
   const BlockDims& m = a.m;
-  int id = xcd_item(blockIdx.x);
-  if (id >= items) return;
-  const int rt = uniform(id % rts); id /= rts;
-  const int i = uniform(id % m.nb); id /= m.nb;
-  const int hk = uniform(id % m.Hkv), b = uniform(id / m.Hkv);
+  const HeadItem it = xcd_item(blockIdx.x, m.B * m.Hkv, m.nb * rts, split);
+  if (it.head < 0) return;
+  const int rt = it.item % rts, i = it.item / rts, hk = it.head % m.Hkv, b = it.head / m.Hkv;
   const BlockSeq s = block_seq(m, b);
   const int t0 = i * m.qblock, rows = min(m.qblock, s.nq - t0) * m.G, base_row = rt * NT / 2;
   if (t0 >= s.nq || base_row >= rows) return;
@@ -204,14 +202,15 @@ bool block_wide_takes(const BlockAttnArgs& a, int dtype, int bits) {
 
 int launch_block_attn_wide(hipStream_t s, int d, const BlockAttnArgs& a) {
   const int rows = a.m.qblock * a.m.G, rt = rows <= 64 ? 64 : 128, rts = (rows + rt - 1) / rt;
-  const long long items = (long long)rts * a.m.nb * a.m.Hkv * a.m.B, grid = xcd_grid(items);
+  const long long heads = (long long)a.m.Hkv * a.m.B, grid = xcd_grid(heads, (long long)rts * a.m.nb);
   if (!grid_fits(grid)) return ADACLUSTER_E_UNSUPPORTED;
+  const int split = xcd_split(heads);
   if (rt == 64) {
-    if (d == 64) block_attn_wide<64, 2><<<(int)grid, 128, 0, s>>>(a, rts, (int)items);
-    else block_attn_wide<128, 2><<<(int)grid, 128, 0, s>>>(a, rts, (int)items);
+    if (d == 64) block_attn_wide<64, 2><<<(int)grid, 128, 0, s>>>(a, rts, split);
+    else block_attn_wide<128, 2><<<(int)grid, 128, 0, s>>>(a, rts, split);
   } else {
-    if (d == 64) block_attn_wide<64, 4><<<(int)grid, 256, 0, s>>>(a, rts, (int)items);
-    else block_attn_wide<128, 4><<<(int)grid, 256, 0, s>>>(a, rts, (int)items);
+    if (d == 64) block_attn_wide<64, 4><<<(int)grid, 256, 0, s>>>(a, rts, split);
+    else block_attn_wide<128, 4><<<(int)grid, 256, 0, s>>>(a, rts, split);
   }
   return launched();
 }
