@@ -46,8 +46,12 @@ __device__ __forceinline__ void expand(RowFrag<T, D>& f, const Raw<T, BITS, D>& 
     if constexpr (BITS == 0) f.p[x] = r.w[x];
     else if constexpr (sizeof(T) == 2) {
       const uint32_t c = r.w[0][x];
+      // (constants in registers: an instruction then masks and joins, which literals do not allow)
+      uint32_t mask = 0x000F000Fu, high = 0x43004300u;
+      asm("" : "+v"(mask));
+      asm("" : "+s"(high));
 #pragma unroll
-      for (int j = 0; j < 4; ++j) f.p[x][j] = (c >> (4 * j) & 0x000F000Fu) | 0x43004300u;
+      for (int j = 0; j < 4; ++j) f.p[x][j] = (c >> (4 * j) & mask) | high;
     } else {
       const uint32_t c = r.w[0][x >> 1] >> (16 * (x & 1));
       const float step = __uint_as_float(pair[x >> 2] << 16), low = __uint_as_float(pair[x >> 2] & 0xFFFF0000u);
@@ -65,14 +69,14 @@ __device__ __forceinline__ void expand(RowFrag<T, D>& f, const Raw<T, BITS, D>& 
 // P is rounded to bfloat16 for the product with V in 16 bits (an error of half a step of bfloat16 of each weight, the row
 // sum is of the unrounded ones); with 4-bit values the weights are multiplied by the steps of their keys first.
 template <typename T, int BITS, int D, int R>
-__global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
+__global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D == 128) ? 2 : 1) void block_attn(BlockAttnArgs a, int rts) {
   constexpr int NF = D * sizeof(T) / 64, ND = D / 16;
   constexpr bool CODES = BITS == 4 && sizeof(T) == 2;           // codes enter the products, steps behind them
   constexpr int NG = CODES ? D / 64 : 1, MW = D / 64;
   constexpr int VBYTES = 32 * D * sizeof(T);
   constexpr int JBYTES = 4 * 16 * D * 4 + 4 * 16 * 2 * 4;
   __shared__ __align__(16) char lds[4 * VBYTES > JBYTES ? 4 * VBYTES : JBYTES];
-  __shared__ __align__(16) uint32_t meta[CODES ? 4 : 1][CODES ? 32 : 1][2 * MW];      // (step, lowest) of a wave's 32 keys and values
+  __shared__ __align__(16) float meta[CODES ? 4 : 1][2][CODES ? 32 : 1][2 * MW];      // a wave's 32 keys, values: (step, lowest), lowest of values + 8 steps
   __shared__ int2 pages_l[LIST];
   __shared__ int32_t counts[4];
   const BlockDims& m = a.m;
@@ -175,7 +179,7 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
     if (R > 1) fetch(next, turn);
     int key0[2];
     RowFrag<T, D> k[2];
-    uint32_t kp[2][4][MW], vp[2][4][MW];              // CODES: (step, lowest) of keys 4 * quarter + j
+    float kp[2][4][2 * MW], vp[2][4][2 * MW];         // CODES: of keys 4 * quarter + j
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       key0[h] = next.key0[h];
@@ -189,7 +193,13 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
       if constexpr (CODES) {
         if (quarter == 0) {
 #pragma unroll
-          for (int x = 0; x < MW; ++x) { meta[wave][16 * h + n16][x] = next.pk[h][x]; meta[wave][16 * h + n16][MW + x] = next.pv[h][x]; }
+          for (int x = 0; x < MW; ++x) {
+            const float ks = __uint_as_float(next.pk[h][x] << 16), vs = __uint_as_float(next.pv[h][x] << 16);
+            meta[wave][0][16 * h + n16][2 * x] = ks;
+            meta[wave][0][16 * h + n16][2 * x + 1] = __uint_as_float(next.pk[h][x] & 0xFFFF0000u);
+            meta[wave][1][16 * h + n16][2 * x] = vs;
+            meta[wave][1][16 * h + n16][2 * x + 1] = fmaf(8.f, vs, __uint_as_float(next.pv[h][x] & 0xFFFF0000u));
+          }
         }
       }
     }
@@ -200,7 +210,7 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int x = 0; x < MW; ++x) { kp[h][j][x] = meta[wave][16 * h + 4 * quarter + j][x]; vp[h][j][x] = meta[wave][16 * h + 4 * quarter + j][MW + x]; }
+          for (int x = 0; x < 2 * MW; ++x) { kp[h][j][x] = meta[wave][0][16 * h + 4 * quarter + j][x]; vp[h][j][x] = meta[wave][1][16 * h + 4 * quarter + j][x]; }
     }
     if (R == 1 && turn + 4 < turns) fetch(next, turn + 4);
 
@@ -219,7 +229,7 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
             x = mma(T{}, k[h].p[2 * g + 1], q[r].p[2 * g + 1], x);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-              sc[h][j] = fmaf(__uint_as_float(kp[h][j][g] << 16), x[j], fmaf(__uint_as_float(kp[h][j][g] & 0xFFFF0000u), qsum[r][g], sc[h][j]));
+              sc[h][j] = fmaf(kp[h][j][2 * g], x[j], fmaf(kp[h][j][2 * g + 1], qsum[r][g], sc[h][j]));
           }
         } else {
 #pragma unroll
@@ -271,11 +281,9 @@ __global__ __launch_bounds__(256) void block_attn(BlockAttnArgs a, int rts) {
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             const int h = x >> 1, j = 2 * (x & 1);
-            const float s0 = __uint_as_float(vp[h][j][g] << 16), s1 = __uint_as_float(vp[h][j + 1][g] << 16);
-            u.w[x] = pack_bf16x2(p[h][j] * s0, p[h][j + 1] * s1);
+            u.w[x] = pack_bf16x2(p[h][j] * vp[h][j][2 * g], p[h][j + 1] * vp[h][j + 1][2 * g]);
             c = __builtin_amdgcn_fdot2_f32_bf16(u.b[x], one, c, false);
-            back = fmaf(p[h][j], fmaf(8.f, s0, __uint_as_float(vp[h][j][g] & 0xFFFF0000u)), back);
-            back = fmaf(p[h][j + 1], fmaf(8.f, s1, __uint_as_float(vp[h][j + 1][g] & 0xFFFF0000u)), back);
+            back = fmaf(p[h][j + 1], vp[h][j + 1][2 * g + 1], fmaf(p[h][j], vp[h][j][2 * g + 1], back));
           }
           corr[r][g] = fmaf(-136.f, c, back);
 #pragma unroll
