@@ -226,8 +226,8 @@ struct BlockGradArgs {
   float* delta;                              // [q_rows][Hq]
   uint32_t* marks;                           // [B][Hkv][max_pages][words]: blocks of queries that list a page
   int words;
-  float* sums;                               // partial sums of pages that many blocks list: [group][np][4 waves][64][64]
-  int groups, np, limit;
+  float* sums;                               // of pages that many blocks list, a share each: [group][np][..]
+  int groups, wg, np, limit;
 };
 size_t block_grad_bytes(const BlockDims& m, int dtype, int d, bool listed);
 int launch_block_attn_backward(hipStream_t s, int dtype, int d, BlockGradArgs a, void* ws);

@@ -173,20 +173,36 @@ __global__ __launch_bounds__(256) void grad_q(BlockGradArgs a, int rts) {
   }
 }
 
+// A page that far more blocks list than others (the first one, say) would be the launch's critical path.  Where a launch has few
+// workgroups, the blocks of such a page are dealt to up to `np` workgroups, each a run of the page's marks; their sums go to
+// memory and grad_kv_add (grad_kv_join) adds them in order.
+struct Share { int first, count, parts; };
+__device__ __forceinline__ Share page_share(const BlockGradArgs& a, const uint32_t* marks, int blocks, int part) {
+  if (a.np == 1) return {0, blocks, 1};
+  int n = 0;
+  for (int w = 0; w * 32 < blocks; ++w) n += __popc((uint32_t)uniform((int)marks[w]));      // (no mark lies past the last block)
+  const int parts = min(a.np, max(1, (n + a.limit - 1) / a.limit));
+  const int first = (int)((long long)n * part / parts);
+  return {first, (int)((long long)n * (part + 1) / parts) - first, parts};
+}
 // dK and dV of KR * 16 keys of one head: the waves take tiles of 32 rows in turns.  S = Q K^T and dP = dO V^T leave a lane one key
 // and four rows: P and dS are the operands of dV^T = dO^T P and dK^T = Q^T dS as they stand.
 template <typename T, int D, int KR>
-__global__ __launch_bounds__(256) void grad_kv(BlockGradArgs a, int groups) {
+__global__ __launch_bounds__(256) void grad_kv(BlockGradArgs a) {
   constexpr int NF = D * sizeof(T) / 64, ND = D / 16;
   constexpr int TBYTES = 32 * D * sizeof(T), JBYTES = 4 * 16 * D * 4;
   __shared__ __align__(16) char lds[8 * TBYTES > JBYTES ? 8 * TBYTES : JBYTES];
   const BlockDims& m = a.m;
-  int id = blockIdx.x;
-  const int kg = id % groups; id /= groups;
-  const int hk = id % m.Hkv, b = id / m.Hkv;
+  // (heads side by side, first pages first, shares behind the first last, as in grad_kv_pair)
+  const int part = uniform((int)(blockIdx.x / (unsigned)a.wg)), group = uniform((int)(blockIdx.x % (unsigned)a.wg));
+  const int hk = group % m.Hkv, b = group / m.Hkv % m.B, kg = group / m.Hkv / m.B;
   const BlockSeq s = block_seq(m, b);
   const int key0 = kg * KR * 16;
   if (key0 >= s.n) return;
+  const uint32_t* const marks = a.sel ? a.marks + (((long long)b * m.Hkv + hk) * m.max_pages + (key0 >> m.lpage)) * a.words : nullptr;
+  const int blocks = (s.nq + m.qblock - 1) / m.qblock;
+  const Share share = page_share(a, marks, blocks, part);
+  if (part >= share.parts) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, quarter = lane >> 4;
   RowFrag<T, D> k[KR], v[KR];
   f32x4_t dk[KR][ND], dv[KR][ND];
@@ -200,15 +216,17 @@ __global__ __launch_bounds__(256) void grad_kv(BlockGradArgs a, int groups) {
   }
   char* const ql = lds + wave * 2 * TBYTES;
   char* const gl = ql + TBYTES;
-  const uint32_t* const marks = a.sel ? a.marks + (((long long)b * m.Hkv + hk) * m.max_pages + (key0 >> m.lpage)) * a.words : nullptr;
-  const int blocks = (s.nq + m.qblock - 1) / m.qblock;
+  int skip = share.first, left = share.count;
   int unit = 0;
   for (int w = 0; w * 32 < blocks; ++w) {
-    uint32_t bits = marks ? marks[w] : ~0u;
+    uint32_t bits = left ? marks ? marks[w] : ~0u : 0;
     if (blocks - w * 32 < 32) bits &= (1u << (blocks - w * 32)) - 1;
     while (bits) {
       const int i = w * 32 + __builtin_ctz(bits), t0 = i * m.qblock, rows = min(m.qblock, s.nq - t0) * m.G;
       bits &= bits - 1;
+      if (skip) { --skip; continue; }
+      if (!left) break;
+      --left;
       for (int base = 0; base < rows; base += 32) {
         const int last = t0 + (min(base + 32, rows) - 1) / m.G;
         if (m.causal && s.first + last < key0) continue;
@@ -272,6 +290,17 @@ __global__ __launch_bounds__(256) void grad_kv(BlockGradArgs a, int groups) {
       for (int x = 0; x < ND; ++x) *(f32x4_t*)(jo + (wave * 16 + n16) * D + 16 * x + 4 * quarter) = side ? dv[r][x] : dk[r][x];
       __syncthreads();
       const int jr = tid >> 4, key = key0 + r * 16 + jr, d0 = (tid & 15) * (D / 16);
+      if (share.parts > 1) {
+        float* const to = a.sums + ((((long long)group * a.np + part) * 2 + side) * (16 * KR) + r * 16 + jr) * D + d0;
+#pragma unroll
+        for (int x = 0; x < D / 16; x += 4) {
+          f32x4_t o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int w = 0; w < 4; ++w) o += *(const f32x4_t*)(jo + (w * 16 + jr) * D + d0 + x);
+          *(f32x4_t*)(to + x) = o;
+        }
+        continue;
+      }
       if (key >= s.n) continue;
       T* const out = (side ? (T*)a.dv + (s.k0 + (long long)key) * a.dvs.token + hk * a.dvs.head
                            : (T*)a.dk + (s.k0 + (long long)key) * a.dks.token + hk * a.dks.head) + d0;
@@ -287,18 +316,31 @@ __global__ __launch_bounds__(256) void grad_kv(BlockGradArgs a, int groups) {
     }
 }
 
-// A page that far more blocks list than others (the first one, say) would be the launch's critical path.  Where a launch has few
-// workgroups, the blocks of such a page are dealt to up to `np` workgroups, each a run of the page's marks; their sums go to
-// memory (a wave's 64 values a lane as they are) and grad_kv_join adds them in order.
-struct Share { int first, count, parts; };
-__device__ __forceinline__ Share page_share(const BlockGradArgs& a, const uint32_t* marks, int blocks, int part) {
-  if (a.np == 1) return {0, blocks, 1};
-  int n = 0;
-  for (int w = 0; w * 32 < blocks; ++w) n += __popc((uint32_t)uniform((int)marks[w]));      // (no mark lies past the last block)
-  const int parts = min(a.np, max(1, (n + a.limit - 1) / a.limit));
-  const int first = (int)((long long)n * part / parts);
-  return {first, (int)((long long)n * (part + 1) / parts) - first, parts};
+// The sums of 16 KR keys whose blocks were dealt to several workgroups.
+template <typename T, int D, int KR>
+__global__ __launch_bounds__(256) void grad_kv_add(BlockGradArgs a) {
+  const BlockDims& m = a.m;
+  const int group = blockIdx.x, hk = group % m.Hkv, b = group / m.Hkv % m.B, key0 = group / m.Hkv / m.B * KR * 16;
+  const BlockSeq s = block_seq(m, b);
+  if (key0 >= s.n) return;
+  const uint32_t* const marks = a.marks + (((long long)b * m.Hkv + hk) * m.max_pages + (key0 >> m.lpage)) * a.words;
+  const Share share = page_share(a, marks, (s.nq + m.qblock - 1) / m.qblock, 0);
+  if (share.parts < 2) return;
+  for (int x = threadIdx.x; x < 2 * KR * 16 * (D / 4); x += 256) {
+    const int d0 = x % (D / 4) * 4, row = x / (D / 4) % (KR * 16), side = x / (D / 4) / (KR * 16), key = key0 + row;
+    if (key >= s.n) continue;
+    f32x4_t o{0.f, 0.f, 0.f, 0.f};
+    for (int part = 0; part < share.parts; ++part)
+      o += *(const f32x4_t*)(a.sums + ((((long long)group * a.np + part) * 2 + side) * (16 * KR) + row) * D + d0);
+    if (!side) o *= a.scale;
+    T* const out = (side ? (T*)a.dv + (s.k0 + (long long)key) * a.dvs.token + hk * a.dvs.head
+                         : (T*)a.dk + (s.k0 + (long long)key) * a.dks.token + hk * a.dks.head) + d0;
+    if constexpr (sizeof(T) == 2) *(uint2*)out = uint2{pack_bf16x2(o[0], o[1]), pack_bf16x2(o[2], o[3])};
+    else *(f32x4_t*)out = o;
+  }
 }
+
+// Where a wave of the kernels for many rows leaves its 64 values a lane.
 __device__ __forceinline__ float* share_slot(const BlockGradArgs& a, int group, int part, int wave, int lane) {
   return a.sums + (((long long)group * a.np + part) * 4 + wave) * 4096 + lane;
 }
@@ -1024,19 +1066,32 @@ __global__ __launch_bounds__(256) void grad_kv_join(BlockGradArgs a) {
   else store_rows<DB>(wave >> 1 ? ok : ov, x, wave >> 1 ? a.scale : 1.f);
 }
 
+// The kernels for many rows: blocks of at least 48 rows over pages of 64 keys or more, bf16 ...
+bool rows_wide(const BlockDims& m, int dtype) { return dtype == ADACLUSTER_BF16 && m.qblock * m.G >= 48 && m.qblock * m.G <= (1 << 20) && m.page >= 64; }
+// ... with offsets inside a block or a sixteenth that 32 bits hold.
+bool wide_takes(const BlockGradArgs& a, int dtype) {
+  const BlockDims& m = a.m;
+  const auto block = [&](const KeyStride& st) { return m.qblock * st.token + m.G * st.head < (1 << 30); };
+  return rows_wide(m, dtype) && a.ks.token < (1 << 25) && a.vs.token < (1 << 25) && block(a.qs) && block(a.dos);
+}
+
 // Workgroups that a page's blocks go to at most, where there are lists and a launch has fewer than 4 096 workgroups (eight rounds of two a CU,
 // and 268 MB of sums at most); and the blocks from which on: a quarter more than a page has on average.  A training pass of one
 // sequence of 8 192 tokens, lists of 32 pages: 4 / 1 heads, d = 128 1 226 -> 541 us, 16 / 4 heads 1 575 -> 1 031, 8 / 2 heads, d = 64 734 -> 392;
 // three sequences, 1 536 workgroups: 3 % of the launch.
-struct Deal { int KG, groups, np, limit; long long wg; };
-Deal deal_of(const BlockDims& m, int d, bool listed) {
+struct Deal { int keys, groups, np, limit; long long wg; size_t bytes; };
+Deal deal_of(const BlockDims& m, int dtype, int d, bool wide, bool listed) {
   Deal x;
-  x.KG = d == 64 && m.page >= 128 ? 4 : 2;
-  x.groups = (m.max_pages << m.lpage) / (32 * x.KG);
+  if (wide) x.keys = d == 64 && m.page >= 128 ? 128 : 64;
+  // 32 keys a workgroup (its registers allow that but for fp32 at d = 128) where that leaves two workgroups a CU (fp32, one head of 4 096
+  // keys: 128 workgroups 216 us, 256 of 16 keys 154, and with the first pages dealt out 78)
+  else x.keys = m.page == 16 || (dtype == ADACLUSTER_F32 && d == 128) || (long long)(m.max_pages << m.lpage) / 32 * m.Hkv * m.B < 512 ? 16 : 32;
+  x.groups = (m.max_pages << m.lpage) / x.keys;
   x.wg = (long long)x.groups * m.Hkv * m.B;
   x.np = listed && x.wg < 4096 ? (int)(x.wg < 512 ? 8 : 4096 / x.wg) : 1;
   const long long mean = (long long)m.nb * m.topk / m.max_pages;
   x.limit = (int)(mean + mean / 4 > 4 ? mean + mean / 4 : 4);
+  x.bytes = x.np > 1 ? (size_t)x.wg * x.np * (wide ? 4 * 4096 : 2 * x.keys * d) * sizeof(float) : 0;
   return x;
 }
 
@@ -1050,35 +1105,24 @@ int go_wide(hipStream_t s, const BlockGradArgs& a, const Deal& x) {
   if constexpr (D == 128) grad_q_pair<<<(int)grid, 256, 0, s>>>(a, rts, split); else grad_q_wide<<<(int)grid, 256, 0, s>>>(a, rts, split);
   if (int rc = launched()) return rc;
   if constexpr (D == 128) grad_kv_pair<<<(int)wk, 256, 0, s>>>(a, split);
-  else if (x.KG == 4) grad_kv_wide<4><<<(int)wk, 256, 0, s>>>(a, split);
+  else if (x.keys == 128) grad_kv_wide<4><<<(int)wk, 256, 0, s>>>(a, split);
   else grad_kv_wide<2><<<(int)wk, 256, 0, s>>>(a, split);
   if (x.np > 1) {
     if (int rc = launched()) return rc;
     if constexpr (D == 128) grad_kv_join<128, 2><<<(int)x.wg, 256, 0, s>>>(a);
-    else if (x.KG == 4) grad_kv_join<64, 4><<<(int)x.wg, 256, 0, s>>>(a);
+    else if (x.keys == 128) grad_kv_join<64, 4><<<(int)x.wg, 256, 0, s>>>(a);
     else grad_kv_join<64, 2><<<(int)x.wg, 256, 0, s>>>(a);
   }
   return launched();
 }
 
-// Blocks of at least 48 rows over pages of 64 keys or more, bf16, with offsets inside a block or a sixteenth that 32 bits hold.
-bool rows_wide(const BlockDims& m) { return m.qblock * m.G >= 48 && m.qblock * m.G <= (1 << 20) && m.page >= 64; }
-bool wide_takes(const BlockGradArgs& a) {
-  const BlockDims& m = a.m;
-  const auto block = [&](const KeyStride& st) { return m.qblock * st.token + m.G * st.head < (1 << 30); };
-  return rows_wide(m) && a.ks.token < (1 << 25) && a.vs.token < (1 << 25) && block(a.qs) && block(a.dos);
-}
-
 template <typename T, int D>
-int go(hipStream_t s, const BlockGradArgs& a) {
+int go(hipStream_t s, const BlockGradArgs& a, const Deal& x, bool wide) {
   const BlockDims& m = a.m;
   constexpr int RPI = 256 / (D / Vec<T>::N);
   const long long deltas = ((long long)m.q_rows * m.Hq + RPI - 1) / RPI;
   const int rows = m.qblock * m.G, R = rows <= 16 ? 1 : 2, rts = (rows + 16 * R - 1) / (16 * R);
-  // 32 keys a workgroup (its registers allow that but for fp32 at d = 128) where that leaves two workgroups a CU (fp32, one head of 4 096
-  // keys: 128 workgroups %s us, 256 of 16 keys %s)
-  const int KR = m.page == 16 || (sizeof(T) == 4 && D == 128) || (long long)(m.max_pages << m.lpage) / 32 * m.Hkv * m.B < 512 ? 1 : 2, groups = (m.max_pages << m.lpage) / (16 * KR);
-  const long long wq = (long long)rts * m.nb * m.Hkv * m.B, wk = (long long)groups * m.Hkv * m.B;
+  const long long wq = (long long)rts * m.nb * m.Hkv * m.B, wk = x.wg * x.np;
   const long long entries = a.sel ? (long long)m.B * m.nb * m.Hkv * m.topk : 0;
   if (!grid_fits(deltas) || !grid_fits(wq) || !grid_fits(wk) || !grid_fits(entries / 256 + 1)) return ADACLUSTER_E_UNSUPPORTED;
   if (a.sel) {
@@ -1088,11 +1132,16 @@ int go(hipStream_t s, const BlockGradArgs& a) {
   }
   grad_delta<T, D><<<(int)deltas, 256, 0, s>>>(a);
   if (int rc = launched()) return rc;
-  if constexpr (sizeof(T) == 2) if (wide_takes(a)) return go_wide<D>(s, a, deal_of(m, D, a.sel != nullptr));
+  if constexpr (sizeof(T) == 2) if (wide) return go_wide<D>(s, a, x);
   if (R == 1) grad_q<T, D, 1><<<(int)wq, 256, 0, s>>>(a, rts); else grad_q<T, D, 2><<<(int)wq, 256, 0, s>>>(a, rts);
   if (int rc = launched()) return rc;
-  if (KR == 1) grad_kv<T, D, 1><<<(int)wk, 256, 0, s>>>(a, groups);
-  else if constexpr (sizeof(T) == 2 || D == 64) grad_kv<T, D, 2><<<(int)wk, 256, 0, s>>>(a, groups);
+  if (x.keys == 16) grad_kv<T, D, 1><<<(int)wk, 256, 0, s>>>(a);
+  else if constexpr (sizeof(T) == 2 || D == 64) grad_kv<T, D, 2><<<(int)wk, 256, 0, s>>>(a);
+  if (x.np > 1) {
+    if (int rc = launched()) return rc;
+    if (x.keys == 16) grad_kv_add<T, D, 1><<<(int)x.wg, 256, 0, s>>>(a);
+    else if constexpr (sizeof(T) == 2 || D == 64) grad_kv_add<T, D, 2><<<(int)x.wg, 256, 0, s>>>(a);
+  }
   return launched();
 }
 
@@ -1102,25 +1151,23 @@ size_t delta_bytes(const BlockDims& m) { return align_up((size_t)m.q_rows * m.Hq
 }  // namespace
 
 size_t block_grad_bytes(const BlockDims& m, int dtype, int d, bool listed) {
-  size_t n = delta_bytes(m) + (listed ? marks_bytes(m) : 0);
-  if (dtype == ADACLUSTER_BF16 && rows_wide(m)) {
-    const Deal x = deal_of(m, d, listed);
-    if (x.np > 1) n += (size_t)x.wg * x.np * 4 * 4096 * sizeof(float);
-  }
-  return n;
+  const size_t few = deal_of(m, dtype, d, false, listed).bytes, many = rows_wide(m, dtype) ? deal_of(m, dtype, d, true, listed).bytes : 0;
+  return delta_bytes(m) + (listed ? marks_bytes(m) : 0) + (few > many ? few : many);      // (which kernels run hangs on the strides too)
 }
 
 int launch_block_attn_backward(hipStream_t s, int dtype, int d, BlockGradArgs a, void* ws) {
-  const Deal x = deal_of(a.m, d, a.sel != nullptr);
+  const bool wide = wide_takes(a, dtype);
+  const Deal x = deal_of(a.m, dtype, d, wide, a.sel != nullptr);
   a.delta = (float*)ws;
   a.marks = (uint32_t*)((char*)ws + delta_bytes(a.m));
   a.sums = (float*)((char*)a.marks + marks_bytes(a.m));
   a.words = (a.m.nb + 31) / 32;
   a.np = x.np;
-  a.groups = x.groups;
   a.limit = x.limit;
-  if (dtype == ADACLUSTER_BF16) return d == 64 ? go<bf16raw, 64>(s, a) : go<bf16raw, 128>(s, a);
-  return d == 64 ? go<float, 64>(s, a) : go<float, 128>(s, a);
+  a.groups = x.groups;
+  a.wg = (int)x.wg;
+  if (dtype == ADACLUSTER_BF16) return d == 64 ? go<bf16raw, 64>(s, a, x, wide) : go<bf16raw, 128>(s, a, x, wide);
+  return d == 64 ? go<float, 64>(s, a, x, wide) : go<float, 128>(s, a, x, wide);
 }
 
 }  // namespace adac
