@@ -293,11 +293,12 @@ int adacluster_quest_scores(int32_t H, int32_t Lq, int32_t Lk, int32_t d, int32_
  *   Blocks      `qblock` consecutive queries of a sequence (counted from its first query of the call) and the query heads of one
  *               head of keys share a list of pages.  nb = ceil(max_q / qblock) records a sequence.
  *   Lists       sel_idx [B][nb][Hkv][topk]: pages in ascending order, -1 behind the end.  An entry that names no page of the
- *               sequence or is not above the entry before it counts as -1.  A block attends to the keys of its pages that
+ *               sequence or is not above the entry before it counts as -1 (lists that do not ascend apart from that: results
+ *               are unspecified).  A block attends to the keys of its pages that
  *               exist (below n_b) and, if causal, are not behind the query.  sel_idx NULL: all pages.
  *   Empty rows  A query with no key of score above -inf has output 0 and lse -inf.  What lies in a page behind a sequence's last
  *               key is not looked at.  Within what a block lists, a value that is an infinity or a NaN reaches the rows it is
- *               masked for inside its own 32 keys.
+ *               masked for inside its own 32 keys (gradients: 64 keys by 64 rows).
  *   Device data is not trusted for addresses: lengths are held to max_pages * page and to the buffers, a page_table entry
  *               outside [0, num_pages) names no keys, cu_q and cu_k are held to [0, q_rows] and [0, k_rows].  Queries of a
  *               sequence past max_q are left out.  Rows of o, lse, dq (dk, dv) that belong to no sequence are left as they were.
@@ -311,8 +312,9 @@ int adacluster_quest_scores(int32_t H, int32_t Lq, int32_t Lk, int32_t d, int32_
  *               A group with a NaN or an infinity, or whose span overflows, is held as NaN.
  *   Boxes       [num_pages][Hkv][2][d] of a pool, [B][max_pages][Hkv][2][d] of packed keys, in dtype: maxima, then minima, over
  *               the keys a page holds, as they were given (before 4 bits).  A NaN does not enter a box.
- * All calls are asynchronous on `stream`, block no thread, allocate nothing and may be captured into a graph.  Unlike in the
- * clustered calls the device that owns the tensors must be the current one, as for any launch.
+ * All calls are asynchronous on `stream`, block no thread, allocate nothing and may be captured into a graph.  The device that
+ * owns the tensors must be the current one.  Limits: max_pages * page and max_q up to 2^29, B * Hkv * ceil(max_q / qblock) up to 2^31,
+ * and what a launch may have of workgroups (2^24; ADACLUSTER_E_UNSUPPORTED past it).
  */
 typedef struct adacluster_block_params {
   int32_t B;                    /* sequences                                                     */
@@ -328,7 +330,7 @@ typedef struct adacluster_block_params {
   int32_t topk;                 /* entries of a list                                             */
   int32_t keep_first;           /* pages from the start that every list holds                    */
   int32_t q_rows, k_rows;       /* rows of q (new tokens), rows of packed k                      */
-  float   softmax_scale;        /* <= 0 means 1/sqrt(d)                                          */
+  float   softmax_scale;        /* <= 0 means 1/sqrt(d); below 2^100                             */
   int64_t q_stride[2], o_stride[2], k_stride[3], v_stride[3];
   int64_t new_k_stride[2], new_v_stride[2];                           /* adacluster_cache_append */
   int64_t do_stride[2], dq_stride[2], dk_stride[2], dv_stride[2];     /* gradients               */

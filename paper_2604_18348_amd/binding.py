@@ -114,7 +114,7 @@ class BlockParams:
 
     @property
     def blocks(self) -> int:
-        return -(-self.max_q // self.qblock)
+        return -(-self.max_q // max(1, self.qblock))
 
 
 @dataclass

@@ -22,14 +22,14 @@ int check(const adacluster_block_params* p, BlockDims* m) {
   if (p->bits != 0 && p->bits != 4) return fail(ADACLUSTER_E_BADDTYPE, "bits must be 0 (as dtype) or 4 (bits=%d)", p->bits);
   if (!shifted(p->page, &m->lpage)) return fail(ADACLUSTER_E_BADSHAPE, "page must be 16, 32, 64 or 128 (page=%d)", p->page);
   if (p->num_pages < 0) return fail(ADACLUSTER_E_BADSHAPE, "num_pages must be >= 0");
-  if (p->max_pages < 1 || (long long)p->max_pages * p->page > (1 << 30)) return fail(ADACLUSTER_E_BADSHAPE, "max_pages must be >= 1, and max_pages * page <= 2^30 (max_pages=%d)", p->max_pages);
-  if (p->max_q < 1 || p->max_q > (1 << 30)) return fail(ADACLUSTER_E_BADSHAPE, "max_q must be in [1,2^30] (max_q=%d)", p->max_q);
+  if (p->max_pages < 1 || (long long)p->max_pages * p->page > (1 << 29)) return fail(ADACLUSTER_E_BADSHAPE, "max_pages must be >= 1, and max_pages * page <= 2^29 (max_pages=%d)", p->max_pages);
+  if (p->max_q < 1 || p->max_q > (1 << 29)) return fail(ADACLUSTER_E_BADSHAPE, "max_q must be in [1,2^29] (max_q=%d)", p->max_q);
   if (p->qblock < 1 || p->qblock > 1024) return fail(ADACLUSTER_E_BADSHAPE, "qblock must be in [1,1024] (qblock=%d)", p->qblock);
   if (p->causal != 0 && p->causal != 1) return fail(ADACLUSTER_E_BADARG, "causal must be 0 or 1");
   if (p->topk < 0 || p->topk > (1 << 24)) return fail(ADACLUSTER_E_BADARG, "topk must be in [0,2^24] (topk=%d)", p->topk);
   if (p->keep_first < 0) return fail(ADACLUSTER_E_BADARG, "keep_first must be >= 0");
   if (p->q_rows < 1 || p->k_rows < 0) return fail(ADACLUSTER_E_BADSHAPE, "q_rows must be >= 1 and k_rows >= 0");
-  if (isnan(p->softmax_scale) || isinf(p->softmax_scale)) return fail(ADACLUSTER_E_BADARG, "softmax_scale must be finite");
+  if (!(p->softmax_scale < 0x1p100f)) return fail(ADACLUSTER_E_BADARG, "softmax_scale must be below 2^100");
   if (((long long)p->max_q + p->qblock - 1) / p->qblock * p->Hkv > (1ll << 31) / p->B)
     return fail(ADACLUSTER_E_BADSHAPE, "more than 2^31 blocks of queries (B * Hkv * max_q / qblock)");
   m->B = p->B; m->Hq = p->Hq; m->Hkv = p->Hkv; m->G = p->Hq / p->Hkv;

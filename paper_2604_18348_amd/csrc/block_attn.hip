@@ -148,159 +148,159 @@ __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D =
     uint32_t pk[2][MW], pv[2][MW];                    // 4 bits: (step, lowest) of the lane's row
   };
   for (int e0 = split; e0 < entries; e0 += a.nsplit * LIST) {
-  const int halves = fill_list<256>(m, b, list, e0, a.nsplit, entries, pages, pages_l, counts) << lsub, turns = (halves + 1) >> 1;
-  auto fetch = [&](Fetch& f, int turn) __attribute__((always_inline)) {
+    const int halves = fill_list<256>(m, b, list, e0, a.nsplit, entries, pages, pages_l, counts) << lsub, turns = (halves + 1) >> 1;
+    auto fetch = [&](Fetch& f, int turn) __attribute__((always_inline)) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int half = 2 * turn + h, sub = half & ((1 << lsub) - 1);
-      const bool some = half < halves;
-      const int2 pp = pages_l[some ? half >> lsub : 0];
-      const int pg = uniform(pp.x), phys = uniform(pp.y);
-      f.key0[h] = some ? (pg << m.lpage) + sub * 16 : INT32_MAX - 64;
-      const bool there = f.key0[h] + n16 < s.n;
-      if constexpr (BITS == 4) {
-        const long long at = ((long long)phys * m.Hkv + hk) * m.page + sub * 16 + n16;
-        load_raw<T, BITS, D>(f.k[h], a.k, at * (D / 2), quarter, there);
-        load_raw<T, BITS, D>(f.v[h], a.v, at * (D / 2), quarter, there);
+      for (int h = 0; h < 2; ++h) {
+        const int half = 2 * turn + h, sub = half & ((1 << lsub) - 1);
+        const bool some = half < halves;
+        const int2 pp = pages_l[some ? half >> lsub : 0];
+        const int pg = uniform(pp.x), phys = uniform(pp.y);
+        f.key0[h] = some ? (pg << m.lpage) + sub * 16 : INT32_MAX - 64;
+        const bool there = f.key0[h] + n16 < s.n;
+        if constexpr (BITS == 4) {
+          const long long at = ((long long)phys * m.Hkv + hk) * m.page + sub * 16 + n16;
+          load_raw<T, BITS, D>(f.k[h], a.k, at * (D / 2), quarter, there);
+          load_raw<T, BITS, D>(f.v[h], a.v, at * (D / 2), quarter, there);
 #pragma unroll
-        for (int x = 0; x < MW; ++x) {                  // (behind the end lies anything: its weight of 0 must meet a number)
-          f.pk[h][x] = there ? a.km[at * MW + x] : 0;
-          f.pv[h][x] = there ? a.vm[at * MW + x] : 0;
+          for (int x = 0; x < MW; ++x) {                  // (behind the end lies anything: its weight of 0 must meet a number)
+            f.pk[h][x] = there ? a.km[at * MW + x] : 0;
+            f.pv[h][x] = there ? a.vm[at * MW + x] : 0;
+          }
+        } else {
+          load_raw<T, BITS, D>(f.k[h], a.k, row_at(m, s, a.ks, phys, pg, sub, hk) + n16 * a.ks.token, quarter, there);
+          load_raw<T, BITS, D>(f.v[h], a.v, row_at(m, s, a.vs, phys, pg, sub, hk) + n16 * a.vs.token, quarter, there);
         }
-      } else {
-        load_raw<T, BITS, D>(f.k[h], a.k, row_at(m, s, a.ks, phys, pg, sub, hk) + n16 * a.ks.token, quarter, there);
-        load_raw<T, BITS, D>(f.v[h], a.v, row_at(m, s, a.vs, phys, pg, sub, hk) + n16 * a.vs.token, quarter, there);
       }
-    }
-  };
-  Fetch next;
-  if (R == 1 && wave < turns) fetch(next, wave);
-  for (int turn = wave; turn < turns; turn += 4) {
-    if (R > 1) fetch(next, turn);
-    int key0[2];
-    RowFrag<T, D> k[2];
-    float kp[2][4][2 * MW], vp[2][4][2 * MW];         // CODES: of keys 4 * quarter + j
+    };
+    Fetch next;
+    if (R == 1 && wave < turns) fetch(next, wave);
+    for (int turn = wave; turn < turns; turn += 4) {
+      if (R > 1) fetch(next, turn);
+      int key0[2];
+      RowFrag<T, D> k[2];
+      float kp[2][4][2 * MW], vp[2][4][2 * MW];         // CODES: of keys 4 * quarter + j
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      key0[h] = next.key0[h];
-      const bool there = key0[h] + n16 < s.n;
-      expand<T, BITS, D>(k[h], next.k[h], next.pk[h], there);
-      RowFrag<T, D> v;
-      expand<T, BITS, D>(v, next.v[h], next.pv[h], there);
-      compiler_fence();
+      for (int h = 0; h < 2; ++h) {
+        key0[h] = next.key0[h];
+        const bool there = key0[h] + n16 < s.n;
+        expand<T, BITS, D>(k[h], next.k[h], next.pk[h], there);
+        RowFrag<T, D> v;
+        expand<T, BITS, D>(v, next.v[h], next.pv[h], there);
+        compiler_fence();
 #pragma unroll
-      for (int f = 0; f < NF; ++f) *(u32x4_t*)(vl + lds_piece<T, D>(16 * h + n16, piece_at<T, BITS>(f, quarter))) = v.p[f];
-      if constexpr (CODES) {
-        if (quarter == 0) {
+        for (int f = 0; f < NF; ++f) *(u32x4_t*)(vl + lds_piece<T, D>(16 * h + n16, piece_at<T, BITS>(f, quarter))) = v.p[f];
+        if constexpr (CODES) {
+          if (quarter == 0) {
 #pragma unroll
-          for (int x = 0; x < MW; ++x) {
-            const float ks = __uint_as_float(next.pk[h][x] << 16), vs = __uint_as_float(next.pv[h][x] << 16);
-            meta[wave][0][16 * h + n16][2 * x] = ks;
-            meta[wave][0][16 * h + n16][2 * x + 1] = __uint_as_float(next.pk[h][x] & 0xFFFF0000u);
-            meta[wave][1][16 * h + n16][2 * x] = vs;
-            meta[wave][1][16 * h + n16][2 * x + 1] = fmaf(8.f, vs, __uint_as_float(next.pv[h][x] & 0xFFFF0000u));
+            for (int x = 0; x < MW; ++x) {
+              const float ks = __uint_as_float(next.pk[h][x] << 16), vs = __uint_as_float(next.pv[h][x] << 16);
+              meta[wave][0][16 * h + n16][2 * x] = ks;
+              meta[wave][0][16 * h + n16][2 * x + 1] = __uint_as_float(next.pk[h][x] & 0xFFFF0000u);
+              meta[wave][1][16 * h + n16][2 * x] = vs;
+              meta[wave][1][16 * h + n16][2 * x + 1] = fmaf(8.f, vs, __uint_as_float(next.pv[h][x] & 0xFFFF0000u));
+            }
           }
         }
       }
-    }
-    compiler_fence();
-    if constexpr (CODES) {
+      compiler_fence();
+      if constexpr (CODES) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+          for (int j = 0; j < 4; ++j)
 #pragma unroll
-          for (int x = 0; x < 2 * MW; ++x) { kp[h][j][x] = meta[wave][0][16 * h + 4 * quarter + j][x]; vp[h][j][x] = meta[wave][1][16 * h + 4 * quarter + j][x]; }
-    }
-    if (R == 1 && turn + 4 < turns) fetch(next, turn + 4);
+            for (int x = 0; x < 2 * MW; ++x) { kp[h][j][x] = meta[wave][0][16 * h + 4 * quarter + j][x]; vp[h][j][x] = meta[wave][1][16 * h + 4 * quarter + j][x]; }
+      }
+      if (R == 1 && turn + 4 < turns) fetch(next, turn + 4);
 
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      f32x4_t sc[2], p[2];
+      for (int r = 0; r < R; ++r) {
+        f32x4_t sc[2], p[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        sc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int h = 0; h < 2; ++h) {
+          sc[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+          if constexpr (CODES) {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              const float start = -128.f * qsum[r][g];     // what the 128 of every code adds to a product
+              f32x4_t x{start, start, start, start};
+              x = mma(T{}, k[h].p[2 * g], q[r].p[2 * g], x);
+              x = mma(T{}, k[h].p[2 * g + 1], q[r].p[2 * g + 1], x);
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+                sc[h][j] = fmaf(kp[h][j][2 * g], x[j], fmaf(kp[h][j][2 * g + 1], qsum[r][g], sc[h][j]));
+            }
+          } else {
+#pragma unroll
+            for (int f = 0; f < NF; ++f) sc[h] = mma(T{}, k[h].p[f], q[r].p[f], sc[h]);
+          }
+          if (key0[h] + 16 > minlim) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[h][j] = key0[h] + 4 * quarter + j < lim[r] ? sc[h][j] : -INFINITY;
+          }
+        }
+        // p = 2^((s - reference) scale): any reference gives the same result as long as nothing overflows.  The turn's sum tells (it
+        // is infinite at a row's first score above -inf): only then is the maximum taken, the reference moved up to it and what
+        // has been summed scaled.
+        float rsum;
+        auto weights = [&]() __attribute__((always_inline)) {
+          const float off = ref[r] * scale;
+          rsum = 0.f;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { p[h][j] = __builtin_amdgcn_exp2f(fmaf(sc[h][j], scale, -off)); rsum += p[h][j]; }
+        };
+        weights();
+        if (__any(!(rsum <= 65536.f))) {
+          float top = ref[r];
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[h][j]);
+          top = quarters_max(top);
+          const float alpha = __builtin_amdgcn_exp2f((ref[r] - top) * scale);
+          ref[r] = top;
+          sum[r] *= alpha;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) corr[r][g] *= alpha;
+#pragma unroll
+          for (int x = 0; x < ND; ++x) acc[r][x] *= alpha;
+          weights();
+        }
+        sum[r] += rsum;
         if constexpr (CODES) {
 #pragma unroll
           for (int g = 0; g < NG; ++g) {
-            const float start = -128.f * qsum[r][g];     // what the 128 of every code adds to a product
-            f32x4_t x{start, start, start, start};
-            x = mma(T{}, k[h].p[2 * g], q[r].p[2 * g], x);
-            x = mma(T{}, k[h].p[2 * g + 1], q[r].p[2 * g + 1], x);
+            // weights times steps, rounded here: what is taken off for the 128 has to be what the product adds.  8 more are taken off
+            // and come back unrounded: the rounding then weighs codes about their middle, not from 0 up.
+            const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
+            union { uint32_t w[4]; bf16x2_t b[4]; bf16x8_t v; } u;
+            float c = 0.f, back = corr[r][g];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              sc[h][j] = fmaf(kp[h][j][2 * g], x[j], fmaf(kp[h][j][2 * g + 1], qsum[r][g], sc[h][j]));
+            for (int x = 0; x < 4; ++x) {
+              const int h = x >> 1, j = 2 * (x & 1);
+              u.w[x] = pack_bf16x2(p[h][j] * vp[h][j][2 * g], p[h][j + 1] * vp[h][j + 1][2 * g]);
+              c = __builtin_amdgcn_fdot2_f32_bf16(u.b[x], one, c, false);
+              back = fmaf(p[h][j + 1], vp[h][j + 1][2 * g + 1], fmaf(p[h][j], vp[h][j][2 * g + 1], back));
+            }
+            corr[r][g] = fmaf(-136.f, c, back);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) acc[r][4 * g + x] = mma_cols<D>(vl, 64 * g + 16 * x, lane, u.v, acc[r][4 * g + x]);
           }
+        } else if constexpr (sizeof(T) == 2) {
+          union { uint32_t w[4]; bf16x8_t v; } u{{pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3])}};
+#pragma unroll
+          for (int x = 0; x < ND; ++x) acc[r][x] = mma_cols<D>(vl, 16 * x, lane, u.v, acc[r][x]);
         } else {
 #pragma unroll
-          for (int f = 0; f < NF; ++f) sc[h] = mma(T{}, k[h].p[f], q[r].p[f], sc[h]);
-        }
-        if (key0[h] + 16 > minlim) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) sc[h][j] = key0[h] + 4 * quarter + j < lim[r] ? sc[h][j] : -INFINITY;
+          for (int x = 0; x < ND; ++x) acc[r][x] = mma_cols<D>(T{}, vl, 16 * x, lane, p[0], p[1], acc[r][x]);
         }
       }
-      // p = 2^((s - reference) scale): any reference gives the same result as long as nothing overflows.  The turn's sum tells (it
-      // is infinite at a row's first score above -inf): only then is the maximum taken, the reference moved up to it and what
-      // has been summed scaled.
-      float rsum;
-      auto weights = [&]() __attribute__((always_inline)) {
-        const float off = ref[r] * scale;
-        rsum = 0.f;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) { p[h][j] = __builtin_amdgcn_exp2f(fmaf(sc[h][j], scale, -off)); rsum += p[h][j]; }
-      };
-      weights();
-      if (__any(!(rsum <= 65536.f))) {
-        float top = ref[r];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[h][j]);
-        top = quarters_max(top);
-        const float alpha = __builtin_amdgcn_exp2f((ref[r] - top) * scale);
-        ref[r] = top;
-        sum[r] *= alpha;
-#pragma unroll
-        for (int g = 0; g < NG; ++g) corr[r][g] *= alpha;
-#pragma unroll
-        for (int x = 0; x < ND; ++x) acc[r][x] *= alpha;
-        weights();
-      }
-      sum[r] += rsum;
-      if constexpr (CODES) {
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          // weights times steps, rounded here: what is taken off for the 128 has to be what the product adds.  8 more are taken off
-          // and come back unrounded: the rounding then weighs codes about their middle, not from 0 up.
-          const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
-          union { uint32_t w[4]; bf16x2_t b[4]; bf16x8_t v; } u;
-          float c = 0.f, back = corr[r][g];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int h = x >> 1, j = 2 * (x & 1);
-            u.w[x] = pack_bf16x2(p[h][j] * vp[h][j][2 * g], p[h][j + 1] * vp[h][j + 1][2 * g]);
-            c = __builtin_amdgcn_fdot2_f32_bf16(u.b[x], one, c, false);
-            back = fmaf(p[h][j + 1], vp[h][j + 1][2 * g + 1], fmaf(p[h][j], vp[h][j][2 * g + 1], back));
-          }
-          corr[r][g] = fmaf(-136.f, c, back);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) acc[r][4 * g + x] = mma_cols<D>(vl, 64 * g + 16 * x, lane, u.v, acc[r][4 * g + x]);
-        }
-      } else if constexpr (sizeof(T) == 2) {
-        union { uint32_t w[4]; bf16x8_t v; } u{{pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3])}};
-#pragma unroll
-        for (int x = 0; x < ND; ++x) acc[r][x] = mma_cols<D>(vl, 16 * x, lane, u.v, acc[r][x]);
-      } else {
-#pragma unroll
-        for (int x = 0; x < ND; ++x) acc[r][x] = mma_cols<D>(T{}, vl, 16 * x, lane, p[0], p[1], acc[r][x]);
-      }
+      compiler_fence();
     }
-    compiler_fence();
-  }
-  __syncthreads();                                    // before the list is filled again
+    __syncthreads();                                  // before the list is filled again
   }
 
   // join the four waves, 16 rows at a time: [wave][row][d], [wave][row] x {maximum, sum}

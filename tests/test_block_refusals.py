@@ -60,7 +60,8 @@ def test_struct_matches_the_header():
     (dict(bits=8), -3), (dict(page=8), -2), (dict(page=48), -2), (dict(page=256), -2), (dict(max_pages=0), -2), (dict(max_pages=1 << 27), -2),
     (dict(max_q=0), -2), (dict(qblock=0), -2), (dict(qblock=1025), -2), (dict(causal=2), -1), (dict(topk=-1), -1), (dict(keep_first=-1), -1),
     (dict(q_rows=0), -2), (dict(k_rows=-1), -2), (dict(num_pages=-1), -2), (dict(softmax_scale=float("nan")), -1),
-    (dict(softmax_scale=float("inf")), -1), (dict(B=60000, max_q=1 << 30), -2),
+    (dict(softmax_scale=float("inf")), -1), (dict(softmax_scale=1e31), -1), (dict(B=60000, max_q=1 << 29), -2),
+    (dict(max_q=(1 << 29) + 1), -2), (dict(max_pages=(1 << 25) + 1), -2),
 ])
 def test_parameters(lib, kw, code):
     assert size(lib, params())[0] == 0

@@ -298,7 +298,7 @@ TRAIN = [  # d, page, Hq, Hkv, lens, qblock, topk, causal
 ]
 
 
-def _close_gradients(x, p, sel, grads, d_o, news=None):
+def _close_gradients(x, p, sel, grads, d_o):
     dq, dk, dv = grads
     for b in range(x.B):
         n, nq = x.lens[b], x.news[b]
@@ -448,10 +448,8 @@ def test_what_lies_outside_a_sequence_does_not_matter():
         idx[0, 0, 0] = torch.tensor([1, 1, 2, 2, 1 << 30, 3])
         idx[0, 0, 1] = torch.tensor([-5, -3, -1, 99, 100, 101])           # nothing: zeros
 
-        def unique(b, p, rec):
-            # an entry counts where it is above the one before it; a page that counts twice has twice the weight, so leave it out here
-            return _lists(b, p, rec)
-        lists = [unique((b, x.lens[b]), p, idx) for b in range(2)]
+        # an entry counts where it is above the one before it; lists that hold a page twice by that are not asked here
+        lists = [_lists((b, x.lens[b]), p, idx) for b in range(2)]
         for b in range(2):
             for i in range(len(lists[b])):
                 for h in range(2):
@@ -672,3 +670,40 @@ def test_large_scores_and_infinities():
         x.cache.k.fill_(math.inf)
         o, lse = B.adacluster_block_attn(x.params(qblock=3), q, x.cu_q.cuda(), cache=x.cache, **x.where())
         assert bool(o[:3].isnan().all()) and bool(lse[:3].isnan().all())
+
+
+@pytest.mark.parametrize("dtype,bits,d,page,Hq,Hkv,qblock", [(BF, 0, 128, 16, 16, 4, 16), (BF, 4, 64, 32, 6, 2, 3), (F, 0, 64, 64, 3, 1, 1),
+                                                             (BF, 0, 64, 128, 40, 8, 33)])
+def test_nothing_is_written_outside_the_outputs_and_the_workspace(dtype, bits, d, page, Hq, Hkv, qblock):
+    from tests.test_gpu_guards import Guards
+    g = Guards()
+    lens, news = [page * 5 + 7, 1, page * 2], [61, 1, 0]
+    x = Batch(dtype, bits, d, page, Hq, Hkv, lens, news, 3, spare=0)
+    p = x.params(qblock=qblock, topk=6)
+    rows = sum(news)
+    cu = x.cu_q.cuda()
+    hold = lambda t: (lambda y: (y.copy_(t), y)[1])(g.tensor(t.shape, t.dtype))  # noqa: E731
+    cache = B.BlockCache(*(None if t is None else hold(t) for t in (x.cache.k, x.cache.v, x.cache.k_meta, x.cache.v_meta, x.cache.boxes)))
+    pages = cache.k.shape[0]
+    ws = lambda call, k_rows=0, n=0: g.tensor((max(1, B.adacluster_block_workspace_bytes(p, call, rows, k_rows, n)),), torch.uint8)  # noqa: E731
+    where = x.where()
+    sel, _ = B.adacluster_block_select(p, x.q.cuda(), cu, cache.boxes, ws=ws(B.BLOCK_SELECT, 0, pages), **where)
+    o, lse = g.tensor((rows, Hq, d), dtype), g.tensor((rows, Hq), torch.float32)
+    for s in (sel, None):
+        B.adacluster_block_attn(p, x.q.cuda(), cu, cache=cache, sel_idx=s, out=o, lse=lse, ws=ws(B.BLOCK_ATTN, 0, pages), **where)
+    held = (x.lens_t - torch.tensor(news, dtype=torch.int32)).cuda()
+    k = torch.randn((rows, Hkv, d), device="cuda").to(dtype)
+    B.adacluster_cache_append(p, k, k, cu, held, where["page_table"], cache)
+    B.adacluster_cache_read(p, cache, cu, held, where["page_table"], rows=rows, out=(g.tensor(k.shape, dtype), g.tensor(k.shape, dtype)))
+    if bits == 0:
+        y = Batch(dtype, 0, d, page, Hq, Hkv, lens, lens, 4, paged=False, spare=0)
+        p = y.params(qblock=qblock, topk=6)
+        rows, cu, q, k, v = sum(lens), y.cu_q.cuda(), y.q.cuda(), y.k.cuda(), y.v.cuda()
+        boxes = B.adacluster_block_boxes(p, k, cu, out=g.tensor((3, p.max_pages, Hkv, 2, d), dtype))
+        sel, _ = B.adacluster_block_select(p, q, cu, boxes, cu_k=cu, ws=ws(B.BLOCK_SELECT, rows))
+        o, lse = g.tensor((rows, Hq, d), dtype), g.tensor((rows, Hq), torch.float32)
+        for s in (sel, None):
+            B.adacluster_block_attn(p, q, cu, k=k, v=v, cu_k=cu, sel_idx=s, out=o, lse=lse, ws=ws(B.BLOCK_ATTN, rows))
+            B.adacluster_block_attn_backward(p, q, k, v, o, lse, torch.randn_like(q), cu, cu, sel_idx=s, ws=ws(B.BLOCK_BACKWARD, rows),
+                                             outs=[g.tensor(t.shape, dtype) for t in (q, k, v)])
+    assert g.check() > 6
