@@ -210,7 +210,7 @@ struct BlockAttnArgs {
   int nsplit;
   float *part_o, *part_ml;                   // [item][split][rows][d], [item][split][rows][2]
 };
-size_t block_attn_bytes(const BlockDims& m, int dtype, int bits, int d, bool listed);
+size_t block_attn_bytes(const BlockDims& m, int d, bool listed);
 int launch_block_attn(hipStream_t s, int dtype, int bits, int d, BlockAttnArgs a, void* ws);
 bool block_wide_takes(const BlockAttnArgs& a, int dtype, int bits);      // (block_wide.hip)
 int launch_block_attn_wide(hipStream_t s, int d, const BlockAttnArgs& a);

@@ -101,6 +101,15 @@ int done(int rc) {
   return rc;
 }
 
+// Without lists nothing hangs on the blocks: as many queries as fill a workgroup's 128 rows (2 x 512 tokens over 16 384 keys, 32 / 8 heads:
+// 603 us, in blocks of 16 queries 769; 8 heads, d = 64 103, 221).
+BlockDims unlisted(BlockDims m) {
+  m.qblock = m.G >= 128 ? 1 : 128 / m.G;
+  if (m.qblock > m.max_q) m.qblock = m.max_q;
+  m.nb = (m.max_q + m.qblock - 1) / m.qblock;
+  return m;
+}
+
 float scale_of(const adacluster_block_params* p) { return p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->d); }
 
 }  // namespace
@@ -113,9 +122,12 @@ int adacluster_block_workspace_bytes(const adacluster_block_params* p, int32_t c
   if (!bytes) return fail(ADACLUSTER_E_BADARG, "bytes is NULL");
   if (call == ADACLUSTER_BLOCK_SELECT) *bytes = block_select_bytes(m, p->dtype);
   else if (call == ADACLUSTER_BLOCK_ATTN) {
-    const size_t x = block_attn_bytes(m, p->dtype, p->bits, p->d, true), y = block_attn_bytes(m, p->dtype, p->bits, p->d, false);
+    const size_t x = block_attn_bytes(m, p->d, true), y = block_attn_bytes(unlisted(m), p->d, false);
     *bytes = p->topk > 0 && x > y ? x : y;
-  } else if (call == ADACLUSTER_BLOCK_BACKWARD) *bytes = block_grad_bytes(m, p->dtype, p->d, true);
+  } else if (call == ADACLUSTER_BLOCK_BACKWARD) {
+    const size_t x = block_grad_bytes(m, p->dtype, p->d, true), y = block_grad_bytes(unlisted(m), p->dtype, p->d, false);
+    *bytes = p->topk > 0 && x > y ? x : y;
+  }
   else return fail(ADACLUSTER_E_BADARG, "unknown call %d", call);
   return 0;
 }
@@ -188,11 +200,12 @@ int adacluster_block_attn(const adacluster_block_params* p, const void* q, const
   if (!cu_q) return fail(ADACLUSTER_E_BADARG, "block_attn: NULL tensor pointer");
   if (int rc = check_keys(&a.m, cu_k, seq_lens, page_table)) return rc;
   a.m.cu_q = cu_q;
+  if (!sel_idx) a.m = unlisted(a.m);
   a.qs = two(p->q_stride); a.os = two(p->o_stride); a.ks = three(a.m, p->k_stride); a.vs = three(a.m, p->v_stride);
   if (int rc = check_rows("q", q, p->dtype, a.qs)) return rc;
   if (int rc = check_rows("o", o, p->dtype, a.os)) return rc;
   if (int rc = check_pool(p, k, v, k_meta, v_meta, a.ks, a.vs)) return rc;
-  if (int rc = check_ws(ws, ws_bytes, block_attn_bytes(a.m, p->dtype, p->bits, p->d, sel_idx != nullptr))) return rc;
+  if (int rc = check_ws(ws, ws_bytes, block_attn_bytes(a.m, p->d, sel_idx != nullptr))) return rc;
   a.q = q; a.k = k; a.v = v; a.km = k_meta; a.vm = v_meta; a.sel = sel_idx; a.o = o; a.lse = lse;
   a.scale_log2e = scale_of(p) * LOG2E;
   return done(launch_block_attn((hipStream_t)stream, p->dtype, p->bits, p->d, a, ws));
@@ -208,6 +221,7 @@ int adacluster_block_attn_backward(const adacluster_block_params* p, const void*
   if (!cu_q || !lse) return fail(ADACLUSTER_E_BADARG, "block_attn_backward: NULL tensor pointer");
   if (int rc = check_keys(&a.m, cu_k, nullptr, nullptr)) return rc;
   a.m.cu_q = cu_q;
+  if (!sel_idx) a.m = unlisted(a.m);
   a.qs = two(p->q_stride); a.os = two(p->o_stride); a.dos = two(p->do_stride); a.dqs = two(p->dq_stride);
   a.ks = three(a.m, p->k_stride); a.vs = three(a.m, p->v_stride); a.dks = two(p->dk_stride); a.dvs = two(p->dv_stride);
   const struct { const char* name; const void* p; const KeyStride* s; } rows[] = {{"q", q, &a.qs}, {"k", k, &a.ks}, {"v", v, &a.vs}, {"o", o, &a.os},

@@ -403,10 +403,12 @@ __global__ __launch_bounds__(256) void block_attn_join(BlockAttnArgs a, int rts,
 }
 
 struct Shape { int R, rts, nsplit; long long items; };
-Shape shape_of(const BlockDims& m, int dtype, bool listed) {
+Shape shape_of(const BlockDims& m, bool listed) {
   Shape s;
-  const int rows = m.qblock * m.G, most = dtype == ADACLUSTER_F32 ? 2 : 4;
-  s.R = rows <= 16 ? 1 : rows <= 32 || most == 2 ? 2 : 4;
+  // 32 rows a wave at most: more registers than a wave has beside what is on its way (64 rows: 16 x 8 rows over 32 768 keys, d = 128 146 us,
+  // now 107; 4-bit chunks of 512 tokens over 48 pages 339, now 295).
+  const int rows = m.qblock * m.G;
+  s.R = rows <= 16 ? 1 : 2;
   s.rts = (rows + 16 * s.R - 1) / (16 * s.R);
   s.items = (long long)s.rts * m.nb * m.Hkv * m.B;
   // Few rows: the list is split until the launch has four workgroups a CU, each wave with two turns of 32 keys at least.
@@ -421,15 +423,14 @@ template <typename T, int BITS, int D>
 void go(hipStream_t s, const BlockAttnArgs& a, const Shape& sh) {
   const int wg = (int)(sh.items * sh.nsplit);
   if (sh.R == 1) block_attn<T, BITS, D, 1><<<wg, 256, 0, s>>>(a, sh.rts);
-  else if (sh.R == 2) block_attn<T, BITS, D, 2><<<wg, 256, 0, s>>>(a, sh.rts);
-  else if constexpr (sizeof(T) == 2) block_attn<T, BITS, D, 4><<<wg, 256, 0, s>>>(a, sh.rts);
+  else block_attn<T, BITS, D, 2><<<wg, 256, 0, s>>>(a, sh.rts);
   if (sh.nsplit > 1) block_attn_join<T, D><<<(int)(sh.items * sh.R), 256, 0, s>>>(a, sh.rts, sh.R);
 }
 
 }  // namespace
 
-size_t block_attn_bytes(const BlockDims& m, int dtype, int bits, int d, bool listed) {
-  const Shape s = shape_of(m, dtype, listed);
+size_t block_attn_bytes(const BlockDims& m, int d, bool listed) {
+  const Shape s = shape_of(m, listed);
   if (s.nsplit == 1) return 0;
   const size_t rows = (size_t)s.items * s.nsplit * 16 * s.R;
   return align_up(rows * d * 4, 256) + align_up(rows * 8, 256);
@@ -437,7 +438,7 @@ size_t block_attn_bytes(const BlockDims& m, int dtype, int bits, int d, bool lis
 
 int launch_block_attn(hipStream_t s, int dtype, int bits, int d, BlockAttnArgs a, void* ws) {
   if (block_wide_takes(a, dtype, bits)) return launch_block_attn_wide(s, d, a);
-  const Shape sh = shape_of(a.m, dtype, a.sel != nullptr);
+  const Shape sh = shape_of(a.m, a.sel != nullptr);
   if (!grid_fits(sh.items * (sh.nsplit > sh.R ? sh.nsplit : sh.R))) return ADACLUSTER_E_UNSUPPORTED;
   a.nsplit = sh.nsplit;
   a.part_o = (float*)ws;

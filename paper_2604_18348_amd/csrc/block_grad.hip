@@ -696,8 +696,8 @@ __global__ __launch_bounds__(256, 3) void grad_kv_wide(BlockGradArgs a, int spli
 
 // The same at d = 128, where a wave of 32 rows would hold 346 registers and a SIMD one wave.  Two waves share 32 rows: each forms the weights
 // and dS of 32 of a tile's 64 keys, passes the one that it does not need itself through LDS as the operand it is, and sums one of the two
-// products, dS K or P K, over all 64.  Two waves a SIMD then, of two workgroups with barriers of their own.  3 sequences up to 8 192 tokens, 16 / 4 heads: 794 us, by grad_q_wide
-// 1 033.
+// products, dS K or P K, over all 64.  Two waves a SIMD then, of two workgroups with barriers of their own.  3 sequences up to 8 192 tokens, 16 / 4 heads: 770 us, 1 033
+// by the kernel for d = 64.
 __global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, int split) {
   constexpr int D = 128, NW = 4, NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB;
@@ -859,7 +859,7 @@ __global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, 
 }
 
 // The same at d = 128, by pairs of waves as in grad_q_pair: each forms weights and dS of 32 of a tile's 64 rows, and sums one of dV and dK
-// over all of them.  64 keys a workgroup: 1 067 us, by grad_kv_wide 1 335.
+// over all of them.  64 keys a workgroup: 1 050 us, 1 335 by the kernel for d = 64.
 __global__ __launch_bounds__(256, 2) void grad_kv_pair(BlockGradArgs a, int split) {
   constexpr int D = 128, KG = 2, TR = 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int PT = TR * CH / 256, TILEB = TR * ROWB;
@@ -1066,13 +1066,14 @@ __global__ __launch_bounds__(256) void grad_kv_join(BlockGradArgs a) {
   else store_rows<DB>(wave >> 1 ? ok : ov, x, wave >> 1 ? a.scale : 1.f);
 }
 
-// The kernels for many rows: blocks of at least 48 rows over pages of 64 keys or more, bf16 ...
-bool rows_wide(const BlockDims& m, int dtype) { return dtype == ADACLUSTER_BF16 && m.qblock * m.G >= 48 && m.qblock * m.G <= (1 << 20) && m.page >= 64; }
+// The kernels for many rows: bf16, pages of 64 keys or more, blocks of more than 32 rows at d = 128 (one sequence of 4 096, blocks of 40 rows: a pass
+// 573 us, 769 by those for few rows), of at least 48 at d = 64 (40 rows: 574 us, 438) ...
+bool rows_wide(const BlockDims& m, int dtype, int d) { return dtype == ADACLUSTER_BF16 && m.qblock * m.G >= (d == 128 ? 33 : 48) && m.qblock * m.G <= (1 << 20) && m.page >= 64; }
 // ... with offsets inside a block or a sixteenth that 32 bits hold.
-bool wide_takes(const BlockGradArgs& a, int dtype) {
+bool wide_takes(const BlockGradArgs& a, int dtype, int d) {
   const BlockDims& m = a.m;
   const auto block = [&](const KeyStride& st) { return m.qblock * st.token + m.G * st.head < (1 << 30); };
-  return rows_wide(m, dtype) && a.ks.token < (1 << 25) && a.vs.token < (1 << 25) && block(a.qs) && block(a.dos);
+  return rows_wide(m, dtype, d) && a.ks.token < (1 << 25) && a.vs.token < (1 << 25) && block(a.qs) && block(a.dos);
 }
 
 // Workgroups that a page's blocks go to at most, where there are lists and a launch has fewer than 4 096 workgroups (eight rounds of two a CU,
@@ -1151,12 +1152,12 @@ size_t delta_bytes(const BlockDims& m) { return align_up((size_t)m.q_rows * m.Hq
 }  // namespace
 
 size_t block_grad_bytes(const BlockDims& m, int dtype, int d, bool listed) {
-  const size_t few = deal_of(m, dtype, d, false, listed).bytes, many = rows_wide(m, dtype) ? deal_of(m, dtype, d, true, listed).bytes : 0;
+  const size_t few = deal_of(m, dtype, d, false, listed).bytes, many = rows_wide(m, dtype, d) ? deal_of(m, dtype, d, true, listed).bytes : 0;
   return delta_bytes(m) + (listed ? marks_bytes(m) : 0) + (few > many ? few : many);      // (which kernels run hangs on the strides too)
 }
 
 int launch_block_attn_backward(hipStream_t s, int dtype, int d, BlockGradArgs a, void* ws) {
-  const bool wide = wide_takes(a, dtype);
+  const bool wide = wide_takes(a, dtype, d);
   const Deal x = deal_of(a.m, dtype, d, wide, a.sel != nullptr);
   a.delta = (float*)ws;
   a.marks = (uint32_t*)((char*)ws + delta_bytes(a.m));

@@ -5,9 +5,11 @@ namespace adac {
 
 namespace {
 
-// NW waves of 32 rows each.  A tile's keys and values go global -> LDS directly, 16 bytes a lane, one tile ahead of
-// the products.  Rows past a sequence's end are read from the last row there is in
-// their sixteenth (or the page's first) and masked: nothing behind the end is touched.
+// NW waves of 32 rows each.  A tile's keys and values go global -> LDS directly, 16 bytes a lane, one tile ahead of the products.  Rows past
+// a sequence's end are read from the last row there is in their sixteenth (or the page's first) and masked: nothing behind the end is
+// touched.  Bound by what lies between the products (exponentials, roundings, LDS reads), so waves a SIMD count: tiles of 32 keys and three
+// waves (two with NW = 2) against 64 keys and two, or one: 3 sequences up to 8 192 tokens, 32 pages of 64, 16 / 4 heads, d = 128 385 us
+// (489), 17 776 tokens, 30 heads, d = 64 730 (744), chunks of 2 x 1 024 tokens, NW = 2, d = 128 193 (303).
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(BlockAttnArgs a, int rts, int split) {
   constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
@@ -190,11 +192,11 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
 
 }  // namespace
 
-// Whether the kernel for many rows takes a call: bf16 keys, at least 48 rows a block and a workgroup a CU (below, the list has to be
-// split), offsets inside a sixteenth that 32 bits hold.
+// Whether the kernel for many rows takes a call: bf16 keys, more than 32 rows a block (blocks of 40 rows, d = 128 146 us, 204 by block_attn)
+// and a workgroup a CU (below, the list has to be split), offsets inside a sixteenth that 32 bits hold.
 bool block_wide_takes(const BlockAttnArgs& a, int dtype, int bits) {
   const int rows = a.m.qblock * a.m.G;
-  if (dtype != ADACLUSTER_BF16 || bits || rows < 48) return false;
+  if (dtype != ADACLUSTER_BF16 || bits || rows < 33) return false;
   const int rt = rows <= 64 ? 64 : 128;
   const long long items = (long long)((rows + rt - 1) / rt) * a.m.nb * a.m.Hkv * a.m.B;
   return items >= 256 && a.ks.token < (1 << 25) && a.vs.token < (1 << 25);
