@@ -45,12 +45,13 @@ __global__ __launch_bounds__(256) void grad_marks(BlockGradArgs a, long long ent
 //
 // In 16 bits rowsum(dO O) comes from a rounded O.  Its error e turns dS into dS - e P, whose rows no longer sum to 0, and a part of K
 // that all keys share then shows in dQ.  The row sums of dS are that error, so sum P K is kept beside dQ and dQ - rowsum(dS) sum P K
-// formed at the end (against 64 bits, 17 776 keys, d=64: dQ 0.0047 off without, 0.0024 with it); the corrected sums go on to grad_kv.
+// formed at the end, with the sums of dS as the product took it (against 64 bits, 17 776 keys, d=64: dQ 0.0047 off without, 0.0024 with
+// it); the sums of the unrounded dS correct what goes on to grad_kv.
 template <typename T, int D, int R>
 __global__ __launch_bounds__(256) void grad_q(BlockGradArgs a, int rts) {
   constexpr int NF = D * sizeof(T) / 64, ND = D / 16;
   constexpr bool FIX = sizeof(T) == 2;
-  constexpr int KBYTES = 32 * D * sizeof(T), JBYTES = (FIX ? 2 : 1) * 4 * 16 * D * 4 + 4 * 16 * 4;
+  constexpr int KBYTES = 32 * D * sizeof(T), JBYTES = (FIX ? 2 : 1) * 4 * 16 * D * 4 + 8 * 16 * 4;
   __shared__ __align__(16) char lds[4 * KBYTES > JBYTES ? 4 * KBYTES : JBYTES];
   const BlockDims& m = a.m;
   int id = blockIdx.x;
@@ -82,10 +83,10 @@ __global__ __launch_bounds__(256) void grad_q(BlockGradArgs a, int rts) {
   const int32_t* const list = a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
   const int lsub = m.lpage - 4, halves = (list ? m.topk : pages) << lsub, turns = (halves + 1) >> 1;
   f32x4_t acc[R][ND], pk[FIX ? R : 1][FIX ? ND : 1];
-  float off[R];
+  float off[R], exact[R];                            // sums of dS, rounded and not
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    off[r] = 0.f;
+    off[r] = exact[r] = 0.f;
 #pragma unroll
     for (int x = 0; x < ND; ++x) {
       acc[r][x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
@@ -126,7 +127,7 @@ __global__ __launch_bounds__(256) void grad_q(BlockGradArgs a, int rts) {
           const float w = __builtin_amdgcn_exp2f(fmaf(sc[j], a.scale_log2e, -lse[r]));
           p[h][j] = sees ? w : 0.f;
           ds[h][j] = sees ? w * (dp[j] - delta[r]) : 0.f;
-          if constexpr (FIX) off[r] += __uint_as_float((uint32_t)f32_to_bf16(ds[h][j]) << 16);      // (as the product takes it)
+          if constexpr (FIX) { off[r] += __uint_as_float((uint32_t)f32_to_bf16(ds[h][j]) << 16); exact[r] += ds[h][j]; }
         }
       }
 #pragma unroll
@@ -148,14 +149,17 @@ __global__ __launch_bounds__(256) void grad_q(BlockGradArgs a, int rts) {
       *(f32x4_t*)(jo + (wave * 16 + n16) * D + 16 * x + 4 * quarter) = acc[r][x];
       if constexpr (FIX) *(f32x4_t*)(jp + (wave * 16 + n16) * D + 16 * x + 4 * quarter) = pk[r][x];
     }
-    if constexpr (FIX) { const float e = quarters_sum(off[r]); if (quarter == 0) js[wave * 16 + n16] = e; }
+    if constexpr (FIX) {
+      const float e = quarters_sum(off[r]), x = quarters_sum(exact[r]);
+      if (quarter == 0) { js[wave * 16 + n16] = e; js[64 + wave * 16 + n16] = x; }
+    }
     __syncthreads();
     const int jr = tid >> 4, row = base_row + r * 16 + jr, d0 = (tid & 15) * (D / 16);
     if (row >= rows) continue;
     float e = 0.f;
     if constexpr (FIX) {
       e = js[jr] + js[16 + jr] + js[32 + jr] + js[48 + jr];
-      if (d0 == 0) a.delta[(long long)(s.q0 + t0 + row / m.G) * m.Hq + hk * m.G + row % m.G] += e;      // (its only reader and writer here)
+      if (d0 == 0) a.delta[(long long)(s.q0 + t0 + row / m.G) * m.Hq + hk * m.G + row % m.G] += js[64 + jr] + js[80 + jr] + js[96 + jr] + js[112 + jr];      // (its only reader and writer here)
     }
     T* const out = (T*)a.dq + (long long)(s.q0 + t0 + row / m.G) * a.dqs.token + (long long)(hk * m.G + row % m.G) * a.dqs.head + d0;
 #pragma unroll
@@ -393,7 +397,7 @@ __global__ __launch_bounds__(256, 3) void grad_q_wide(BlockGradArgs a, int rts, 
   f32x16_t dq[DB], pk[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dq[db] = pk[db] = zero16();
-  float off = 0.f;
+  float off = 0.f, exact[2] = {0.f, 0.f};            // sums of dS, rounded and not
   const float sc = a.scale_log2e;
 
   int lrow[PT], piece[PT];
@@ -468,6 +472,8 @@ __global__ __launch_bounds__(256, 3) void grad_q_wide(BlockGradArgs a, int rts, 
           for (int s2 = 0; s2 < 2; ++s2) {
             const bf16x8_t pf = pack8(sa, s2), df = pack8(dp, s2);
             off = sum8(df, off);
+#pragma unroll
+            for (int v = 0; v < 8; ++v) exact[v & 1] += dp[8 * s2 + v];
             const char* const p = kt + (kb * 32 + 16 * s2) * ROWB;
 #pragma unroll
             for (int db = 0; db < DB; ++db) {
@@ -483,7 +489,7 @@ __global__ __launch_bounds__(256, 3) void grad_q_wide(BlockGradArgs a, int rts, 
     }
   }
   if (!there) return;
-  const float e = off + __shfl_xor(off, 32);
+  const float e = off + __shfl_xor(off, 32), x = exact[0] + exact[1], fix = x + __shfl_xor(x, 32);
   bf16raw* const out = (bf16raw*)a.dq + (long long)(s.q0 + tok) * a.dqs.token + (long long)head * a.dqs.head + 4 * hb;
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
@@ -493,7 +499,7 @@ __global__ __launch_bounds__(256, 3) void grad_q_wide(BlockGradArgs a, int rts, 
     for (int x = 0; x < 4; ++x)
       *(uint2*)(out + db * 32 + 8 * x) = uint2{pack_bf16x2(dq[db][4 * x], dq[db][4 * x + 1]), pack_bf16x2(dq[db][4 * x + 2], dq[db][4 * x + 3])};
   }
-  if (hb == 0) a.delta[rec] = delta + e;             // (its only reader and writer in this launch)
+  if (hb == 0) a.delta[rec] = delta + fix;             // (its only reader and writer in this launch)
 }
 
 // dK and dV of 32 KG keys (a page, or a part of one), bf16, from blocks of many rows: KG waves of 32 keys side by side, and 4 / KG groups of
@@ -703,7 +709,7 @@ __global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, 
   constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB;
   __shared__ __align__(16) char lds[4 * TILEB];
   __shared__ __align__(16) u32x4_t pass[2][2][2][64];         // [rows][from][sixteen] of a lane's operands
-  __shared__ float offs[2][2][32];
+  __shared__ float2 offs[2][2][32];
   __shared__ int2 pages_l[LIST];
   __shared__ int32_t counts[NW];
   const BlockDims& m = a.m;
@@ -740,7 +746,7 @@ __global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, 
   f32x16_t acc[DB];                                 // of dS K in the first wave of a pair, of P K in the second
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = zero16();
-  float off = 0.f;
+  float off = 0.f, exact[2] = {0.f, 0.f};            // sums of dS, rounded and not
   const float sc = a.scale_log2e;
 
   int lrow[PT], piece[PT];
@@ -814,6 +820,8 @@ __global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, 
         for (int s2 = 0; s2 < 2; ++s2) {
           const bf16x8_t pf = pack8(sa, s2), df = pack8(dp, s2);
           off = sum8(df, off);
+#pragma unroll
+          for (int v = 0; v < 8; ++v) exact[v & 1] += dp[8 * s2 + v];
           own[s2] = half ? pf : df;
           *(bf16x8_t*)&pass[rg][half][s2][lane] = half ? df : pf;
         }
@@ -835,7 +843,9 @@ __global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, 
     }
   }
   off += __shfl_xor(off, 32);
-  if (hb == 0) offs[rg][half][c] = off;
+  float fix = exact[0] + exact[1];
+  fix += __shfl_xor(fix, 32);
+  if (hb == 0) offs[rg][half][c] = float2{off, fix};
   float* const pk = (float*)lds + rg * 64 * 64;      // P K to the first wave of a pair: [value][lane]
   if (half) {
 #pragma unroll
@@ -845,7 +855,7 @@ __global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, 
   }
   __syncthreads();
   if (half || !there) return;
-  const float e = offs[rg][0][c] + offs[rg][1][c];
+  const float e = offs[rg][0][c].x + offs[rg][1][c].x;
   bf16raw* const out = (bf16raw*)a.dq + (long long)(s.q0 + tok) * a.dqs.token + (long long)head * a.dqs.head + 4 * hb;
 #pragma unroll
   for (int db = 0; db < DB; ++db) {
@@ -855,7 +865,7 @@ __global__ __launch_bounds__(256, 2) void grad_q_pair(BlockGradArgs a, int rts, 
     for (int x = 0; x < 4; ++x)
       *(uint2*)(out + db * 32 + 8 * x) = uint2{pack_bf16x2(acc[db][4 * x], acc[db][4 * x + 1]), pack_bf16x2(acc[db][4 * x + 2], acc[db][4 * x + 3])};
   }
-  if (hb == 0) a.delta[rec] = delta + e;             // (its only reader and writer in this launch)
+  if (hb == 0) a.delta[rec] = delta + offs[rg][0][c].y + offs[rg][1][c].y;             // (its only reader and writer in this launch)
 }
 
 // The same at d = 128, by pairs of waves as in grad_q_pair: each forms weights and dS of 32 of a tile's 64 rows, and sums one of dV and dK
