@@ -35,11 +35,16 @@ __device__ __forceinline__ uint32_t quantise(const float* v, uint32_t* pair) {
 #pragma unroll
   for (int i = 0; i < VEC; ++i) { lo = fminf(lo, v[i]); hi = fmaxf(hi, v[i]); good = good && finite(v[i]); }
   int ok = good;
-#pragma unroll
-  for (int x = 1; x < 64 / VEC; x <<= 1) {
-    lo = fminf(lo, __shfl_xor(lo, x)); hi = fmaxf(hi, __shfl_xor(hi, x));
-    ok &= __shfl_xor(ok, x);
-  }
+  const auto join = [&](auto ctrl) __attribute__((always_inline)) {      // with the lane that the DPP control names
+    constexpr int C = decltype(ctrl)::value;
+    lo = fminf(lo, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(lo), C, 0xF, 0xF, false)));
+    hi = fmaxf(hi, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(hi), C, 0xF, 0xF, false)));
+    ok &= __builtin_amdgcn_update_dpp(0, ok, C, 0xF, 0xF, false);
+  };
+  join(std::integral_constant<int, 0xB1>{});        // lanes 1 apart
+  join(std::integral_constant<int, 0x4E>{});        // 2 apart
+  join(std::integral_constant<int, 0x141>{});       // the other four of eight
+  if constexpr (VEC == 4) join(std::integral_constant<int, 0x140>{});      // the other eight of sixteen
   const uint32_t lob = bf16_down(lo);
   const float low = __uint_as_float(lob << 16), span = hi - low;
   const uint32_t stb = bf16_up(span * (1.0f / 15.0f));
@@ -47,7 +52,17 @@ __device__ __forceinline__ uint32_t quantise(const float* v, uint32_t* pair) {
   if (!(ok && finite(span) && finite(step))) { *pair = 0x7FC07FC0u; return 0; }
   *pair = lob << 16 | stb;
   uint32_t codes = 0;
-  if (step > 0.f) {
+  if (step >= 0x1p-100f && step <= 0x1p100f) {
+    // (v - low) / step as the division rounds it, from one reciprocal: with y = 1 / step rounded to nearest and q near the quotient,
+    // q + (x - q step) y, the remainder exact by an fma, is the quotient rounded to nearest (Markstein, "Computation of elementary
+    // functions on the IBM RISC System/6000 processor", 1990).  Divisions: 25 000 tokens of 8 heads, d = 128 40 us, 32 so.
+    const float y = 1.0f / step;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      const float x = v[i] - low, q = x * y, r = fmaf(fmaf(-q, step, x), y, q);
+      codes |= (uint32_t)fminf(fmaxf(rintf(r), 0.f), 15.f) << (4 * i);
+    }
+  } else if (step > 0.f) {
 #pragma unroll
     for (int i = 0; i < VEC; ++i) codes |= (uint32_t)fminf(fmaxf(rintf((v[i] - low) / step), 0.f), 15.f) << (4 * i);
   }

@@ -432,6 +432,25 @@ def test_four_bit_groups_at_their_limits():
         assert bool(((got.cpu()[good] - x[good]).abs() <= room.unsqueeze(-1)).all())
 
 
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_four_bit_codes_are_those_of_the_division(dtype):
+    """Every code of a million values of all scales, many of them half-way between two: as the definition's division rounds them."""
+    n = 4096
+    p = B.BlockParams(B=1, Hq=4, Hkv=4, d=64, dtype=_kind(dtype), bits=4, page=128, max_pages=n // 128, max_q=n)
+    g = torch.Generator().manual_seed(12)
+    k = torch.randn((n, 4, 64), generator=g) * torch.exp2(torch.randint(-120, 120, (n, 1, 1), generator=g).float())
+    v = torch.randint(-64, 65, (n, 4, 64), generator=g) * torch.exp2(torch.randint(-8, 8, (n, 4, 1), generator=g).float())
+    k, v = k.to(dtype), v.to(dtype)
+    cache = B.alloc_cache(p, n // 128)
+    cu, old = torch.tensor([0, n], dtype=torch.int32).cuda(), torch.zeros(1, dtype=torch.int32).cuda()
+    table = torch.arange(n // 128, dtype=torch.int32).cuda().view(1, -1)
+    B.adacluster_cache_append(p, k.cuda(), v.cuda(), cu, old, table, cache)
+    for got, meta, x in ((cache.k, cache.k_meta, k), (cache.v, cache.v_meta, v)):
+        codes, want = ref.quantise(x)
+        flat = lambda t: t.cpu().transpose(1, 2).flatten(0, 1)  # noqa: E731
+        assert torch.equal(flat(got), codes) and torch.equal(flat(meta).float(), want.float())
+
+
 def test_what_lies_outside_a_sequence_does_not_matter():
     """NaN behind a sequence's end and in pages it does not list, table entries that name no page, lists with entries that are none."""
     for dtype, bits in ((BF, 0), (F, 0), (BF, 4), (F, 4)):
