@@ -628,6 +628,8 @@ def adacluster_block_select(p: BlockParams, q, cu_q, boxes, cu_k=None, seq_lens=
     _boxes(boxes, (n, p.Hkv, 2, p.d) if paged else (p.B, p.max_pages, p.Hkv, 2, p.d), p, dev)
     idx = torch.empty((p.B, p.blocks, p.Hkv, p.topk), dtype=torch.int32, device=dev)
     cnt = torch.empty((p.B, p.blocks, p.Hkv), dtype=torch.int32, device=dev)
+    if not q.shape[0]:                                  # a step without queries
+        return idx.fill_(-1), cnt.zero_()
     ws, size = _block_ws(cp, BLOCK_SELECT, dev, ws)
     _on(dev, "adacluster_block_select", cp, q.data_ptr(), cu_q.data_ptr(), _ptr(cu_k), _ptr(seq_lens), _ptr(page_table), boxes.data_ptr(),
         idx.data_ptr(), cnt.data_ptr(), _ptr(ws), size)
@@ -659,6 +661,8 @@ def adacluster_block_attn(p: BlockParams, q, cu_q, k=None, v=None, cu_k=None, ca
     if o.shape[0] != rows:
         raise ValueError("out must have the rows of q")
     cp = _block_c(p, rows, k_rows, n, q=_rows("q", q, dt, p.Hq, p.d, dev), o=_rows("out", o, dt, p.Hq, p.d, dev), k=ks, v=vs)
+    if not rows:
+        return o, lse
     ws, size = _block_ws(cp, BLOCK_ATTN, dev, ws)
     _on(dev, "adacluster_block_attn", cp, q.data_ptr(), cu_q.data_ptr(), k.data_ptr(), v.data_ptr(), _ptr(km), _ptr(vm), _ptr(cu_k), _ptr(seq_lens),
         _ptr(page_table), _ptr(sel_idx), o.data_ptr(), lse.data_ptr(), _ptr(ws), size)

@@ -672,6 +672,19 @@ def test_calls_on_another_stream():
         assert torch.equal(got[0], want[0]) and torch.equal(got[1][:n], want[1][:n]) and torch.equal(got[2][:n], want[2][:n])
 
 
+def test_a_step_without_queries():
+    x = Batch(BF, 0, 64, 16, 2, 1, [40, 20], [0, 0], 6, spare=0)
+    p = x.params(topk=3)
+    q, cu = x.q.cuda(), x.cu_q.cuda()
+    sel, cnt = B.adacluster_block_select(p, q, cu, x.cache.boxes, **x.where())
+    assert bool((sel == -1).all()) and bool((cnt == 0).all())
+    o, lse = B.adacluster_block_attn(p, q, cu, cache=x.cache, sel_idx=sel, **x.where())
+    assert o.shape == (0, 2, 64) and lse.shape == (0, 2)
+    k = torch.empty((0, 1, 64), dtype=BF, device="cuda")
+    B.adacluster_cache_append(p, k, k, cu, x.lens_t.cuda(), x.table.cuda(), x.cache)
+    assert B.adacluster_cache_read(p, x.cache, cu, x.lens_t.cuda(), x.table.cuda(), rows=0)[0].shape == (0, 1, 64)
+
+
 def test_large_scores_and_infinities():
     """Scores past the range of an exponential; keys of infinity make rows of NaN or of weight one, as the definition says."""
     for dtype in (BF, F):
