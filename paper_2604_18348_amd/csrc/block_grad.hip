@@ -1076,9 +1076,10 @@ __global__ __launch_bounds__(256) void grad_kv_join(BlockGradArgs a) {
   else store_rows<DB>(wave >> 1 ? ok : ov, x, wave >> 1 ? a.scale : 1.f);
 }
 
-// The kernels for many rows: bf16, pages of 64 keys or more, blocks of more than 32 rows at d = 128 (one sequence of 4 096, blocks of 40 rows: a pass
-// 573 us, 769 by those for few rows), of at least 48 at d = 64 (40 rows: 574 us, 438) ...
-bool rows_wide(const BlockDims& m, int dtype, int d) { return dtype == ADACLUSTER_BF16 && m.qblock * m.G >= (d == 128 ? 33 : 48) && m.qblock * m.G <= (1 << 20) && m.page >= 64; }
+// The kernels for many rows: bf16, blocks of more than 32 rows at d = 128 (one sequence of 4 096, blocks of 40 rows: a pass
+// 573 us, 769 by those for few rows), of at least 48 at d = 64 (40 rows: 574 us, 438);
+// dK and dV over pages of 64 keys or more ...
+bool rows_wide(const BlockDims& m, int dtype, int d) { return dtype == ADACLUSTER_BF16 && m.qblock * m.G >= (d == 128 ? 33 : 48) && m.qblock * m.G <= (1 << 20); }
 // ... with offsets inside a block or a sixteenth that 32 bits hold.
 bool wide_takes(const BlockGradArgs& a, int dtype, int d) {
   const BlockDims& m = a.m;
@@ -1107,14 +1108,22 @@ Deal deal_of(const BlockDims& m, int dtype, int d, bool wide, bool listed) {
 }
 
 template <int D>
-int go_wide(hipStream_t s, const BlockGradArgs& a, const Deal& x) {
+int go_wide_q(hipStream_t s, const BlockGradArgs& a) {
   const BlockDims& m = a.m;
   const int rows = m.qblock * m.G, per = D == 128 ? 64 : 128, rts = (rows + per - 1) / per;
-  const long long heads = (long long)m.Hkv * m.B, grid = xcd_grid(heads, (long long)rts * m.nb), wk = xcd_grid(heads, x.groups) * x.np;
+  const long long heads = (long long)m.Hkv * m.B, grid = xcd_grid(heads, (long long)rts * m.nb);
   const int split = xcd_split(heads);
-  if (!grid_fits(grid) || !grid_fits(wk)) return ADACLUSTER_E_UNSUPPORTED;
+  if (!grid_fits(grid)) return ADACLUSTER_E_UNSUPPORTED;
   if constexpr (D == 128) grad_q_pair<<<(int)grid, 256, 0, s>>>(a, rts, split); else grad_q_wide<<<(int)grid, 256, 0, s>>>(a, rts, split);
-  if (int rc = launched()) return rc;
+  return launched();
+}
+
+template <int D>
+int go_wide_kv(hipStream_t s, const BlockGradArgs& a, const Deal& x) {
+  const BlockDims& m = a.m;
+  const long long heads = (long long)m.Hkv * m.B, wk = xcd_grid(heads, x.groups) * x.np;
+  const int split = xcd_split(heads);
+  if (!grid_fits(wk)) return ADACLUSTER_E_UNSUPPORTED;
   if constexpr (D == 128) grad_kv_pair<<<(int)wk, 256, 0, s>>>(a, split);
   else if (x.keys == 128) grad_kv_wide<4><<<(int)wk, 256, 0, s>>>(a, split);
   else grad_kv_wide<2><<<(int)wk, 256, 0, s>>>(a, split);
@@ -1143,9 +1152,16 @@ int go(hipStream_t s, const BlockGradArgs& a, const Deal& x, bool wide) {
   }
   grad_delta<T, D><<<(int)deltas, 256, 0, s>>>(a);
   if (int rc = launched()) return rc;
-  if constexpr (sizeof(T) == 2) if (wide) return go_wide<D>(s, a, x);
-  if (R == 1) grad_q<T, D, 1><<<(int)wq, 256, 0, s>>>(a, rts); else grad_q<T, D, 2><<<(int)wq, 256, 0, s>>>(a, rts);
-  if (int rc = launched()) return rc;
+  if constexpr (sizeof(T) == 2) {
+    if (wide) {
+      if (int rc = go_wide_q<D>(s, a)) return rc;
+      if (m.page >= 64) return go_wide_kv<D>(s, a, x);
+    }
+  }
+  if (!wide) {
+    if (R == 1) grad_q<T, D, 1><<<(int)wq, 256, 0, s>>>(a, rts); else grad_q<T, D, 2><<<(int)wq, 256, 0, s>>>(a, rts);
+    if (int rc = launched()) return rc;
+  }
   if (x.keys == 16) grad_kv<T, D, 1><<<(int)wk, 256, 0, s>>>(a);
   else if constexpr (sizeof(T) == 2 || D == 64) grad_kv<T, D, 2><<<(int)wk, 256, 0, s>>>(a);
   if (x.np > 1) {
@@ -1162,13 +1178,13 @@ size_t delta_bytes(const BlockDims& m) { return align_up((size_t)m.q_rows * m.Hq
 }  // namespace
 
 size_t block_grad_bytes(const BlockDims& m, int dtype, int d, bool listed) {
-  const size_t few = deal_of(m, dtype, d, false, listed).bytes, many = rows_wide(m, dtype, d) ? deal_of(m, dtype, d, true, listed).bytes : 0;
+  const size_t few = deal_of(m, dtype, d, false, listed).bytes, many = rows_wide(m, dtype, d) && m.page >= 64 ? deal_of(m, dtype, d, true, listed).bytes : 0;
   return delta_bytes(m) + (listed ? marks_bytes(m) : 0) + (few > many ? few : many);      // (which kernels run hangs on the strides too)
 }
 
 int launch_block_attn_backward(hipStream_t s, int dtype, int d, BlockGradArgs a, void* ws) {
   const bool wide = wide_takes(a, dtype, d);
-  const Deal x = deal_of(a.m, dtype, d, wide, a.sel != nullptr);
+  const Deal x = deal_of(a.m, dtype, d, wide && a.m.page >= 64, a.sel != nullptr);
   a.delta = (float*)ws;
   a.marks = (uint32_t*)((char*)ws + delta_bytes(a.m));
   a.sums = (float*)((char*)a.marks + marks_bytes(a.m));

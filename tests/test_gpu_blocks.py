@@ -288,7 +288,9 @@ TRAIN = [  # d, page, Hq, Hkv, lens, qblock, topk, causal
     (128, 128, 8, 8, [1100], 128, 3, 1),
     (128, 64, 4, 1, [2100], 16, 9, 1),                       # first pages that nearly every block lists, more than others: dealt out
     (64, 128, 4, 1, [2300, 300], 16, 5, 1),
-    (64, 64, 8, 2, [1500], 32, 6, 0),                        # (to here)
+    (64, 64, 8, 2, [1500], 32, 6, 0),
+    (64, 16, 8, 1, [300, 77], 16, 6, 1),                     # small pages: dQ by those kernels, dK and dV by the others
+    (128, 16, 15, 3, [250], 13, 9, 0),                       # (to here)
     (64, 16, 2, 1, [50, 1], 4, 4, 1),
     (128, 32, 6, 2, [100, 33, 0], 16, 3, 1),
     (64, 64, 3, 3, [200, 65], 64, 2, 0),
