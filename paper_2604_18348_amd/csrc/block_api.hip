@@ -110,7 +110,8 @@ BlockDims unlisted(BlockDims m) {
   return m;
 }
 
-float scale_of(const adacluster_block_params* p) { return p->softmax_scale > 0.f ? p->softmax_scale : 1.0f / sqrtf((float)p->d); }
+double scale_of(const adacluster_block_params* p) { return p->softmax_scale > 0.f ? p->softmax_scale : 1.0 / sqrt((double)p->d); }
+float log2_scale(const adacluster_block_params* p) { return (float)(scale_of(p) * 1.4426950408889634); }      // (rounded once: logits of 20 feel it)
 
 }  // namespace
 
@@ -207,7 +208,7 @@ int adacluster_block_attn(const adacluster_block_params* p, const void* q, const
   if (int rc = check_pool(p, k, v, k_meta, v_meta, a.ks, a.vs)) return rc;
   if (int rc = check_ws(ws, ws_bytes, block_attn_bytes(a.m, p->d, sel_idx != nullptr))) return rc;
   a.q = q; a.k = k; a.v = v; a.km = k_meta; a.vm = v_meta; a.sel = sel_idx; a.o = o; a.lse = lse;
-  a.scale_log2e = scale_of(p) * LOG2E;
+  a.scale_log2e = log2_scale(p);
   return done(launch_block_attn((hipStream_t)stream, p->dtype, p->bits, p->d, a, ws));
 }
 
@@ -229,8 +230,8 @@ int adacluster_block_attn_backward(const adacluster_block_params* p, const void*
   for (const auto& r : rows) if (int rc = check_rows(r.name, r.p, p->dtype, *r.s)) return rc;
   if (int rc = check_ws(ws, ws_bytes, block_grad_bytes(a.m, p->dtype, p->d, sel_idx != nullptr))) return rc;
   a.q = q; a.k = k; a.v = v; a.o = o; a.lse = lse; a.d_o = d_o; a.sel = sel_idx; a.dq = dq; a.dk = dk; a.dv = dv;
-  a.scale = scale_of(p);
-  a.scale_log2e = a.scale * LOG2E;
+  a.scale = (float)scale_of(p);
+  a.scale_log2e = log2_scale(p);
   return done(launch_block_attn_backward((hipStream_t)stream, p->dtype, p->d, a, ws));
 }
 
