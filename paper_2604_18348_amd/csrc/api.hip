@@ -34,7 +34,6 @@ int adac::fail(int code, const char* fmt, ...) {
 
 namespace {
 
-
 // Optional stage timing: hipEvents recorded at the stage boundaries of a call.  A stage is timed
 // from the event in from[] (default: the previous recorded stage boundary); the fused call runs
 // the two clusterings side by side, so both of those are timed from the start of the call.
