@@ -126,14 +126,14 @@ __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D =
   const int32_t* const list = a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
   const int lsub = m.lpage - 4, entries = list ? m.topk : pages;
 
-  // The weights are taken relative to a reference that moves only when a turn's sum leaves its range (see below); the lowest
-  // value that is finite when scaled too, so that turns a row sees nothing of leave sum and accumulator at zero.
+  // The weights are taken relative to a reference that moves only when a turn's sum leaves its range (see below); from where it
+  // starts, turns a row sees nothing of leave sum and accumulator at zero.
   const float scale = a.scale_log2e;
   float ref[R], sum[R], corr[R][NG];
   f32x4_t acc[R][ND];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    ref[r] = -3.402823466e38f / fmaxf(scale, 1.f); sum[r] = 0.f;
+    ref[r] = softmax_start(scale); sum[r] = 0.f;
 #pragma unroll
     for (int g = 0; g < NG; ++g) corr[r][g] = 0.f;
 #pragma unroll

@@ -51,10 +51,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
   f32x16_t oacc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) oacc[db] = zero16();
-  // The weights are taken relative to a reference that moves only when a tile's sum leaves its range (see below); the lowest
-  // value that is finite when scaled too, so that tiles a row sees nothing of leave sum and accumulator at zero.
-  const float sc = a.scale_log2e, lowest = -3.402823466e38f / fmaxf(sc, 1.f);
-  float mref = lowest, lrun = 0.f;
+  // The weights are taken relative to a reference that moves only when a tile's sum leaves its range (see below); from where it
+  // starts, tiles a row sees nothing of leave sum and accumulator at zero.
+  const float sc = a.scale_log2e;
+  float mref = softmax_start(sc), lrun = 0.f;
 
   int lrow[PT], piece[PT];                         // this thread's pieces of a tile
 #pragma unroll

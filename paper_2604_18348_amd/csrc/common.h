@@ -32,6 +32,12 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return *reinterpret_cast<uint32_t*>(&y);
 }
 
+// Where the reference of a running soft-max with weights 2^((s - reference) scale) starts: below the scores, and finite when scaled too,
+// so that a score of -inf has the weight 0 before any other has moved it (relative to -inf it would be NaN).  The quotient and
+// its product with the scale are rounded, each by 2^-24 at most: from the lowest float itself, an eighth of the scales above 1
+// get to -inf.
+__device__ __forceinline__ float softmax_start(float scale) { return -3.4028e38f / fmaxf(scale, 1.f); }
+
 template <typename T> struct Elem;
 template <> struct Elem<float> {
   static __device__ __forceinline__ float load(const float* p) { return *p; }
