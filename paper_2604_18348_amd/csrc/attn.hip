@@ -723,10 +723,10 @@ __global__ __launch_bounds__(NW * 64, MINB) void attn_mfma(AttnArgs a) {
     for (int v = 0; v < 16; ++v) oacc[db][v] = 0.f;
   // Soft-max state of this lane's query: probabilities are taken relative to a reference mref that is only
   // moved when it has to be (see soft-max below); lrun is the sum of the probabilities so far.  The reference starts at
-  // the lowest value that is finite when scaled too: every score above -inf is far enough above it to move it, and tiles
+  // a value that is finite when scaled too: every score above -inf is far enough above it to move it, and tiles
   // of -inf alone, at the start of the share or all through it, leave it there with a sum and an accumulator of zero (from
   // -inf they would make both NaN, and the launch of small dense calls, whose shares start anywhere in a list, with them).
-  float mref = -3.402823466e38f / fmaxf(a.scale_log2e, 1.f), lrun = 0.f;
+  float mref = softmax_start(a.scale_log2e), lrun = 0.f;
 
   // Where a 16-byte chunk sits inside its (unpadded) tile row: chunk q of row r is in slot q ^ swz(r).  A row
   // is 256 B (d=128: every row starts at bank 0) or 128 B (d=64: rows two apart do), so the slot alone decides
@@ -1150,7 +1150,7 @@ __global__ __launch_bounds__(F32_WAVES * 64, D == 64 ? 3 : 2) void attn_f32(Attn
     for (int v = 0; v < 16; ++v) o[db][v] = 0.f;
   // The running maximum starts at a number no score lies below, and that stays one as an exponent of 2: relative to it a
   // score of -inf is a probability of 0 (relative to -inf it would be NaN).
-  float m = -3.4028234e38f / fmaxf(1.f, a.scale_log2e), l = 0.f;
+  float m = softmax_start(a.scale_log2e), l = 0.f;
   for (int t = t0; t < T; t += tstep) {
     wait_vmcnt<0>();                                       // the K tile has landed
     asm volatile("" ::: "memory");
