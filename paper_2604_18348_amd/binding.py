@@ -12,7 +12,7 @@ import functools
 import os
 import operator
 import struct
-from dataclasses import dataclass
+from dataclasses import dataclass, replace
 
 import torch
 
@@ -552,6 +552,8 @@ def alloc_cache(p: BlockParams, num_pages, device="cuda"):
 
 
 def adacluster_block_workspace_bytes(p: BlockParams, call, q_rows, k_rows=0, num_pages=0) -> int:
+    if not q_rows:                                      # a step without queries
+        return 0
     return _block_bytes(_block_c(p, q_rows, k_rows, num_pages), call)
 
 
@@ -598,8 +600,10 @@ def adacluster_block_boxes(p: BlockParams, k, cu_k, out=None):
     shape = (p.B, p.max_pages, p.Hkv, 2, p.d)
     boxes = torch.empty(shape, dtype=dt, device=dev) if out is None else out
     _boxes(boxes, shape, p, dev)
-    _on(dev, "adacluster_block_boxes", _block_c(p, 1, k.shape[0], k=(0, *_rows("k", k, dt, p.Hkv, p.d, dev))), k.data_ptr(), cu_k.data_ptr(),
-        boxes.data_ptr())
+    strides = _rows("k", k, dt, p.Hkv, p.d, dev)
+    if not k.shape[0]:                                  # no keys: every page is past its sequence's last
+        return boxes.zero_()
+    _on(dev, "adacluster_block_boxes", _block_c(p, 1, k.shape[0], k=(0, *strides)), k.data_ptr(), cu_k.data_ptr(), boxes.data_ptr())
     return boxes
 
 
@@ -628,7 +632,7 @@ def adacluster_block_select(p: BlockParams, q, cu_q, boxes, cu_k=None, seq_lens=
     _boxes(boxes, (n, p.Hkv, 2, p.d) if paged else (p.B, p.max_pages, p.Hkv, 2, p.d), p, dev)
     idx = torch.empty((p.B, p.blocks, p.Hkv, p.topk), dtype=torch.int32, device=dev)
     cnt = torch.empty((p.B, p.blocks, p.Hkv), dtype=torch.int32, device=dev)
-    if not q.shape[0]:                                  # a step without queries
+    if not q.shape[0] or k_rows == 0:                   # a step without queries, or without keys
         return idx.fill_(-1), cnt.zero_()
     ws, size = _block_ws(cp, BLOCK_SELECT, dev, ws)
     _on(dev, "adacluster_block_select", cp, q.data_ptr(), cu_q.data_ptr(), _ptr(cu_k), _ptr(seq_lens), _ptr(page_table), boxes.data_ptr(),
@@ -660,6 +664,9 @@ def adacluster_block_attn(p: BlockParams, q, cu_q, k=None, v=None, cu_k=None, ca
         _lse(lse, rows, p, dev)
     if o.shape[0] != rows:
         raise ValueError("out must have the rows of q")
+    if cache is None and not k_rows and rows:           # every sequence is without keys
+        k = v = _row_of_none(p.Hkv, p.d, dt, dev)
+        k_rows, ks, vs, cu_k, sel_idx = 1, _NO3, _NO3, torch.zeros_like(cu_k), None
     cp = _block_c(p, rows, k_rows, n, q=_rows("q", q, dt, p.Hq, p.d, dev), o=_rows("out", o, dt, p.Hq, p.d, dev), k=ks, v=vs)
     if not rows:
         return o, lse
@@ -674,6 +681,11 @@ def _kv(p, k, v, dev):
         raise ValueError("k and v must be given, with the same rows")
     dt = _tdtype(p)
     return k.shape[0], (0, *_rows("k", k, dt, p.Hkv, p.d, dev)), (0, *_rows("v", v, dt, p.Hkv, p.d, dev))
+
+
+def _row_of_none(heads, d, dt, dev):
+    """What a call is given in the place of a tensor without rows: a row that belongs to no sequence."""
+    return torch.zeros((1, heads, d), dtype=dt, device=dev)
 
 
 def _lse(lse, rows, p, dev):
@@ -696,9 +708,22 @@ def adacluster_block_attn_backward(p: BlockParams, q, k, v, o, lse, d_o, cu_q, c
     if not (o.shape[0] == d_o.shape[0] == dq.shape[0] == rows and dk.shape[0] == dv.shape[0] == k_rows):
         raise ValueError("o, d_o and dq must have the rows of q, dk and dv those of k")
     at = lambda name, t, heads: _rows(name, t, dt, heads, p.d, dev)  # noqa: E731
-    cp = _block_c(p, rows, k_rows, 0, q=at("q", q, p.Hq), o=at("o", o, p.Hq), k=ks, v=vs, d_o=at("d_o", d_o, p.Hq), dq=at("dq", dq, p.Hq),
-                  dk=at("dk", dk, p.Hkv), dv=at("dv", dv, p.Hkv))
+    strides = dict(q=at("q", q, p.Hq), o=at("o", o, p.Hq), k=ks, v=vs, d_o=at("d_o", d_o, p.Hq), dq=at("dq", dq, p.Hq), dk=at("dk", dk, p.Hkv),
+                   dv=at("dv", dv, p.Hkv))
+    grads = dq, dk, dv
+    if not rows and not k_rows:
+        return grads
+    if not rows:                                        # every sequence is without queries: dk and dv are zero
+        p, rows, ws, sel_idx = replace(p, max_q=1), 1, None, None
+        q = o = d_o = dq = _row_of_none(p.Hq, p.d, dt, dev)
+        lse, cu_q = torch.zeros((1, p.Hq), device=dev), torch.zeros_like(cu_q)
+        strides.update(q=_NO2, o=_NO2, d_o=_NO2, dq=_NO2)
+    elif not k_rows:                                    # ... without keys: dq is zero
+        k = v = dk = dv = _row_of_none(p.Hkv, p.d, dt, dev)
+        k_rows, cu_k, sel_idx = 1, torch.zeros_like(cu_k), None
+        strides.update(k=_NO3, v=_NO3, dk=_NO2, dv=_NO2)
+    cp = _block_c(p, rows, k_rows, 0, **strides)
     ws, size = _block_ws(cp, BLOCK_BACKWARD, dev, ws)
     _on(dev, "adacluster_block_attn_backward", cp, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), d_o.data_ptr(),
         cu_q.data_ptr(), cu_k.data_ptr(), _ptr(sel_idx), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(ws), size)
-    return dq, dk, dv
+    return grads
