@@ -536,7 +536,8 @@ def _on(device, name, *args):
         _check(rc, name)
 
 
-_raw_stream = torch._C._cuda_getCurrentRawStream      # (torch.cuda.current_stream(i).cuda_stream makes an object on the way: 2 us)
+def _raw_stream(i):
+    return torch._C._cuda_getCurrentRawStream(i)      # (torch.cuda.current_stream(i).cuda_stream makes an object on the way: 2 us)
 
 
 def alloc_cache(p: BlockParams, num_pages, device="cuda"):
