@@ -526,7 +526,7 @@ __global__ __launch_bounds__(256) void attn_stats(int Cq, int maxr, int maxtiles
 int launch_attn_stats(hipStream_t s, int H, int Cq, int maxr, int maxtiles, const KState* st, const int32_t* tiles,
                       const int32_t* ntiles, const int32_t* rng_pre, const int32_t* rng_cnt, adacluster_head_stats* out) {
   attn_stats<<<H, 256, 0, s>>>(Cq, maxr, maxtiles, st, tiles, ntiles, rng_pre, rng_cnt, out);
-  return hipGetLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL;
+  return launched();
 }
 
 struct AttnArgs {
@@ -1572,14 +1572,14 @@ int launch_plan_sparse(hipStream_t s, int dtype, int d, int H, int Cq, int cap, 
     const auto plan = segs ? plan_tiles<true> : plan_tiles<false>;
     plan<<<H, 256, 0, s>>>(Cq, maxr, maxtiles, BM, SPLIT_SLOTS, split, tp.deal, q_offs, q_offs_stride, rng_pre, rng_cnt, tiles, ntiles, merge, nmerge);
   }
-  return hipGetLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL;
+  return launched();
 }
 
 int launch_plan_dense(hipStream_t s, int H, int N, int maxtiles, DenseShape shape, int32_t* rng_start, int32_t* rng_pre,
                       int32_t* rng_cnt, int32_t* tiles, int32_t* ntiles, int32_t* merge, int32_t* nmerge, int row_scale, int32_t* krow, size_t kstride) {
   plan_dense<<<dim3(H, 9), 256, 0, s>>>(N, maxtiles, shape.BM, shape.pieces, SPLIT_SLOTS, row_scale, rng_start, rng_pre, rng_cnt, tiles, ntiles, merge,
                                         nmerge, krow, kstride);
-  return hipGetLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL;
+  return launched();
 }
 
 int launch_attention(hipStream_t s, int dtype, int d, int H, int N, int Cq, int BM, int most, int maxtiles, float scale,
@@ -1621,7 +1621,7 @@ int launch_attention(hipStream_t s, int dtype, int d, int H, int N, int Cq, int 
       else attn_merge_f32<128><<<gm, 256, 0, s>>>(a, splits);
     }
   }
-  return hipGetLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL;
+  return launched();
 }
 
 }  // namespace adac

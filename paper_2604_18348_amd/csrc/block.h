@@ -234,6 +234,5 @@ int launch_block_attn_backward(hipStream_t s, int dtype, int d, BlockGradArgs a,
 
 // a launch of more workgroups than a grid may have threads for is refused before it is made
 static inline bool grid_fits(long long workgroups) { return workgroups <= (1ll << 32) / 256 - 1; }
-static inline int launched() { return hipGetLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL; }
 
 }  // namespace adac

@@ -2946,7 +2946,6 @@ __global__ __launch_bounds__(256) void mse_final(const double* __restrict__ part
 // ------------------------------------------------------------------------------------------
 // host-side launchers
 // ------------------------------------------------------------------------------------------
-static inline int chk() { return hipGetLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL; }
 
 int reduce_part_rows() { return REDUCE_ROWS; }
 int pass_sum_centres() { return ACC_MAXM; }
@@ -3032,7 +3031,7 @@ int launch_assign(hipStream_t s, int dtype, int d, int H, int N, int n_bound, in
       else assign_f32<128, 4><<<g, 512, 0, s>>>(x, c, ce, bias, labels, dist2);
     }
   }
-  return chk();
+  return launched();
 }
 
 static OpenCfg open_cfg(int N, int cap, const StageRules& r, const KState* in, KState* out, const StageFilter* f, const StageReport& rep) {
@@ -3075,7 +3074,7 @@ int launch_stage_pass(hipStream_t s, int dtype, int d, int H, int N, int n_bound
       if (open) stage_pass_f32<DIM, PASS_OPEN><<<g, 512, 0, s>>>(x, c, lp, cent_f32, bias, dist2, nb, turns, in, to, oc);
       else if (prev) stage_pass_f32<DIM, PASS_COMBINE><<<g, 512, 0, s>>>(x, c, lp, cent_f32, bias, dist2, nb, turns, in, to, oc);
       else stage_pass_f32<DIM, PASS_READ><<<g, 512, 0, s>>>(x, c, lp, cent_f32, bias, dist2, nb, turns, in, to, oc);
-      return chk();
+      return launched();
     };
     return d == 64 ? launch(std::integral_constant<int, 64>{}) : launch(std::integral_constant<int, 128>{});
   }
@@ -3089,7 +3088,7 @@ int launch_stage_pass(hipStream_t s, int dtype, int d, int H, int N, int n_bound
       else stage_pass<DIM, 8, PASS_READ><<<g, 512, 0, s>>>(x, c, lp, cent_f32, bias, dist2, in, to, oc);
     } else if (open) stage_pass<DIM, 4, PASS_OPEN><<<g, 256, 0, s>>>(x, c, lp, cent_f32, bias, dist2, in, to, oc);
     else stage_pass<DIM, 4, PASS_READ><<<g, 256, 0, s>>>(x, c, lp, cent_f32, bias, dist2, in, to, oc);
-    return chk();
+    return launched();
   };
   return d == 64 ? launch(std::integral_constant<int, 64>{}) : launch(std::integral_constant<int, 128>{});
 }
@@ -3101,7 +3100,7 @@ int launch_form_centres(hipStream_t s, int d, int H, int n_bound, int m_bound, i
   const dim3 g((m_bound * (d / 4) + 255) / 256, H);
   if (d == 64) form_centres_f32<64><<<g, 256, 0, s>>>(in, st, cap, (float*)cent_lp, cent_f32, bias);
   else form_centres_f32<128><<<g, 256, 0, s>>>(in, st, cap, (float*)cent_lp, cent_f32, bias);
-  return chk();
+  return launched();
 }
 
 // one-read pass of the query clustering (bf16, at most pass_sum_centres() centres): NP = walks per head
@@ -3112,7 +3111,7 @@ int launch_qpass(hipStream_t s, int d, int H, int N, int m, int cap, int weighte
   dim3 g(NP, H);
   if (d == 64) qpass_mfma<64><<<g, 256, 0, s>>>((const bf16raw*)X, N, m, cap, subs, weighted, (const bf16raw*)cent_lp, bias, psum, pcnt, NP);
   else qpass_mfma<128><<<g, 256, 0, s>>>((const bf16raw*)X, N, m, cap, subs, weighted, (const bf16raw*)cent_lp, bias, psum, pcnt, NP);
-  return chk();
+  return launched();
 }
 
 int launch_seg_reduce(hipStream_t s, int dtype, int d, int H, int N, int mode, int m_const, int m_bound, int P,
@@ -3132,7 +3131,7 @@ int launch_seg_reduce(hipStream_t s, int dtype, int d, int H, int N, int mode, i
     if (d == 64) seg_reduce<float, 64><<<g, 64, 0, s>>>((const float*)X, c, perm, offs, offs_stride, poff, pcl, psum, pnorm, pmin, pmax);
     else seg_reduce<float, 128><<<g, 64, 0, s>>>((const float*)X, c, perm, offs, offs_stride, poff, pcl, psum, pnorm, pmin, pmax);
   }
-  return chk();
+  return launched();
 }
 
 int launch_finalize(hipStream_t s, int dtype, int d, int H, int mode, int m_const, int m_bound, int P, int cap,
@@ -3154,7 +3153,7 @@ int launch_finalize(hipStream_t s, int dtype, int d, int H, int mode, int m_cons
     finalize_centroids<128><<<g, 64 * FIN_ROWS, 0, s>>>(c, offs, offs_stride, poff, psum, pnorm, pmin, pmax, master, assign_lp,
                                              assign_f32, bias, out_cent, fallback, out_sizes, out_mean_norm,
                                              out_bmin, out_bmax);
-  return chk();
+  return launched();
 }
 
 bool direct_update_fits(int dtype, int n_bound, int m_bound) {
@@ -3193,7 +3192,7 @@ int launch_cluster_stats(hipStream_t s, int dtype, int d, int H, int N, int mode
   using std::integral_constant;
   if (dtype == ADACLUSTER_BF16) { if (d == 64) launch(bf16raw{}, integral_constant<int, 64>{}); else launch(bf16raw{}, integral_constant<int, 128>{}); }
   else { if (d == 64) launch(float{}, integral_constant<int, 64>{}); else launch(float{}, integral_constant<int, 128>{}); }
-  return chk();
+  return launched();
 }
 
 int launch_update_direct(hipStream_t s, int d, int H, int N, int m_bound, int cap, int master_stride, const KState* st,
@@ -3202,7 +3201,7 @@ int launch_update_direct(hipStream_t s, int d, int H, int N, int m_bound, int ca
   dim3 g(m_bound, H);
   if (d == 64) update_direct_f32<64><<<g, 256, 0, s>>>((const float*)X, N, cap, master_stride, st, labels, ulist, master, (float*)assign_lp, assign_f32, bias);
   else update_direct_f32<128><<<g, 256, 0, s>>>((const float*)X, N, cap, master_stride, st, labels, ulist, master, (float*)assign_lp, assign_f32, bias);
-  return chk();
+  return launched();
 }
 
 int launch_init_centroids(hipStream_t s, int dtype, int d, int H, int N, int m_const, int m_bound,
@@ -3219,12 +3218,12 @@ int launch_init_centroids(hipStream_t s, int dtype, int d, int H, int N, int m_c
     if (d == 64) init_centroids<float, 64><<<g, nt, 0, s>>>((const float*)X, N, m_const, w, spherical, source_master, cap, master_stride, lp, master, assign_lp, assign_f32, bias);
     else init_centroids<float, 128><<<g, nt, 0, s>>>((const float*)X, N, m_const, w, spherical, source_master, cap, master_stride, lp, master, assign_lp, assign_f32, bias);
   }
-  return chk();
+  return launched();
 }
 
 int launch_tau_abs(hipStream_t s, float tau_abs, float* tau_out) {
   tau_set<<<1, 64, 0, s>>>(tau_abs, tau_out);
-  return chk();
+  return launched();
 }
 
 int stage_points_per_count(int dtype) { return dtype == ADACLUSTER_BF16 ? ASSIGN_POINTS_LP : ASSIGN_POINTS_F32; }
@@ -3238,7 +3237,7 @@ int launch_keep_count(hipStream_t s, const KState* st, int H, int N, const float
   }
   keep_count<<<dim3((N + KEEP_ITEMS - 1) / KEEP_ITEMS, H), 256, 0, s>>>(st, dist2, N, t, tau, cnt, cnt_stride, surv, stage_of);
   *items = KEEP_ITEMS;
-  return chk();
+  return launched();
 }
 
 int launch_stage_open(hipStream_t s, int dtype, int d, int H, int N, int cap, const StageRules& rules, int n_bound, int m_bound,
@@ -3256,7 +3255,7 @@ int launch_stage_open(hipStream_t s, int dtype, int d, int H, int N, int cap, co
     if (d == 64) stage_open<float, 64><<<g, 256, 0, s>>>((const float*)X, c);
     else stage_open<float, 128><<<g, 256, 0, s>>>((const float*)X, c);
   }
-  return chk();
+  return launched();
 }
 
 // Up to how many points a list goes to the one-launch kernel.  A stage there costs a head's workgroup, whatever the number
@@ -3296,7 +3295,7 @@ int launch_kstages_small(hipStream_t s, int d, int H, int N, int cap, const Stag
   }
   if (d == 64) kstages_small<64><<<H, SmallStage<64>::NW * 64, 0, s>>>((const bf16raw*)X, st, cfg);
   else kstages_small<128><<<H, SmallStage<128>::NW * 64, 0, s>>>((const bf16raw*)X, st, cfg);
-  return chk();
+  return launched();
 }
 
 int launch_mse(hipStream_t s, int dtype, int d, int H, int N, int cap, const void* X, const int32_t* labels,
@@ -3311,13 +3310,13 @@ int launch_mse(hipStream_t s, int dtype, int d, int H, int N, int cap, const voi
     else mse_partial<float, 128><<<g, MSE_THREADS, 0, s>>>((const float*)X, labels, cent, N, cap, nblk, part);
   }
   mse_final<<<H, 256, 0, s>>>(part, nblk, N, mse);
-  return chk();
+  return launched();
 }
 
 int launch_fill_i32(hipStream_t s, int32_t* p, size_t n, int32_t v) {
   if (n == 0) return 0;
   fill_i32<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(p, n, v);
-  return chk();
+  return launched();
 }
 
 }  // namespace adac

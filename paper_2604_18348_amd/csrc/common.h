@@ -46,6 +46,9 @@ template <> struct Elem<bf16raw> {
   static __device__ __forceinline__ float load(const bf16raw* p) { return bf16_to_f32(*p); }
 };
 
+// What a launch left: 0, or ADACLUSTER_E_INTERNAL.  The error stays for the entry point, which names it in its message and thereby clears it.
+static inline int launched() { return hipPeekAtLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL; }
+
 // Direct global -> LDS loads, written as inline assembly on purpose.  The compiler orders every LDS read
 // behind an outstanding direct-to-LDS load that it cannot prove to touch another object (it then drains ALL
 // loads in flight: vmcnt(0)), and its proof is fragile (it fails across the branches of a four-stage ring).

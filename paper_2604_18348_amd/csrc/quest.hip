@@ -283,7 +283,7 @@ int launch_quest_scores(hipStream_t s, int dtype, int form, int clamp, int H, in
     if (d == 64) { if (nw == 2) go(quest_mfma<64, 2>); else if (nw == 4) go(quest_mfma<64, 4>); else if (nw == 8) go(quest_mfma<64, 8>); else go(quest_mfma<64, 16>); }
     else { if (nw == 2) go(quest_mfma<128, 2>); else if (nw == 4) go(quest_mfma<128, 4>); else if (nw == 8) go(quest_mfma<128, 8>); else go(quest_mfma<128, 16>); }
   }
-  return hipGetLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL;
+  return launched();
 }
 
 // ------------------------------------------------------------------------------------------
@@ -318,7 +318,7 @@ int launch_mfma_probe(hipStream_t s, int iters, float* sink, size_t sink_floats,
   if (sink_floats < (size_t)PROBE_THREADS) return ADACLUSTER_E_BADARG;
   mfma_probe<<<PROBE_BLOCKS, PROBE_THREADS, 0, s>>>(iters, sink);
   *flops = (double)PROBE_BLOCKS * (PROBE_THREADS / 64) * (double)iters * PROBE_CHAINS * (2.0 * 32 * 32 * 16);
-  return hipGetLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL;
+  return launched();
 }
 
 }  // namespace adac

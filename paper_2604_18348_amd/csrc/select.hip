@@ -505,7 +505,7 @@ int launch_select(hipStream_t s, int H, int Cq, int cap, int d, int score_mode, 
       granted[dev].store((int)shm);
     }
     kernel<<<dim3(Cq, H), 256, shm, s>>>(c, scores, ScoreTables{q_cent, k_cent, k_bmin, k_bmax}, q_mean_norm, k_sizes, k_count, full_flag, sel_idx, sel_cnt, sel_keys);
-    return hipGetLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL;
+    return launched();
   };
   auto select = [&](auto topp, auto keys) {
     using std::integral_constant;

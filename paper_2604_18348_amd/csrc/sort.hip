@@ -295,7 +295,7 @@ int launch_sort(hipStream_t st, int H, int N, int n_bound, int m_bound,
     sort_small<<<H, 1024, 0, st>>>(labels, ulist, N, sort_scratch_ints(N), passes, a, m_dev, m_stride, m_bound, sc.lab_a, sc.val_a, sc.lab_b,
                                    perm, offs, offs_stride, poff, part_rows);
     if (poff_done && poff) *poff_done = 1;
-    return hipGetLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL;
+    return launched();
   }
   const int nseg = sort_segments(n_bound), stride = label_bins(m_bound);
   // dynamic LDS for the bound, so that as many workgroups share a CU as it allows (7 169 bins: 57 KB)
@@ -320,7 +320,7 @@ int launch_sort(hipStream_t st, int H, int N, int n_bound, int m_bound,
   else if (nseg * H > 256 || waves == 8) sort(integral_constant<int, 8>{}, std::true_type{});
   else sort(integral_constant<int, 16>{}, std::true_type{});
   if (poff_done && poff) *poff_done = pcl ? 2 : 1;
-  return hipGetLastError() == hipSuccess ? 0 : ADACLUSTER_E_INTERNAL;
+  return launched();
 }
 
 }  // namespace adac
