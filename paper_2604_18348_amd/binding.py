@@ -12,6 +12,7 @@ import functools
 import os
 import operator
 import struct
+import warnings
 from dataclasses import dataclass, replace
 
 import torch
@@ -575,7 +576,8 @@ def adacluster_cache_append(p: BlockParams, k, v, cu_new, seq_lens, page_table, 
 
 
 def adacluster_cache_read(p: BlockParams, cache: BlockCache, cu_new, first, page_table, rows, out=None):
-    """Tokens of the cache as values -> k, v [rows,Hkv,d]: of sequence b those from position first[b] on, to its rows by cu_new."""
+    """Tokens of the cache as values -> k, v [rows,Hkv,d]: of sequence b those from position first[b] on, to its rows by cu_new.
+    Rows that belong to no sequence, or to positions past max_pages * page, are not written: without `out` they hold anything."""
     dev, dt = _gpu(cache.k), _tdtype(p)
     _ints("cu_new", cu_new, (p.B + 1,), dev)
     _ints("first", first, (p.B,), dev)
@@ -644,8 +646,13 @@ def adacluster_block_select(p: BlockParams, q, cu_q, boxes, cu_k=None, seq_lens=
 def adacluster_block_attn(p: BlockParams, q, cu_q, k=None, v=None, cu_k=None, cache: BlockCache = None, seq_lens=None, page_table=None,
                           sel_idx=None, out=None, lse=None, ws=None):
     """Attention of q [rows,Hq,d] over packed k, v [rows,Hkv,d] with cu_k, or over a cache with seq_lens and page_table; over the
-    pages of sel_idx, or all -> o like q, lse float32 [rows,Hq]."""
+    pages of sel_idx, or all -> o like q, lse float32 [rows,Hq].  Rows that belong to no sequence are not written: without `out` and
+    `lse` they hold anything.  Nothing is recorded for autograd: the gradients are adacluster_block_attn_backward's, called from the
+    backward method of a torch.autograd.Function, say (a call on tensors that require gradients, with gradients enabled, warns)."""
     dev, dt = _gpu(q), _tdtype(p)
+    if torch.is_grad_enabled() and (q.requires_grad or cache is None and any(t is not None and t.requires_grad for t in (k, v))):
+        warnings.warn("adacluster_block_attn records nothing for autograd: no gradient reaches q, k or v through its output "
+                      "(adacluster_block_attn_backward has the gradients)", stacklevel=2)
     rows = q.shape[0]
     _ints("cu_q", cu_q, (p.B + 1,), dev)
     _keys_of(p, cu_k, seq_lens, page_table, dev, cache is not None)
