@@ -96,7 +96,6 @@ __device__ __forceinline__ int fill_list(const BlockDims& m, int b, const int32_
 }
 
 // Where the 16 keys of a sixteenth `sub` of page pg start, in elements from the tensor's base: keys of one head.
-struct Rows { long long at; int key0; };         // key0: position of the first; INT_MAX: there are none
 struct KeyStride { long long page, token, head; };
 __device__ __forceinline__ long long row_at(const BlockDims& m, const BlockSeq& s, const KeyStride& st, int phys, int pg, int sub, int hk) {
   return m.num_pages ? phys * st.page + (sub * 16) * st.token + hk * st.head

@@ -1,4 +1,4 @@
-// What the bf16 kernels for many rows share: tiles of 64 rows staged in LDS by direct loads, read by all waves (internal).
+// What the bf16 kernels for many rows share: tiles of 32 (forward) or 64 rows staged in LDS by direct loads, read by all waves (internal).
 //
 // 32x32x16 products (v_mfma_f32_32x32x16_bf16): half the LDS reads a product of the 16x16 tiles.  A result holds in lane l column
 // l % 32 and, in value v, row 8 (v / 4) + 4 (l / 32) + v % 4; eight consecutive values are the operand of the next product, whose
@@ -11,7 +11,7 @@ namespace adac {
 
 typedef __attribute__((address_space(3))) void lds_void_t;
 
-constexpr int TILE = 64;               // rows of a tile, staged as four sixteenths of pages
+constexpr int TILE = 64;               // rows of a tile of the gradients, staged as four sixteenths of pages
 
 // Rows of D bf16 in LDS, unpadded.  Piece q (16 bytes) of row r sits in slot q ^ swz(r).  Sixteen rows that are read at one piece
 // (operands that are rows) lie in sixteen different slots, and the four rows of a transposing read (operands that are columns: 64

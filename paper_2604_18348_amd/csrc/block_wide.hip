@@ -1,4 +1,4 @@
-// Attention of blocks of many rows over listed pages, bf16: the walk of block_attn with tiles of 64 keys staged once for all waves.
+// Attention of blocks of many rows over listed pages, bf16: the walk of block_attn with tiles of 32 keys staged once for all waves.
 #include "block_wide.h"
 
 namespace adac {
@@ -13,7 +13,7 @@ namespace {
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(BlockAttnArgs a, int rts, int split) {
   constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
-  constexpr int TK = 32, NKB = TK / 32, PARTS = TK / 16;      // keys a tile
+  constexpr int TK = 32, PARTS = TK / 16;      // keys a tile: one product's rows
   constexpr int PT = TK * CH / NT, TILEB = TK * ROWB;
   __shared__ __align__(16) char lds[4 * TILEB];
   __shared__ int2 pages_l[LIST];
@@ -99,13 +99,9 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
       if (wave_has_rows) {
         const char* const kt = lds + (t & 1) * 2 * TILEB;
         const char* const vt = kt + TILEB;
-        f32x16_t sacc[NKB];
+        f32x16_t sacc = zero16();
 #pragma unroll
-        for (int kb = 0; kb < NKB; ++kb) {
-          sacc[kb] = zero16();
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) sacc[kb] = mfma32(*(const bf16x8_t*)(kt + kb * 32 * ROWB + kaddr[ks]), qf[ks], sacc[kb]);
-        }
+        for (int ks = 0; ks < KS; ++ks) sacc = mfma32(*(const bf16x8_t*)(kt + kaddr[ks]), qf[ks], sacc);
         int key0[PARTS];
         bool whole = true;
 #pragma unroll
@@ -116,45 +112,37 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
         }
         if (!whole) {
 #pragma unroll
-          for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v)
-              if (key0[kb * 2 + (v >> 3)] + 8 * ((v >> 2) & 1) + 4 * hb + (v & 3) >= lim) sacc[kb][v] = -INFINITY;
+          for (int v = 0; v < 16; ++v)
+            if (key0[v >> 3] + 8 * ((v >> 2) & 1) + 4 * hb + (v & 3) >= lim) sacc[v] = -INFINITY;
         }
         // p = 2^((s - reference) scale): any reference gives the same result as long as nothing overflows.  The row sum of the tile
         // tells (on the first tile with a score above -inf it is infinite): only then is the tile's maximum taken, the reference
         // moved up to it and the accumulator scaled.
-        bf16x8_t pf[NKB][2];
+        bf16x8_t pf[2];
         float rsum;
         auto weights = [&]() __attribute__((always_inline)) {
           const float off = mref * sc;
-          float part[2 * NKB];
+          float part[2];
 #pragma unroll
-          for (int kb = 0; kb < NKB; ++kb)
+          for (int s2 = 0; s2 < 2; ++s2) {
+            union { uint32_t w[4]; bf16x8_t v; } u;
+            part[s2] = 0.f;
 #pragma unroll
-            for (int s2 = 0; s2 < 2; ++s2) {
-              const f32x16_t& x = sacc[kb];
-              union { uint32_t w[4]; bf16x8_t v; } u;
-              part[2 * kb + s2] = 0.f;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float p0 = __builtin_amdgcn_exp2f(fmaf(x[8 * s2 + 2 * j], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(x[8 * s2 + 2 * j + 1], sc, -off));
-                u.w[j] = pack_bf16x2(p0, p1);
-                part[2 * kb + s2] += p0;            // (not the rounded ones: the sum's logarithm is an output)
-                part[2 * kb + s2] += p1;
-              }
-              pf[kb][s2] = u.v;
+            for (int j = 0; j < 4; ++j) {
+              const float p0 = __builtin_amdgcn_exp2f(fmaf(sacc[8 * s2 + 2 * j], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(sacc[8 * s2 + 2 * j + 1], sc, -off));
+              u.w[j] = pack_bf16x2(p0, p1);
+              part[s2] += p0;                       // (not the rounded ones: the sum's logarithm is an output)
+              part[s2] += p1;
             }
+            pf[s2] = u.v;
+          }
           rsum = part[0] + part[1];
-          if constexpr (NKB == 2) rsum += part[2] + part[3];
         };
         weights();
         if (__any(!(rsum <= 65536.f))) {
-          float top = sacc[0][0];
+          float top = sacc[0];
 #pragma unroll
-          for (int kb = 0; kb < NKB; ++kb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) top = fmaxf(top, sacc[kb][v]);
+          for (int v = 0; v < 16; ++v) top = fmaxf(top, sacc[v]);
           top = fmaxf(top, __shfl_xor(top, 32));
           const float next = fmaxf(mref, top), alpha = __builtin_amdgcn_exp2f((mref - next) * sc);
           mref = next;
@@ -165,13 +153,11 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
         }
         lrun += rsum;
 #pragma unroll
-        for (int kb = 0; kb < NKB; ++kb)
+        for (int s2 = 0; s2 < 2; ++s2) {
+          const char* const p = vt + 16 * s2 * ROWB;
 #pragma unroll
-          for (int s2 = 0; s2 < 2; ++s2) {
-            const char* const p = vt + (kb * 32 + 16 * s2) * ROWB;
-#pragma unroll
-            for (int db = 0; db < DB; ++db) oacc[db] = mfma32(join_tr(read_tr(p + vaddr[db][0]), read_tr(p + vaddr[db][1])), pf[kb][s2], oacc[db]);
-          }
+          for (int db = 0; db < DB; ++db) oacc[db] = mfma32(join_tr(read_tr(p + vaddr[db][0]), read_tr(p + vaddr[db][1])), pf[s2], oacc[db]);
+        }
       }
       wait_vmcnt<0>();
       lds_barrier();
