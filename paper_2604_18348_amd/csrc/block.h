@@ -129,12 +129,23 @@ __device__ __forceinline__ f32x4_t mma(float, const u32x4_t& a, const u32x4_t& b
 // acc[16 columns of X from d0][.] += X^T W over 32 rows of X in LDS (row-major, lds_piece); w0, w1: what the lane holds of W's
 // rows 4 quarter .. + 3 of either half, as a result tile leaves it.
 template <int D>
-__device__ __forceinline__ f32x4_t mma_cols(const char* lds, int d0, int lane, const bf16x8_t& w, f32x4_t acc) {
+__device__ __forceinline__ bf16x8_t read_cols(const char* lds, int d0, int lane) {
   const int r = 4 * (lane >> 4) + ((lane >> 2) & 3), u = d0 / 8 + ((lane >> 1) & 1), in = (lane & 1) * 8;
   const s16x4_tr lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_t*)(lds + lds_piece<bf16raw, D>(r, u) + in));
   const s16x4_tr hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_tr_t*)(lds + lds_piece<bf16raw, D>(r + 16, u) + in));
   union { struct { s16x4_tr lo, hi; } s; bf16x8_t v; } a{{lo, hi}};
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, w, acc, 0, 0, 0);
+  return a.v;
+}
+template <int D>
+__device__ __forceinline__ f32x4_t mma_cols(const char* lds, int d0, int lane, const bf16x8_t& w, f32x4_t acc) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(read_cols<D>(lds, d0, lane), w, acc, 0, 0, 0);
+}
+// ... with W in two parts, of which the columns of X are read once
+template <int D>
+__device__ __forceinline__ f32x4_t mma_cols(const char* lds, int d0, int lane, const bf16x8_t& w, const bf16x8_t& rest, f32x4_t acc) {
+  const bf16x8_t a = read_cols<D>(lds, d0, lane);
+  acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, rest, acc, 0, 0, 0);
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w, acc, 0, 0, 0);
 }
 template <int D>
 __device__ __forceinline__ f32x4_t mma_cols(bf16raw, const char* lds, int d0, int lane, const f32x4_t& w0, const f32x4_t& w1, f32x4_t acc) {

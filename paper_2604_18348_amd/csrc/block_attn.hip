@@ -66,8 +66,11 @@ __device__ __forceinline__ void expand(RowFrag<T, D>& f, const Raw<T, BITS, D>& 
 // LDS of its own to have their columns, and keeps a running maximum and sum (fp32).  At the end the four waves' results are
 // joined; with nsplit > 1 they are left as partial results, which block_attn_join joins.
 //
-// P is rounded to bfloat16 for the product with V in 16 bits (an error of half a step of bfloat16 of each weight, the row
-// sum is of the unrounded ones); with 4-bit values the weights are multiplied by the steps of their keys first.
+// The product with V in 16 bits wants P in bfloat16 (the row sum is of the unrounded weights).  Up to 16 rows of 16-bit keys wait for memory,
+// so there a weight enters in two parts, its rounding and the rounding of what that leaves (2^-16 of it): 64 sequences of up to 32 768
+// tokens, 2 048 keys each, d = 128 219.9 us with one part, 220.6 with two, off from 64 bits by 0.0022 and 0.0017, of which 0.0017 is the
+// rounding of O.  With more rows it is rounded (an error of half a step of bfloat16 of each weight); with 4-bit values the weights
+// are multiplied by the steps of their keys first, and then rounded: that kernel is bound by its vector arithmetic.
 template <typename T, int BITS, int D, int R>
 __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D == 128) ? 2 : 1) void block_attn(BlockAttnArgs a, int rts) {
   constexpr int NF = D * sizeof(T) / 64, ND = D / 16;
@@ -291,8 +294,19 @@ __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D =
           }
         } else if constexpr (sizeof(T) == 2) {
           union { uint32_t w[4]; bf16x8_t v; } u{{pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3])}};
+          union { uint32_t w[4]; bf16x8_t v; } rest;
+          if constexpr (R == 1) {
 #pragma unroll
-          for (int x = 0; x < ND; ++x) acc[r][x] = mma_cols<D>(vl, 16 * x, lane, u.v, acc[r][x]);
+            for (int x = 0; x < 4; ++x) {
+              const int h = x >> 1, j = 2 * (x & 1);
+              rest.w[x] = pack_bf16x2(p[h][j] - __uint_as_float(u.w[x] << 16), p[h][j + 1] - __uint_as_float(u.w[x] & 0xFFFF0000u));
+            }
+          }
+#pragma unroll
+          for (int x = 0; x < ND; ++x) {
+            if constexpr (R == 1) acc[r][x] = mma_cols<D>(vl, 16 * x, lane, u.v, rest.v, acc[r][x]);
+            else acc[r][x] = mma_cols<D>(vl, 16 * x, lane, u.v, acc[r][x]);
+          }
         } else {
 #pragma unroll
           for (int x = 0; x < ND; ++x) acc[r][x] = mma_cols<D>(T{}, vl, 16 * x, lane, p[0], p[1], acc[r][x]);
