@@ -299,12 +299,17 @@ int adacluster_quest_scores(int32_t H, int32_t Lq, int32_t Lk, int32_t d, int32_
  *   Empty rows  A query with no key of score above -inf has output 0 and lse -inf.  What lies in a page behind a sequence's last
  *               key is not looked at.  Within what a block lists, a value that is an infinity or a NaN reaches the rows it is
  *               masked for inside its own 32 keys (gradients: 64 keys by 64 rows).
+ *   Range       scale * q.k of a visible key must be finite in fp32.  Weights reach 2^16 relative to the first keys of a row before they are
+ *               scaled down, so results are finite for sure where values stay below 2^112 / n_b in magnitude (4 bits: 2^108 / n_b).
+ *   Bits        A call repeats bit for bit.  How a list is shared out, and which kernel takes a call, follow from B, Hkv, max_q,
+ *               max_pages, topk and strides, so a sequence may have other last bits in another batch.
  *   Device data is not trusted for addresses: lengths are held to max_pages * page and to the buffers, a page_table entry
  *               outside [0, num_pages) names no keys, cu_q and cu_k are held to [0, q_rows] and [0, k_rows].  Queries of a
  *               sequence past max_q are left out.  Rows of o, lse, dq (dk, dv) that belong to no sequence are left as they were.
  *   Layout      q, o, d_o, dq: row t, head h at t * stride[0] + h * stride[1] (elements), d contiguous; packed k, v, dk, dv
  *               the same; the pool: page g, token t, head h at g * stride[0] + t * stride[1] + h * stride[2] (packed keys:
- *               stride[0] is not used).  Bases and strides must be multiples of 16 bytes.  lse is fp32 [q_rows][Hq].
+ *               stride[0] is not used).  Bases and strides must be multiples of 16 bytes.  lse is fp32 [q_rows][Hq].  The rows of
+ *               an output must not overlap each other or another tensor of the call.
  *   4 bits      (bits = 4; dtype stays that of q, o and new tokens.)  codes uint8 [num_pages][Hkv][page][d/2], dimension 2j in
  *               the low half of byte j; meta [num_pages][Hkv][page][d/64] pairs of bfloat16 (step, lowest; step in the lower
  *               half of the 32 bits).  A value is lowest + code * step; 64 dimensions share a pair: lowest = their minimum
@@ -367,7 +372,8 @@ int adacluster_block_boxes(const adacluster_block_params* p, const void* k, cons
  *   S(h, p) = sum_d u_hd (u_hd >= 0 ? max_pd : min_pd)   (Eq. 1: the larger product; qblock 1: an upper bound on a page's logits),
  * and a page's score is the largest over the query heads that share the keys.  Always listed: the pages of the block's own
  * positions (causal) and the first keep_first ones; the others by score while there is room, a tie to the lower page.  If causal
- * no page behind the block's last position is listed.  Scores are formed in fp64; one that is NaN counts as -inf.
+ * no page behind the block's last position is listed.  Scores are formed in fp64 (where fp32 only bounds them first, no list
+ * depends on it); one that is NaN counts as -inf.
  * topk must hold keep_first + ceil((qblock - 1) / page) + 1 pages if causal, keep_first otherwise.
  *   sel_idx [B][nb][Hkv][topk], sel_cnt [B][nb][Hkv] out, fully overwritten (blocks that have no query: count 0).
  */

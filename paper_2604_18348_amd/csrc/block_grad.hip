@@ -3,6 +3,9 @@
 // dK and dV summed over the query heads that share the keys.  P is formed again from the scores and the row's logarithm of its sum.
 // Two kernels, so that no sum is made with atomics: one goes over a block's list of keys for dQ, one over the blocks of queries that
 // list a page for dK and dV (bit masks, set beforehand from the lists; the order of a sum is the order of the bits).
+//
+// In 16 bits P and dS are rounded to bfloat16 for their products, by half a step each: the other operands are bfloat16 too, and parts that
+// kept more would double products that the matrix cores already spend a third of the time on.  Sums, P, dP and dS themselves are fp32.
 #include "block_wide.h"
 #include "launch.h"
 
