@@ -360,6 +360,7 @@ template <int DB> __device__ __forceinline__ void store_rows(bf16raw* out, const
 }
 
 // dQ of blocks of many rows, bf16: grad_q on tiles of 64 keys that all waves share (the walk of block_attn_wide), 32 rows a wave.
+// Three waves a SIMD cost 26 spilled registers (grad_kv_wide<4> 8), most of them outside the tile loop.
 __global__ __launch_bounds__(256, 3) void grad_q_wide(BlockGradArgs a, int rts, int split) {
   constexpr int D = 64, NW = 4, NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB;

@@ -75,16 +75,18 @@ def _shares(x, p, listed):
     return max(1, min(-(-1024 // items), turns // 8))
 
 
-@pytest.mark.parametrize("dtype,bits,d", [(BF, 0, 64), (BF, 0, 128), (F, 0, 64), (BF, 4, 128), (F, 4, 64)])
-@pytest.mark.parametrize("Hq,news,qblock,topk,lens,listed", [
+FEW = [  # Hq, news, qblock, topk, lens, listed
     (1, 1024, 1, 700, [11503], True),                        # one row a workgroup, no shares
     (1, 520, 1, 1100, [18500], True),                        # two shares of 550 pages
     (32, 1024, 1, 700, [11503], True),                       # 32 rows
-    (128, 300, 1, 1, [8501], False),                         # without lists: 128 rows a block, four workgroups of 32
-])
-def test_few_rows_over_more_pages_than_are_held(Hq, news, qblock, topk, lens, listed, dtype, bits, d):
-    if Hq == 128 and (dtype, bits) == (BF, 0):
-        pytest.skip("16-bit keys go to the kernel for many rows")
+]
+WHOLE = (128, 300, 1, 1, [8501], False)                      # without lists: 128 rows a block, four workgroups of 32 (16-bit keys: of 128)
+KINDS = [(F, 0, 64), (BF, 4, 128), (F, 4, 64)]
+
+
+@pytest.mark.parametrize("dtype,bits,d,layout", [(*k, f) for k in [(BF, 0, 64), (BF, 0, 128)] + KINDS for f in FEW] + [(*k, WHOLE) for k in KINDS])
+def test_few_rows_over_more_pages_than_are_held(layout, dtype, bits, d):
+    Hq, news, qblock, topk, lens, listed = layout
     x = Batch(dtype, bits, d, 16, Hq, 1, lens, [news], 51, extra_pages=0)
     p = x.params(qblock=qblock, topk=topk)
     assert not ((dtype, bits) == (BF, 0) and _runs_wide(x, p, listed)[0])
