@@ -235,8 +235,7 @@ __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D =
                 sc[h][j] = fmaf(kp[h][j][2 * g], x[j], fmaf(kp[h][j][2 * g + 1], qsum[r][g], sc[h][j]));
             }
           } else {
-#pragma unroll
-            for (int f = 0; f < NF; ++f) sc[h] = mma(T{}, k[h].p[f], q[r].p[f], sc[h]);
+            sc[h] = dots(k[h], q[r]);
           }
           if (key0[h] + 16 > minlim) {
 #pragma unroll

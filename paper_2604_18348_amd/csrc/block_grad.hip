@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256) void grad_marks(BlockGradArgs a, long long ent
 // it); the sums of the unrounded dS correct what goes on to grad_kv.
 template <typename T, int D, int R>
 __global__ __launch_bounds__(256) void grad_q(BlockGradArgs a, int rts) {
-  constexpr int NF = D * sizeof(T) / 64, ND = D / 16;
+  constexpr int ND = D / 16;
   constexpr bool FIX = sizeof(T) == 2;
   constexpr int KBYTES = 32 * D * sizeof(T), JBYTES = (FIX ? 2 : 1) * 4 * 16 * D * 4 + 8 * 16 * 4;
   __shared__ __align__(16) char lds[4 * KBYTES > JBYTES ? 4 * KBYTES : JBYTES];
@@ -121,9 +121,7 @@ __global__ __launch_bounds__(256) void grad_q(BlockGradArgs a, int rts) {
       f32x4_t p[2], ds[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        f32x4_t sc{0.f, 0.f, 0.f, 0.f}, dp{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int f = 0; f < NF; ++f) { sc = mma(T{}, k[h].p[f], q[r].p[f], sc); dp = mma(T{}, v[h].p[f], g[r].p[f], dp); }
+        const f32x4_t sc = dots(k[h], q[r]), dp = dots(v[h], g[r]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const bool sees = key0[h] + 4 * quarter + j < lim[r];
@@ -196,7 +194,7 @@ __device__ __forceinline__ Share page_share(const BlockGradArgs& a, const uint32
 // and four rows: P and dS are the operands of dV^T = dO^T P and dK^T = Q^T dS as they stand.
 template <typename T, int D, int KR>
 __global__ __launch_bounds__(256) void grad_kv(BlockGradArgs a) {
-  constexpr int NF = D * sizeof(T) / 64, ND = D / 16;
+  constexpr int ND = D / 16;
   constexpr int TBYTES = 32 * D * sizeof(T), JBYTES = 4 * 16 * D * 4;
   __shared__ __align__(16) char lds[8 * TBYTES > JBYTES ? 8 * TBYTES : JBYTES];
   const BlockDims& m = a.m;
@@ -266,9 +264,7 @@ __global__ __launch_bounds__(256) void grad_kv(BlockGradArgs a) {
           f32x4_t p[2], ds[2];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            f32x4_t sc{0.f, 0.f, 0.f, 0.f}, dp{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int f = 0; f < NF; ++f) { sc = mma(T{}, q[h].p[f], k[r].p[f], sc); dp = mma(T{}, g[h].p[f], v[r].p[f], dp); }
+            const f32x4_t sc = dots(q[h], k[r]), dp = dots(g[h], v[r]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const bool sees = key0 + 16 * r + n16 < lim[h][j];
@@ -360,7 +356,7 @@ template <int DB> __device__ __forceinline__ void store_rows(bf16raw* out, const
 }
 
 // dQ of blocks of many rows, bf16: grad_q on tiles of 64 keys that all waves share (the walk of block_attn_wide), 32 rows a wave.
-// Three waves a SIMD cost 26 spilled registers (grad_kv_wide<4> 8), most of them outside the tile loop.
+// Three waves a SIMD cost 26 spilled registers (grad_kv_wide<4> 8), none of them reloaded between products.
 __global__ __launch_bounds__(256, 3) void grad_q_wide(BlockGradArgs a, int rts, int split) {
   constexpr int D = 64, NW = 4, NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int PT = TILE * CH / NT, TILEB = TILE * ROWB;

@@ -1,5 +1,5 @@
 """Attention of up to 16 rows a block over 16-bit keys: the weights lose nothing in the product with the values, so that the output is
-off by its own rounding to bfloat16 and by what products in 32 bits and weights of 16 bits of fraction leave."""
+off by its own rounding to bfloat16 and by what products in 32 bits and weights of 16 bits of fraction leave.  Scores in fp32."""
 import math
 
 import pytest
@@ -35,3 +35,20 @@ def test_outputs_are_off_by_their_own_rounding(d, page, Hq, Hkv, lens, news, qbl
         at = slice(int(x.cu_q[b]), int(x.cu_q[b + 1]))
         _within(o[at], r["o"], r["o_tol"] + 1.01 * (2.0 ** -16 * weighed + ref.half(BF) * r["o"].abs()), "o of sequence %d" % b)
         _within(lse[at], r["lse"], r["lse_tol"], "lse of sequence %d" % b)
+
+
+@pytest.mark.parametrize("Hq,nq", [(1, 1), (4, 30)])
+def test_scores_in_fp32_are_two_sums(Hq, nq):
+    """One key, so lse is the score: 1 and 127 terms of 1.5 2^-27, each of them (and four together) below half a step of 1.  One chain of sums
+    leaves 1; of two chains one keeps its 64 terms, 96 * 2^-27 = 7.2e-7.  The logarithm's two roundings take 2.4e-7 of it at most."""
+    d = 128
+    p = B.BlockParams(B=1, Hq=Hq, Hkv=1, d=d, dtype=B.F32, page=16, max_pages=1, max_q=nq, causal=0, softmax_scale=1.0)
+    q = torch.ones((nq, Hq, d), device="cuda")
+    cu_q, cu_k = (torch.tensor([0, n], dtype=torch.int32, device="cuda") for n in (nq, 1))
+    got = []
+    for rest in (0.0, 1.5 * 2.0 ** -27):
+        k = torch.full((1, 1, d), rest, device="cuda")
+        k[..., 0] = 1
+        got.append(B.adacluster_block_attn(p, q, cu_q, k=k, v=k, cu_k=cu_k)[1].double())
+    assert bool(((got[0] - 1).abs() <= 2.0 ** -22).all())
+    assert bool((got[1] - got[0] >= 96 * 2.0 ** -27 - 2.4e-7).all()), (got[1] - got[0]).min()
