@@ -263,7 +263,8 @@ def _run_own(s):
     case, kind = s["case"], s["case"]["kind"]
     if "p" not in s:                                                     # what a program makes once for its cache
         s["p"] = A.BlockParams(B=case["B"], Hq=case["Hq"], Hkv=case["Hkv"], d=case["d"], dtype=A.BF16 if case["dtype"] == "bf16" else A.F32,
-                               bits=case["bits"], page=case["page"], max_pages=s["table"].shape[1], max_q=case["new"], keep_first=case["first"])
+                               bits=case["bits"], page=case["page"], max_pages=s["table"].shape[1], max_q=max(case["new"], case["keep"]),
+                               keep_first=case["first"])
         s["cache"] = A.BlockCache(k=s["kc"], v=s["vc"], k_meta=s["km"], v_meta=s["vm"], boxes=s["boxes"])
     p, cache = s["p"], s["cache"]
     if kind == "prefix":
