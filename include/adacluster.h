@@ -397,6 +397,52 @@ int adacluster_block_attn_backward(const adacluster_block_params* p, const void*
                                    const int32_t* sel_idx, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Attention over a paged cache for groups of sequences that share their first positions (one system prompt, samples of one prompt,
+ * drafts): adacluster_block_attn over all pages, with the keys that a group shares read once for all its rows.
+ *   cu_group [groups+1]: group g holds the sequences cu_group[g] .. cu_group[g+1]-1 (ascending; sequences outside are on their own).
+ *   prefix_lens [groups]: positions that they share.  Those in whole pages, as far as the group's first sequence has keys, are read
+ *     from the pages that the FIRST sequence's row of page_table names, for all of them; what the other rows name there is not looked
+ *     at.  Positions behind them are every sequence's own.
+ * Everything else is as in adacluster_block_attn (a query sees positions up to its own if causal; empty rows, range, layout), in the
+ * same workspace rules: adacluster_prefix_workspace_bytes.  topk, qblock and keep_first are not used.  lse may be NULL.
+ * q_rows * Hq / Hkv must be below 2^31.  cu_group that does not ascend: results are unspecified, no access is out of bounds.
+ */
+int adacluster_prefix_workspace_bytes(const adacluster_block_params* p, int32_t groups, size_t* bytes /* host */);
+int adacluster_prefix_attn(const adacluster_block_params* p, int32_t groups, const void* q, const int32_t* cu_q,
+                           const void* k_pool, const void* v_pool, const uint32_t* k_meta, const uint32_t* v_meta,
+                           const int32_t* seq_lens, const int32_t* page_table, const int32_t* cu_group, const int32_t* prefix_lens,
+                           void* o, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The weight that cached keys get from attention.  For position j of sequence b and head g of keys
+ *   new_weights[b][g][j] = decay weights[b][g][j] + sum over the queries t that see j and the query heads h of g of exp(scale q_th . k_j - lse_th)
+ * with lse [q_rows][Hq] of attention over the same queries and ALL keys (adacluster_block_attn without lists, adacluster_prefix_attn);
+ * rows whose lse is -inf add nothing.  0 from the sequence's last key on.  decay in [0,1]; 0, or weights NULL: what was there is not
+ * read.  Both [B][Hkv][max_pages * page] fp32; new_weights may be weights.  Sums are fp32 in a fixed order.
+ * Queries, positions and pages are those of adacluster_block_attn over a paged cache (a page that is not named: no weight).
+ */
+int adacluster_cache_weights(const adacluster_block_params* p, const void* q, const int32_t* cu_q, const float* lse,
+                             const void* k_pool, const uint32_t* k_meta, const int32_t* seq_lens, const int32_t* page_table,
+                             const float* weights, float decay, float* new_weights, void* stream);
+
+/*
+ * The tokens that sequences keep.  A sequence of n > keep tokens keeps, for every head of keys by itself, its first keep_first pages, its
+ * last `recent` tokens, and of the others those of the largest weights, `keep` tokens in all (a tie: the lower position; a NaN weighs
+ * less than any number); one of n <= keep keeps all.  They become its positions 0 .. in their order, in the pages that new_table
+ * [B][max_pages] names: keys and values (codes) as they are, weights along with them, and the boxes of those pages anew, over what
+ * the tokens are read as (adacluster_cache_read).  keep >= keep_first * page + recent.
+ *   kept [B][Hkv][keep] out: the positions that stay, ascending, -1 behind the end.  new_lens [B] out: min(n, keep).
+ *   weights [B][Hkv][max_pages * page] in; new_weights the same shape out (another tensor), fully overwritten, 0 behind the end.
+ * A page of new_table must belong to one sequence of the call and must not be one that page_table names, but for a page whose tokens all
+ * stay in their place (keep_first; a sequence that keeps everything): its entry may name the page itself, which is then left as
+ * it is, and may be shared.  Tokens whose page new_table does not name are dropped; a token of a page that page_table does not name is zero.
+ * Slots of the new pages behind the end are left as they were.  The old pages are the caller's to give away.
+ */
+int adacluster_cache_evict(const adacluster_block_params* p, const int32_t* seq_lens, const int32_t* page_table, const float* weights,
+                           int32_t keep, int32_t recent, const int32_t* new_table, int32_t* kept, int32_t* new_lens, float* new_weights,
+                           void* k_pool, void* v_pool, uint32_t* k_meta, uint32_t* v_meta, void* boxes, void* stream);
+
+/*
  * Stage timing for benchmarks.  adacluster_profile_enable(1) creates HIP events; while enabled,
  * adacluster_attn, adacluster_sparse_attn and adacluster_dense_attn record them on the call's
  * stream at their stage boundaries (adacluster_qcluster and adacluster_kcluster record their own).

@@ -168,11 +168,16 @@ def load_library():
     lib.adacluster_block_select.argtypes = [BP] + [vp] * 9 + [sz, vp]
     lib.adacluster_block_attn.argtypes = [BP] + [vp] * 13 + [sz, vp]
     lib.adacluster_block_attn_backward.argtypes = [BP] + [vp] * 13 + [sz, vp]
+    lib.adacluster_prefix_workspace_bytes.argtypes = [BP, ctypes.c_int32, ctypes.POINTER(sz)]
+    lib.adacluster_prefix_attn.argtypes = [BP, ctypes.c_int32] + [vp] * 13 + [sz, vp]
+    lib.adacluster_cache_weights.argtypes = [BP] + [vp] * 8 + [ctypes.c_float, vp, vp]
+    lib.adacluster_cache_evict.argtypes = [BP] + [vp] * 3 + [ctypes.c_int32] * 2 + [vp] * 10
     lib.adacluster_profile_enable.argtypes = [ctypes.c_int]
     lib.adacluster_profile_read.argtypes = [ctypes.POINTER(ctypes.c_float)]
     for n in ("profile_enable", "profile_read", "centroid_capacity", "workspace_bytes", "last_error", "qcluster", "kcluster", "select",
               "sparse_attn", "attn", "dense_attn", "compactness", "compactness_noalloc", "quest_scores", "stats_fetch", "mfma_probe",
-              "block_workspace_bytes", "cache_append", "cache_read", "block_boxes", "block_select", "block_attn", "block_attn_backward"):
+              "block_workspace_bytes", "cache_append", "cache_read", "block_boxes", "block_select", "block_attn", "block_attn_backward",
+              "prefix_workspace_bytes", "prefix_attn", "cache_weights", "cache_evict"):
         getattr(lib, "adacluster_" + n).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -184,6 +189,7 @@ EXPORTED = ["adacluster_centroid_capacity", "adacluster_workspace_bytes", "adacl
             "adacluster_compactness_noalloc", "adacluster_quest_scores", "adacluster_stats_fetch", "adacluster_mfma_probe",
             "adacluster_block_workspace_bytes", "adacluster_cache_append", "adacluster_cache_read", "adacluster_block_boxes",
             "adacluster_block_select", "adacluster_block_attn", "adacluster_block_attn_backward",
+            "adacluster_prefix_workspace_bytes", "adacluster_prefix_attn", "adacluster_cache_weights", "adacluster_cache_evict",
             "adacluster_profile_enable", "adacluster_profile_read"]
 
 STAGES = ["qcluster", "kcluster", "select", "permute", "plan", "attention", "kreduce"]
@@ -735,3 +741,106 @@ def adacluster_block_attn_backward(p: BlockParams, q, k, v, o, lse, d_o, cu_q, c
     _on(dev, "adacluster_block_attn_backward", cp, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), d_o.data_ptr(),
         cu_q.data_ptr(), cu_k.data_ptr(), _ptr(sel_idx), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), _ptr(ws), size)
     return grads
+
+
+# ---- a cache whose sequences share prefixes and drop tokens ---------------------------------------------------------------
+
+
+@functools.lru_cache(maxsize=1024)
+def _prefix_bytes(cp: bytes, groups):
+    n = ctypes.c_size_t(0)
+    _check(load_library().adacluster_prefix_workspace_bytes(cp, groups, ctypes.byref(n)), "prefix_workspace_bytes")
+    return n.value
+
+
+def adacluster_prefix_workspace_bytes(p: BlockParams, groups, q_rows, num_pages) -> int:
+    if not q_rows:                                      # a step without queries
+        return 0
+    return _prefix_bytes(_block_c(p, q_rows, 0, num_pages), groups)
+
+
+def adacluster_prefix_attn(p: BlockParams, q, cu_q, cache: BlockCache, seq_lens, page_table, cu_group, prefix_lens, out=None, lse=None, ws=None):
+    """adacluster_block_attn of q [rows,Hq,d] over all pages of a cache, for groups of sequences that share their first prefix_lens[g]
+    positions: sequences cu_group[g] .. cu_group[g+1]-1, whose shared pages (the first one's) are read once -> o like q, lse float32
+    [rows,Hq].  Rows that belong to no sequence are not written: without `out` and `lse` they hold anything.  Nothing is
+    recorded for autograd."""
+    dev, dt = _gpu(q), _tdtype(p)
+    rows, groups = q.shape[0], prefix_lens.shape[0]
+    _ints("cu_q", cu_q, (p.B + 1,), dev)
+    _ints("cu_group", cu_group, (groups + 1,), dev)
+    _ints("prefix_lens", prefix_lens, (groups,), dev)
+    _keys_of(p, None, seq_lens, page_table, dev, True)
+    n, ks, vs = _pool(p, cache, dev, False)
+    o = torch.empty_like(q) if out is None else out
+    if lse is None:
+        lse = torch.empty((rows, p.Hq), dtype=torch.float32, device=dev)
+    else:
+        _lse(lse, rows, p, dev)
+    if o.shape[0] != rows:
+        raise ValueError("out must have the rows of q")
+    cp = _block_c(p, rows, 0, n, q=_rows("q", q, dt, p.Hq, p.d, dev), o=_rows("out", o, dt, p.Hq, p.d, dev), k=ks, v=vs)
+    if not rows:
+        return o, lse
+    if ws is None:
+        size = _prefix_bytes(cp, groups)
+        ws = torch.empty(size, dtype=torch.uint8, device=dev)
+    else:
+        ws, size = _block_ws(cp, None, dev, ws)
+    _on(dev, "adacluster_prefix_attn", cp, groups, q.data_ptr(), cu_q.data_ptr(), cache.k.data_ptr(), cache.v.data_ptr(), _ptr(cache.k_meta),
+        _ptr(cache.v_meta), seq_lens.data_ptr(), page_table.data_ptr(), cu_group.data_ptr(), prefix_lens.data_ptr(), o.data_ptr(), lse.data_ptr(),
+        _ptr(ws), size)
+    return o, lse
+
+
+def _weights(name, t, p, dev):
+    shape = (p.B, p.Hkv, p.max_pages * p.page)
+    if t.shape != shape or t.dtype != torch.float32 or not t.is_contiguous() or t.device != dev:
+        raise ValueError(f"{name} must be a contiguous float32 tensor {shape} on {dev}")
+
+
+def adacluster_cache_weights(p: BlockParams, q, cu_q, lse, cache: BlockCache, seq_lens, page_table, weights=None, decay=1.0, out=None):
+    """decay * weights + what every cached key gets from the queries q [rows,Hq,d] whose attention over all keys left lse [rows,Hq], summed
+    over queries and the heads that share the key -> float32 [B,Hkv,max_pages*page], 0 from a sequence's last key on.  weights None: from
+    nothing.  out: may be weights."""
+    dev, dt = _gpu(q), _tdtype(p)
+    rows = q.shape[0]
+    _ints("cu_q", cu_q, (p.B + 1,), dev)
+    _keys_of(p, None, seq_lens, page_table, dev, True)
+    _lse(lse, rows, p, dev)
+    n, ks, _ = _pool(p, cache, dev, False)
+    if weights is not None:
+        _weights("weights", weights, p, dev)
+    if out is None:
+        out = torch.empty((p.B, p.Hkv, p.max_pages * p.page), dtype=torch.float32, device=dev)
+    else:
+        _weights("out", out, p, dev)
+    strides = _rows("q", q, dt, p.Hq, p.d, dev)
+    if not rows:                                        # a step without queries: what was there, decayed
+        q, lse, strides, rows, cu_q = _row_of_none(p.Hq, p.d, dt, dev), torch.zeros((1, p.Hq), device=dev), _NO2, 1, torch.zeros_like(cu_q)
+    _on(dev, "adacluster_cache_weights", _block_c(p, rows, 0, n, q=strides, k=ks), q.data_ptr(), cu_q.data_ptr(), lse.data_ptr(), cache.k.data_ptr(),
+        _ptr(cache.k_meta), seq_lens.data_ptr(), page_table.data_ptr(), _ptr(weights), decay, out.data_ptr())
+    return out
+
+
+def adacluster_cache_evict(p: BlockParams, cache: BlockCache, seq_lens, page_table, weights, keep, recent, new_table, out=None):
+    """Moves the `keep` tokens of every sequence and head that stay (its first keep_first pages, its last `recent` tokens, the others by
+    weight) to the pages of new_table -> kept int32 [B,Hkv,keep] (-1 behind the end), new lengths int32 [B], new weights like weights (out:
+    where to).  A page of new_table may be one of page_table only where all its tokens stay in their place."""
+    dev = _gpu(cache.k)
+    _keys_of(p, None, seq_lens, page_table, dev, True)
+    _ints("new_table", new_table, (p.B, p.max_pages), dev)
+    _weights("weights", weights, p, dev)
+    n, ks, vs = _pool(p, cache, dev, True)
+    if out is None:
+        out = torch.empty_like(weights)
+    else:
+        _weights("out", out, p, dev)
+    keep, recent = operator.index(keep), operator.index(recent)
+    if keep < 1:
+        raise ValueError("keep must be at least 1")
+    kept = torch.empty((p.B, p.Hkv, keep), dtype=torch.int32, device=dev)
+    lens = torch.empty((p.B,), dtype=torch.int32, device=dev)
+    _on(dev, "adacluster_cache_evict", _block_c(p, 1, 0, n, k=ks, v=vs), seq_lens.data_ptr(), page_table.data_ptr(), weights.data_ptr(), keep, recent,
+        new_table.data_ptr(), kept.data_ptr(), lens.data_ptr(), out.data_ptr(), cache.k.data_ptr(), cache.v.data_ptr(), _ptr(cache.k_meta),
+        _ptr(cache.v_meta), cache.boxes.data_ptr())
+    return kept, lens, out

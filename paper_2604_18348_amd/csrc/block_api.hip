@@ -113,6 +113,18 @@ BlockDims unlisted(BlockDims m) {
 double scale_of(const adacluster_block_params* p) { return p->softmax_scale > 0.f ? p->softmax_scale : 1.0 / sqrt((double)p->d); }
 float log2_scale(const adacluster_block_params* p) { return (float)(scale_of(p) * 1.4426950408889634); }      // (rounded once: logits of 20 feel it)
 
+// what the shape of a call of prefix_attn follows from
+int prefix_args(const adacluster_block_params* p, int32_t groups, BlockAttnArgs* a) {
+  if (int rc = check(p, &a->m)) return rc;
+  if (!p->num_pages) return fail(ADACLUSTER_E_BADARG, "prefix_attn: num_pages must be >= 1 (a paged cache)");
+  if (groups < 0 || groups > p->B) return fail(ADACLUSTER_E_BADSHAPE, "groups must be in [0,B] (groups=%d)", groups);
+  if ((long long)p->q_rows * a->m.G > INT32_MAX) return fail(ADACLUSTER_E_UNSUPPORTED, "prefix_attn: q_rows * Hq / Hkv must be below 2^31");
+  a->m = unlisted(a->m);
+  a->gr.groups = groups;
+  a->qs = two(p->q_stride); a->os = two(p->o_stride); a->ks = three(a->m, p->k_stride); a->vs = three(a->m, p->v_stride);
+  return 0;
+}
+
 }  // namespace
 
 extern "C" {
@@ -233,6 +245,71 @@ int adacluster_block_attn_backward(const adacluster_block_params* p, const void*
   a.scale = (float)scale_of(p);
   a.scale_log2e = log2_scale(p);
   return done(launch_block_attn_backward((hipStream_t)stream, p->dtype, p->d, a, ws));
+}
+
+int adacluster_prefix_workspace_bytes(const adacluster_block_params* p, int32_t groups, size_t* bytes) {
+  BlockAttnArgs a{};
+  if (int rc = prefix_args(p, groups, &a)) return rc;
+  if (!bytes) return fail(ADACLUSTER_E_BADARG, "bytes is NULL");
+  *bytes = prefix_attn_bytes(p->dtype, p->bits, p->d, a);
+  return 0;
+}
+
+int adacluster_prefix_attn(const adacluster_block_params* p, int32_t groups, const void* q, const int32_t* cu_q, const void* k_pool, const void* v_pool,
+                           const uint32_t* k_meta, const uint32_t* v_meta, const int32_t* seq_lens, const int32_t* page_table, const int32_t* cu_group,
+                           const int32_t* prefix_lens, void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
+  BlockAttnArgs a{};
+  if (int rc = prefix_args(p, groups, &a)) return rc;
+  if (!cu_q || (groups && (!cu_group || !prefix_lens))) return fail(ADACLUSTER_E_BADARG, "prefix_attn: NULL tensor pointer");
+  if (int rc = check_keys(&a.m, nullptr, seq_lens, page_table)) return rc;
+  a.m.cu_q = cu_q;
+  if (int rc = check_rows("q", q, p->dtype, a.qs)) return rc;
+  if (int rc = check_rows("o", o, p->dtype, a.os)) return rc;
+  if (int rc = check_pool(p, k_pool, v_pool, k_meta, v_meta, a.ks, a.vs)) return rc;
+  if (int rc = check_ws(ws, ws_bytes, prefix_attn_bytes(p->dtype, p->bits, p->d, a))) return rc;
+  a.q = q; a.k = k_pool; a.v = v_pool; a.km = k_meta; a.vm = v_meta; a.o = o; a.lse = lse;
+  a.gr.cu_group = cu_group; a.gr.prefix = prefix_lens;
+  a.scale_log2e = log2_scale(p);
+  return done(launch_prefix_attn((hipStream_t)stream, p->dtype, p->bits, p->d, a, ws));
+}
+
+int adacluster_cache_weights(const adacluster_block_params* p, const void* q, const int32_t* cu_q, const float* lse, const void* k_pool,
+                             const uint32_t* k_meta, const int32_t* seq_lens, const int32_t* page_table, const float* weights, float decay,
+                             float* new_weights, void* stream) {
+  WeightsArgs a{};
+  if (int rc = check(p, &a.m)) return rc;
+  if (!p->num_pages) return fail(ADACLUSTER_E_BADARG, "cache_weights: num_pages must be >= 1");
+  if (!(decay >= 0.f && decay <= 1.f)) return fail(ADACLUSTER_E_BADARG, "cache_weights: decay must be in [0,1]");
+  if (!cu_q || !lse || !new_weights) return fail(ADACLUSTER_E_BADARG, "cache_weights: NULL tensor pointer");
+  if (!aligned(weights, 16) || !aligned(new_weights, 16)) return fail(ADACLUSTER_E_BADARG, "cache_weights: weights must start at multiples of 16 bytes");
+  if (int rc = check_keys(&a.m, nullptr, seq_lens, page_table)) return rc;
+  a.m.cu_q = cu_q;
+  a.qs = two(p->q_stride); a.ks = three(a.m, p->k_stride);
+  if (int rc = check_rows("q", q, p->dtype, a.qs)) return rc;
+  if (int rc = check_pool(p, k_pool, k_pool, k_meta, k_meta, a.ks, a.ks)) return rc;
+  a.q = q; a.k = k_pool; a.km = k_meta; a.lse = lse; a.w = decay == 0.f ? nullptr : weights; a.out = new_weights;
+  a.scale_log2e = log2_scale(p); a.decay = decay;
+  return done(launch_cache_weights((hipStream_t)stream, p->dtype, p->bits, p->d, a));
+}
+
+int adacluster_cache_evict(const adacluster_block_params* p, const int32_t* seq_lens, const int32_t* page_table, const float* weights, int32_t keep,
+                           int32_t recent, const int32_t* new_table, int32_t* kept, int32_t* new_lens, float* new_weights, void* k_pool, void* v_pool,
+                           uint32_t* k_meta, uint32_t* v_meta, void* boxes, void* stream) {
+  EvictArgs a{};
+  if (int rc = check(p, &a.m)) return rc;
+  if (!p->num_pages) return fail(ADACLUSTER_E_BADARG, "cache_evict: num_pages must be >= 1");
+  if (keep < 1 || keep > (1 << 29) || recent < 0) return fail(ADACLUSTER_E_BADARG, "cache_evict: keep must be in [1,2^29] and recent >= 0 (keep=%d recent=%d)", keep, recent);
+  if ((long long)p->keep_first * p->page + recent > keep)
+    return fail(ADACLUSTER_E_BADARG, "cache_evict: keep must hold the first pages and the last tokens: %d * %d + %d > %d", p->keep_first, p->page, recent, keep);
+  if (!weights || !new_table || !kept || !new_lens || !new_weights || !boxes) return fail(ADACLUSTER_E_BADARG, "cache_evict: NULL tensor pointer");
+  if (!aligned(weights, 16)) return fail(ADACLUSTER_E_BADARG, "cache_evict: weights must start at a multiple of 16 bytes");
+  if (weights == new_weights) return fail(ADACLUSTER_E_BADARG, "cache_evict: new_weights must not be weights");
+  if (int rc = check_keys(&a.m, nullptr, seq_lens, page_table)) return rc;
+  a.ks = three(a.m, p->k_stride); a.vs = three(a.m, p->v_stride);
+  if (int rc = check_pool(p, k_pool, v_pool, k_meta, v_meta, a.ks, a.vs)) return rc;
+  a.w = weights; a.new_table = new_table; a.keep = keep; a.recent = recent; a.kept = kept; a.new_lens = new_lens; a.new_w = new_weights;
+  a.kp = k_pool; a.vp = v_pool; a.km = k_meta; a.vm = v_meta; a.boxes = boxes;
+  return done(launch_cache_evict((hipStream_t)stream, p->dtype, p->bits, p->d, a));
 }
 
 }  // extern "C"

@@ -72,7 +72,7 @@ __device__ __forceinline__ void expand(RowFrag<T, D>& f, const Raw<T, BITS, D>& 
 // rounding of O.  With more rows it is rounded (an error of half a step of bfloat16 of each weight); with 4-bit values the weights
 // are multiplied by the steps of their keys first, and then rounded (in two parts 32 sequences over whole caches of up to 16 384 tokens
 // 132.7 -> 140.7 us, for values that are off by half a step of 4 bits as it is).
-template <typename T, int BITS, int D, int R>
+template <typename T, int BITS, int D, int R, Rows ROWS = Rows::OWN>
 __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D == 128) ? 2 : 1) void block_attn(BlockAttnArgs a, int rts) {
   constexpr int NF = D * sizeof(T) / 64, ND = D / 16;
   constexpr bool CODES = BITS == 4 && sizeof(T) == 2;           // codes enter the products, steps behind them
@@ -87,23 +87,53 @@ __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D =
   int id = blockIdx.x;
   const int split = id % a.nsplit; id /= a.nsplit;
   const int item = id;
-  const int rt = id % rts; id /= rts;
-  const int i = id % m.nb; id /= m.nb;
-  const int hk = id % m.Hkv, b = id / m.Hkv;
-  const BlockSeq s = block_seq(m, b);
-  const int t0 = i * m.qblock, rows = min(m.qblock, s.nq - t0) * m.G, base_row = rt * R * 16;
-  if (t0 >= s.nq || base_row >= rows) return;
+  int hk, b, i = 0, t0 = 0, rows, base_row, from = 0, every = a.nsplit;      // from: the first page of the list; every: workgroups that share it
+  BlockSeq s;
+  Group group;
+  if constexpr (ROWS == Rows::GROUP) {
+    hk = id % m.Hkv; id /= m.Hkv;
+    const int g = last_group(a.gr.groups, [&](int x) { return first_tile(m, group_at(m, a.gr, x).q0, x, R * 16) <= id; });
+    if (g < 0) return;
+    group = group_at(m, a.gr, g);
+    b = group.b0;
+    base_row = (id - first_tile(m, group.q0, g, R * 16)) * R * 16;
+    rows = (group.q1 - group.q0) * m.G;
+    s = BlockSeq{group.q0, group.q1 - group.q0, 0, group.pages << m.lpage, 0};
+    every = splits_of(m, group.pages, a.nsplit);
+    if (base_row < 0 || base_row >= rows || split >= every) return;      // (below 0: groups that do not ascend)
+  } else {
+    const int rt = id % rts; id /= rts;
+    i = id % m.nb; id /= m.nb;
+    hk = id % m.Hkv; b = id / m.Hkv;
+    s = block_seq(m, b);
+    t0 = i * m.qblock; rows = min(m.qblock, s.nq - t0) * m.G; base_row = rt * R * 16;
+    if (t0 >= s.nq || base_row >= rows) return;
+    if constexpr (ROWS == Rows::TAIL) {
+      const int g = group_of(a.gr, b);
+      if (g >= 0) from = group_at(m, a.gr, g).pages;
+      every = splits_of(m, ((s.n + m.page - 1) >> m.lpage) - from, a.nsplit);
+      if (split >= every) return;
+    }
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n16 = lane & 15, quarter = lane >> 4;
 
   // queries: operand pieces, and the keys below `lim` that a row sees
   RowFrag<T, D> q[R];
   int lim[R];
   float qsum[R][NG];
+  int group_min = INT32_MAX;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int row = base_row + r * 16 + n16, t = t0 + row / m.G;
-    const bool there = row < rows;
-    lim[r] = there ? (m.causal ? min(s.n, s.first + t + 1) : s.n) : INT32_MAX;      // (a row that is not there needs no mask)
+    bool there = row < rows;
+    if constexpr (ROWS == Rows::GROUP) {
+      const int l = there ? row_limit(m, group, s.q0 + t) : -1;
+      there = l >= 0;
+      lim[r] = there ? l : INT32_MAX;
+      group_min = min(group_min, lim[r]);
+    } else {
+      lim[r] = there ? (m.causal ? min(s.n, s.first + t + 1) : s.n) : INT32_MAX;      // (a row that is not there needs no mask)
+    }
     const T* const p = (const T*)a.q + (long long)(s.q0 + t) * a.qs.token + (long long)(hk * m.G + row % m.G) * a.qs.head;
 #pragma unroll
     for (int f = 0; f < NF; ++f) q[r].p[f] = there ? *(const u32x4_t*)(p + piece_at<T, BITS>(f, quarter) * Vec<T>::N) : u32x4_t{0, 0, 0, 0};
@@ -124,10 +154,15 @@ __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D =
     }
   }
   const int last = min(base_row + R * 16, rows) - 1;
-  const int maxlim = m.causal ? min(s.n, s.first + t0 + last / m.G + 1) : s.n;      // (no row sees further)
-  const int minlim = m.causal ? min(s.n, s.first + t0 + base_row / m.G + 1) : s.n;      // keys below: seen by all rows
+  int maxlim = m.causal ? min(s.n, s.first + t0 + last / m.G + 1) : s.n;      // (no row sees further)
+  int minlim = m.causal ? min(s.n, s.first + t0 + base_row / m.G + 1) : s.n;      // keys below: seen by all rows
+  if constexpr (ROWS == Rows::GROUP) {
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) group_min = min(group_min, __shfl_xor(group_min, x));
+    maxlim = s.n; minlim = uniform(group_min);
+  }
   const int pages = maxlim > 0 ? (maxlim + m.page - 1) >> m.lpage : 0;
-  const int32_t* const list = a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
+  const int32_t* const list = ROWS == Rows::OWN && a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
   const int lsub = m.lpage - 4, entries = list ? m.topk : pages;
 
   // The weights are taken relative to a reference that moves only when a turn's sum leaves its range (see below); from where it
@@ -151,8 +186,8 @@ __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D =
     Raw<T, BITS, D> k[2], v[2];
     uint32_t pk[2][MW], pv[2][MW];                    // 4 bits: (step, lowest) of the lane's row
   };
-  for (int e0 = split; e0 < entries; e0 += a.nsplit * LIST) {
-    const int halves = fill_list<256>(m, b, list, e0, a.nsplit, entries, pages, pages_l, counts) << lsub, turns = (halves + 1) >> 1;
+  for (int e0 = from + split; e0 < entries; e0 += every * LIST) {
+    const int halves = fill_list<256>(m, b, list, e0, every, entries, pages, pages_l, counts) << lsub, turns = (halves + 1) >> 1;
     auto fetch = [&](Fetch& f, int turn) __attribute__((always_inline)) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -352,7 +387,7 @@ __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D =
       for (int x = 0; x < D / 16; ++x) o[x] = fmaf(f, jo[(w * 16 + jr) * D + d0 + x], o[x]);
     }
     if (row >= rows) continue;
-    if (a.nsplit > 1) {
+    if (ROWS != Rows::OWN || a.nsplit > 1) {
       const long long rec = ((long long)item * a.nsplit + split) * (16 * R) + r * 16 + jr;
 #pragma unroll
       for (int x = 0; x < D / 16; x += 4) *(f32x4_t*)(a.part_o + rec * D + d0 + x) = f32x4_t{o[x], o[x + 1], o[x + 2], o[x + 3]};
@@ -441,7 +476,29 @@ void go(hipStream_t s, const BlockAttnArgs& a, const Shape& sh) {
   if (sh.nsplit > 1) block_attn_join<T, D><<<(int)(sh.items * sh.R), 256, 0, s>>>(a, sh.rts, sh.R);
 }
 
+template <typename T, int BITS, int D>
+void part(hipStream_t s, Rows rows, int R, int rts, int wg, const BlockAttnArgs& a) {
+  if (rows == Rows::GROUP) {
+    if (R == 1) block_attn<T, BITS, D, 1, Rows::GROUP><<<wg, 256, 0, s>>>(a, rts);
+    else block_attn<T, BITS, D, 2, Rows::GROUP><<<wg, 256, 0, s>>>(a, rts);
+  } else {
+    if (R == 1) block_attn<T, BITS, D, 1, Rows::TAIL><<<wg, 256, 0, s>>>(a, rts);
+    else block_attn<T, BITS, D, 2, Rows::TAIL><<<wg, 256, 0, s>>>(a, rts);
+  }
+}
+
 }  // namespace
+
+void launch_block_attn_part(hipStream_t s, int dtype, int bits, int d, Rows rows, int R, int rts, long long items, const BlockAttnArgs& a) {
+  const int wg = (int)(items * a.nsplit);
+  if (dtype == ADACLUSTER_BF16) {
+    if (bits == 4) { if (d == 64) part<bf16raw, 4, 64>(s, rows, R, rts, wg, a); else part<bf16raw, 4, 128>(s, rows, R, rts, wg, a); }
+    else { if (d == 64) part<bf16raw, 0, 64>(s, rows, R, rts, wg, a); else part<bf16raw, 0, 128>(s, rows, R, rts, wg, a); }
+  } else {
+    if (bits == 4) { if (d == 64) part<float, 4, 64>(s, rows, R, rts, wg, a); else part<float, 4, 128>(s, rows, R, rts, wg, a); }
+    else { if (d == 64) part<float, 0, 64>(s, rows, R, rts, wg, a); else part<float, 0, 128>(s, rows, R, rts, wg, a); }
+  }
+}
 
 size_t block_attn_bytes(const BlockDims& m, int d, bool listed) {
   const Shape s = shape_of(m, listed);

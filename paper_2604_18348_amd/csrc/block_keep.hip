@@ -1,0 +1,362 @@
+// What a sequence keeps of its cache: the weight that every cached key gets from attention, the tokens chosen by it, and their move to
+// other pages.
+#include "block.h"
+
+namespace adac {
+
+namespace {
+
+// ---- weights of keys --------------------------------------------------------------------------------------------------------
+//
+// w_j = decay w_j + sum over the rows r that see key j of 2^(scale log2(e) q_r . k_j - log2(e) lse_r): lse is the logarithm of the row's sum, so
+// no maximum runs along.  A workgroup owns 128 keys of one head of a sequence, 32 a wave, whose operands stay in registers while the
+// rows go by, 16 at a time: no two workgroups add to a weight, and a call repeats bit for bit.
+//
+// 4 bits, bf16: a code c enters as the bfloat16 16 + c (0x4180 | c << 3: exact), which leaves the dimensions of a word of eight in the
+// order of code_order; the accumulator starts at -16 sum q, and steps and lowest values come behind the product, a group of 64.  (The
+// 128 + c of attention needs a shift less and is off by five times as much, which the weights of many rows average out there.)
+template <typename T, int BITS, int D> struct Keys {
+  static constexpr bool CODES = BITS == 4 && sizeof(T) == 2;
+  static constexpr int NG = D / 64;
+  RowFrag<T, D> f;
+  float step[CODES ? 4 : 1][NG], low[CODES ? 4 : 1][NG];      // of keys 4 quarter + j
+  int end;                                                    // keys from here on do not exist
+};
+// piece x of a lane's row: its place in a row of D elements
+template <typename T, int BITS> __device__ __forceinline__ int piece_of(int x, int quarter) {
+  if constexpr (BITS == 0) return 4 * x + quarter;
+  else if constexpr (sizeof(T) == 2) return 8 * (x >> 1) + 2 * quarter + (x & 1);
+  else return 16 * (x >> 2) + 4 * quarter + (x & 3);
+}
+
+// 16 keys from position key0 on (a page holds them all); those that do not exist are zero.
+template <typename T, int BITS, int D>
+__device__ __forceinline__ void load_keys(Keys<T, BITS, D>& k, const WeightsArgs& a, int n, int b, int hk, int key0, int n16, int quarter) {
+  constexpr int NF = D * sizeof(T) / 64, NG = D / 64;
+  const BlockDims& m = a.m;
+  const int phys = key0 < n ? pool_page(m, b, key0 >> m.lpage) : -1, in = key0 & (m.page - 1);
+  const bool there = phys >= 0 && key0 + n16 < n;
+  k.end = phys >= 0 ? n : 0;
+  if constexpr (BITS == 0) {
+    load_frag<T, D>(k.f, (const T*)a.k + (there ? phys * a.ks.page + (in + n16) * a.ks.token + hk * a.ks.head : 0), quarter, there);
+  } else {
+    const long long row = ((long long)max(phys, 0) * m.Hkv + hk) * m.page + in;
+    uint32_t c[NG][2];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const uint2 w = there ? ((const uint2*)((const char*)a.k + (row + n16) * (D / 2)))[quarter + 4 * g] : uint2{0, 0};
+      c[g][0] = w.x; c[g][1] = w.y;
+    }
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int x = 0; x < NF; ++x) {
+        const uint32_t w = c[x >> 1][x & 1];
+        k.f.p[x] = u32x4_t{(w << 3 & 0x00780078u) | 0x41804180u, (w >> 1 & 0x00780078u) | 0x41804180u, (w >> 5 & 0x00780078u) | 0x41804180u,
+                           (w >> 9 & 0x00780078u) | 0x41804180u};
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          const uint32_t pair = phys >= 0 && key0 + 4 * quarter + j < n ? a.km[(row + 4 * quarter + j) * NG + g] : 0;
+          k.step[j][g] = __uint_as_float(pair << 16);
+          k.low[j][g] = __uint_as_float(pair & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+      for (int x = 0; x < NF; ++x) {
+        const uint32_t pair = there ? a.km[(row + n16) * NG + (x >> 2)] : 0, w = c[x >> 2][(x >> 1) & 1] >> (16 * (x & 1));
+        const float step = __uint_as_float(pair << 16), low = __uint_as_float(pair & 0xFFFF0000u);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k.f.p[x][j] = there ? __float_as_uint(fmaf((float)(w >> (4 * j) & 15), step, low)) : 0u;
+      }
+    }
+  }
+}
+
+template <typename T, int BITS, int D>
+__global__ __launch_bounds__(256) void cache_weights(WeightsArgs a, int chunks) {
+  using K = Keys<T, BITS, D>;
+  constexpr int NF = D * sizeof(T) / 64, NG = K::NG;
+  const BlockDims& m = a.m;
+  const int chunk = blockIdx.x % chunks, hk = blockIdx.x / chunks % m.Hkv, b = blockIdx.x / chunks / m.Hkv;
+  const BlockSeq s = block_seq(m, b);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, quarter = lane >> 4;
+  const int key0 = chunk * 128 + wave * 32, most = m.max_pages << m.lpage;
+  if (key0 >= most) return;
+  f32x4_t w[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) w[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  if (key0 < s.n) {
+    K k[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load_keys<T, BITS, D>(k[h], a, s.n, b, hk, key0 + 16 * h, n16, quarter);
+    // causal: the first query that sees key0
+    const int t0 = m.causal ? max(0, key0 - s.first) : 0, rows = s.nq * m.G;
+    for (int row0 = t0 * m.G; row0 < rows; row0 += 16) {
+      const int row = row0 + n16, t = row / m.G;
+      const bool there = row < rows;
+      RowFrag<T, D> q;
+      const T* const p = (const T*)a.q + (long long)(s.q0 + t) * a.qs.token + (long long)(hk * m.G + row % m.G) * a.qs.head;
+#pragma unroll
+      for (int f = 0; f < NF; ++f) q.p[f] = there ? *(const u32x4_t*)(p + piece_of<T, BITS>(f, quarter) * Vec<T>::N) : u32x4_t{0, 0, 0, 0};
+      const float lse = there ? a.lse[(long long)(s.q0 + t) * m.Hq + hk * m.G + row % m.G] : INFINITY;
+      const float off = lse == -INFINITY ? INFINITY : lse * LOG2E;      // (a row without keys weighs none)
+      const int lim = there ? (m.causal ? min(s.n, s.first + t + 1) : s.n) : 0;
+      float qsum[NG];
+      if constexpr (K::CODES) {
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          float sum = 0.f;
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            u32x4_t& x = q.p[2 * g + c];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum += __uint_as_float(x[j] << 16) + __uint_as_float(x[j] & 0xFFFF0000u);
+            // dimensions 0..7 -> 0 4 1 5 2 6 3 7
+            x = u32x4_t{(x[0] & 0xFFFFu) | x[2] << 16, x[0] >> 16 | (x[2] & 0xFFFF0000u), (x[1] & 0xFFFFu) | x[3] << 16, x[1] >> 16 | (x[3] & 0xFFFF0000u)};
+          }
+          qsum[g] = quarters_sum(sum);
+        }
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        f32x4_t sc;
+        if constexpr (K::CODES) {
+          sc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            const float start = -16.f * qsum[g];
+            f32x4_t x{start, start, start, start};
+            x = mma(T{}, k[h].f.p[2 * g], q.p[2 * g], x);
+            x = mma(T{}, k[h].f.p[2 * g + 1], q.p[2 * g + 1], x);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[j] = fmaf(k[h].step[j][g], x[j], fmaf(k[h].low[j][g], qsum[g], sc[j]));
+          }
+        } else {
+          sc = dots(k[h].f, q);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float p = __builtin_amdgcn_exp2f(fmaf(sc[j], a.scale_log2e, -off));
+          w[h][j] += key0 + 16 * h + 4 * quarter + j < min(lim, k[h].end) ? p : 0.f;
+        }
+      }
+    }
+  }
+  // over the lanes of a quarter: they hold different rows
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int x = 1; x < 16; x *= 2) w[h][j] += __shfl_xor(w[h][j], x);
+    const int at = key0 + 16 * h + 4 * quarter;
+    if (n16 || at >= most) continue;                  // (a page holds 16 keys at least)
+    const long long to = ((long long)b * m.Hkv + hk) * most + at;
+    const f32x4_t before = a.w && at < s.n ? *(const f32x4_t*)(a.w + to) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+    f32x4_t x;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = at + j < s.n ? (a.w ? fmaf(a.decay, before[j], w[h][j]) : w[h][j]) : 0.f;
+    *(f32x4_t*)(a.out + to) = x;
+  }
+}
+
+// ---- the tokens that stay ----------------------------------------------------------------------------------------------------
+
+// Order of weights as whole numbers: larger ones first, the two zeros the same, a NaN behind everything.
+__device__ __forceinline__ uint32_t order_of(float w) {
+  if (w != w) return 0;
+  const uint32_t u = __float_as_uint(w == 0.f ? 0.f : w);
+  return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+constexpr int PICK_NT = 1024, DIGIT = 11, BINS = 1 << DIGIT;
+
+// A workgroup chooses for one head of a sequence: the weight at the border by a radix search (three digits of 11, 11 and 10 bits from the
+// top), then one pass over the positions that numbers those above it, those at it as long as there is room, and the ones that stay
+// whatever they weigh, and writes them and their weights in order.
+__global__ __launch_bounds__(PICK_NT) void evict_pick(EvictArgs a) {
+  __shared__ uint32_t bins[BINS];
+  __shared__ uint32_t sums[2][PICK_NT / 64];
+  __shared__ uint32_t found[2];
+  const BlockDims& m = a.m;
+  const int hk = blockIdx.x % m.Hkv, b = blockIdx.x / m.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int most = m.max_pages << m.lpage, n = min(max(m.seq_lens[b], 0), most), keep = a.keep;
+  const long long at = (long long)b * m.Hkv + hk;
+  const float* const w = a.w + at * most;
+  float* const out = a.new_w + at * most;
+  int32_t* const kept = a.kept + at * keep;
+  const int end = min(n, keep);
+  if (hk == 0 && tid == 0) a.new_lens[b] = end;
+  // (stay whatever they weigh: positions below `first` and from `last` on)
+  const int first = (int)min((long long)n, (long long)m.keep_first << m.lpage), last = max(first, n - a.recent);
+  uint32_t border = 0, room = 0xFFFFFFFFu;             // weights above the border stay, and the first `room` at it
+  if (n > keep) {
+    room = keep - first - (n - last);                  // (of the positions between: fewer than there are)
+    border = 0;
+    uint32_t mask = 0;
+    for (int shift = 32 - DIGIT; ; shift = max(0, shift - DIGIT)) {
+      const int bits = shift == 32 - DIGIT || shift == 32 - 2 * DIGIT ? DIGIT : 32 - 2 * DIGIT;
+      for (int x = tid; x < BINS; x += PICK_NT) bins[x] = 0;
+      __syncthreads();
+      for (int p = first + tid; p < last; p += PICK_NT) {
+        const uint32_t key = order_of(w[p]);
+        if ((key & mask) == border) atomicAdd(&bins[key >> shift & ((1u << bits) - 1)], 1u);
+      }
+      __syncthreads();
+      // the digit at the border: from the largest down, two bins a thread
+      const int hi = BINS - 1 - 2 * tid;
+      const uint32_t c0 = bins[hi], c1 = bins[hi - 1];
+      uint32_t run = c0 + c1;
+#pragma unroll
+      for (int x = 1; x < 64; x *= 2) { const uint32_t v = __shfl_up(run, x); if (lane >= x) run += v; }
+      if (lane == 63) sums[0][wave] = run;
+      __syncthreads();
+      uint32_t before = run - c0 - c1;
+      for (int x = 0; x < wave; ++x) before += sums[0][x];
+      // (room may be 0: the border is then above the largest weight there is, in the bin where nothing has been counted yet)
+      if (before < room && before + c0 >= room) { found[0] = hi; found[1] = room - before; }
+      else if (before + c0 < room && before + c0 + c1 >= room) { found[0] = hi - 1; found[1] = room - before - c0; }
+      if (room == 0 && tid == 0) { found[0] = BINS - 1; found[1] = 0; }
+      __syncthreads();
+      border |= found[0] << shift & (bits == DIGIT ? ~0u : (1u << bits) - 1);
+      room = found[1];
+      mask |= ((1u << bits) - 1) << shift;
+      __syncthreads();
+      if (shift == 0) break;
+    }
+  }
+  // number them: 4 positions a thread
+  uint32_t done = 0, ties = 0;
+  for (int p0 = 0; p0 < n; p0 += 4 * PICK_NT) {
+    const int p = p0 + 4 * tid;
+    f32x4_t v{0.f, 0.f, 0.f, 0.f};
+    if (p < n) v = *(const f32x4_t*)(w + p);
+    uint32_t tie = 0, sure = 0;                        // bits of the four
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (p + j >= n) continue;
+      const uint32_t key = order_of(v[j]);
+      if (n <= keep || p + j < first || p + j >= last || key > border) sure |= 1u << j;
+      else if (key == border) tie |= 1u << j;
+    }
+    uint32_t run = __popc(tie);
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) { const uint32_t u = __shfl_up(run, x); if (lane >= x) run += u; }
+    if (lane == 63) sums[0][wave] = run;
+    __syncthreads();
+    uint32_t rank = ties + run - __popc(tie);
+    for (int x = 0; x < PICK_NT / 64; ++x) { if (x < wave) rank += sums[0][x]; ties += sums[0][x]; }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (tie >> j & 1) { if (rank < room) sure |= 1u << j; ++rank; }
+    run = __popc(sure);
+#pragma unroll
+    for (int x = 1; x < 64; x *= 2) { const uint32_t u = __shfl_up(run, x); if (lane >= x) run += u; }
+    if (lane == 63) sums[1][wave] = run;
+    __syncthreads();
+    uint32_t to = done + run - __popc(sure);
+    for (int x = 0; x < PICK_NT / 64; ++x) { if (x < wave) to += sums[1][x]; done += sums[1][x]; }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (sure >> j & 1) { kept[to] = p + j; out[to] = v[j]; ++to; }
+    __syncthreads();
+  }
+  for (int p = end + tid; p < keep; p += PICK_NT) kept[p] = -1;
+  for (int p = end + tid; p < most; p += PICK_NT) out[p] = 0.f;
+}
+
+// ---- their move -----------------------------------------------------------------------------------------------------------------
+
+// A workgroup fills one page of one head: rows as they are, 16 bytes a lane (4 bits: codes), and the page's box of them.
+template <typename T, int BITS, int D>
+__global__ __launch_bounds__(256) void evict_move(EvictArgs a, int pages) {
+  constexpr int VEC = Vec<T>::N, LPR = D / VEC, RPI = 256 / LPR;          // lanes a row, rows a turn
+  const BlockDims& m = a.m;
+  const int pg = blockIdx.x % pages, hk = blockIdx.x / pages % m.Hkv, b = blockIdx.x / pages / m.Hkv;
+  const int most = m.max_pages << m.lpage, n = min(min(max(m.seq_lens[b], 0), most), a.keep);
+  const int p0 = pg << m.lpage, p1 = min(n, p0 + m.page);
+  if (p0 >= p1) return;
+  const int to = a.new_table[(long long)b * m.max_pages + pg];
+  if ((unsigned)to >= (unsigned)m.num_pages) return;
+  const int tid = threadIdx.x, col = tid % LPR * VEC;
+  const int32_t* const kept = a.kept + ((long long)b * m.Hkv + hk) * a.keep;
+  // a page that stays as it is, in its place
+  if (kept[p1 - 1] == p1 - 1 && to == m.table[(long long)b * m.max_pages + pg] && (p1 - p0 == m.page || m.seq_lens[b] <= a.keep)) return;
+  float mx[VEC], mn[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) { mx[i] = -INFINITY; mn[i] = INFINITY; }
+  for (int p = p0 + tid / LPR; p < p1; p += RPI) {
+    const int src = kept[p], from = pool_page(m, b, src >> m.lpage), in = src & (m.page - 1), slot = p & (m.page - 1);
+    float v[VEC];
+    if constexpr (BITS == 4) {
+      const long long x = ((long long)from * m.Hkv + hk) * m.page + in, y = ((long long)to * m.Hkv + hk) * m.page + slot;
+      uint32_t kc = 0, vc = 0, kp = 0, vp = 0;
+      if (from >= 0) {
+        kp = a.km[x * (D / 64) + col / 64]; vp = a.vm[x * (D / 64) + col / 64];
+        if constexpr (VEC == 8) { kc = ((const uint32_t*)a.kp)[x * (D / 8) + col / 8]; vc = ((const uint32_t*)a.vp)[x * (D / 8) + col / 8]; }
+        else { kc = ((const uint16_t*)a.kp)[x * (D / 4) + col / 4]; vc = ((const uint16_t*)a.vp)[x * (D / 4) + col / 4]; }
+      }
+      if constexpr (VEC == 8) { ((uint32_t*)a.kp)[y * (D / 8) + col / 8] = kc; ((uint32_t*)a.vp)[y * (D / 8) + col / 8] = vc; }
+      else { ((uint16_t*)a.kp)[y * (D / 4) + col / 4] = (uint16_t)kc; ((uint16_t*)a.vp)[y * (D / 4) + col / 4] = (uint16_t)vc; }
+      if (col % 64 == 0) { a.km[y * (D / 64) + col / 64] = kp; a.vm[y * (D / 64) + col / 64] = vp; }
+      const float step = __uint_as_float(kp << 16), low = __uint_as_float(kp & 0xFFFF0000u);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = fmaf((float)(kc >> (4 * i) & 15), step, low);
+    } else {
+      u32x4_t kw{0, 0, 0, 0}, vw{0, 0, 0, 0};
+      if (from >= 0) {
+        kw = *(const u32x4_t*)((const T*)a.kp + from * a.ks.page + in * a.ks.token + hk * a.ks.head + col);
+        vw = *(const u32x4_t*)((const T*)a.vp + from * a.vs.page + in * a.vs.token + hk * a.vs.head + col);
+      }
+      *(u32x4_t*)((T*)a.kp + to * a.ks.page + slot * a.ks.token + hk * a.ks.head + col) = kw;
+      *(u32x4_t*)((T*)a.vp + to * a.vs.page + slot * a.vs.token + hk * a.vs.head + col) = vw;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) v[i] = sizeof(T) == 2 ? __uint_as_float(i & 1 ? kw[i / 2] & 0xFFFF0000u : kw[i / 2] << 16) : __uint_as_float(kw[i % 4]);
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) { mx[i] = fmaxf(mx[i], v[i]); mn[i] = fminf(mn[i], v[i]); }
+  }
+  __shared__ float s_mx[256 * VEC], s_mn[256 * VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) { s_mx[tid * VEC + i] = mx[i]; s_mn[tid * VEC + i] = mn[i]; }
+  __syncthreads();
+  T* const box = (T*)a.boxes + ((long long)to * m.Hkv + hk) * 2 * D;
+  for (int c = tid; c < D; c += 256) {
+    float x = s_mx[c], y = s_mn[c];
+    for (int r = 1; r < RPI; ++r) { x = fmaxf(x, s_mx[r * D + c]); y = fminf(y, s_mn[r * D + c]); }
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t z = pack_bf16x2(x, y);             // (codes: values that bfloat16 rounds, as adacluster_cache_read does)
+      box[c] = (T)(z & 0xFFFFu); box[D + c] = (T)(z >> 16);
+    } else { box[c] = x; box[D + c] = y; }
+  }
+}
+
+}  // namespace
+
+int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, const WeightsArgs& a) {
+  const int chunks = (int)((((long long)a.m.max_pages << a.m.lpage) + 127) / 128);
+  const long long wg = (long long)chunks * a.m.Hkv * a.m.B;
+  if (!grid_fits(wg)) return ADACLUSTER_E_UNSUPPORTED;
+#define CALL(T, D) if (bits == 4) cache_weights<T, 4, D><<<(int)wg, 256, 0, s>>>(a, chunks); else cache_weights<T, 0, D><<<(int)wg, 256, 0, s>>>(a, chunks)
+  if (dtype == ADACLUSTER_BF16) { if (d == 64) { CALL(bf16raw, 64); } else { CALL(bf16raw, 128); } }
+  else { if (d == 64) { CALL(float, 64); } else { CALL(float, 128); } }
+#undef CALL
+  return launched();
+}
+
+int launch_cache_evict(hipStream_t s, int dtype, int bits, int d, const EvictArgs& a) {
+  const int pages = (a.keep + a.m.page - 1) >> a.m.lpage;
+  const long long wg = (long long)pages * a.m.Hkv * a.m.B;
+  if (!grid_fits(wg) || !grid_fits(4ll * a.m.Hkv * a.m.B)) return ADACLUSTER_E_UNSUPPORTED;
+  evict_pick<<<a.m.B * a.m.Hkv, PICK_NT, 0, s>>>(a);
+  if (int rc = launched()) return rc;
+#define CALL(T, D) if (bits == 4) evict_move<T, 4, D><<<(int)wg, 256, 0, s>>>(a, pages); else evict_move<T, 0, D><<<(int)wg, 256, 0, s>>>(a, pages)
+  if (dtype == ADACLUSTER_BF16) { if (d == 64) { CALL(bf16raw, 64); } else { CALL(bf16raw, 128); } }
+  else { if (d == 64) { CALL(float, 64); } else { CALL(float, 128); } }
+#undef CALL
+  return launched();
+}
+
+}  // namespace adac

@@ -10,7 +10,7 @@ namespace {
 // touched.  Bound by what lies between the products (exponentials, roundings, LDS reads), so waves a SIMD count: tiles of 32 keys and three
 // waves (two with NW = 2) against 64 keys and two, or one: 3 sequences up to 8 192 tokens, 32 pages of 64, 16 / 4 heads, d = 128 385 us
 // (489), 17 776 tokens, 30 heads, d = 64 730 (744), chunks of 2 x 1 024 tokens, NW = 2, d = 128 193 (303).
-template <int D, int NW>
+template <int D, int NW, Rows ROWS = Rows::OWN>
 __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(BlockAttnArgs a, int rts, int split) {
   constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int TK = 32, PARTS = TK / 16;      // keys a tile: one product's rows
@@ -19,16 +19,35 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
   __shared__ int2 pages_l[LIST];
   __shared__ int32_t counts[NW];
   const BlockDims& m = a.m;
-  const HeadItem it = xcd_item(blockIdx.x, m.B * m.Hkv, m.nb * rts, split);
+  // (GROUP: rts tiles; a share of the keys is walked by all tiles side by side)
+  const HeadItem it = ROWS == Rows::OWN ? xcd_item(blockIdx.x, m.B * m.Hkv, m.nb * rts, split) : xcd_item(blockIdx.x, m.Hkv, rts * a.nsplit, split);
   if (it.head < 0) return;
-  const int rt = it.item % rts, i = it.item / rts, hk = it.head % m.Hkv, b = it.head / m.Hkv;
-  const BlockSeq s = block_seq(m, b);
-  const int t0 = i * m.qblock, rows = min(m.qblock, s.nq - t0) * m.G, base_row = rt * NT / 2;
-  if (t0 >= s.nq || base_row >= rows) return;
+  const int rt = it.item % rts, i = it.item / rts, hk = it.head % m.Hkv;
+  int b = it.head / m.Hkv, t0 = 0, rows, base_row, from = 0, to = INT32_MAX;
+  BlockSeq s;
+  Group group;
+  if constexpr (ROWS == Rows::GROUP) {
+    const int g = last_group(a.gr.groups, [&](int x) { return first_tile(m, group_at(m, a.gr, x).q0, x, NT / 2) <= rt; });
+    if (g < 0) return;
+    group = group_at(m, a.gr, g);
+    b = group.b0;
+    base_row = (rt - first_tile(m, group.q0, g, NT / 2)) * (NT / 2);
+    rows = (group.q1 - group.q0) * m.G;
+    s = BlockSeq{group.q0, group.q1 - group.q0, 0, group.pages << m.lpage, 0};
+    const int shares = splits_of(m, group.pages, a.nsplit);
+    if (base_row < 0 || base_row >= rows || i >= shares) return;      // (below 0: groups that do not ascend)
+    from = (int)((long long)group.pages * i / shares);
+    to = (int)((long long)group.pages * (i + 1) / shares);
+  } else {
+    s = block_seq(m, b);
+    t0 = i * m.qblock; rows = min(m.qblock, s.nq - t0) * m.G; base_row = rt * NT / 2;
+    if (t0 >= s.nq || base_row >= rows) return;
+  }
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
 
   const int row = base_row + wave * 32 + c, tok = t0 + row / m.G, head = hk * m.G + row % m.G;
-  const bool there = row < rows;
+  const int group_lim = ROWS == Rows::GROUP && row < rows ? row_limit(m, group, s.q0 + tok) : -1;
+  const bool there = ROWS == Rows::GROUP ? group_lim >= 0 : row < rows;
   bf16x8_t qf[KS];
   {
     const bf16raw* const p = (const bf16raw*)a.q + (long long)(s.q0 + tok) * a.qs.token + (long long)head * a.qs.head + hb * 8;
@@ -38,15 +57,21 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
       qf[ks] = *(const bf16x8_t*)&w;
     }
   }
-  const int lim = there ? (m.causal ? min(s.n, s.first + tok + 1) : s.n) : INT32_MAX;      // (a row that is not there needs no mask)
+  const int lim = there ? (ROWS == Rows::GROUP ? group_lim : m.causal ? min(s.n, s.first + tok + 1) : s.n) : INT32_MAX;      // (a row that is not there needs no mask)
   const int wave_first = base_row + wave * 32;
   const bool wave_has_rows = wave_first < rows;
-  const int minlim = m.causal ? min(s.n, s.first + t0 + wave_first / m.G + 1) : s.n;       // keys below: seen by all rows of the wave
+  int minlim = m.causal ? min(s.n, s.first + t0 + wave_first / m.G + 1) : s.n;       // keys below: seen by all rows of the wave
   const int last = min(base_row + NT / 2, rows) - 1;
-  const int maxlim = m.causal ? min(s.n, s.first + t0 + last / m.G + 1) : s.n;
+  int maxlim = m.causal ? min(s.n, s.first + t0 + last / m.G + 1) : s.n;
+  if constexpr (ROWS == Rows::GROUP) {
+    int low = lim;
+#pragma unroll
+    for (int x = 1; x < 32; x *= 2) low = min(low, __shfl_xor(low, x));
+    minlim = uniform(low); maxlim = s.n;
+  }
   const int pages = maxlim > 0 ? (maxlim + m.page - 1) >> m.lpage : 0;
-  const int32_t* const list = a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
-  const int entries = list ? m.topk : pages;
+  const int32_t* const list = ROWS == Rows::OWN && a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
+  const int entries = list ? m.topk : min(pages, to);
 
   f32x16_t oacc[DB];
 #pragma unroll
@@ -73,7 +98,7 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
 #pragma unroll
     for (int x = 0; x < 2; ++x) vaddr[db][x] = col_operand<D>(lane, db, x);
 
-  for (int e0 = 0; e0 < entries; e0 += LIST) {
+  for (int e0 = from; e0 < entries; e0 += LIST) {
     const int n = fill_list<NT>(m, b, list, e0, 1, entries, pages, pages_l, counts);
     const int parts = n << lsub, tiles = (parts + PARTS - 1) / PARTS;
     if (!tiles) continue;
@@ -167,6 +192,16 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
 
   if (!there) return;
   const float all = lrun + __shfl_xor(lrun, 32), inv = all == 0.f ? 0.f : 1.f / all;
+  if constexpr (ROWS == Rows::GROUP) {
+    const long long rec = (((long long)rt * m.Hkv + hk) * a.nsplit + i) * (NT / 2) + wave * 32 + c;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *(f32x4_t*)(a.part_o + rec * D + db * 32 + 8 * x + 4 * hb) = f32x4_t{oacc[db][4 * x], oacc[db][4 * x + 1], oacc[db][4 * x + 2], oacc[db][4 * x + 3]};
+    if (hb == 0) { a.part_ml[rec * 2] = mref * sc; a.part_ml[rec * 2 + 1] = all; }
+    return;
+  }
   bf16raw* const out = (bf16raw*)a.o + (long long)(s.q0 + tok) * a.os.token + (long long)head * a.os.head + 4 * hb;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
@@ -201,6 +236,17 @@ int launch_block_attn_wide(hipStream_t s, int d, const BlockAttnArgs& a) {
     else block_attn_wide<128, 4><<<(int)grid, 256, 0, s>>>(a, rts, split);
   }
   return launched();
+}
+
+void launch_block_attn_wide_part(hipStream_t s, int d, int TR, int tiles, const BlockAttnArgs& a) {
+  const int grid = (int)xcd_grid(a.m.Hkv, (long long)tiles * a.nsplit), split = xcd_split(a.m.Hkv);
+  if (TR == 64) {
+    if (d == 64) block_attn_wide<64, 2, Rows::GROUP><<<grid, 128, 0, s>>>(a, tiles, split);
+    else block_attn_wide<128, 2, Rows::GROUP><<<grid, 128, 0, s>>>(a, tiles, split);
+  } else {
+    if (d == 64) block_attn_wide<64, 4, Rows::GROUP><<<grid, 256, 0, s>>>(a, tiles, split);
+    else block_attn_wide<128, 4, Rows::GROUP><<<grid, 256, 0, s>>>(a, tiles, split);
+  }
 }
 
 }  // namespace adac
