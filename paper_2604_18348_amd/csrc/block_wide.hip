@@ -15,7 +15,8 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
   constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int TK = 32, PARTS = TK / 16;      // keys a tile: one product's rows
   constexpr int PT = TK * CH / NT, TILEB = TK * ROWB;
-  __shared__ __align__(16) char lds[4 * TILEB];
+  constexpr int STAGES = ROWS == Rows::OWN ? 2 : 3;
+  __shared__ __align__(16) char lds[STAGES * 2 * TILEB];
   __shared__ int2 pages_l[LIST];
   __shared__ int32_t counts[NW];
   const BlockDims& m = a.m;
@@ -117,12 +118,26 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
       }
     };
     issue(0, 0);
-    wait_vmcnt<0>();
-    lds_barrier();
+    if constexpr (STAGES == 2) {
+      wait_vmcnt<0>();
+      lds_barrier();
+    } else if (tiles > 1) {
+      issue(1, 1);
+    }
+    int stage = 0;
     for (int t = 0; t < tiles; ++t) {
-      if (t + 1 < tiles) issue((t + 1) & 1, t + 1);
+      if constexpr (STAGES == 2) {
+        if (t + 1 < tiles) issue((t + 1) & 1, t + 1);
+        stage = t & 1;
+      } else {                                      // two tiles on their way: the prefix of one group waits for memory, not for products
+        if (t + 1 < tiles) wait_vmcnt<2 * PT>();
+        else wait_vmcnt<0>();
+        lds_barrier();
+        if (t) stage = stage == 2 ? 0 : stage + 1;
+        if (t + 2 < tiles) issue(stage == 0 ? 2 : stage - 1, t + 2);
+      }
       if (wave_has_rows) {
-        const char* const kt = lds + (t & 1) * 2 * TILEB;
+        const char* const kt = lds + stage * 2 * TILEB;
         const char* const vt = kt + TILEB;
         f32x16_t sacc = zero16();
 #pragma unroll
@@ -184,8 +199,10 @@ __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(Bloc
           for (int db = 0; db < DB; ++db) oacc[db] = mfma32(join_tr(read_tr(p + vaddr[db][0]), read_tr(p + vaddr[db][1])), pf[s2], oacc[db]);
         }
       }
-      wait_vmcnt<0>();
-      lds_barrier();
+      if constexpr (STAGES == 2) {
+        wait_vmcnt<0>();
+        lds_barrier();
+      }
     }
     lds_barrier();                                  // before the list is filled again
   }
