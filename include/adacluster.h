@@ -420,10 +420,12 @@ int adacluster_prefix_attn(const adacluster_block_params* p, int32_t groups, con
  * rows whose lse is -inf add nothing.  0 from the sequence's last key on.  decay in [0,1]; 0, or weights NULL: what was there is not
  * read.  Both [B][Hkv][max_pages * page] fp32; new_weights may be weights.  Sums are fp32 in a fixed order.
  * Queries, positions and pages are those of adacluster_block_attn over a paged cache (a page that is not named: no weight).
+ * max_q * Hq / Hkv must be below 2^31.
  */
+int adacluster_weights_workspace_bytes(const adacluster_block_params* p, size_t* bytes /* host; may be 0, and ws NULL then */);
 int adacluster_cache_weights(const adacluster_block_params* p, const void* q, const int32_t* cu_q, const float* lse,
                              const void* k_pool, const uint32_t* k_meta, const int32_t* seq_lens, const int32_t* page_table,
-                             const float* weights, float decay, float* new_weights, void* stream);
+                             const float* weights, float decay, float* new_weights, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * The tokens that sequences keep.  A sequence of n > keep tokens keeps, for every head of keys by itself, its first keep_first pages, its

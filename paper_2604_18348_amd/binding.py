@@ -170,14 +170,15 @@ def load_library():
     lib.adacluster_block_attn_backward.argtypes = [BP] + [vp] * 13 + [sz, vp]
     lib.adacluster_prefix_workspace_bytes.argtypes = [BP, ctypes.c_int32, ctypes.POINTER(sz)]
     lib.adacluster_prefix_attn.argtypes = [BP, ctypes.c_int32] + [vp] * 13 + [sz, vp]
-    lib.adacluster_cache_weights.argtypes = [BP] + [vp] * 8 + [ctypes.c_float, vp, vp]
+    lib.adacluster_weights_workspace_bytes.argtypes = [BP, ctypes.POINTER(sz)]
+    lib.adacluster_cache_weights.argtypes = [BP] + [vp] * 8 + [ctypes.c_float, vp, vp, sz, vp]
     lib.adacluster_cache_evict.argtypes = [BP] + [vp] * 3 + [ctypes.c_int32] * 2 + [vp] * 10
     lib.adacluster_profile_enable.argtypes = [ctypes.c_int]
     lib.adacluster_profile_read.argtypes = [ctypes.POINTER(ctypes.c_float)]
     for n in ("profile_enable", "profile_read", "centroid_capacity", "workspace_bytes", "last_error", "qcluster", "kcluster", "select",
               "sparse_attn", "attn", "dense_attn", "compactness", "compactness_noalloc", "quest_scores", "stats_fetch", "mfma_probe",
               "block_workspace_bytes", "cache_append", "cache_read", "block_boxes", "block_select", "block_attn", "block_attn_backward",
-              "prefix_workspace_bytes", "prefix_attn", "cache_weights", "cache_evict"):
+              "prefix_workspace_bytes", "prefix_attn", "weights_workspace_bytes", "cache_weights", "cache_evict"):
         getattr(lib, "adacluster_" + n).restype = ctypes.c_int
     _lib = lib
     return lib
@@ -189,7 +190,8 @@ EXPORTED = ["adacluster_centroid_capacity", "adacluster_workspace_bytes", "adacl
             "adacluster_compactness_noalloc", "adacluster_quest_scores", "adacluster_stats_fetch", "adacluster_mfma_probe",
             "adacluster_block_workspace_bytes", "adacluster_cache_append", "adacluster_cache_read", "adacluster_block_boxes",
             "adacluster_block_select", "adacluster_block_attn", "adacluster_block_attn_backward",
-            "adacluster_prefix_workspace_bytes", "adacluster_prefix_attn", "adacluster_cache_weights", "adacluster_cache_evict",
+            "adacluster_prefix_workspace_bytes", "adacluster_prefix_attn", "adacluster_weights_workspace_bytes",
+            "adacluster_cache_weights", "adacluster_cache_evict",
             "adacluster_profile_enable", "adacluster_profile_read"]
 
 STAGES = ["qcluster", "kcluster", "select", "permute", "plan", "attention", "kreduce"]
@@ -792,13 +794,24 @@ def adacluster_prefix_attn(p: BlockParams, q, cu_q, cache: BlockCache, seq_lens,
     return o, lse
 
 
+@functools.lru_cache(maxsize=1024)
+def _weights_bytes(cp: bytes):
+    n = ctypes.c_size_t(0)
+    _check(load_library().adacluster_weights_workspace_bytes(cp, ctypes.byref(n)), "weights_workspace_bytes")
+    return n.value
+
+
+def adacluster_weights_workspace_bytes(p: BlockParams, q_rows, num_pages) -> int:
+    return _weights_bytes(_block_c(p, max(1, q_rows), 0, num_pages))
+
+
 def _weights(name, t, p, dev):
     shape = (p.B, p.Hkv, p.max_pages * p.page)
     if t.shape != shape or t.dtype != torch.float32 or not t.is_contiguous() or t.device != dev:
         raise ValueError(f"{name} must be a contiguous float32 tensor {shape} on {dev}")
 
 
-def adacluster_cache_weights(p: BlockParams, q, cu_q, lse, cache: BlockCache, seq_lens, page_table, weights=None, decay=1.0, out=None):
+def adacluster_cache_weights(p: BlockParams, q, cu_q, lse, cache: BlockCache, seq_lens, page_table, weights=None, decay=1.0, out=None, ws=None):
     """decay * weights + what every cached key gets from the queries q [rows,Hq,d] whose attention over all keys left lse [rows,Hq], summed
     over queries and the heads that share the key -> float32 [B,Hkv,max_pages*page], 0 from a sequence's last key on.  weights None: from
     nothing.  out: may be weights."""
@@ -817,8 +830,14 @@ def adacluster_cache_weights(p: BlockParams, q, cu_q, lse, cache: BlockCache, se
     strides = _rows("q", q, dt, p.Hq, p.d, dev)
     if not rows:                                        # a step without queries: what was there, decayed
         q, lse, strides, rows, cu_q = _row_of_none(p.Hq, p.d, dt, dev), torch.zeros((1, p.Hq), device=dev), _NO2, 1, torch.zeros_like(cu_q)
-    _on(dev, "adacluster_cache_weights", _block_c(p, rows, 0, n, q=strides, k=ks), q.data_ptr(), cu_q.data_ptr(), lse.data_ptr(), cache.k.data_ptr(),
-        _ptr(cache.k_meta), seq_lens.data_ptr(), page_table.data_ptr(), _ptr(weights), decay, out.data_ptr())
+    cp = _block_c(p, rows, 0, n, q=strides, k=ks)
+    if ws is None:
+        size = _weights_bytes(cp)
+        ws = torch.empty(size, dtype=torch.uint8, device=dev) if size else None
+    else:
+        ws, size = _block_ws(cp, None, dev, ws)
+    _on(dev, "adacluster_cache_weights", cp, q.data_ptr(), cu_q.data_ptr(), lse.data_ptr(), cache.k.data_ptr(), _ptr(cache.k_meta), seq_lens.data_ptr(),
+        page_table.data_ptr(), _ptr(weights), decay, out.data_ptr(), _ptr(ws), size)
     return out
 
 

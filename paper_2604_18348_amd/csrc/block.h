@@ -310,8 +310,12 @@ struct WeightsArgs {
   float* out;                                // [B][Hkv][max_pages * page]
   KeyStride qs, ks;
   float scale_log2e, decay;
+  const u32x4_t* sums;                       // 4 bits: sums of q over 64 dimensions, [q_rows][Hq]
+  float* part;                               // [nsplit] like out: sums over a share of the rows
+  int nsplit;
 };
-int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, const WeightsArgs& a);
+size_t cache_weights_bytes(int dtype, int bits, const BlockDims& m);
+int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, WeightsArgs a, void* ws);
 struct EvictArgs {
   BlockDims m;
   const float* w;

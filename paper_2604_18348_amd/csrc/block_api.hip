@@ -273,9 +273,18 @@ int adacluster_prefix_attn(const adacluster_block_params* p, int32_t groups, con
   return done(launch_prefix_attn((hipStream_t)stream, p->dtype, p->bits, p->d, a, ws));
 }
 
+int adacluster_weights_workspace_bytes(const adacluster_block_params* p, size_t* bytes) {
+  BlockDims m;
+  if (int rc = check(p, &m)) return rc;
+  if (!p->num_pages) return fail(ADACLUSTER_E_BADARG, "cache_weights: num_pages must be >= 1");
+  if (!bytes) return fail(ADACLUSTER_E_BADARG, "bytes is NULL");
+  *bytes = cache_weights_bytes(p->dtype, p->bits, m);
+  return 0;
+}
+
 int adacluster_cache_weights(const adacluster_block_params* p, const void* q, const int32_t* cu_q, const float* lse, const void* k_pool,
                              const uint32_t* k_meta, const int32_t* seq_lens, const int32_t* page_table, const float* weights, float decay,
-                             float* new_weights, void* stream) {
+                             float* new_weights, void* ws, size_t ws_bytes, void* stream) {
   WeightsArgs a{};
   if (int rc = check(p, &a.m)) return rc;
   if (!p->num_pages) return fail(ADACLUSTER_E_BADARG, "cache_weights: num_pages must be >= 1");
@@ -287,9 +296,11 @@ int adacluster_cache_weights(const adacluster_block_params* p, const void* q, co
   a.qs = two(p->q_stride); a.ks = three(a.m, p->k_stride);
   if (int rc = check_rows("q", q, p->dtype, a.qs)) return rc;
   if (int rc = check_pool(p, k_pool, k_pool, k_meta, k_meta, a.ks, a.ks)) return rc;
+  if ((long long)p->max_q * a.m.G > INT32_MAX) return fail(ADACLUSTER_E_UNSUPPORTED, "cache_weights: max_q * Hq / Hkv must be below 2^31");
+  if (int rc = check_ws(ws, ws_bytes, cache_weights_bytes(p->dtype, p->bits, a.m))) return rc;
   a.q = q; a.k = k_pool; a.km = k_meta; a.lse = lse; a.w = decay == 0.f ? nullptr : weights; a.out = new_weights;
   a.scale_log2e = log2_scale(p); a.decay = decay;
-  return done(launch_cache_weights((hipStream_t)stream, p->dtype, p->bits, p->d, a));
+  return done(launch_cache_weights((hipStream_t)stream, p->dtype, p->bits, p->d, a, ws));
 }
 
 int adacluster_cache_evict(const adacluster_block_params* p, const int32_t* seq_lens, const int32_t* page_table, const float* weights, int32_t keep,

@@ -1,6 +1,6 @@
 // What a sequence keeps of its cache: the weight that every cached key gets from attention, the tokens chosen by it, and their move to
 // other pages.
-#include "block.h"
+#include "block_wide.h"
 
 namespace adac {
 
@@ -160,6 +160,234 @@ __global__ __launch_bounds__(256) void cache_weights(WeightsArgs a, int chunks) 
     for (int j = 0; j < 4; ++j) x[j] = at + j < s.n ? (a.w ? fmaf(a.decay, before[j], w[h][j]) : w[h][j]) : 0.f;
     *(f32x4_t*)(a.out + to) = x;
   }
+}
+
+// Many rows (bf16): 32 x 32 products.  A wave keeps the operands of KT * 32 keys in registers while 64 rows at a time go through LDS, staged once for
+// all four waves by direct loads, one stage ahead.  Bound by the exponentials: 16 cycles of a SIMD for a wave's 64, beside 8 of a
+// multiply and an addition, where the product at d = 128 takes 16.
+//
+// 4 bits: a code c is a bfloat16 by itself.  Per group g of 64 dimensions x_g = c . q, and score = sum over g of step_g x_g + low_g sum_g q:
+// the last is one more product, of (low, low, low) with sum_g q in three bfloat16 parts (24 bits), which weights_sums has left.
+
+// The sums of q over 64 dimensions, in three parts each: 16 bytes a row and head, as the lanes below 32 want them.
+template <int D>
+__global__ __launch_bounds__(256) void weights_sums(WeightsArgs a, u32x4_t* __restrict__ parts) {
+  const BlockDims& m = a.m;
+  const long long id = (long long)blockIdx.x * 64 + threadIdx.x / 4;      // 4 lanes a row and head
+  if (id >= (long long)m.q_rows * m.Hq) return;                           // (whole quads)
+  const int l = threadIdx.x & 3;
+  const bf16raw* const p = (const bf16raw*)a.q + (id / m.Hq) * a.qs.token + (id % m.Hq) * a.qs.head + l * 16;
+  uint32_t h[3 * (D / 64)];
+#pragma unroll
+  for (int g = 0; g < D / 64; ++g) {
+    float s = 0.f;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const u32x4_t w = *(const u32x4_t*)(p + g * 64 + x * 8);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s += __uint_as_float(w[j] << 16) + __uint_as_float(w[j] & 0xFFFF0000u);
+    }
+    s += __shfl_xor(s, 1);
+    s += __shfl_xor(s, 2);
+#pragma unroll
+    for (int x = 0; x < 3; ++x) {                     // (cut, not rounded: what is left is exact)
+      h[3 * g + x] = __float_as_uint(s) >> 16;
+      s -= __uint_as_float(h[3 * g + x] << 16);
+    }
+  }
+  if (l == 0) parts[id] = D == 128 ? u32x4_t{h[0] | h[1] << 16, h[2] | h[D == 128 ? 3 : 0] << 16, h[D == 128 ? 4 : 0] | h[D == 128 ? 5 : 0] << 16, 0} : u32x4_t{h[0] | h[1] << 16, h[2], 0, 0};
+}
+
+constexpr int STAGE_ROWS = 64;
+template <int BITS, int D>
+__global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int chunks, int split) {
+  constexpr int KT = BITS ? 1 : 2, KS = D / 16, CH = D / 8, ROWB = D * 2, NG = D / 64;
+  constexpr int PT = STAGE_ROWS * CH / 256, STAGEB = STAGE_ROWS * ROWB;
+  __shared__ __align__(16) char lds[2 * STAGEB];
+  __shared__ __align__(16) u32x4_t sums_l[BITS ? 2 : 1][BITS ? STAGE_ROWS : 1];
+  __shared__ float lse_l[2][STAGE_ROWS];
+  const BlockDims& m = a.m;
+  const HeadItem it = xcd_item(blockIdx.x, m.B * m.Hkv, chunks * a.nsplit, split);
+  if (it.head < 0) return;
+  const int chunk = it.item / a.nsplit, share = it.item % a.nsplit, hk = it.head % m.Hkv, b = it.head / m.Hkv;
+  const BlockSeq s = block_seq(m, b);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
+  const int most = m.max_pages << m.lpage, first_key = chunk * 128 * KT, key0 = first_key + wave * 32 * KT;
+
+  // the rows of this share that see a key of the workgroup: [row0, rows)
+  const int all_rows = s.nq * m.G, from = (int)((long long)all_rows * share / a.nsplit);
+  int rows = (int)((long long)all_rows * (share + 1) / a.nsplit);
+  const int t0 = m.causal ? max(0, first_key - s.first) : 0;
+  const int row0 = (int)max((long long)from, (long long)t0 * m.G);
+  if (first_key >= s.n) rows = 0;
+  f32x16_t w[KT];
+#pragma unroll
+  for (int x = 0; x < KT; ++x) w[x] = zero16();
+  if (row0 < rows) {
+    bf16x8_t k[KT][KS], low;
+    float step[NG][BITS ? 16 : 1];
+#pragma unroll
+    for (int x = 0; x < KT; ++x) {
+      const int key = key0 + 32 * x + c, phys = key < s.n ? pool_page(m, b, key >> m.lpage) : -1, in = key & (m.page - 1);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        union { uint32_t w[4]; u32x4_t q; bf16x8_t v; } u;
+        u.q = u32x4_t{0, 0, 0, 0};
+        if constexpr (BITS == 0) {
+          if (phys >= 0) u.q = *(const u32x4_t*)((const bf16raw*)a.k + phys * a.ks.page + in * a.ks.token + hk * a.ks.head + ks * 16 + hb * 8);
+        } else {
+          const uint32_t code = phys >= 0 ? ((const uint32_t*)a.k)[(((long long)phys * m.Hkv + hk) * m.page + in) * (D / 8) + ks * 2 + hb] : 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) u.w[j] = __float_as_uint((float)(code >> (8 * j) & 15)) >> 16 | __float_as_uint((float)(code >> (8 * j + 4) & 15));
+        }
+        k[x][ks] = u.v;
+      }
+      if constexpr (BITS == 4) {
+        union { uint32_t w[4]; bf16x8_t v; } u{{0, 0, 0, 0}};
+        if (phys >= 0 && hb == 0) {
+          const uint32_t* const p = a.km + (((long long)phys * m.Hkv + hk) * m.page + in) * NG;
+          const uint32_t l0 = p[0] >> 16, l1 = NG == 2 ? p[NG - 1] >> 16 : 0;
+          u.w[0] = l0 | l0 << 16; u.w[1] = l0 | l1 << 16; u.w[2] = l1 | l1 << 16;
+        }
+        low = u.v;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int kv = key0 + 8 * (v / 4) + 4 * hb + v % 4, pv = kv < s.n ? pool_page(m, b, kv >> m.lpage) : -1;
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+            step[g][v] = pv >= 0 ? __uint_as_float(a.km[(((long long)pv * m.Hkv + hk) * m.page + (kv & (m.page - 1))) * NG + g] << 16) : 0.f;
+        }
+      }
+    }
+    // Rows from which on all keys of the wave are seen.  (Keys that do not exist are left out at the end.)
+    const int last = min(key0 + 32 * KT, s.n) - 1;
+    const long long free_row = m.causal ? (long long)max(0, last - s.first) * m.G : 0;
+
+    // This thread's pieces of a stage: their rows are followed, 64 further a stage, without a division.
+    const int ht = STAGE_ROWS / m.G, hr = STAGE_ROWS % m.G;
+    const long long ahead = (ht * a.qs.token + hr * a.qs.head) * 2, wrap = (a.qs.token - m.G * a.qs.head) * 2;
+    const char* const base = (const char*)a.q + (s.q0 * a.qs.token + (long long)hk * m.G * a.qs.head) * 2;
+    const char* src[PT];
+    int head[PT], piece[PT];
+#pragma unroll
+    for (int x = 0; x < PT; ++x) {
+      const int item = tid + x * 256, r = item / CH, row = row0 + r;
+      head[x] = row % m.G;
+      piece[x] = ((item % CH) ^ swz<D>(r)) * 16;
+      src[x] = base + ((row / m.G) * a.qs.token + head[x] * a.qs.head) * 2;
+    }
+    long long lrow = (long long)(s.q0 + (row0 + lane) / m.G) * m.Hq + hk * m.G + (row0 + lane) % m.G;      // of lse and of the sums
+    int lhead = (row0 + lane) % m.G;
+    const long long lahead = (long long)ht * m.Hq + hr, lwrap = m.Hq - m.G, lbase = (long long)s.q0 * m.Hq + hk * m.G;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t*)lds, lse0 = (uint32_t)(uintptr_t)(lds_void_t*)&lse_l[0][0], sums0 = (uint32_t)(uintptr_t)(lds_void_t*)&sums_l[0][0];
+    auto issue = [&](int stage, int r0) __attribute__((always_inline)) {      // (rows past the end: the sequence's first, masked)
+#pragma unroll
+      for (int x = 0; x < PT; ++x) {
+        const int r = (tid + x * 256) / CH;
+        dma_b128(lds0 + stage * STAGEB + (wave * 64 + x * 256) * 16, (r0 + r < rows ? src[x] : base) + piece[x]);
+        head[x] += hr; src[x] += ahead;
+        if (head[x] >= m.G) { head[x] -= m.G; src[x] += wrap; }
+      }
+      if (wave == 0) {
+        const long long at = r0 + lane < rows ? lrow : lbase;
+        dma_b32(lse0 + stage * STAGE_ROWS * 4, (const void*)(a.lse + at));
+        if constexpr (BITS == 4) dma_b128(sums0 + stage * STAGE_ROWS * 16, (const void*)(a.sums + at));
+        lhead += hr; lrow += lahead;
+        if (lhead >= m.G) { lhead -= m.G; lrow += lwrap; }
+      }
+    };
+    issue(0, row0);
+    wait_vmcnt<0>();
+    lds_barrier();
+    for (int r0 = row0, stage = 0; r0 < rows; r0 += STAGE_ROWS, stage ^= 1) {
+      if (r0 + STAGE_ROWS < rows) issue(stage ^ 1, r0 + STAGE_ROWS);
+#pragma unroll
+      for (int half = 0; half < STAGE_ROWS / 32; ++half) {
+        const char* const qt = lds + stage * STAGEB + half * 32 * ROWB;
+        bf16x8_t q[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) q[ks] = *(const bf16x8_t*)(qt + row_operand<D>(lane, ks));
+        const int row = r0 + half * 32 + c;
+        const float lse = lse_l[stage][half * 32 + c];
+        const float off = lse == -INFINITY ? INFINITY : lse * LOG2E;      // (a row without keys weighs none)
+        bf16x8_t sums;
+        if constexpr (BITS == 4) {
+          union { u32x4_t w; bf16x8_t v; } u;
+          u.w = hb ? u32x4_t{0, 0, 0, 0} : sums_l[stage][half * 32 + c];
+          sums = u.v;
+        }
+#pragma unroll
+        for (int x = 0; x < KT; ++x) {
+          f32x16_t sc = zero16();
+          if constexpr (BITS == 0) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) sc = mfma32(k[x][ks], q[ks], sc);
+          } else {
+            sc = mfma32(low, sums, sc);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              f32x16_t y = zero16();
+#pragma unroll
+              for (int ks = 0; ks < 4; ++ks) y = mfma32(k[x][4 * g + ks], q[4 * g + ks], y);
+#pragma unroll
+              for (int v = 0; v < 16; ++v) sc[v] = fmaf(step[g][v], y[v], sc[v]);
+            }
+          }
+          if (r0 + half * 32 >= free_row && r0 + half * 32 + 32 <= rows) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) w[x][v] += __builtin_amdgcn_exp2f(fmaf(sc[v], a.scale_log2e, -off));
+          } else {
+            const int lim = row >= rows ? 0 : m.causal ? s.first + row / m.G + 1 - (key0 + 32 * x + 4 * hb) : 32;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+              const float p = __builtin_amdgcn_exp2f(fmaf(sc[v], a.scale_log2e, -off));
+              w[x][v] += 8 * (v / 4) + v % 4 < lim ? p : 0.f;
+            }
+          }
+        }
+      }
+      wait_vmcnt<0>();
+      lds_barrier();
+    }
+  }
+  // Over the 32 rows that the lanes hold: at every step a lane passes on half of its keys, and is left with one of the 16.
+#pragma unroll
+  for (int x = 0; x < KT; ++x) {
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = w[x][i];
+#pragma unroll
+    for (int bit = 16, n = 8; bit >= 2; bit >>= 1, n >>= 1) {
+      const bool up = lane & bit;
+#pragma unroll
+      for (int i = 0; i < n; ++i) {
+        const float give = up ? v[i] : v[i + n], mine = up ? v[i + n] : v[i];
+        v[i] = mine + __shfl_xor(give, bit);
+      }
+    }
+    v[0] += __shfl_xor(v[0], 1);
+    const int i = c >> 1, at = key0 + 32 * x + 8 * (i / 4) + 4 * hb + i % 4;
+    if ((c & 1) || at >= most) continue;
+    const long long to = ((long long)b * m.Hkv + hk) * most + at;
+    const float sum = at < s.n && pool_page(m, b, at >> m.lpage) >= 0 ? v[0] : 0.f;
+    if (a.nsplit > 1) a.part[(long long)share * m.B * m.Hkv * most + to] = sum;
+    else a.out[to] = at >= s.n ? 0.f : a.w ? fmaf(a.decay, a.w[to], sum) : sum;
+  }
+}
+
+// The sums of shares of the rows, in order.
+__global__ __launch_bounds__(256) void weights_join(WeightsArgs a) {
+  const BlockDims& m = a.m;
+  const int most = m.max_pages << m.lpage;
+  const long long all = (long long)m.B * m.Hkv * most, to = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (to >= all) return;
+  const int at = (int)(to % most), n = min(max(m.seq_lens[to / most / m.Hkv], 0), most);
+  f32x4_t sum = *(const f32x4_t*)(a.part + to);
+  for (int z = 1; z < a.nsplit; ++z) sum += *(const f32x4_t*)(a.part + z * all + to);
+  const f32x4_t before = a.w && at < n ? *(const f32x4_t*)(a.w + to) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) sum[j] = at + j < n ? (a.w ? fmaf(a.decay, before[j], sum[j]) : sum[j]) : 0.f;
+  *(f32x4_t*)(a.out + to) = sum;
 }
 
 // ---- the tokens that stay ----------------------------------------------------------------------------------------------------
@@ -335,7 +563,54 @@ __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int pages) {
 
 }  // namespace
 
-int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, const WeightsArgs& a) {
+namespace {
+struct WeightsShape { bool wide; int chunks, nsplit; size_t sums, part; };
+WeightsShape weights_shape(int dtype, int bits, const BlockDims& m) {
+  WeightsShape s{};
+  const long long rows = (long long)m.max_q * m.G, keys = (long long)m.max_pages << m.lpage;
+  s.wide = dtype == ADACLUSTER_BF16 && rows > 32;
+  s.nsplit = 1;
+  if (!s.wide) return s;
+  s.chunks = (int)((keys + (bits ? 127 : 255)) / (bits ? 128 : 256));
+  // Few keys for many rows: the rows are shared until the launch has the two workgroups a CU that it holds, 512 rows each at least.
+  const long long wg = (long long)s.chunks * m.Hkv * m.B;
+  long long n = 512 / wg;
+  if (n > rows / 512) n = rows / 512;
+  if (n > 1) s.nsplit = (int)n;
+  s.sums = bits ? align_up((size_t)m.q_rows * m.Hq * 16, 256) : 0;
+  s.part = s.nsplit > 1 ? (size_t)s.nsplit * m.B * m.Hkv * keys * 4 : 0;
+  return s;
+}
+}  // namespace
+
+size_t cache_weights_bytes(int dtype, int bits, const BlockDims& m) {
+  const WeightsShape s = weights_shape(dtype, bits, m);
+  return s.sums + s.part;
+}
+
+int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, WeightsArgs a, void* ws) {
+  const WeightsShape sh = weights_shape(dtype, bits, a.m);
+  if (sh.wide) {
+    const long long heads = (long long)a.m.Hkv * a.m.B, grid = xcd_grid(heads, (long long)sh.chunks * sh.nsplit);
+    const long long pre = ((long long)a.m.q_rows * a.m.Hq + 63) / 64;
+    if (!grid_fits(grid) || !grid_fits(pre)) return ADACLUSTER_E_UNSUPPORTED;
+    a.sums = (const u32x4_t*)ws;
+    a.part = (float*)((char*)ws + sh.sums);
+    a.nsplit = sh.nsplit;
+    const int split = xcd_split(heads);
+    if (bits) {
+      if (d == 64) weights_sums<64><<<(int)pre, 256, 0, s>>>(a, (u32x4_t*)ws); else weights_sums<128><<<(int)pre, 256, 0, s>>>(a, (u32x4_t*)ws);
+      if (int rc = launched()) return rc;
+      if (d == 64) cache_weights_wide<4, 64><<<(int)grid, 256, 0, s>>>(a, sh.chunks, split);
+      else cache_weights_wide<4, 128><<<(int)grid, 256, 0, s>>>(a, sh.chunks, split);
+    } else {
+      if (d == 64) cache_weights_wide<0, 64><<<(int)grid, 256, 0, s>>>(a, sh.chunks, split);
+      else cache_weights_wide<0, 128><<<(int)grid, 256, 0, s>>>(a, sh.chunks, split);
+    }
+    if (int rc = launched()) return rc;
+    if (sh.nsplit > 1) weights_join<<<(int)((heads * ((long long)a.m.max_pages << a.m.lpage) / 4 + 255) / 256), 256, 0, s>>>(a);
+    return launched();
+  }
   const int chunks = (int)((((long long)a.m.max_pages << a.m.lpage) + 127) / 128);
   const long long wg = (long long)chunks * a.m.Hkv * a.m.B;
   if (!grid_fits(wg)) return ADACLUSTER_E_UNSUPPORTED;

@@ -60,6 +60,8 @@ LAYOUTS = [  # d, page, Hq, Hkv, lens, news
     (128, 16, 32, 8, [700, 650], [64, 33]),
     (64, 64, 64, 1, [500], [3]),
     (128, 128, 12, 4, [1000, 999], [257, 129]),
+    (64, 16, 8, 1, [300], [290]),                                 # (16 bits: few keys for many rows, which are shared out)
+    (128, 32, 15, 3, [200, 7, 90], [200, 1, 90]),
 ]
 
 
@@ -106,6 +108,23 @@ def test_weights_of_many_rows_in_place_equal_those_apart():
     apart = B.adacluster_cache_weights(p, q, cu, lse, x.cache, weights=w, decay=0.5, **x.where())
     B.adacluster_cache_weights(p, q, cu, lse, x.cache, weights=w, decay=0.5, out=w, **x.where())
     assert torch.equal(apart, w)
+
+
+@pytest.mark.parametrize("news", [1, 8, 40, 100])
+def test_weights_of_scores_that_no_query_makes(news):
+    """The last key is infinite: the only query that sees it scores -inf, all others +inf, and rows behind the last one score nothing."""
+    x = Batch(BF, 0, 64, 16, 2, 2, [130], [news], 6)
+    x.q = x.q.abs() + 0.1
+    x.q[news - 1] *= -1
+    at = 129
+    x.cache.k[int(x.table[0, at // 16]), :, at % 16] = math.inf
+    p = x.params()
+    q, cu = x.q.cuda(), x.cu_q.cuda()
+    _, lse = B.adacluster_block_attn(p, q, cu, cache=x.cache, **x.where())
+    got = B.adacluster_cache_weights(p, q, cu, lse, x.cache, **x.where())
+    want, tol = _weights(x, 0, lse.cpu(), 1 / 8, 1, None, torch.arange(130) < at)
+    _within(got[0, :, :at], want[:, :at], tol[:, :at], "weights")
+    assert bool((got[0, :, at:] == 0).all())
 
 
 @pytest.mark.parametrize("dtype,bits", [(BF, 0), (F, 0), (BF, 4), (F, 4)])

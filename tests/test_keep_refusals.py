@@ -50,10 +50,10 @@ def test_prefix(lib):
     assert prefix(lib, params(), ws=Z) == -4 and prefix(lib, params(), ws=ctypes.c_void_p(272)) == -4 and prefix(lib, params(), n=need - 1) == -4
 
 
-def weights(lib, c, decay=1.0, out=ONE, **kw):
+def weights(lib, c, decay=1.0, out=ONE, ws=ONE, n=1 << 40, **kw):
     a = dict(q=ONE, cu_q=ONE, lse=ONE, k=ONE, km=Z, lens=ONE, table=ONE, w=ONE)
     a.update(kw)
-    return lib.adacluster_cache_weights(ctypes.byref(c), *a.values(), decay, out, Z)
+    return lib.adacluster_cache_weights(ctypes.byref(c), *a.values(), decay, out, ws, n, Z)
 
 
 def test_weights(lib):
@@ -69,6 +69,13 @@ def test_weights(lib):
     c = params()
     c.k_stride[2] = 63
     assert weights(lib, c) == -1 and "16 bytes" in message(lib)
+    out = ctypes.c_size_t(7)
+    f = lib.adacluster_weights_workspace_bytes
+    assert f(ctypes.byref(params(num_pages=0, k_rows=4)), ctypes.byref(out)) == -1 and f(ctypes.byref(params()), None) == -1 and f(None, ctypes.byref(out)) == -1
+    assert f(ctypes.byref(params(B=1, Hkv=1, max_q=2000)), ctypes.byref(out)) == 0 and out.value > 0      # few keys for many rows: shares of them
+    many = params(B=1, Hkv=1, max_q=2000)
+    assert weights(lib, many, ws=Z) == -4 and weights(lib, many, n=out.value - 1) == -4 and weights(lib, many, ws=ctypes.c_void_p(272)) == -4
+    assert weights(lib, params(B=1, Hq=65535, Hkv=1, max_q=1 << 20)) == -5
 
 
 def evict(lib, c, keep=20, recent=2, **kw):
