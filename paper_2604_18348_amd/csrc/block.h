@@ -310,11 +310,11 @@ struct WeightsArgs {
   float* out;                                // [B][Hkv][max_pages * page]
   KeyStride qs, ks;
   float scale_log2e, decay;
-  const u32x4_t* sums;                       // 4 bits: sums of q over 64 dimensions, [q_rows][Hq]
+  const u32x4_t* sums;                       // 4 bits: two records a row and head (weights_sums)
   float* part;                               // [nsplit] like out: sums over a share of the rows
   int nsplit;
 };
-size_t cache_weights_bytes(int dtype, int bits, const BlockDims& m);
+size_t cache_weights_bytes(int dtype, int bits, const BlockDims& m, const KeyStride& qs);
 int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, WeightsArgs a, void* ws);
 struct EvictArgs {
   BlockDims m;

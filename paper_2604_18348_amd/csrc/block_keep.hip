@@ -166,10 +166,12 @@ __global__ __launch_bounds__(256) void cache_weights(WeightsArgs a, int chunks) 
 // all four waves by direct loads, one stage ahead.  Bound by the exponentials: 16 cycles of a SIMD for a wave's 64, beside 8 of a
 // multiply and an addition, where the product at d = 128 takes 16.
 //
-// 4 bits: a code c is a bfloat16 by itself.  Per group g of 64 dimensions x_g = c . q, and score = sum over g of step_g x_g + low_g sum_g q:
-// the last is one more product, of (low, low, low) with sum_g q in three bfloat16 parts (24 bits), which weights_sums has left.
+// 4 bits: a code c is a bfloat16 by itself.  Per group g of 64 dimensions x_g = c . q, and score = sum over g of step_g x_g + low_g sum_g q.
+// The latter, scaled, less the row's log2(e) lse is one more product, of (low, low, low, .., -1, -1, -1) with three bfloat16 parts (24 bits) of every
+// factor, which weights_sums has left: what remains is two multiplications, the exponential and an addition.
 
-// The sums of q over 64 dimensions, in three parts each: 16 bytes a row and head, as the lanes below 32 want them.
+// 32 bytes a row and head: the sums of q over 64 dimensions, times scale log2(e), in three parts each, for the lanes below 32, and log2(e) lse
+// in three parts for the others, which meet -1.
 template <int D>
 __global__ __launch_bounds__(256) void weights_sums(WeightsArgs a, u32x4_t* __restrict__ parts) {
   const BlockDims& m = a.m;
@@ -177,7 +179,11 @@ __global__ __launch_bounds__(256) void weights_sums(WeightsArgs a, u32x4_t* __re
   if (id >= (long long)m.q_rows * m.Hq) return;                           // (whole quads)
   const int l = threadIdx.x & 3;
   const bf16raw* const p = (const bf16raw*)a.q + (id / m.Hq) * a.qs.token + (id % m.Hq) * a.qs.head + l * 16;
-  uint32_t h[3 * (D / 64)];
+  uint32_t h[9] = {0, 0, 0, 0, 0, 0, 0, 0, 0};
+  const auto cut = [&](float s, int at) __attribute__((always_inline)) {      // (cut, not rounded: what is left is exact)
+#pragma unroll
+    for (int x = 0; x < 3; ++x) { h[at + x] = __float_as_uint(s) >> 16; s -= __uint_as_float(h[at + x] << 16); }
+  };
 #pragma unroll
   for (int g = 0; g < D / 64; ++g) {
     float s = 0.f;
@@ -189,189 +195,287 @@ __global__ __launch_bounds__(256) void weights_sums(WeightsArgs a, u32x4_t* __re
     }
     s += __shfl_xor(s, 1);
     s += __shfl_xor(s, 2);
-#pragma unroll
-    for (int x = 0; x < 3; ++x) {                     // (cut, not rounded: what is left is exact)
-      h[3 * g + x] = __float_as_uint(s) >> 16;
-      s -= __uint_as_float(h[3 * g + x] << 16);
-    }
+    cut(s * a.scale_log2e, 3 * g);
   }
-  if (l == 0) parts[id] = D == 128 ? u32x4_t{h[0] | h[1] << 16, h[2] | h[D == 128 ? 3 : 0] << 16, h[D == 128 ? 4 : 0] | h[D == 128 ? 5 : 0] << 16, 0} : u32x4_t{h[0] | h[1] << 16, h[2], 0, 0};
+  const float lse = a.lse[id];
+  cut(fabsf(lse) == INFINITY ? 0x1p126f : lse * LOG2E, 6);      // (a row without keys weighs none)
+  if (l == 0) parts[2 * id] = u32x4_t{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, 0};
+  if (l == 1) parts[2 * id + 1] = u32x4_t{h[6] | h[7] << 16, h[8], 0, 0};
 }
 
-constexpr int STAGE_ROWS = 64;
+constexpr int STAGE_ROWS = 64, STAGES = 4;      // of q in LDS: all rows of a share stay there if they fit
+
 template <int BITS, int D>
-__global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int chunks, int split) {
+__global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int chunks, int items, int split) {
   constexpr int KT = BITS ? 1 : 2, KS = D / 16, CH = D / 8, ROWB = D * 2, NG = D / 64;
   constexpr int PT = STAGE_ROWS * CH / 256, STAGEB = STAGE_ROWS * ROWB;
-  __shared__ __align__(16) char lds[2 * STAGEB];
-  __shared__ __align__(16) u32x4_t sums_l[BITS ? 2 : 1][BITS ? STAGE_ROWS : 1];
-  __shared__ float lse_l[2][STAGE_ROWS];
+  __shared__ __align__(16) char lds[STAGES * STAGEB];
+  __shared__ __align__(16) u32x4_t sums_l[BITS ? STAGES : 1][2][BITS ? STAGE_ROWS : 1];      // (of both halves of the lanes)
+  __shared__ __align__(16) float step_l[BITS ? 4 : 1][NG][BITS ? 32 : 1];
+  __shared__ float lse_l[BITS ? 1 : STAGES][STAGE_ROWS];
   const BlockDims& m = a.m;
-  const HeadItem it = xcd_item(blockIdx.x, m.B * m.Hkv, chunks * a.nsplit, split);
+  const HeadItem it = xcd_item(blockIdx.x, m.B * m.Hkv, items * a.nsplit, split);
   if (it.head < 0) return;
-  const int chunk = it.item / a.nsplit, share = it.item % a.nsplit, hk = it.head % m.Hkv, b = it.head / m.Hkv;
+  const int share = it.item % a.nsplit, hk = it.head % m.Hkv, b = it.head / m.Hkv;
   const BlockSeq s = block_seq(m, b);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
-  const int most = m.max_pages << m.lpage, first_key = chunk * 128 * KT, key0 = first_key + wave * 32 * KT;
+  const int most = m.max_pages << m.lpage;
+  // the rows of this share, in stages
+  const int all_rows = s.nq * m.G, from = (int)((long long)all_rows * share / a.nsplit), rows = (int)((long long)all_rows * (share + 1) / a.nsplit);
+  const int stages = (rows - from + STAGE_ROWS - 1) / STAGE_ROWS;
 
-  // the rows of this share that see a key of the workgroup: [row0, rows)
-  const int all_rows = s.nq * m.G, from = (int)((long long)all_rows * share / a.nsplit);
-  int rows = (int)((long long)all_rows * (share + 1) / a.nsplit);
-  const int t0 = m.causal ? max(0, first_key - s.first) : 0;
-  const int row0 = (int)max((long long)from, (long long)t0 * m.G);
-  if (first_key >= s.n) rows = 0;
-  f32x16_t w[KT];
-#pragma unroll
-  for (int x = 0; x < KT; ++x) w[x] = zero16();
-  if (row0 < rows) {
-    bf16x8_t k[KT][KS], low;
-    float step[NG][BITS ? 16 : 1];
-#pragma unroll
-    for (int x = 0; x < KT; ++x) {
-      const int key = key0 + 32 * x + c, phys = key < s.n ? pool_page(m, b, key >> m.lpage) : -1, in = key & (m.page - 1);
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        union { uint32_t w[4]; u32x4_t q; bf16x8_t v; } u;
-        u.q = u32x4_t{0, 0, 0, 0};
-        if constexpr (BITS == 0) {
-          if (phys >= 0) u.q = *(const u32x4_t*)((const bf16raw*)a.k + phys * a.ks.page + in * a.ks.token + hk * a.ks.head + ks * 16 + hb * 8);
-        } else {
-          const uint32_t code = phys >= 0 ? ((const uint32_t*)a.k)[(((long long)phys * m.Hkv + hk) * m.page + in) * (D / 8) + ks * 2 + hb] : 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) u.w[j] = __float_as_uint((float)(code >> (8 * j) & 15)) >> 16 | __float_as_uint((float)(code >> (8 * j + 4) & 15));
-        }
-        k[x][ks] = u.v;
-      }
-      if constexpr (BITS == 4) {
-        union { uint32_t w[4]; bf16x8_t v; } u{{0, 0, 0, 0}};
-        if (phys >= 0 && hb == 0) {
-          const uint32_t* const p = a.km + (((long long)phys * m.Hkv + hk) * m.page + in) * NG;
-          const uint32_t l0 = p[0] >> 16, l1 = NG == 2 ? p[NG - 1] >> 16 : 0;
-          u.w[0] = l0 | l0 << 16; u.w[1] = l0 | l1 << 16; u.w[2] = l1 | l1 << 16;
-        }
-        low = u.v;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int kv = key0 + 8 * (v / 4) + 4 * hb + v % 4, pv = kv < s.n ? pool_page(m, b, kv >> m.lpage) : -1;
-#pragma unroll
-          for (int g = 0; g < NG; ++g)
-            step[g][v] = pv >= 0 ? __uint_as_float(a.km[(((long long)pv * m.Hkv + hk) * m.page + (kv & (m.page - 1))) * NG + g] << 16) : 0.f;
-        }
-      }
-    }
-    // Rows from which on all keys of the wave are seen.  (Keys that do not exist are left out at the end.)
-    const int last = min(key0 + 32 * KT, s.n) - 1;
-    const long long free_row = m.causal ? (long long)max(0, last - s.first) * m.G : 0;
-
-    // This thread's pieces of a stage: their rows are followed, 64 further a stage, without a division.
-    const int ht = STAGE_ROWS / m.G, hr = STAGE_ROWS % m.G;
-    const long long ahead = (ht * a.qs.token + hr * a.qs.head) * 2, wrap = (a.qs.token - m.G * a.qs.head) * 2;
-    const char* const base = (const char*)a.q + (s.q0 * a.qs.token + (long long)hk * m.G * a.qs.head) * 2;
-    const char* src[PT];
-    int head[PT], piece[PT];
+  // Where this thread's pieces of a stage lie, in bytes from the token of the stage's first row (below 2^32: the host sees to it); if the
+  // heads of a key do not divide 64 they change from stage to stage, without a division.
+  const int ht = STAGE_ROWS / m.G, hr = STAGE_ROWS % m.G;
+  const uint32_t token = (uint32_t)(a.qs.token * 2), head = (uint32_t)(a.qs.head * 2);
+  uint32_t src[PT], lsrc = 0;                          // lsrc: of lse and of the sums, as an index
+  int h[PT], lh = 0, stage_t = 0, stage_h = 0;         // heads; the stage's first row
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t*)lds, lse0 = (uint32_t)(uintptr_t)(lds_void_t*)&lse_l[0][0], sums0 = (uint32_t)(uintptr_t)(lds_void_t*)&sums_l[0][0];
+  const uint32_t piece = ((tid % CH) ^ swz<D>(tid / CH)) * 16;      // (of all its pieces: the slots repeat every 16 rows)
+  const auto start = [&](int stage) {
+    const int r0 = from + stage * STAGE_ROWS;
+    stage_t = uniform(r0 / m.G); stage_h = uniform(r0 % m.G);
 #pragma unroll
     for (int x = 0; x < PT; ++x) {
-      const int item = tid + x * 256, r = item / CH, row = row0 + r;
-      head[x] = row % m.G;
-      piece[x] = ((item % CH) ^ swz<D>(r)) * 16;
-      src[x] = base + ((row / m.G) * a.qs.token + head[x] * a.qs.head) * 2;
+      const int r = stage_h + (tid + x * 256) / CH;
+      h[x] = r % m.G;
+      src[x] = r / m.G * token + h[x] * head + piece;
     }
-    long long lrow = (long long)(s.q0 + (row0 + lane) / m.G) * m.Hq + hk * m.G + (row0 + lane) % m.G;      // of lse and of the sums
-    int lhead = (row0 + lane) % m.G;
-    const long long lahead = (long long)ht * m.Hq + hr, lwrap = m.Hq - m.G, lbase = (long long)s.q0 * m.Hq + hk * m.G;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t*)lds, lse0 = (uint32_t)(uintptr_t)(lds_void_t*)&lse_l[0][0], sums0 = (uint32_t)(uintptr_t)(lds_void_t*)&sums_l[0][0];
-    auto issue = [&](int stage, int r0) __attribute__((always_inline)) {      // (rows past the end: the sequence's first, masked)
+    lh = (stage_h + lane) % m.G;
+    lsrc = (stage_h + lane) / m.G * m.Hq + lh;
+  };
+  const auto issue = [&](int stage) __attribute__((always_inline)) {      // (rows past the end: the stage's first, masked)
+    const int r0 = from + stage * STAGE_ROWS, slot = stage % STAGES;
+    const char* const q = uniform((const char*)a.q + ((long long)(s.q0 + stage_t) * a.qs.token + (long long)hk * m.G * a.qs.head) * 2);
+    const long long l = (long long)(s.q0 + stage_t) * m.Hq + hk * m.G;
+    const bool whole = r0 + STAGE_ROWS <= rows;
 #pragma unroll
-      for (int x = 0; x < PT; ++x) {
-        const int r = (tid + x * 256) / CH;
-        dma_b128(lds0 + stage * STAGEB + (wave * 64 + x * 256) * 16, (r0 + r < rows ? src[x] : base) + piece[x]);
-        head[x] += hr; src[x] += ahead;
-        if (head[x] >= m.G) { head[x] -= m.G; src[x] += wrap; }
+    for (int x = 0; x < PT; ++x) {
+      const uint32_t off = whole || r0 + (tid + x * 256) / CH < rows ? src[x] : stage_h * head + piece;
+      dma_b128(lds0 + slot * STAGEB + (wave * 64 + x * 256) * 16, off, q);
+    }
+    if (wave == 0) {
+      const uint32_t off = whole || r0 + lane < rows ? lsrc : (uint32_t)stage_h;
+      if constexpr (BITS == 0) {
+        dma_b32(lse0 + slot * STAGE_ROWS * 4, off * 4, uniform((const char*)(a.lse + l)));
+      } else {
+        dma_b128(sums0 + slot * STAGE_ROWS * 32, off * 32, uniform((const char*)(a.sums + 2 * l)));
+        dma_b128(sums0 + slot * STAGE_ROWS * 32 + STAGE_ROWS * 16, off * 32 + 16, uniform((const char*)(a.sums + 2 * l)));
       }
-      if (wave == 0) {
-        const long long at = r0 + lane < rows ? lrow : lbase;
-        dma_b32(lse0 + stage * STAGE_ROWS * 4, (const void*)(a.lse + at));
-        if constexpr (BITS == 4) dma_b128(sums0 + stage * STAGE_ROWS * 16, (const void*)(a.sums + at));
-        lhead += hr; lrow += lahead;
-        if (lhead >= m.G) { lhead -= m.G; lrow += lwrap; }
+    }
+    stage_t += ht;
+    if (hr) {
+      stage_h += hr;
+      const bool next = stage_h >= m.G;                 // (the token of the first row moves on by one more)
+      if (next) { stage_h -= m.G; ++stage_t; }
+      const auto turn = [&](int& hx, uint32_t& at, uint32_t per_head, uint32_t per_token) __attribute__((always_inline)) {
+        hx += hr;
+        at += hr * per_head;
+        if (hx >= m.G) { hx -= m.G; at += per_token - m.G * per_head; }
+        if (next) at -= per_token;
+      };
+#pragma unroll
+      for (int x = 0; x < PT; ++x) turn(h[x], src[x], head, token);
+      turn(lh, lsrc, 1, m.Hq);
+    }
+  };
+
+  // 4 bits: a chunk's codes and pairs are loaded one chunk ahead, its places in the pool two.
+  struct Raw { uint32_t code[KS], pair[NG], named; };
+  const auto place = [&](int chunk) __attribute__((always_inline)) {      // of the lane's key, as a row of the pool; -1: no such key
+    const int key = chunk * 128 * KT + wave * 32 * KT + c;
+    const int phys = key < s.n ? pool_page(m, b, key >> m.lpage) : -1;
+    return phys < 0 ? -1ll : ((long long)phys * m.Hkv + hk) * m.page + (key & (m.page - 1));
+  };
+  const auto fetch = [&](Raw& r, long long row) __attribute__((always_inline)) {
+    r.named = (uint32_t)__ballot(row >= 0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) r.code[ks] = row >= 0 ? ((const uint32_t*)a.k)[row * (D / 8) + ks * 2 + hb] : 0;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) r.pair[g] = row >= 0 ? a.km[row * NG + g] : 0;
+  };
+  const int chunk0 = it.item / a.nsplit, mine = 8 * (c / 8) + 4 * hb + (c >> 1) % 4;      // the key of 32 that the lane is left with at the end
+  Raw next;
+  long long after = -1;
+  if constexpr (BITS == 4) { fetch(next, place(chunk0)); if (chunk0 + items < chunks) after = place(chunk0 + items); }
+
+  int qrow[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) qrow[ks] = row_operand<D>(lane, ks);
+  bool loaded = false;                                  // the rows are in LDS, from the first that a chunk so far has wanted on
+  for (int chunk = chunk0; chunk < chunks; chunk += items) {
+    const int first_key = chunk * 128 * KT, key0 = first_key + wave * 32 * KT;
+    // the first stage with a row that sees a key of the workgroup
+    const long long row0 = m.causal ? (long long)max(0, first_key - s.first) * m.G : 0;
+    const int stage0 = first_key >= s.n || row0 >= rows ? stages : (int)max(0ll, row0 - from) / STAGE_ROWS;
+    float w[KT][16], before[KT];
+    uint32_t named[KT];                                 // keys that there are
+#pragma unroll
+    for (int x = 0; x < KT; ++x)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) w[x][v] = 0.f;
+#pragma unroll
+    for (int x = 0; x < KT; ++x) { named[x] = 0; before[x] = 0.f; }
+    if (stage0 < stages) {
+      if (!loaded) { start(stage0); issue(stage0); }
+      if (a.w && a.nsplit == 1) {                       // what the end adds to
+#pragma unroll
+        for (int x = 0; x < KT; ++x) if (mine + 32 * x < s.n - key0) before[x] = a.w[((long long)b * m.Hkv + hk) * most + key0 + 32 * x + mine];
       }
-    };
-    issue(0, row0);
-    wait_vmcnt<0>();
-    lds_barrier();
-    for (int r0 = row0, stage = 0; r0 < rows; r0 += STAGE_ROWS, stage ^= 1) {
-      if (r0 + STAGE_ROWS < rows) issue(stage ^ 1, r0 + STAGE_ROWS);
-#pragma unroll
-      for (int half = 0; half < STAGE_ROWS / 32; ++half) {
-        const char* const qt = lds + stage * STAGEB + half * 32 * ROWB;
-        bf16x8_t q[KS];
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) q[ks] = *(const bf16x8_t*)(qt + row_operand<D>(lane, ks));
-        const int row = r0 + half * 32 + c;
-        const float lse = lse_l[stage][half * 32 + c];
-        const float off = lse == -INFINITY ? INFINITY : lse * LOG2E;      // (a row without keys weighs none)
-        bf16x8_t sums;
-        if constexpr (BITS == 4) {
-          union { u32x4_t w; bf16x8_t v; } u;
-          u.w = hb ? u32x4_t{0, 0, 0, 0} : sums_l[stage][half * 32 + c];
-          sums = u.v;
-        }
+      bf16x8_t k[KT][KS], low;
+      float step[NG][BITS ? 16 : 1];
+      if constexpr (BITS == 0) {
 #pragma unroll
         for (int x = 0; x < KT; ++x) {
-          f32x16_t sc = zero16();
-          if constexpr (BITS == 0) {
+          const int key = key0 + 32 * x + c, phys = key < s.n ? pool_page(m, b, key >> m.lpage) : -1;
+          named[x] = (uint32_t)__ballot(phys >= 0);
+          const bf16raw* const p = (const bf16raw*)a.k + (phys < 0 ? 0 : phys * a.ks.page + (key & (m.page - 1)) * a.ks.token + hk * a.ks.head);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) sc = mfma32(k[x][ks], q[ks], sc);
+          for (int ks = 0; ks < KS; ++ks) {
+            const u32x4_t u = phys < 0 ? u32x4_t{0, 0, 0, 0} : *(const u32x4_t*)(p + ks * 16 + hb * 8);
+            k[x][ks] = *(const bf16x8_t*)&u;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          union { uint32_t w[4]; bf16x8_t v; } u;
+          const uint32_t even = next.code[ks] & 0x0F0F0F0Fu, odd = next.code[ks] >> 4 & 0x0F0F0F0Fu;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) u.w[j] = __float_as_uint((float)(even >> (8 * j) & 255)) >> 16 | __float_as_uint((float)(odd >> (8 * j) & 255));
+          k[0][ks] = u.v;
+        }
+        named[0] = next.named;
+        const uint32_t l0 = next.pair[0] >> 16, l1 = NG == 2 ? next.pair[NG - 1] >> 16 : 0;
+        union { uint32_t w[4]; bf16x8_t v; } u{{l0 | l0 << 16, l0 | l1 << 16, l1 | l1 << 16, 0}};
+        if (hb) { u.w[0] = 0xBF80BF80u; u.w[1] = 0xBF80u; u.w[2] = 0; }
+        low = u.v;
+        compiler_fence();
+#pragma unroll
+        for (int g = 0; g < NG; ++g) step_l[wave][g][c] = __uint_as_float(next.pair[g] << 16) * a.scale_log2e;
+        compiler_fence();
+#pragma unroll
+        for (int g = 0; g < NG; ++g)
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const f32x4_t z = *(const f32x4_t*)&step_l[wave][g][8 * y + 4 * hb];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) step[g][4 * y + j] = z[j];
+          }
+        compiler_fence();
+        if (chunk + items < chunks) { fetch(next, after); if (chunk + 2 * items < chunks) after = place(chunk + 2 * items); }
+      }
+      // Rows from which on all keys of the wave are seen.  (Keys that do not exist are left out at the end.)
+      const int last = min(key0 + 32 * KT, s.n) - 1;
+      const long long free_row = m.causal ? (long long)max(0, last - s.first) * m.G : 0;
+      if (!loaded) { wait_vmcnt<0>(); lds_barrier(); }
+      for (int stage = stage0; stage < stages; ++stage) {
+        if (!loaded && stage + 1 < stages) issue(stage + 1);
+        const int slot = stage % STAGES, r0 = from + stage * STAGE_ROWS;
+        const char* const qt = lds + slot * STAGEB;
+        const auto rows_of = [&](int half, bf16x8_t* q) __attribute__((always_inline)) {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) q[ks] = *(const bf16x8_t*)(qt + qrow[ks] + half * 32 * ROWB);
+        };
+        const auto offset = [&](int half) __attribute__((always_inline)) {
+          const float lse = lse_l[BITS ? 0 : slot][half * 32 + c];
+          return lse == -INFINITY ? INFINITY : lse * LOG2E;      // (a row without keys weighs none)
+        };
+        // exponents of 32 keys and 32 rows
+        const auto scores = [&](int x, int half, const bf16x8_t* q, f32x16_t* y) __attribute__((always_inline)) {
+          if constexpr (BITS == 0) {
+            y[0] = zero16();
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) y[0] = mfma32(k[x][ks], q[ks], y[0]);
           } else {
-            sc = mfma32(low, sums, sc);
 #pragma unroll
             for (int g = 0; g < NG; ++g) {
-              f32x16_t y = zero16();
+              y[g] = zero16();
 #pragma unroll
-              for (int ks = 0; ks < 4; ++ks) y = mfma32(k[x][4 * g + ks], q[4 * g + ks], y);
+              for (int ks = 0; ks < 4; ++ks) y[g] = mfma32(k[0][4 * g + ks], q[4 * g + ks], y[g]);
+            }
+            y[NG] = mfma32(low, *(const bf16x8_t*)&sums_l[slot][hb][half * 32 + c], zero16());
+          }
+        };
+        const auto weight = [&](const f32x16_t* y, float off, int v) __attribute__((always_inline)) {
+          if constexpr (BITS == 0) return __builtin_amdgcn_exp2f(fmaf(y[0][v], a.scale_log2e, -off));
+          float e = y[NG][v];
 #pragma unroll
-              for (int v = 0; v < 16; ++v) sc[v] = fmaf(step[g][v], y[v], sc[v]);
+          for (int g = 0; g < NG; ++g) e = fmaf(step[g][v], y[g][v], e);
+          return __builtin_amdgcn_exp2f(e);
+        };
+        constexpr int NY = BITS ? NG + 1 : 1, MT = KS + (BITS ? 1 : 0);
+        if (r0 >= free_row && r0 + STAGE_ROWS <= rows) {
+          // The products of a tile in turn with the weights of the one before, as written: left to itself the compiler puts all products
+          // first, and a wave's matrix core waits for its exponentials.
+          f32x16_t y[2][NY];
+          bf16x8_t q[KS];
+          rows_of(0, q);
+          const float off[2] = {BITS ? 0.f : offset(0), BITS ? 0.f : offset(1)};
+          scores(0, 0, q, y[0]);
+#pragma unroll
+          for (int i = 1; i <= 2 * KT; ++i) {
+            const int x = i % KT, half = i / KT, px = (i - 1) % KT, ph = (i - 1) / KT;
+            const bool more = i < 2 * KT;
+            f32x16_t* const z = y[i & 1];
+            if (KT == 1 && more) rows_of(half, q);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+              if (more) {
+                if (j == KS) z[NY - 1] = mfma32(low, *(const bf16x8_t*)&sums_l[slot][hb][half * 32 + c], zero16());
+                else if (BITS == 0) z[0] = mfma32(k[x][j], q[j], j ? z[0] : zero16());
+                else z[j / 4] = mfma32(k[0][j], q[j], j % 4 ? z[j / 4] : zero16());
+                if (x == KT - 1 && half == 0 && j < KS) q[j] = *(const bf16x8_t*)(qt + qrow[j] + 32 * ROWB);      // (KT 2: the second half's)
+              }
+#pragma unroll
+              for (int v = 16 * max(0, j - 1) / (MT - 1); v < 16 * j / (MT - 1); ++v) w[px][v] += weight(y[(i - 1) & 1], off[ph], v);
+              if (more) __builtin_amdgcn_sched_barrier(0);
             }
           }
-          if (r0 + half * 32 >= free_row && r0 + half * 32 + 32 <= rows) {
+        } else {
 #pragma unroll
-            for (int v = 0; v < 16; ++v) w[x][v] += __builtin_amdgcn_exp2f(fmaf(sc[v], a.scale_log2e, -off));
-          } else {
-            const int lim = row >= rows ? 0 : m.causal ? s.first + row / m.G + 1 - (key0 + 32 * x + 4 * hb) : 32;
+          for (int half = 0; half < 2; ++half) {
+            bf16x8_t q[KS];
+            rows_of(half, q);
+            const float off = BITS ? 0.f : offset(half);
+            const int row = r0 + half * 32 + c;
+            const int lim = row >= rows ? 0 : m.causal ? s.first + row / m.G + 1 - (key0 + 4 * hb) : 32 * KT;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-              const float p = __builtin_amdgcn_exp2f(fmaf(sc[v], a.scale_log2e, -off));
-              w[x][v] += 8 * (v / 4) + v % 4 < lim ? p : 0.f;
+            for (int x = 0; x < KT; ++x) {
+              f32x16_t y[NY];
+              scores(x, half, q, y);
+#pragma unroll
+              for (int v = 0; v < 16; ++v) {
+                const float p = weight(y, off, v);
+                w[x][v] += 32 * x + 8 * (v / 4) + v % 4 < lim ? p : 0.f;
+              }
             }
           }
         }
+        if (!loaded) { wait_vmcnt<0>(); lds_barrier(); }
       }
-      wait_vmcnt<0>();
-      lds_barrier();
+      loaded = stages <= STAGES;
     }
-  }
-  // Over the 32 rows that the lanes hold: at every step a lane passes on half of its keys, and is left with one of the 16.
+    // Over the 32 rows that the lanes hold: at every step a lane passes on half of its keys, and is left with one of the 16.
 #pragma unroll
-  for (int x = 0; x < KT; ++x) {
-    float v[16];
+    for (int x = 0; x < KT; ++x) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = w[x][i];
+      for (int bit = 16, n = 8; bit >= 2; bit >>= 1, n >>= 1) {
+        const bool up = lane & bit;
 #pragma unroll
-    for (int bit = 16, n = 8; bit >= 2; bit >>= 1, n >>= 1) {
-      const bool up = lane & bit;
-#pragma unroll
-      for (int i = 0; i < n; ++i) {
-        const float give = up ? v[i] : v[i + n], mine = up ? v[i + n] : v[i];
-        v[i] = mine + __shfl_xor(give, bit);
+        for (int i = 0; i < n; ++i) {
+          const float give = up ? w[x][i] : w[x][i + n], mine = up ? w[x][i + n] : w[x][i];
+          w[x][i] = mine + __shfl_xor(give, bit);
+        }
       }
+      w[x][0] += __shfl_xor(w[x][0], 1);
+      const int at = key0 + 32 * x + mine;
+      if ((c & 1) || at >= most) continue;
+      const long long to = ((long long)b * m.Hkv + hk) * most + at;
+      const float sum = named[x] >> mine & 1 ? w[x][0] : 0.f;
+      if (a.nsplit > 1) a.part[(long long)share * m.B * m.Hkv * most + to] = sum;
+      else a.out[to] = at >= s.n ? 0.f : a.w ? fmaf(a.decay, stage0 < stages ? before[x] : a.w[to], sum) : sum;
     }
-    v[0] += __shfl_xor(v[0], 1);
-    const int i = c >> 1, at = key0 + 32 * x + 8 * (i / 4) + 4 * hb + i % 4;
-    if ((c & 1) || at >= most) continue;
-    const long long to = ((long long)b * m.Hkv + hk) * most + at;
-    const float sum = at < s.n && pool_page(m, b, at >> m.lpage) >= 0 ? v[0] : 0.f;
-    if (a.nsplit > 1) a.part[(long long)share * m.B * m.Hkv * most + to] = sum;
-    else a.out[to] = at >= s.n ? 0.f : a.w ? fmaf(a.decay, a.w[to], sum) : sum;
   }
 }
 
@@ -564,11 +668,11 @@ __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int pages) {
 }  // namespace
 
 namespace {
-struct WeightsShape { bool wide; int chunks, nsplit; size_t sums, part; };
-WeightsShape weights_shape(int dtype, int bits, const BlockDims& m) {
+struct WeightsShape { bool wide; int chunks, items, nsplit; size_t sums, part; };      // items: workgroups that share a head's chunks of keys
+WeightsShape weights_shape(int dtype, int bits, const BlockDims& m, const KeyStride& qs) {
   WeightsShape s{};
   const long long rows = (long long)m.max_q * m.G, keys = (long long)m.max_pages << m.lpage;
-  s.wide = dtype == ADACLUSTER_BF16 && rows > 32;
+  s.wide = dtype == ADACLUSTER_BF16 && rows > 32 && qs.token < (1 << 24) && qs.head < (1 << 24);      // (offsets of 64 rows in 32 bits)
   s.nsplit = 1;
   if (!s.wide) return s;
   s.chunks = (int)((keys + (bits ? 127 : 255)) / (bits ? 128 : 256));
@@ -577,21 +681,27 @@ WeightsShape weights_shape(int dtype, int bits, const BlockDims& m) {
   long long n = 512 / wg;
   if (n > rows / 512) n = rows / 512;
   if (n > 1) s.nsplit = (int)n;
-  s.sums = bits ? align_up((size_t)m.q_rows * m.Hq * 16, 256) : 0;
+  // Where the rows stay in LDS a workgroup takes several chunks of keys, four workgroups a CU in all.
+  s.items = s.chunks;
+  if (rows <= STAGES * STAGE_ROWS) {
+    const long long most = (1024 + (long long)m.Hkv * m.B - 1) / ((long long)m.Hkv * m.B);
+    if (most < s.items) s.items = (int)most;
+  }
+  s.sums = bits ? align_up((size_t)m.q_rows * m.Hq * 32, 256) : 0;
   s.part = s.nsplit > 1 ? (size_t)s.nsplit * m.B * m.Hkv * keys * 4 : 0;
   return s;
 }
 }  // namespace
 
-size_t cache_weights_bytes(int dtype, int bits, const BlockDims& m) {
-  const WeightsShape s = weights_shape(dtype, bits, m);
+size_t cache_weights_bytes(int dtype, int bits, const BlockDims& m, const KeyStride& qs) {
+  const WeightsShape s = weights_shape(dtype, bits, m, qs);
   return s.sums + s.part;
 }
 
 int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, WeightsArgs a, void* ws) {
-  const WeightsShape sh = weights_shape(dtype, bits, a.m);
+  const WeightsShape sh = weights_shape(dtype, bits, a.m, a.qs);
   if (sh.wide) {
-    const long long heads = (long long)a.m.Hkv * a.m.B, grid = xcd_grid(heads, (long long)sh.chunks * sh.nsplit);
+    const long long heads = (long long)a.m.Hkv * a.m.B, grid = xcd_grid(heads, (long long)sh.items * sh.nsplit);
     const long long pre = ((long long)a.m.q_rows * a.m.Hq + 63) / 64;
     if (!grid_fits(grid) || !grid_fits(pre)) return ADACLUSTER_E_UNSUPPORTED;
     a.sums = (const u32x4_t*)ws;
@@ -601,11 +711,11 @@ int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, WeightsArgs 
     if (bits) {
       if (d == 64) weights_sums<64><<<(int)pre, 256, 0, s>>>(a, (u32x4_t*)ws); else weights_sums<128><<<(int)pre, 256, 0, s>>>(a, (u32x4_t*)ws);
       if (int rc = launched()) return rc;
-      if (d == 64) cache_weights_wide<4, 64><<<(int)grid, 256, 0, s>>>(a, sh.chunks, split);
-      else cache_weights_wide<4, 128><<<(int)grid, 256, 0, s>>>(a, sh.chunks, split);
+      if (d == 64) cache_weights_wide<4, 64><<<(int)grid, 256, 0, s>>>(a, sh.chunks, sh.items, split);
+      else cache_weights_wide<4, 128><<<(int)grid, 256, 0, s>>>(a, sh.chunks, sh.items, split);
     } else {
-      if (d == 64) cache_weights_wide<0, 64><<<(int)grid, 256, 0, s>>>(a, sh.chunks, split);
-      else cache_weights_wide<0, 128><<<(int)grid, 256, 0, s>>>(a, sh.chunks, split);
+      if (d == 64) cache_weights_wide<0, 64><<<(int)grid, 256, 0, s>>>(a, sh.chunks, sh.items, split);
+      else cache_weights_wide<0, 128><<<(int)grid, 256, 0, s>>>(a, sh.chunks, sh.items, split);
     }
     if (int rc = launched()) return rc;
     if (sh.nsplit > 1) weights_join<<<(int)((heads * ((long long)a.m.max_pages << a.m.lpage) / 4 + 255) / 256), 256, 0, s>>>(a);
