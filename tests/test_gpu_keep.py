@@ -223,7 +223,8 @@ class Evicted:
                 assert kept[b, g].tolist() == stay + [-1] * (self.keep - m), (b, g)
                 full = torch.zeros_like(self.w[b, g])
                 full[:m] = self.w[b, g, stay]
-                assert torch.equal(new_w[b, g].cpu().view(torch.int32), full.view(torch.int32)), (b, g)      # (bits: a NaN stays one)
+                got = new_w[b, g].cpu()
+                assert torch.equal(got.isnan(), full.isnan()) and torch.equal(got.nan_to_num(7.0), full.nan_to_num(7.0)), (b, g)
                 for pg in range(-(-m // page)):
                     to, here = int(self.new_table[b, pg]), stay[pg * page:(pg + 1) * page]
                     if not 0 <= to < want[0].shape[0] or to == int(x.table[b, pg]):
