@@ -102,8 +102,14 @@ __device__ __forceinline__ int row_limit(const BlockDims& m, const Group& g, int
   if (i < 0 || i >= s.nq) return -1;
   return m.causal ? max(0, min(s.n, s.first + i + 1)) : s.n;
 }
-// How many of `nsplit` workgroups share `pages` pages: 256 keys each at least.
-__device__ __forceinline__ int splits_of(const BlockDims& m, int pages, int nsplit) { return min(nsplit, max(1, ((pages << m.lpage) + 255) >> 8)); }
+// How many of `nsplit` workgroups with `rows` rows each share `pages` pages: 256 keys each at least, and four times as many as rows, so that
+// a partial result (four bytes a value) stays a quarter of what it is made of (128 rows over 16 384 keys of 8 heads, d = 128: 43 us with
+// 256 keys each, 36 with 512).
+__host__ __device__ constexpr int share_keys(int rows) { return rows > 64 ? 4 * rows : 256; }
+__device__ __forceinline__ int splits_of(const BlockDims& m, int pages, int nsplit, int rows) {
+  const int keys = share_keys(rows);
+  return min(nsplit, max(1, ((pages << m.lpage) + keys - 1) / keys));
+}
 
 // Entry e of a list of pages (NULL: all pages in order), or -1: past the pages, or not above the entry before it.
 __device__ __forceinline__ int list_page(const int32_t* __restrict__ list, int e, int pages) {
@@ -295,7 +301,7 @@ int launch_block_attn_wide(hipStream_t s, int d, const BlockAttnArgs& a);
 
 // A launch of block_attn in one of the split forms: R * 16 rows a workgroup, `items` of them (GROUP: tiles * Hkv), a.nsplit each.
 void launch_block_attn_part(hipStream_t s, int dtype, int bits, int d, Rows rows, int R, int rts, long long items, const BlockAttnArgs& a);
-void launch_block_attn_wide_part(hipStream_t s, int d, int TR, int tiles, const BlockAttnArgs& a);      // GROUP: 64 or 128 rows (block_wide.hip)
+void launch_block_attn_wide_part(hipStream_t s, int bits, int d, int TR, int tiles, const BlockAttnArgs& a);      // GROUP: 64 or 128 rows (block_wide.hip)
 
 // (block_prefix.hip)
 size_t prefix_attn_bytes(int dtype, int bits, int d, const BlockAttnArgs& a);

@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D =
     base_row = (id - first_tile(m, group.q0, g, R * 16)) * R * 16;
     rows = (group.q1 - group.q0) * m.G;
     s = BlockSeq{group.q0, group.q1 - group.q0, 0, group.pages << m.lpage, 0};
-    every = splits_of(m, group.pages, a.nsplit);
+    every = splits_of(m, group.pages, a.nsplit, 16 * R);
     if (base_row < 0 || base_row >= rows || split >= every) return;      // (below 0: groups that do not ascend)
   } else {
     const int rt = id % rts; id /= rts;
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(256, R == 1 && !(sizeof(T) == 4 && BITS == 0 && D =
     if constexpr (ROWS == Rows::TAIL) {
       const int g = group_of(a.gr, b);
       if (g >= 0) from = group_at(m, a.gr, g).pages;
-      every = splits_of(m, ((s.n + m.page - 1) >> m.lpage) - from, a.nsplit);
+      every = splits_of(m, ((s.n + m.page - 1) >> m.lpage) - from, a.nsplit, 16 * R);
       if (split >= every) return;
     }
   }

@@ -21,23 +21,24 @@ PrefixShape shape_of(int dtype, int bits, const BlockAttnArgs& a) {
   PrefixShape s;
   const long long most = (long long)m.B * m.max_q, queries = m.q_rows < most ? m.q_rows : most;
   const long long rows = (queries * m.G + a.gr.groups - 1) / (a.gr.groups > 0 ? a.gr.groups : 1);      // of a group, on average
-  s.wide = dtype == ADACLUSTER_BF16 && !bits && rows > 32 && a.ks.token < (1 << 25) && a.vs.token < (1 << 25);
-  s.TR = s.wide ? (rows <= 64 ? 64 : 128) : rows <= 16 ? 16 : 32;
+  s.wide = dtype == ADACLUSTER_BF16 && rows > 32 && (bits || (a.ks.token < (1 << 25) && a.vs.token < (1 << 25)));
+  s.TR = s.wide ? (rows <= 64 && bits ? 64 : 128) : rows <= 16 ? 16 : 32;
   s.tiles = a.gr.groups ? (int)((long long)m.q_rows * m.G / s.TR) + a.gr.groups : 0;
-  // Few tiles: the pages are split among the workgroups that the GPU holds at a time, 256 keys each at least.
+  // Few tiles: the pages are split among the workgroups that the GPU holds at a time.
   const long long busy = (rows + s.TR - 1) / s.TR * a.gr.groups * m.Hkv, keys = (long long)m.max_pages << m.lpage;
-  const auto share = [&](long long items, int places) {
+  const auto share = [&](long long items, int places, int tile) {
+    const int least = share_keys(tile);
     long long n = items > 0 ? places / items : 1;
-    if (n > (keys + 255) / 256) n = (keys + 255) / 256;
+    if (n > (keys + least - 1) / least) n = (keys + least - 1) / least;
     return (int)(n < 1 ? 1 : n);
   };
-  s.nsplit = share(busy, s.wide ? 768 : s.TR == 16 ? 512 : 256);
+  s.nsplit = share(busy, s.wide ? (bits ? 512 : 768) : s.TR == 16 ? 512 : 256, s.TR);
   s.tail = m;
   const int r = m.qblock * m.G;
   s.R = r <= 16 ? 1 : 2;
   s.rts = (r + 16 * s.R - 1) / (16 * s.R);
   s.items = (long long)s.rts * m.nb * m.Hkv * m.B;
-  s.tsplit = share(s.items, s.R == 1 ? 512 : 256);
+  s.tsplit = share(s.items, s.R == 1 ? 512 : 256, 16 * s.R);
   s.rows = (size_t)s.tiles * m.Hkv * s.nsplit * s.TR;
   s.trows = (size_t)s.items * s.tsplit * 16 * s.R;
   return s;
@@ -73,9 +74,9 @@ __global__ __launch_bounds__(256) void prefix_join(BlockAttnArgs a, int rts, int
       group = group_at(m, a.gr, g);
       const int x = (t - group.q0) * m.G + head % m.G;
       rec = ((long long)(first_tile(m, group.q0, g, TR) + x / TR) * m.Hkv + hk) * nsplit * TR + x % TR;
-      parts = group.pages && t >= group.q0 && t < group.q1 ? splits_of(m, group.pages, nsplit) : 0;      // (else rows do not ascend)
+      parts = group.pages && t >= group.q0 && t < group.q1 ? splits_of(m, group.pages, nsplit, TR) : 0;      // (else rows do not ascend)
     }
-    own = splits_of(m, ((s.n + m.page - 1) >> m.lpage) - group.pages, a.nsplit);
+    own = splits_of(m, ((s.n + m.page - 1) >> m.lpage) - group.pages, a.nsplit, 16 * R);
     const int blk = i / m.qblock, row = (i - blk * m.qblock) * m.G + head % m.G, rt = row / (16 * R);
     trec = (((((long long)b * m.Hkv + hk) * m.nb + blk) * rts + rt) * a.nsplit) * (16 * R) + row % (16 * R);
   }
@@ -150,7 +151,7 @@ int launch_prefix_attn(hipStream_t st, int dtype, int bits, int d, BlockAttnArgs
   if (s.tiles) {
     BlockAttnArgs x = a;
     x.nsplit = s.nsplit; x.part_o = so; x.part_ml = sml;
-    if (s.wide) launch_block_attn_wide_part(st, d, s.TR, s.tiles, x);
+    if (s.wide) launch_block_attn_wide_part(st, bits, d, s.TR, s.tiles, x);
     else launch_block_attn_part(st, dtype, bits, d, Rows::GROUP, s.TR / 16, 1, (long long)s.tiles * a.m.Hkv, x);
     if (int rc = launched()) return rc;
   }
