@@ -57,59 +57,8 @@ __device__ __forceinline__ int pool_page(const BlockDims& m, int b, int pg) {
   return (unsigned)t < (unsigned)m.num_pages ? t : -1;
 }
 
-// ---- groups of sequences that share their first pages ----
-struct BlockGroups { int groups; const int32_t *cu_group, *prefix; };      // groups 0: none
-
-// Sequences [b0, b1) of group g, their query rows [q0, q1), and the whole pages of what they share (of what the first one holds).
-struct Group { int b0, b1, q0, q1, pages; };
-__device__ __forceinline__ Group group_at(const BlockDims& m, const BlockGroups& gr, int g) {
-  Group x{0, 0, 0, 0, 0};
-  x.b0 = min(max(gr.cu_group[g], 0), m.B);
-  x.b1 = min(max(gr.cu_group[g + 1], x.b0), m.B);
-  x.q0 = min(max(m.cu_q[x.b0], 0), m.q_rows);
-  x.q1 = min(max(m.cu_q[x.b1], x.q0), m.q_rows);
-  if (x.b0 < x.b1) x.pages = min(max(gr.prefix[g], 0), min(max(m.seq_lens[x.b0], 0), m.max_pages << m.lpage)) >> m.lpage;
-  return x;
-}
-// The last of the groups for which `at_most` holds, or -1: by whole waves, of a condition that holds for the first ones.
-template <typename F> __device__ __forceinline__ int last_group(int groups, F at_most) {
-  int n = 0;
-  for (int g0 = 0; g0 < groups; g0 += 64) {
-    const int g = g0 + (threadIdx.x & 63);
-    n += __popcll(__ballot(g < groups && at_most(min(g, groups - 1))));
-  }
-  return n - 1;
-}
-// The group of sequence b, or -1.
-__device__ __forceinline__ int group_of(const BlockGroups& gr, int b) {
-  const int g = last_group(gr.groups, [&](int x) { return gr.cu_group[x] <= b; });
-  return g >= 0 && b < gr.cu_group[g + 1] ? g : -1;
-}
-// Tiles of TR rows (a query of a head each) start anew at every group: the first tile of a group whose rows start at q0.  Groups
-// that follow each other have different ones, and all lie below q_rows * G / TR + groups.
-__device__ __forceinline__ int first_tile(const BlockDims& m, int q0, int g, int TR) { return q0 * m.G / TR + g; }
-
-// The key below which query row t of the group sees, or -1 (a row of no sequence).
-__device__ __forceinline__ int row_limit(const BlockDims& m, const Group& g, int t) {
-  int b = g.b0 + (t - g.q0);                           // (one query a sequence)
-  if (m.max_q > 1 || b >= g.b1 || m.cu_q[b] > t || m.cu_q[b + 1] <= t) {
-    int lo = g.b0, hi = g.b1;                          // cu_q[lo] <= t < cu_q[hi]
-    while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (m.cu_q[mid] <= t) lo = mid; else hi = mid; }
-    b = lo;
-  }
-  const BlockSeq s = block_seq(m, b);
-  const int i = t - s.q0;
-  if (i < 0 || i >= s.nq) return -1;
-  return m.causal ? max(0, min(s.n, s.first + i + 1)) : s.n;
-}
-// How many of `nsplit` workgroups with `rows` rows each share `pages` pages: 256 keys each at least, and four times as many as rows, so that
-// a partial result (four bytes a value) stays a quarter of what it is made of (128 rows over 16 384 keys of 8 heads, d = 128: 43 us with
-// 256 keys each, 36 with 512).
-__host__ __device__ constexpr int share_keys(int rows) { return rows > 64 ? 4 * rows : 256; }
-__device__ __forceinline__ int splits_of(const BlockDims& m, int pages, int nsplit, int rows) {
-  const int keys = share_keys(rows);
-  return min(nsplit, max(1, ((pages << m.lpage) + keys - 1) / keys));
-}
+// Groups of sequences that share their first pages (prefix_part.h); groups 0: none.
+struct BlockGroups { int groups; const int32_t *cu_group, *prefix; };
 
 // Entry e of a list of pages (NULL: all pages in order), or -1: past the pages, or not above the entry before it.
 __device__ __forceinline__ int list_page(const int32_t* __restrict__ list, int e, int pages) {
@@ -289,23 +238,24 @@ struct BlockAttnArgs {
   float scale_log2e;
   int nsplit;
   float *part_o, *part_ml;                   // [item][split][rows][d], [item][split][rows][2]
-  BlockGroups gr;
 };
-// Whose rows a workgroup of the attention kernels has: those of a sequence, with its whole list of keys; those of all sequences of a
-// group, over the pages that they share; those of a sequence, over its pages behind them.  The latter two leave partial results.
-enum class Rows { OWN, GROUP, TAIL };
 size_t block_attn_bytes(const BlockDims& m, int d, bool listed);
 int launch_block_attn(hipStream_t s, int dtype, int bits, int d, BlockAttnArgs a, void* ws);
 bool block_wide_takes(const BlockAttnArgs& a, int dtype, int bits);      // (block_wide.hip)
 int launch_block_attn_wide(hipStream_t s, int d, const BlockAttnArgs& a);
 
-// A launch of block_attn in one of the split forms: R * 16 rows a workgroup, `items` of them (GROUP: tiles * Hkv), a.nsplit each.
-void launch_block_attn_part(hipStream_t s, int dtype, int bits, int d, Rows rows, int R, int rts, long long items, const BlockAttnArgs& a);
-void launch_block_attn_wide_part(hipStream_t s, int bits, int d, int TR, int tiles, const BlockAttnArgs& a);      // GROUP: 64 or 128 rows (block_wide.hip)
-
 // (block_prefix.hip)
-size_t prefix_attn_bytes(int dtype, int bits, int d, const BlockAttnArgs& a);
-int launch_prefix_attn(hipStream_t s, int dtype, int bits, int d, BlockAttnArgs a, void* ws);
+// Two kinds of partial results, [item][share][rows][d] and [item][share][rows][2]: of tiles of a group's rows over the pages it shares, and of a
+// sequence's rows over its pages behind them.
+struct PrefixArgs : BlockAttnArgs {
+  BlockGroups gr;
+  int grid, split;                           // workgroups of the former, which come first, and their division among the XCDs
+  int tiles, TR, shares;                     // tiles of all groups at most, rows of a tile, workgroups that share a group's pages at most
+  int rts, TT, tshares;                      // of the latter: tiles of a block of queries, their rows, shares
+  float *group_o, *group_ml, *tail_o, *tail_ml;
+};
+size_t prefix_attn_bytes(int dtype, int bits, int d, const PrefixArgs& a);
+int launch_prefix_attn(hipStream_t s, int dtype, int bits, int d, PrefixArgs a, void* ws);
 
 // (block_keep.hip)
 struct WeightsArgs {

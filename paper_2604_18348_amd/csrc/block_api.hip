@@ -114,7 +114,7 @@ double scale_of(const adacluster_block_params* p) { return p->softmax_scale > 0.
 float log2_scale(const adacluster_block_params* p) { return (float)(scale_of(p) * 1.4426950408889634); }      // (rounded once: logits of 20 feel it)
 
 // what the shape of a call of prefix_attn follows from
-int prefix_args(const adacluster_block_params* p, int32_t groups, BlockAttnArgs* a) {
+int prefix_args(const adacluster_block_params* p, int32_t groups, PrefixArgs* a) {
   if (int rc = check(p, &a->m)) return rc;
   if (!p->num_pages) return fail(ADACLUSTER_E_BADARG, "prefix_attn: num_pages must be >= 1 (a paged cache)");
   if (groups < 0 || groups > p->B) return fail(ADACLUSTER_E_BADSHAPE, "groups must be in [0,B] (groups=%d)", groups);
@@ -248,7 +248,7 @@ int adacluster_block_attn_backward(const adacluster_block_params* p, const void*
 }
 
 int adacluster_prefix_workspace_bytes(const adacluster_block_params* p, int32_t groups, size_t* bytes) {
-  BlockAttnArgs a{};
+  PrefixArgs a{};
   if (int rc = prefix_args(p, groups, &a)) return rc;
   if (!bytes) return fail(ADACLUSTER_E_BADARG, "bytes is NULL");
   *bytes = prefix_attn_bytes(p->dtype, p->bits, p->d, a);
@@ -258,7 +258,7 @@ int adacluster_prefix_workspace_bytes(const adacluster_block_params* p, int32_t 
 int adacluster_prefix_attn(const adacluster_block_params* p, int32_t groups, const void* q, const int32_t* cu_q, const void* k_pool, const void* v_pool,
                            const uint32_t* k_meta, const uint32_t* v_meta, const int32_t* seq_lens, const int32_t* page_table, const int32_t* cu_group,
                            const int32_t* prefix_lens, void* o, float* lse, void* ws, size_t ws_bytes, void* stream) {
-  BlockAttnArgs a{};
+  PrefixArgs a{};
   if (int rc = prefix_args(p, groups, &a)) return rc;
   if (!cu_q || (groups && (!cu_group || !prefix_lens))) return fail(ADACLUSTER_E_BADARG, "prefix_attn: NULL tensor pointer");
   if (int rc = check_keys(&a.m, nullptr, seq_lens, page_table)) return rc;

@@ -1,54 +1,32 @@
 // Attention over a paged cache for groups of sequences that share their first pages: the shared pages meet the rows of the whole group
-// at once, every sequence's rows its own pages behind them, and a row's partial results are joined.
-#include "block.h"
+// at once, every sequence's rows its own pages behind them, both in one launch; then a row's partial results are joined.
+#include "block_few.h"
+#include "block_wide.h"
 
 namespace adac {
 
 namespace {
 
-struct PrefixShape {
-  int TR;                          // rows of a tile of a group: 16 or 32 (block_attn), 64 or 128 (block_attn_wide)
-  bool wide;
-  int tiles, nsplit;               // of all groups at most; workgroups that share a group's pages
-  BlockDims tail;                  // blocks of queries of a sequence
-  int R, rts, tsplit;
-  long long items;                 // of the tails
-  size_t rows, trows;              // of partial results
-};
-
-PrefixShape shape_of(int dtype, int bits, const BlockAttnArgs& a) {
-  const BlockDims& m = a.m;
-  PrefixShape s;
-  const long long most = (long long)m.B * m.max_q, queries = m.q_rows < most ? m.q_rows : most;
-  const long long rows = (queries * m.G + a.gr.groups - 1) / (a.gr.groups > 0 ? a.gr.groups : 1);      // of a group, on average
-  s.wide = dtype == ADACLUSTER_BF16 && rows > 32 && (bits || (a.ks.token < (1 << 25) && a.vs.token < (1 << 25)));
-  s.TR = s.wide ? (rows <= 64 && bits ? 64 : 128) : rows <= 16 ? 16 : 32;
-  s.tiles = a.gr.groups ? (int)((long long)m.q_rows * m.G / s.TR) + a.gr.groups : 0;
-  // Few tiles: the pages are split among the workgroups that the GPU holds at a time.
-  const long long busy = (rows + s.TR - 1) / s.TR * a.gr.groups * m.Hkv, keys = (long long)m.max_pages << m.lpage;
-  const auto share = [&](long long items, int places, int tile) {
-    const int least = share_keys(tile);
-    long long n = items > 0 ? places / items : 1;
-    if (n > (keys + least - 1) / least) n = (keys + least - 1) / least;
-    return (int)(n < 1 ? 1 : n);
-  };
-  s.nsplit = share(busy, s.wide ? (bits ? 512 : 768) : s.TR == 16 ? 512 : 256, s.TR);
-  s.tail = m;
-  const int r = m.qblock * m.G;
-  s.R = r <= 16 ? 1 : 2;
-  s.rts = (r + 16 * s.R - 1) / (16 * s.R);
-  s.items = (long long)s.rts * m.nb * m.Hkv * m.B;
-  s.tsplit = share(s.items, s.R == 1 ? 512 : 256, 16 * s.R);
-  s.rows = (size_t)s.tiles * m.Hkv * s.nsplit * s.TR;
-  s.trows = (size_t)s.items * s.tsplit * 16 * s.R;
-  return s;
+template <typename T, int BITS, int D, int R>
+__global__ __launch_bounds__(256, (few_waves<T, BITS, D, R>())) void prefix_few(PrefixArgs a) {
+  __shared__ FewLds<T, BITS, D> sh;
+  few_rows<T, BITS, D, R, true>(a, 1, blockIdx.x, sh);
+}
+template <int D>
+__global__ __launch_bounds__(256, 3) void prefix_wide(PrefixArgs a) {
+  __shared__ WideLds<D, 4, true> sh;
+  wide_rows<D, 4, true>(a, 1, 1, sh);
+}
+template <int D>
+__global__ __launch_bounds__(256, 2) void prefix_codes(PrefixArgs a) {
+  __shared__ CodesLds<D> sh;
+  wide_codes<D>(a, sh);
 }
 
 // Joins a row's partial results: those of the pages its group shares, then those of its own.  D / 4 lanes read a result; `per` such
 // slots share a row's results, each every per-th with a running maximum, and are joined through LDS.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void prefix_join(BlockAttnArgs a, int rts, int R, int TR, int nsplit, int per, const float* __restrict__ shared_o,
-                                                   const float* __restrict__ shared_ml) {
+__global__ __launch_bounds__(256) void prefix_join(PrefixArgs a, int per) {
   constexpr int LPR = D / 4, SLOTS = 256 / LPR;
   __shared__ __align__(16) float jo[SLOTS][D];
   __shared__ float jm[SLOTS][2];
@@ -73,18 +51,18 @@ __global__ __launch_bounds__(256) void prefix_join(BlockAttnArgs a, int rts, int
     if (g >= 0) {
       group = group_at(m, a.gr, g);
       const int x = (t - group.q0) * m.G + head % m.G;
-      rec = ((long long)(first_tile(m, group.q0, g, TR) + x / TR) * m.Hkv + hk) * nsplit * TR + x % TR;
-      parts = group.pages && t >= group.q0 && t < group.q1 ? splits_of(m, group.pages, nsplit, TR) : 0;      // (else rows do not ascend)
+      rec = ((long long)(first_tile(m, group.q0, g, a.TR) + x / a.TR) * m.Hkv + hk) * a.shares * a.TR + x % a.TR;
+      parts = group.pages && t >= group.q0 && t < group.q1 ? splits_of(m, group.pages, a.shares, a.TR) : 0;      // (else rows do not ascend)
     }
-    own = splits_of(m, ((s.n + m.page - 1) >> m.lpage) - group.pages, a.nsplit, 16 * R);
-    const int blk = i / m.qblock, row = (i - blk * m.qblock) * m.G + head % m.G, rt = row / (16 * R);
-    trec = (((((long long)b * m.Hkv + hk) * m.nb + blk) * rts + rt) * a.nsplit) * (16 * R) + row % (16 * R);
+    own = splits_of(m, ((s.n + m.page - 1) >> m.lpage) - group.pages, a.tshares, a.TT);
+    const int blk = i / m.qblock, row = (i - blk * m.qblock) * m.G + head % m.G, rt = row / a.TT;
+    trec = (((((long long)b * m.Hkv + hk) * m.nb + blk) * a.rts + rt) * a.tshares) * a.TT + row % a.TT;
   }
   const auto at = [&](int z, const float*& ml) __attribute__((always_inline)) {
     const bool sh = z < parts;
-    const long long x = sh ? rec + (long long)z * TR : trec + (long long)(z - parts) * 16 * R;
-    ml = (sh ? shared_ml : a.part_ml) + x * 2;
-    return (sh ? shared_o : a.part_o) + x * D + d0;
+    const long long x = sh ? rec + (long long)z * a.TR : trec + (long long)(z - parts) * a.TT;
+    ml = (sh ? a.group_ml : a.tail_ml) + x * 2;
+    return (sh ? a.group_o : a.tail_o) + x * D + d0;
   };
   float top = -INFINITY, all = 0.f;
   f32x4_t o{0.f, 0.f, 0.f, 0.f};
@@ -134,40 +112,82 @@ __global__ __launch_bounds__(256) void prefix_join(BlockAttnArgs a, int rts, int
   if (d0 == 0 && a.lse) a.lse[(long long)t * m.Hq + head] = all == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(all)) * LN2;
 }
 
+// Which kernel, what it is given: fills a's shape.  `rows`, `trows`: of partial results.
+struct PrefixShape { bool wide; int R; size_t rows, trows; };
+PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
+  const BlockDims& m = a->m;
+  PrefixShape s;
+  const long long most = (long long)m.B * m.max_q, queries = m.q_rows < most ? m.q_rows : most;
+  const int groups = a->gr.groups, block = m.qblock * m.G;
+  const long long rows = groups ? (queries * m.G + groups - 1) / groups : block;      // of a group, on average
+  s.wide = dtype == ADACLUSTER_BF16 && (rows > 16 || block > 16) && (bits || (a->ks.token < (1 << 25) && a->vs.token < (1 << 25)));
+  s.R = rows > 16 || block > 16 ? 2 : 1;
+  a->TR = s.wide ? 128 : 16 * s.R;
+  a->TT = s.wide ? (block > 32 ? 128 : 32) : 16 * s.R;
+  a->tiles = groups ? (int)((long long)m.q_rows * m.G / a->TR) + groups : 0;
+  a->rts = (block + a->TT - 1) / a->TT;
+  const long long items = (long long)a->rts * m.nb * m.Hkv * m.B, busy = (rows + a->TR - 1) / a->TR * groups * m.Hkv;
+  // Few tiles: the pages are split among the workgroups that the GPU holds at a time.
+  const long long keys = (long long)m.max_pages << m.lpage;
+  const int places = s.wide ? (bits ? 512 : 768) : s.R == 1 ? 512 : 256;
+  const auto share = [&](long long items, int tile) {
+    const int least = share_keys(tile);
+    long long n = items > 0 ? places / items : 1;
+    if (n > (keys + least - 1) / least) n = (keys + least - 1) / least;
+    return (int)(n < 1 ? 1 : n);
+  };
+  a->shares = share(busy, a->TR);
+  a->tshares = share(items, a->TT);
+  a->split = xcd_split(m.Hkv);
+  s.rows = (size_t)a->tiles * m.Hkv * a->shares * a->TR;
+  s.trows = (size_t)items * a->tshares * a->TT;
+  return s;
+}
+
+template <typename T, int BITS, int D>
+void go(hipStream_t st, const PrefixShape& s, int wg, const PrefixArgs& a) {
+  if constexpr (sizeof(T) == 2) {
+    if (s.wide) {
+      if constexpr (BITS) prefix_codes<D><<<wg, 256, 0, st>>>(a);
+      else prefix_wide<D><<<wg, 256, 0, st>>>(a);
+      return;
+    }
+  }
+  if (s.R == 1) prefix_few<T, BITS, D, 1><<<wg, 256, 0, st>>>(a);
+  else prefix_few<T, BITS, D, 2><<<wg, 256, 0, st>>>(a);
+}
+
 }  // namespace
 
-size_t prefix_attn_bytes(int dtype, int bits, int d, const BlockAttnArgs& a) {
-  const PrefixShape s = shape_of(dtype, bits, a);
+size_t prefix_attn_bytes(int dtype, int bits, int d, const PrefixArgs& a) {
+  PrefixArgs x = a;
+  const PrefixShape s = shape_of(dtype, bits, &x);
   return align_up(s.rows * d * 4, 256) + align_up(s.rows * 8, 256) + align_up(s.trows * d * 4, 256) + align_up(s.trows * 8, 256);
 }
 
-int launch_prefix_attn(hipStream_t st, int dtype, int bits, int d, BlockAttnArgs a, void* ws) {
-  const PrefixShape s = shape_of(dtype, bits, a);
-  if (!grid_fits((long long)s.tiles * a.m.Hkv * s.nsplit) || !grid_fits(s.items * (s.tsplit > s.R ? s.tsplit : s.R))) return ADACLUSTER_E_UNSUPPORTED;
+int launch_prefix_attn(hipStream_t st, int dtype, int bits, int d, PrefixArgs a, void* ws) {
+  const PrefixShape s = shape_of(dtype, bits, &a);
   char* p = (char*)ws;
   const auto take = [&](size_t n) { char* const x = p; p += align_up(n, 256); return (float*)x; };
-  float* const so = take(s.rows * d * 4);
-  float* const sml = take(s.rows * 8);
-  if (s.tiles) {
-    BlockAttnArgs x = a;
-    x.nsplit = s.nsplit; x.part_o = so; x.part_ml = sml;
-    if (s.wide) launch_block_attn_wide_part(st, bits, d, s.TR, s.tiles, x);
-    else launch_block_attn_part(st, dtype, bits, d, Rows::GROUP, s.TR / 16, 1, (long long)s.tiles * a.m.Hkv, x);
-    if (int rc = launched()) return rc;
-  }
-  a.nsplit = s.tsplit;
-  a.part_o = take(s.trows * d * 4);
-  a.part_ml = take(s.trows * 8);
-  launch_block_attn_part(st, dtype, bits, d, Rows::TAIL, s.R, s.rts, s.items, a);
-  if (int rc = launched()) return rc;
-  // up to eight results a slot, and two workgroups a CU
+  a.group_o = take(s.rows * d * 4);
+  a.group_ml = take(s.rows * 8);
+  a.tail_o = take(s.trows * d * 4);
+  a.tail_ml = take(s.trows * 8);
+  const long long grid = a.tiles ? xcd_grid(a.m.Hkv, (long long)a.tiles * a.shares) : 0, wg = grid + (long long)a.rts * a.m.nb * a.m.Hkv * a.m.B * a.tshares;
+  // the join: up to eight results a slot, and two workgroups a CU
   const int slots = 1024 / d;
   const long long rows = (long long)a.m.B * a.m.max_q * a.m.Hq;
   int per = 1;
-  while (per < slots && (per * 8 < s.nsplit + s.tsplit || rows * per < 512 * slots)) per *= 2;
-  const long long wg = (rows * per + slots - 1) / slots;
-  if (!grid_fits(wg)) return ADACLUSTER_E_UNSUPPORTED;
-#define JOIN(T, D) prefix_join<T, D><<<(int)wg, 256, 0, st>>>(a, s.rts, s.R, s.TR, s.nsplit, per, so, sml)
+  while (per < slots && (per * 8 < a.shares + a.tshares || rows * per < 512 * slots)) per *= 2;
+  const long long jwg = (rows * per + slots - 1) / slots;
+  if (!grid_fits(wg) || !grid_fits(jwg)) return ADACLUSTER_E_UNSUPPORTED;
+  a.grid = (int)grid;
+#define GO(T, D) if (bits) go<T, 4, D>(st, s, (int)wg, a); else go<T, 0, D>(st, s, (int)wg, a)
+  if (dtype == ADACLUSTER_BF16) { if (d == 64) { GO(bf16raw, 64); } else { GO(bf16raw, 128); } }
+  else { if (d == 64) { GO(float, 64); } else { GO(float, 128); } }
+#undef GO
+  if (int rc = launched()) return rc;
+#define JOIN(T, D) prefix_join<T, D><<<(int)jwg, 256, 0, st>>>(a, per)
   if (dtype == ADACLUSTER_BF16) { if (d == 64) JOIN(bf16raw, 64); else JOIN(bf16raw, 128); }
   else { if (d == 64) JOIN(float, 64); else JOIN(float, 128); }
 #undef JOIN

@@ -1,11 +1,11 @@
-// What the bf16 kernels for many rows share: tiles of 32 (forward) or 64 rows staged in LDS by direct loads, read by all waves (internal).
+// What the bf16 kernels for many rows share: tiles of 32 (forward) or 64 rows staged in LDS by direct loads, read by all waves; the forward walks (internal).
 //
 // 32x32x16 products (v_mfma_f32_32x32x16_bf16): half the LDS reads a product of the 16x16 tiles.  A result holds in lane l column
 // l % 32 and, in value v, row 8 (v / 4) + 4 (l / 32) + v % 4; eight consecutive values are the operand of the next product, whose
 // other operand is read column-wise (two transposing reads: rows 4 (l / 32) .. + 3 and 8 further) to match.
 #pragma once
 
-#include "block.h"
+#include "prefix_part.h"
 
 namespace adac {
 
@@ -67,5 +67,477 @@ __device__ __forceinline__ HeadItem xcd_item(int id, int heads, int items, int s
 }
 static inline int xcd_split(long long heads) { return heads % 8 == 0 ? 1 : heads % 4 == 0 ? 2 : heads % 2 == 0 ? 4 : 8; }
 static inline long long xcd_grid(long long heads, long long items) { const int s = xcd_split(heads); return heads * s * ((items + s - 1) / s); }
+
+// NW waves of 32 rows each.  A tile's keys and values go global -> LDS directly, 16 bytes a lane, one tile ahead of the products.  Rows past
+// a sequence's end are read from the last row there is in their sixteenth (or the page's first) and masked: nothing behind the end is
+// touched.  Bound by what lies between the products (exponentials, roundings, LDS reads), so waves a SIMD count: tiles of 32 keys and three
+// waves (two with NW = 2) against 64 keys and two, or one: 3 sequences up to 8 192 tokens, 32 pages of 64, 16 / 4 heads, d = 128 385 us
+// (489), 17 776 tokens, 30 heads, d = 64 730 (744), chunks of 2 x 1 024 tokens, NW = 2, d = 128 193 (303).
+template <int D, int NW, bool PART> struct WideLds {
+  static constexpr int TILEB = 32 * D * 2, STAGES = PART ? 3 : 2;
+  __align__(16) char lds[STAGES * 2 * TILEB];
+  int2 pages_l[LIST];
+  int32_t counts[NW];
+};
+// PART: a share of a group's or a sequence's pages (prefix_part.h), whose result is left as a partial one.
+template <int D, int NW, bool PART, typename Args>
+__device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, WideLds<D, NW, PART>& sh) {
+  constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
+  constexpr int TK = 32, PARTS = TK / 16;      // keys a tile: one product's rows
+  constexpr int PT = TK * CH / NT, TILEB = TK * ROWB;
+  constexpr int STAGES = WideLds<D, NW, PART>::STAGES;
+  char* const lds = sh.lds;
+  int2* const pages_l = sh.pages_l;
+  int32_t* const counts = sh.counts;
+  const BlockDims& m = a.m;
+  int hk, b, i = 0, t0, rows, base_row, from = 0, to = INT32_MAX;      // pages or entries of the list
+  BlockSeq s;
+  Part part;
+  if constexpr (PART) {
+    if (!part_of(a, blockIdx.x, part)) return;
+    hk = part.hk; b = part.b; s = part.s; t0 = part.t0; rows = part.rows; base_row = part.base_row; from = part.from; to = part.to;
+  } else {
+    const HeadItem it = xcd_item(blockIdx.x, m.B * m.Hkv, m.nb * rts, split);
+    if (it.head < 0) return;
+    const int rt = it.item % rts;
+    i = it.item / rts; hk = it.head % m.Hkv; b = it.head / m.Hkv;
+    s = block_seq(m, b);
+    t0 = i * m.qblock; rows = min(m.qblock, s.nq - t0) * m.G; base_row = rt * NT / 2;
+    if (t0 >= s.nq || base_row >= rows) return;
+  }
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
+
+  const int row = base_row + wave * 32 + c, tok = t0 + row / m.G, head = hk * m.G + row % m.G;
+  int part_lim = -1;
+  if constexpr (PART) { if (row < rows) part_lim = part_limit(m, part, tok); }
+  const bool there = PART ? part_lim >= 0 : row < rows;
+  bf16x8_t qf[KS];
+  {
+    const bf16raw* const p = (const bf16raw*)a.q + (long long)(s.q0 + tok) * a.qs.token + (long long)head * a.qs.head + hb * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const u32x4_t w = there ? *(const u32x4_t*)(p + ks * 16) : u32x4_t{0, 0, 0, 0};
+      qf[ks] = *(const bf16x8_t*)&w;
+    }
+  }
+  const int lim = there ? (PART ? part_lim : m.causal ? min(s.n, s.first + tok + 1) : s.n) : INT32_MAX;      // (a row that is not there needs no mask)
+  const int wave_first = base_row + wave * 32;
+  const bool wave_has_rows = wave_first < rows;
+  int minlim = m.causal ? min(s.n, s.first + t0 + wave_first / m.G + 1) : s.n;       // keys below: seen by all rows of the wave
+  const int last = min(base_row + NT / 2, rows) - 1;
+  int maxlim = m.causal ? min(s.n, s.first + t0 + last / m.G + 1) : s.n;
+  if constexpr (PART) {
+    int low = lim;
+#pragma unroll
+    for (int x = 1; x < 32; x *= 2) low = min(low, __shfl_xor(low, x));
+    minlim = uniform(low); maxlim = s.n;
+  }
+  const int pages = maxlim > 0 ? (maxlim + m.page - 1) >> m.lpage : 0;
+  const int32_t* const list = !PART && a.sel ? a.sel + (((long long)b * m.nb + i) * m.Hkv + hk) * m.topk : nullptr;
+  const int entries = list ? m.topk : min(pages, to);
+
+  f32x16_t oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) oacc[db] = zero16();
+  // The weights are taken relative to a reference that moves only when a tile's sum leaves its range (see below); from where it
+  // starts, tiles a row sees nothing of leave sum and accumulator at zero.
+  const float sc = a.scale_log2e;
+  float mref = softmax_start(sc), lrun = 0.f;
+
+  int lrow[PT], piece[PT];                         // this thread's pieces of a tile
+#pragma unroll
+  for (int x = 0; x < PT; ++x) {
+    const int item = tid + x * NT;
+    lrow[x] = item / CH;
+    piece[x] = ((item % CH) ^ swz<D>(lrow[x])) * 16;
+  }
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void_t*)lds;
+  const int lsub = m.lpage - 4, ktok = (int)(a.ks.token * 2), vtok = (int)(a.vs.token * 2);
+  int kaddr[KS], vaddr[DB][2];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) kaddr[ks] = row_operand<D>(lane, ks);
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) vaddr[db][x] = col_operand<D>(lane, db, x);
+
+  for (int e0 = from; e0 < entries; e0 += LIST) {
+    const int n = fill_list<NT>(m, b, list, e0, 1, entries, pages, pages_l, counts);
+    const int parts = n << lsub, tiles = (parts + PARTS - 1) / PARTS;
+    if (!tiles) continue;
+    auto issue = [&](int stage, int t) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < PT; ++x) {                // a wave's request lies inside one sixteenth of a page
+        const int part = min(t * PARTS + (((wave * 64 + x * NT) / CH) >> 4), parts - 1);
+        const int2 pp = pages_l[part >> lsub];
+        const int pg = uniform(pp.x), phys = uniform(pp.y);
+        int sub = part & ((1 << lsub) - 1), have = s.n - ((pg << m.lpage) + sub * 16);      // rows of it that exist
+        if (have <= 0) { sub = 0; have = 1; }
+        const int r = min(lrow[x] & 15, have - 1);
+        const uint32_t dst = lds0 + stage * 2 * TILEB + (wave * 64 + x * NT) * 16;
+        dma_b128(dst, (uint32_t)(r * ktok + piece[x]), uniform((const char*)a.k + row_at(m, s, a.ks, phys, pg, sub, hk) * 2));
+        dma_b128(dst + TILEB, (uint32_t)(r * vtok + piece[x]), uniform((const char*)a.v + row_at(m, s, a.vs, phys, pg, sub, hk) * 2));
+      }
+    };
+    issue(0, 0);
+    if constexpr (STAGES == 2) {
+      wait_vmcnt<0>();
+      lds_barrier();
+    } else if (tiles > 1) {
+      issue(1, 1);
+    }
+    int stage = 0;
+    for (int t = 0; t < tiles; ++t) {
+      if constexpr (STAGES == 2) {
+        if (t + 1 < tiles) issue((t + 1) & 1, t + 1);
+        stage = t & 1;
+      } else {                                      // two tiles on their way: the prefix of one group waits for memory, not for products
+        if (t + 1 < tiles) wait_vmcnt<2 * PT>();
+        else wait_vmcnt<0>();
+        lds_barrier();
+        if (t) stage = stage == 2 ? 0 : stage + 1;
+        if (t + 2 < tiles) issue(stage == 0 ? 2 : stage - 1, t + 2);
+      }
+      if (wave_has_rows) {
+        const char* const kt = lds + stage * 2 * TILEB;
+        const char* const vt = kt + TILEB;
+        f32x16_t sacc = zero16();
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sacc = mfma32(*(const bf16x8_t*)(kt + kaddr[ks]), qf[ks], sacc);
+        int key0[PARTS];
+        bool whole = true;
+#pragma unroll
+        for (int x = 0; x < PARTS; ++x) {
+          const int part = t * PARTS + x, pg = uniform(pages_l[min(part, parts - 1) >> lsub].x);
+          key0[x] = part < parts ? (pg << m.lpage) + (part & ((1 << lsub) - 1)) * 16 : INT32_MAX - 64;
+          whole = whole && key0[x] + 16 <= minlim;
+        }
+        if (!whole) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if (key0[v >> 3] + 8 * ((v >> 2) & 1) + 4 * hb + (v & 3) >= lim) sacc[v] = -INFINITY;
+        }
+        // p = 2^((s - reference) scale): any reference gives the same result as long as nothing overflows.  The row sum of the tile
+        // tells (on the first tile with a score above -inf it is infinite): only then is the tile's maximum taken, the reference
+        // moved up to it and the accumulator scaled.
+        bf16x8_t pf[2];
+        float rsum;
+        auto weights = [&]() __attribute__((always_inline)) {
+          const float off = mref * sc;
+          float part[2];
+#pragma unroll
+          for (int s2 = 0; s2 < 2; ++s2) {
+            union { uint32_t w[4]; bf16x8_t v; } u;
+            part[s2] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float p0 = __builtin_amdgcn_exp2f(fmaf(sacc[8 * s2 + 2 * j], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(sacc[8 * s2 + 2 * j + 1], sc, -off));
+              u.w[j] = pack_bf16x2(p0, p1);
+              part[s2] += p0;                       // (not the rounded ones: the sum's logarithm is an output)
+              part[s2] += p1;
+            }
+            pf[s2] = u.v;
+          }
+          rsum = part[0] + part[1];
+        };
+        weights();
+        if (__any(!(rsum <= 65536.f))) {
+          float top = sacc[0];
+#pragma unroll
+          for (int v = 0; v < 16; ++v) top = fmaxf(top, sacc[v]);
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float next = fmaxf(mref, top), alpha = __builtin_amdgcn_exp2f((mref - next) * sc);
+          mref = next;
+          lrun *= alpha;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+          weights();
+        }
+        lrun += rsum;
+#pragma unroll
+        for (int s2 = 0; s2 < 2; ++s2) {
+          const char* const p = vt + 16 * s2 * ROWB;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) oacc[db] = mfma32(join_tr(read_tr(p + vaddr[db][0]), read_tr(p + vaddr[db][1])), pf[s2], oacc[db]);
+        }
+      }
+      if constexpr (STAGES == 2) {
+        wait_vmcnt<0>();
+        lds_barrier();
+      }
+    }
+    lds_barrier();                                  // before the list is filled again
+  }
+
+  if (!there) return;
+  const float all = lrun + __shfl_xor(lrun, 32), inv = all == 0.f ? 0.f : 1.f / all;
+  if constexpr (PART) {
+    const long long rec = part.rec + wave * 32 + c;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        *(f32x4_t*)(part.o + rec * D + db * 32 + 8 * x + 4 * hb) = f32x4_t{oacc[db][4 * x], oacc[db][4 * x + 1], oacc[db][4 * x + 2], oacc[db][4 * x + 3]};
+    if (hb == 0) { part.ml[rec * 2] = mref * sc; part.ml[rec * 2 + 1] = all; }
+    return;
+  }
+  bf16raw* const out = (bf16raw*)a.o + (long long)(s.q0 + tok) * a.os.token + (long long)head * a.os.head + 4 * hb;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *(uint2*)(out + db * 32 + 8 * x) = uint2{pack_bf16x2(oacc[db][4 * x] * inv, oacc[db][4 * x + 1] * inv), pack_bf16x2(oacc[db][4 * x + 2] * inv, oacc[db][4 * x + 3] * inv)};
+  if (hb == 0 && a.lse) a.lse[(long long)(s.q0 + tok) * m.Hq + head] = all == 0.f ? -INFINITY : fmaf(mref, sc, __builtin_amdgcn_logf(all)) * LN2;
+}
+
+// The same walk over 4-bit pages, for parts.  A tile's codes come one tile ahead into registers and go to LDS as bfloat16: those
+// of keys by themselves, those of values less 8.  Per group g of 64 dimensions
+//   scores   sum of step_g (c . q) + low_g sum q, scaled: the latter one more product, of (low, low, low) with three bfloat16 parts of sum q;
+//   values   weights times step_g, rounded to bfloat16, times c - 8 (a rounding weighs codes about their middle), and the sum of weights
+//            times low_g + 8 step_g, unrounded.
+// Steps are applied to 16 keys a lane, which reads them from LDS: with them LDS is what bounds it (24 of 48 wide reads a tile).
+template <int D> struct CodesLds {
+  static constexpr int TK = 32, NG = D / 64, TILEB = TK * D * 2;
+  __align__(16) char lds[4 * TILEB];
+  __align__(16) float kstep_l[2][NG][TK], vstep_l[2][NG][TK], vlow_l[2][NG][TK];
+  uint32_t klow_l[2][TK][NG];
+  int2 pages_l[LIST];
+  int32_t counts[4];
+};
+template <int D>
+__device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D>& sh) {
+  constexpr int NT = 256, KS = D / 16, DB = D / 32, NG = D / 64, ROWB = D * 2, WORDS = D / 8;      // words of eight codes a row
+  constexpr int TK = 32, PT = TK * WORDS / NT, TILEB = TK * ROWB;
+  char* const lds = sh.lds;
+  auto &kstep_l = sh.kstep_l, &vstep_l = sh.vstep_l, &vlow_l = sh.vlow_l;
+  auto& klow_l = sh.klow_l;
+  int2* const pages_l = sh.pages_l;
+  int32_t* const counts = sh.counts;
+  const BlockDims& m = a.m;
+  Part part;
+  if (!part_of(a, blockIdx.x, part)) return;
+  const BlockSeq& s = part.s;
+  const int hk = part.hk, b = part.b, rows = part.rows, base_row = part.base_row, from = part.from, to = part.to;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
+
+  const int row = base_row + wave * 32 + c, tok = part.t0 + row / m.G, head = hk * m.G + row % m.G;
+  const int part_lim = row < rows ? part_limit(m, part, tok) : -1;
+  const bool there = part_lim >= 0;
+  const int lim = there ? part_lim : INT32_MAX;
+  const float sc = a.scale_log2e;
+  bf16x8_t qf[KS], qsum;
+  {
+    const bf16raw* const p = (const bf16raw*)a.q + (long long)(s.q0 + tok) * a.qs.token + (long long)head * a.qs.head + hb * 8;
+    float sum[NG];
+#pragma unroll
+    for (int x = 0; x < NG; ++x) sum[x] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const u32x4_t w = there ? *(const u32x4_t*)(p + ks * 16) : u32x4_t{0, 0, 0, 0};
+      qf[ks] = *(const bf16x8_t*)&w;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sum[ks / 4] += __uint_as_float(w[j] << 16) + __uint_as_float(w[j] & 0xFFFF0000u);
+    }
+    uint32_t h[6] = {0, 0, 0, 0, 0, 0};
+#pragma unroll
+    for (int x = 0; x < NG; ++x) {
+      float v = (sum[x] + __shfl_xor(sum[x], 32)) * sc;
+#pragma unroll
+      for (int y = 0; y < 3; ++y) { h[3 * x + y] = __float_as_uint(v) >> 16; v -= __uint_as_float(h[3 * x + y] << 16); }      // (cut: what is left is exact)
+    }
+    union { uint32_t w[4]; bf16x8_t v; } u{{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, 0}};
+    if (hb) u.w[0] = u.w[1] = u.w[2] = 0;
+    qsum = u.v;
+  }
+  const bool wave_has_rows = base_row + wave * 32 < rows;
+  int minlim = lim;
+#pragma unroll
+  for (int x = 1; x < 32; x *= 2) minlim = min(minlim, __shfl_xor(minlim, x));
+  minlim = uniform(minlim);
+
+  f32x16_t oacc[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) oacc[db] = zero16();
+  // The weights are taken relative to a reference (scaled here) that moves only when a tile's sum leaves its range, as above.
+  float mref = -3.4028e38f, lrun = 0.f, corr[NG];
+#pragma unroll
+  for (int x = 0; x < NG; ++x) corr[x] = 0.f;
+
+  int kaddr[KS], vaddr[DB][2];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) kaddr[ks] = row_operand<D>(lane, ks);
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) vaddr[db][x] = col_operand<D>(lane, db, x);
+
+  const int lsub = m.lpage - 4;
+  for (int e0 = from; e0 < to; e0 += LIST) {
+    const int n = fill_list<NT>(m, b, nullptr, e0, 1, to, to, pages_l, counts);
+    const int parts = n << lsub, count = (parts + 1) / 2;
+    if (!count) continue;
+    uint32_t kc[PT], vc[PT], pair[(2 * TK * NG + NT - 1) / NT];
+    const auto fetch = [&](int t) __attribute__((always_inline)) {      // (past the last: that one again, masked; behind the end lies
+                                                      // anything: its weight of 0 must meet a number)
+      long long at[2];                                // the rows of the pool where the sixteenths start, and their positions
+      int key[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int part = min(t * 2 + x, parts - 1);
+        const int2 pp = pages_l[part >> lsub];
+        const int in = (part & ((1 << lsub) - 1)) * 16;
+        at[x] = (((long long)uniform(pp.y) * m.Hkv + hk) << m.lpage) + in;
+        key[x] = (uniform(pp.x) << m.lpage) + in;
+      }
+#pragma unroll
+      for (int x = 0; x < PT; ++x) {
+        const int item = tid + x * NT, half = ((wave * 64 + x * NT) / WORDS) >> 4;
+        const uint32_t off = ((item / WORDS & 15) * WORDS + item % WORDS) * 4;
+        kc[x] = *(const uint32_t*)((const char*)a.k + (half ? at[1] : at[0]) * (WORDS * 4) + off);
+        vc[x] = *(const uint32_t*)((const char*)a.v + (half ? at[1] : at[0]) * (WORDS * 4) + off);
+      }
+#pragma unroll
+      for (int x = 0; x < (2 * TK * NG + NT - 1) / NT; ++x) {          // a pair of a key or value and group a thread
+        const int item = tid + x * NT, r = item / NG % TK;
+        if (item >= 2 * TK * NG) break;
+        const int first = r >> 4 ? key[1] : key[0];
+        pair[x] = first + (r & 15) < s.n ? (item < TK * NG ? a.km : a.vm)[((r >> 4 ? at[1] : at[0]) + (r & 15)) * NG + item % NG] : 0;
+      }
+    };
+    const auto expand = [&](int stage) __attribute__((always_inline)) {
+#pragma unroll
+      for (int x = 0; x < PT; ++x) {
+        const int item = tid + x * NT, r = item / WORDS, at = r * ROWB + ((item % WORDS) ^ swz<D>(r)) * 16;
+        u32x4_t k, v;
+        const uint32_t even = kc[x] & 0x0F0F0F0Fu, odd = kc[x] >> 4 & 0x0F0F0F0Fu, mid = vc[x] ^ 0x88888888u;      // (a code less 8: four bits with a sign)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          k[j] = __float_as_uint((float)(even >> (8 * j) & 255)) >> 16 | __float_as_uint((float)(odd >> (8 * j) & 255));
+          v[j] = __float_as_uint((float)((int)(mid << (28 - 8 * j)) >> 28)) >> 16 | __float_as_uint((float)((int)(mid << (24 - 8 * j)) >> 28));
+        }
+        *(u32x4_t*)(lds + stage * 2 * TILEB + at) = k;
+        *(u32x4_t*)(lds + stage * 2 * TILEB + TILEB + at) = v;
+      }
+#pragma unroll
+      for (int x = 0; x < (2 * TK * NG + NT - 1) / NT; ++x) {
+        const int item = tid + x * NT, r = item / NG % TK, gr = item % NG;
+        if (item >= 2 * TK * NG) break;
+        const float step = __uint_as_float(pair[x] << 16), low = __uint_as_float(pair[x] & 0xFFFF0000u);
+        if (item < TK * NG) { kstep_l[stage][gr][r] = step * sc; klow_l[stage][r][gr] = pair[x] >> 16; }
+        else { vstep_l[stage][gr][r] = step; vlow_l[stage][gr][r] = fmaf(8.f, step, low); }
+      }
+    };
+    fetch(0);
+    expand(0);
+    __syncthreads();
+    for (int t = 0; t < count; ++t) {
+      const int stage = t & 1;
+      if (t + 1 < count) fetch(t + 1);
+      if (wave_has_rows) {
+        const char* const kt = lds + stage * 2 * TILEB;
+        const char* const vt = kt + TILEB;
+        f32x16_t sacc;
+        {
+          const uint32_t l0 = klow_l[stage][c][0], l1 = NG == 2 ? klow_l[stage][c][NG - 1] : 0;
+          union { uint32_t w[4]; bf16x8_t v; } u{{l0 | l0 << 16, l0 | l1 << 16, l1 | l1 << 16, 0}};
+          sacc = mfma32(u.v, qsum, zero16());
+          f32x16_t y[NG];
+#pragma unroll
+          for (int x = 0; x < NG; ++x) {
+            y[x] = zero16();
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks) y[x] = mfma32(*(const bf16x8_t*)(kt + kaddr[4 * x + ks]), qf[4 * x + ks], y[x]);
+          }
+#pragma unroll
+          for (int x = 0; x < NG; ++x)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+              const f32x4_t step = *(const f32x4_t*)&kstep_l[stage][x][8 * z + 4 * hb];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) sacc[4 * z + j] = fmaf(step[j], y[x][4 * z + j], sacc[4 * z + j]);
+            }
+        }
+        int key0[2];
+        bool whole = true;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int part = t * 2 + x, pg = uniform(pages_l[min(part, parts - 1) >> lsub].x);
+          key0[x] = part < parts ? (pg << m.lpage) + (part & ((1 << lsub) - 1)) * 16 : INT32_MAX - 64;
+          whole = whole && key0[x] + 16 <= minlim;
+        }
+        if (!whole) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if (key0[v >> 3] + 8 * ((v >> 2) & 1) + 4 * hb + (v & 3) >= lim) sacc[v] = -INFINITY;
+        }
+        float p[16], rsum;
+        const auto weights = [&]() __attribute__((always_inline)) {
+          float part[2] = {0.f, 0.f};
+#pragma unroll
+          for (int v = 0; v < 16; ++v) { p[v] = __builtin_amdgcn_exp2f(sacc[v] - mref); part[v >> 3] += p[v]; }
+          rsum = part[0] + part[1];
+        };
+        weights();
+        if (__any(!(rsum <= 65536.f))) {
+          float top = sacc[0];
+#pragma unroll
+          for (int v = 0; v < 16; ++v) top = fmaxf(top, sacc[v]);
+          top = fmaxf(top, __shfl_xor(top, 32));
+          const float next = fmaxf(mref, top), alpha = __builtin_amdgcn_exp2f(mref - next);
+          mref = next;
+          lrun *= alpha;
+#pragma unroll
+          for (int x = 0; x < NG; ++x) corr[x] *= alpha;
+#pragma unroll
+          for (int db = 0; db < DB; ++db) oacc[db] *= alpha;
+          weights();
+        }
+        lrun += rsum;
+#pragma unroll
+        for (int x = 0; x < NG; ++x) {
+          bf16x8_t pf[2];
+#pragma unroll
+          for (int s2 = 0; s2 < 2; ++s2) {
+            union { uint32_t w[4]; bf16x8_t v; } u;
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              const int at = 16 * s2 + 8 * z + 4 * hb, v0 = 8 * s2 + 4 * z;
+              const f32x4_t step = *(const f32x4_t*)&vstep_l[stage][x][at], low = *(const f32x4_t*)&vlow_l[stage][x][at];
+#pragma unroll
+              for (int j = 0; j < 2; ++j) u.w[2 * z + j] = pack_bf16x2(p[v0 + 2 * j] * step[2 * j], p[v0 + 2 * j + 1] * step[2 * j + 1]);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) corr[x] = fmaf(p[v0 + j], low[j], corr[x]);
+            }
+            pf[s2] = u.v;
+          }
+#pragma unroll
+          for (int s2 = 0; s2 < 2; ++s2) {
+            const char* const q = vt + 16 * s2 * ROWB;
+#pragma unroll
+            for (int db = 2 * x; db < 2 * x + 2; ++db) oacc[db] = mfma32(join_tr(read_tr(q + vaddr[db][0]), read_tr(q + vaddr[db][1])), pf[s2], oacc[db]);
+          }
+        }
+      }
+      if (t + 1 < count) expand(stage ^ 1);
+      __syncthreads();
+    }
+  }
+
+  if (!there) return;
+  const float all = lrun + __shfl_xor(lrun, 32);
+#pragma unroll
+  for (int x = 0; x < NG; ++x) corr[x] += __shfl_xor(corr[x], 32);
+  const long long rec = part.rec + wave * 32 + c;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      f32x4_t o;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] = oacc[db][4 * x + j] + corr[db / 2];
+      *(f32x4_t*)(part.o + rec * D + db * 32 + 8 * x + 4 * hb) = o;
+    }
+  if (hb == 0) { part.ml[rec * 2] = mref; part.ml[rec * 2 + 1] = all; }
+}
 
 }  // namespace adac
