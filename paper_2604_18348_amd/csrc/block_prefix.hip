@@ -17,10 +17,14 @@ __global__ __launch_bounds__(256, 3) void prefix_wide(PrefixArgs a) {
   __shared__ WideLds<D, 4, true> sh;
   wide_rows<D, 4, true>(a, 1, 1, sh);
 }
-template <int D>
-__global__ __launch_bounds__(256, 2) void prefix_codes(PrefixArgs a) {
-  __shared__ CodesLds<D> sh;
-  wide_codes<D>(a, sh);
+// 4 bits: a sequence's own few rows take codes straight into their products (16 rows; with the others' walk 109 us, so 7?)
+template <int D, int WK>
+__global__ __launch_bounds__(256, 2) void prefix_codes(PrefixArgs a, bool few) {
+  using Codes = CodesLds<D, WK>;
+  using Few = FewLds<bf16raw, 4, D>;
+  __shared__ __align__(16) char sh[sizeof(Codes) > sizeof(Few) ? sizeof(Codes) : sizeof(Few)];
+  if (few && (int)blockIdx.x >= a.grid) few_rows<bf16raw, 4, D, 1, true>(a, 1, blockIdx.x, *(Few*)sh);
+  else wide_codes<D, WK>(a, *(Codes*)sh);
 }
 
 // Joins a row's partial results: those of the pages its group shares, then those of its own.  D / 4 lanes read a result; `per` such
@@ -122,8 +126,8 @@ PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
   const long long rows = groups ? (queries * m.G + groups - 1) / groups : block;      // of a group, on average
   s.wide = dtype == ADACLUSTER_BF16 && (rows > 16 || block > 16) && (bits || (a->ks.token < (1 << 25) && a->vs.token < (1 << 25)));
   s.R = rows > 16 || block > 16 ? 2 : 1;
-  a->TR = s.wide ? 128 : 16 * s.R;
-  a->TT = s.wide ? (block > 32 ? 128 : 32) : 16 * s.R;
+  a->TR = s.wide ? (bits && rows <= 64 && block <= 64 ? 64 : 128) : 16 * s.R;
+  a->TT = s.wide ? (bits && block <= 16 ? 16 : bits ? a->TR : block > 32 ? 128 : 32) : 16 * s.R;
   a->tiles = groups ? (int)((long long)m.q_rows * m.G / a->TR) + groups : 0;
   a->rts = (block + a->TT - 1) / a->TT;
   const long long items = (long long)a->rts * m.nb * m.Hkv * m.B, busy = (rows + a->TR - 1) / a->TR * groups * m.Hkv;
@@ -148,7 +152,10 @@ template <typename T, int BITS, int D>
 void go(hipStream_t st, const PrefixShape& s, int wg, const PrefixArgs& a) {
   if constexpr (sizeof(T) == 2) {
     if (s.wide) {
-      if constexpr (BITS) prefix_codes<D><<<wg, 256, 0, st>>>(a);
+      if constexpr (BITS) {
+        if (a.TR == 64) prefix_codes<D, 2><<<wg, 256, 0, st>>>(a, a.TT == 16);
+        else prefix_codes<D, 1><<<wg, 256, 0, st>>>(a, a.TT == 16);
+      }
       else prefix_wide<D><<<wg, 256, 0, st>>>(a);
       return;
     }

@@ -183,8 +183,8 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
     if constexpr (STAGES == 2) {
       wait_vmcnt<0>();
       lds_barrier();
-    } else if (tiles > 1) {
-      issue(1, 1);
+    } else {
+      for (int x = 1; x < STAGES - 1 && x < tiles; ++x) issue(x, x);
     }
     int stage = 0;
     for (int t = 0; t < tiles; ++t) {
@@ -192,11 +192,12 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
         if (t + 1 < tiles) issue((t + 1) & 1, t + 1);
         stage = t & 1;
       } else {                                      // two tiles on their way: the prefix of one group waits for memory, not for products
-        if (t + 1 < tiles) wait_vmcnt<2 * PT>();
+        if (STAGES > 3 && t + 2 < tiles) wait_vmcnt<4 * PT>();
+        else if (t + 1 < tiles) wait_vmcnt<2 * PT>();
         else wait_vmcnt<0>();
         lds_barrier();
-        if (t) stage = stage == 2 ? 0 : stage + 1;
-        if (t + 2 < tiles) issue(stage == 0 ? 2 : stage - 1, t + 2);
+        if (t) stage = stage == STAGES - 1 ? 0 : stage + 1;
+        if (t + STAGES - 1 < tiles) issue(stage == 0 ? STAGES - 1 : stage - 1, t + STAGES - 1);
       }
       if (wave_has_rows) {
         const char* const kt = lds + stage * 2 * TILEB;
@@ -296,18 +297,19 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
 //   values   weights times step_g, rounded to bfloat16, times c - 8 (a rounding weighs codes about their middle), and the sum of weights
 //            times low_g + 8 step_g, unrounded.
 // Steps are applied to 16 keys a lane, which reads them from LDS: with them LDS is what bounds it (24 of 48 wide reads a tile).
-template <int D> struct CodesLds {
-  static constexpr int TK = 32, NG = D / 64, TILEB = TK * D * 2;
+// WK of the four waves share rows, each with 32 keys of a tile of its own, and are joined at the end.
+template <int D, int WK> struct CodesLds {
+  static constexpr int TK = 32 * WK, NG = D / 64, TILEB = TK * D * 2;
   __align__(16) char lds[4 * TILEB];
   __align__(16) float kstep_l[2][NG][TK], vstep_l[2][NG][TK], vlow_l[2][NG][TK];
   uint32_t klow_l[2][TK][NG];
   int2 pages_l[LIST];
   int32_t counts[4];
 };
-template <int D>
-__device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D>& sh) {
+template <int D, int WK>
+__device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, WK>& sh) {
   constexpr int NT = 256, KS = D / 16, DB = D / 32, NG = D / 64, ROWB = D * 2, WORDS = D / 8;      // words of eight codes a row
-  constexpr int TK = 32, PT = TK * WORDS / NT, TILEB = TK * ROWB;
+  constexpr int TK = 32 * WK, SUBS = 2 * WK, PT = TK * WORDS / NT, TILEB = TK * ROWB, PAIRS = (2 * TK * NG + NT - 1) / NT;      // SUBS: sixteenths of a tile
   char* const lds = sh.lds;
   auto &kstep_l = sh.kstep_l, &vstep_l = sh.vstep_l, &vlow_l = sh.vlow_l;
   auto& klow_l = sh.klow_l;
@@ -320,7 +322,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D>& sh)
   const int hk = part.hk, b = part.b, rows = part.rows, base_row = part.base_row, from = part.from, to = part.to;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
 
-  const int row = base_row + wave * 32 + c, tok = part.t0 + row / m.G, head = hk * m.G + row % m.G;
+  const int rw = wave / WK, kw = wave % WK, row = base_row + rw * 32 + c, tok = part.t0 + row / m.G, head = hk * m.G + row % m.G;
   const int part_lim = row < rows ? part_limit(m, part, tok) : -1;
   const bool there = part_lim >= 0;
   const int lim = there ? part_lim : INT32_MAX;
@@ -349,7 +351,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D>& sh)
     if (hb) u.w[0] = u.w[1] = u.w[2] = 0;
     qsum = u.v;
   }
-  const bool wave_has_rows = base_row + wave * 32 < rows;
+  const bool wave_has_rows = base_row + rw * 32 < rows;
   int minlim = lim;
 #pragma unroll
   for (int x = 1; x < 32; x *= 2) minlim = min(minlim, __shfl_xor(minlim, x));
@@ -365,51 +367,49 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D>& sh)
 
   int kaddr[KS], vaddr[DB][2];
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) kaddr[ks] = row_operand<D>(lane, ks);
+  for (int ks = 0; ks < KS; ++ks) kaddr[ks] = kw * 32 * ROWB + row_operand<D>(lane, ks);
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int x = 0; x < 2; ++x) vaddr[db][x] = col_operand<D>(lane, db, x);
+    for (int x = 0; x < 2; ++x) vaddr[db][x] = kw * 32 * ROWB + col_operand<D>(lane, db, x);
 
   const int lsub = m.lpage - 4;
   for (int e0 = from; e0 < to; e0 += LIST) {
     const int n = fill_list<NT>(m, b, nullptr, e0, 1, to, to, pages_l, counts);
-    const int parts = n << lsub, count = (parts + 1) / 2;
+    const int parts = n << lsub, count = (parts + SUBS - 1) / SUBS;
     if (!count) continue;
-    uint32_t kc[PT], vc[PT], pair[(2 * TK * NG + NT - 1) / NT];
-    const auto fetch = [&](int t) __attribute__((always_inline)) {      // (past the last: that one again, masked; behind the end lies
+    struct Raw { uint32_t kc[PT], vc[PT], pair[PAIRS]; } next, later;      // one and two tiles ahead
+    const auto fetch = [&](Raw& f, int t) __attribute__((always_inline)) {      // (past the last: that one again, masked; behind the end lies
                                                       // anything: its weight of 0 must meet a number)
-      long long at[2];                                // the rows of the pool where the sixteenths start, and their positions
-      int key[2];
+      long long at[SUBS];                             // the rows of the pool where the sixteenths start
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int part = min(t * 2 + x, parts - 1);
-        const int2 pp = pages_l[part >> lsub];
-        const int in = (part & ((1 << lsub) - 1)) * 16;
-        at[x] = (((long long)uniform(pp.y) * m.Hkv + hk) << m.lpage) + in;
-        key[x] = (uniform(pp.x) << m.lpage) + in;
+      for (int x = 0; x < SUBS; ++x) {
+        const int part = min(t * SUBS + x, parts - 1);
+        at[x] = (((long long)uniform(pages_l[part >> lsub].y) * m.Hkv + hk) << m.lpage) + (part & ((1 << lsub) - 1)) * 16;
       }
 #pragma unroll
       for (int x = 0; x < PT; ++x) {
-        const int item = tid + x * NT, half = ((wave * 64 + x * NT) / WORDS) >> 4;
+        const int item = tid + x * NT;
         const uint32_t off = ((item / WORDS & 15) * WORDS + item % WORDS) * 4;
-        kc[x] = *(const uint32_t*)((const char*)a.k + (half ? at[1] : at[0]) * (WORDS * 4) + off);
-        vc[x] = *(const uint32_t*)((const char*)a.v + (half ? at[1] : at[0]) * (WORDS * 4) + off);
+        const long long row = WORDS == 16 ? at[x] : wave & 2 ? at[(2 * x + 1) % SUBS] : at[2 * x % SUBS];      // (256 threads take 16 or 32 rows)
+        f.kc[x] = *(const uint32_t*)((const char*)a.k + row * (WORDS * 4) + off);
+        f.vc[x] = *(const uint32_t*)((const char*)a.v + row * (WORDS * 4) + off);
       }
 #pragma unroll
-      for (int x = 0; x < (2 * TK * NG + NT - 1) / NT; ++x) {          // a pair of a key or value and group a thread
-        const int item = tid + x * NT, r = item / NG % TK;
+      for (int x = 0; x < PAIRS; ++x) {               // a pair of a key or value and group a thread
+        const int item = tid + x * NT, r = item / NG % TK, part = min(t * SUBS + (r >> 4), parts - 1);
         if (item >= 2 * TK * NG) break;
-        const int first = r >> 4 ? key[1] : key[0];
-        pair[x] = first + (r & 15) < s.n ? (item < TK * NG ? a.km : a.vm)[((r >> 4 ? at[1] : at[0]) + (r & 15)) * NG + item % NG] : 0;
+        const int2 pp = pages_l[part >> lsub];
+        const int in = (part & ((1 << lsub) - 1)) * 16 + (r & 15);
+        f.pair[x] = (pp.x << m.lpage) + in < s.n ? (item < TK * NG ? a.km : a.vm)[((((long long)pp.y * m.Hkv + hk) << m.lpage) + in) * NG + item % NG] : 0;
       }
     };
-    const auto expand = [&](int stage) __attribute__((always_inline)) {
+    const auto expand = [&](const Raw& f, int stage) __attribute__((always_inline)) {
 #pragma unroll
       for (int x = 0; x < PT; ++x) {
         const int item = tid + x * NT, r = item / WORDS, at = r * ROWB + ((item % WORDS) ^ swz<D>(r)) * 16;
         u32x4_t k, v;
-        const uint32_t even = kc[x] & 0x0F0F0F0Fu, odd = kc[x] >> 4 & 0x0F0F0F0Fu, mid = vc[x] ^ 0x88888888u;      // (a code less 8: four bits with a sign)
+        const uint32_t even = f.kc[x] & 0x0F0F0F0Fu, odd = f.kc[x] >> 4 & 0x0F0F0F0Fu, mid = f.vc[x] ^ 0x88888888u;      // (a code less 8: four bits with a sign)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           k[j] = __float_as_uint((float)(even >> (8 * j) & 255)) >> 16 | __float_as_uint((float)(odd >> (8 * j) & 255));
@@ -419,26 +419,27 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D>& sh)
         *(u32x4_t*)(lds + stage * 2 * TILEB + TILEB + at) = v;
       }
 #pragma unroll
-      for (int x = 0; x < (2 * TK * NG + NT - 1) / NT; ++x) {
+      for (int x = 0; x < PAIRS; ++x) {
         const int item = tid + x * NT, r = item / NG % TK, gr = item % NG;
         if (item >= 2 * TK * NG) break;
-        const float step = __uint_as_float(pair[x] << 16), low = __uint_as_float(pair[x] & 0xFFFF0000u);
-        if (item < TK * NG) { kstep_l[stage][gr][r] = step * sc; klow_l[stage][r][gr] = pair[x] >> 16; }
+        const float step = __uint_as_float(f.pair[x] << 16), low = __uint_as_float(f.pair[x] & 0xFFFF0000u);
+        if (item < TK * NG) { kstep_l[stage][gr][r] = step * sc; klow_l[stage][r][gr] = f.pair[x] >> 16; }
         else { vstep_l[stage][gr][r] = step; vlow_l[stage][gr][r] = fmaf(8.f, step, low); }
       }
     };
-    fetch(0);
-    expand(0);
+    fetch(later, 0);
+    if (count > 1) fetch(next, 1);
+    expand(later, 0);
     __syncthreads();
     for (int t = 0; t < count; ++t) {
       const int stage = t & 1;
-      if (t + 1 < count) fetch(t + 1);
+      if (t + 2 < count) fetch(later, t + 2);
       if (wave_has_rows) {
         const char* const kt = lds + stage * 2 * TILEB;
         const char* const vt = kt + TILEB;
         f32x16_t sacc;
         {
-          const uint32_t l0 = klow_l[stage][c][0], l1 = NG == 2 ? klow_l[stage][c][NG - 1] : 0;
+          const uint32_t l0 = klow_l[stage][32 * kw + c][0], l1 = NG == 2 ? klow_l[stage][32 * kw + c][NG - 1] : 0;
           union { uint32_t w[4]; bf16x8_t v; } u{{l0 | l0 << 16, l0 | l1 << 16, l1 | l1 << 16, 0}};
           sacc = mfma32(u.v, qsum, zero16());
           f32x16_t y[NG];
@@ -452,7 +453,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D>& sh)
           for (int x = 0; x < NG; ++x)
 #pragma unroll
             for (int z = 0; z < 4; ++z) {
-              const f32x4_t step = *(const f32x4_t*)&kstep_l[stage][x][8 * z + 4 * hb];
+              const f32x4_t step = *(const f32x4_t*)&kstep_l[stage][x][32 * kw + 8 * z + 4 * hb];
 #pragma unroll
               for (int j = 0; j < 4; ++j) sacc[4 * z + j] = fmaf(step[j], y[x][4 * z + j], sacc[4 * z + j]);
             }
@@ -461,7 +462,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D>& sh)
         bool whole = true;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const int part = t * 2 + x, pg = uniform(pages_l[min(part, parts - 1) >> lsub].x);
+          const int part = t * SUBS + 2 * kw + x, pg = uniform(pages_l[min(part, parts - 1) >> lsub].x);
           key0[x] = part < parts ? (pg << m.lpage) + (part & ((1 << lsub) - 1)) * 16 : INT32_MAX - 64;
           whole = whole && key0[x] + 16 <= minlim;
         }
@@ -501,7 +502,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D>& sh)
             union { uint32_t w[4]; bf16x8_t v; } u;
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
-              const int at = 16 * s2 + 8 * z + 4 * hb, v0 = 8 * s2 + 4 * z;
+              const int at = 32 * kw + 16 * s2 + 8 * z + 4 * hb, v0 = 8 * s2 + 4 * z;
               const f32x4_t step = *(const f32x4_t*)&vstep_l[stage][x][at], low = *(const f32x4_t*)&vlow_l[stage][x][at];
 #pragma unroll
               for (int j = 0; j < 2; ++j) u.w[2 * z + j] = pack_bf16x2(p[v0 + 2 * j] * step[2 * j], p[v0 + 2 * j + 1] * step[2 * j + 1]);
@@ -518,25 +519,50 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D>& sh)
           }
         }
       }
-      if (t + 1 < count) expand(stage ^ 1);
+      if (t + 1 < count) { expand(next, stage ^ 1); next = later; }
       __syncthreads();
     }
   }
 
-  if (!there) return;
-  const float all = lrun + __shfl_xor(lrun, 32);
+  float all = lrun + __shfl_xor(lrun, 32);
 #pragma unroll
   for (int x = 0; x < NG; ++x) corr[x] += __shfl_xor(corr[x], 32);
-  const long long rec = part.rec + wave * 32 + c;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      f32x4_t o;
+    for (int x = 0; x < 16; ++x) oacc[db][x] += corr[db / 2];
+  if constexpr (WK == 2) {                            // the second wave's result to the first, a lane's values side by side
+    f32x4_t* const jo = (f32x4_t*)lds + rw * (DB * 4 * 64);
+    float2* const jm = (float2*)((f32x4_t*)lds + 2 * (DB * 4 * 64)) + rw * 64;
+    if (kw == 1) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = oacc[db][4 * x + j] + corr[db / 2];
-      *(f32x4_t*)(part.o + rec * D + db * 32 + 8 * x + 4 * hb) = o;
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) jo[(db * 4 + x) * 64 + lane] = f32x4_t{oacc[db][4 * x], oacc[db][4 * x + 1], oacc[db][4 * x + 2], oacc[db][4 * x + 3]};
+      jm[lane] = float2{mref, all};
     }
+    __syncthreads();
+    if (kw == 1) return;
+    const float2 other = jm[lane];
+    const float next = fmaxf(mref, other.x), f0 = __builtin_amdgcn_exp2f(mref - next), f1 = __builtin_amdgcn_exp2f(other.x - next);
+    mref = next;
+    all = fmaf(f1, other.y, all * f0);
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const f32x4_t v = jo[(db * 4 + x) * 64 + lane];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) oacc[db][4 * x + j] = fmaf(f1, v[j], oacc[db][4 * x + j] * f0);
+      }
+  }
+  if (!there) return;
+  const long long rec = part.rec + rw * 32 + c;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      *(f32x4_t*)(part.o + rec * D + db * 32 + 8 * x + 4 * hb) = f32x4_t{oacc[db][4 * x], oacc[db][4 * x + 1], oacc[db][4 * x + 2], oacc[db][4 * x + 3]};
   if (hb == 0) { part.ml[rec * 2] = mref; part.ml[rec * 2 + 1] = all; }
 }
 

@@ -72,7 +72,8 @@ __device__ __forceinline__ bool part_of(const PrefixArgs& a, int id, Part& p) {
   const BlockDims& m = a.m;
   p.shared = id < a.grid;
   int pages, shares, share;
-  if (p.shared) {                  // a share of the keys is walked by all tiles side by side
+  if (p.shared) {
+                                   // a share of the keys is walked by all tiles side by side
     const int per = (a.tiles * a.shares + a.split - 1) / a.split, unit = (id & 7) + 8 * ((id >> 3) / per), item = (id >> 3) % per * a.split + unit % a.split;
     if (item >= a.tiles * a.shares) return false;
     const int tile = uniform(item % a.tiles);
