@@ -8,23 +8,19 @@ namespace adac {
 namespace {
 
 template <typename T, int BITS, int D, int R>
-__global__ __launch_bounds__(256, (few_waves<T, BITS, D, R>())) void prefix_few(PrefixArgs a) {
+__global__ __launch_bounds__(256, (few_waves<T, BITS, D, R>())) void prefix_few(PrefixArgs a, int first) {
   __shared__ FewLds<T, BITS, D> sh;
-  few_rows<T, BITS, D, R, true>(a, 1, blockIdx.x, sh);
+  few_rows<T, BITS, D, R, true>(a, 1, first + blockIdx.x, sh);
 }
 template <int D>
 __global__ __launch_bounds__(256, 3) void prefix_wide(PrefixArgs a) {
   __shared__ WideLds<D, 4, true> sh;
   wide_rows<D, 4, true>(a, 1, 1, sh);
 }
-// 4 bits: a sequence's own few rows take codes straight into their products (16 rows; with the others' walk 109 us, so 7?)
-template <int D, int WK>
-__global__ __launch_bounds__(256, 2) void prefix_codes(PrefixArgs a, bool few) {
-  using Codes = CodesLds<D, WK>;
-  using Few = FewLds<bf16raw, 4, D>;
-  __shared__ __align__(16) char sh[sizeof(Codes) > sizeof(Few) ? sizeof(Codes) : sizeof(Few)];
-  if (few && (int)blockIdx.x >= a.grid) few_rows<bf16raw, 4, D, 1, true>(a, 1, blockIdx.x, *(Few*)sh);
-  else wide_codes<D, WK>(a, *(Codes*)sh);
+template <int D, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void prefix_codes(PrefixArgs a) {
+  __shared__ CodesLds<D, NW> sh;
+  wide_codes<D, NW>(a, sh);
 }
 
 // Joins a row's partial results: those of the pages its group shares, then those of its own.  D / 4 lanes read a result; `per` such
@@ -150,18 +146,20 @@ PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
 
 template <typename T, int BITS, int D>
 void go(hipStream_t st, const PrefixShape& s, int wg, const PrefixArgs& a) {
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 2 && BITS == 0) {
+    if (s.wide) { prefix_wide<D><<<wg, 256, 0, st>>>(a); return; }
+  }
+  if constexpr (sizeof(T) == 2 && BITS == 4) {
     if (s.wide) {
-      if constexpr (BITS) {
-        if (a.TR == 64) prefix_codes<D, 2><<<wg, 256, 0, st>>>(a, a.TT == 16);
-        else prefix_codes<D, 1><<<wg, 256, 0, st>>>(a, a.TT == 16);
-      }
-      else prefix_wide<D><<<wg, 256, 0, st>>>(a);
+      // a sequence's own few rows take codes straight into their products, in a launch of their own
+      const int n = a.TT == 16 ? a.grid : wg;
+      if (n) { if (a.TR == 64) prefix_codes<D, 2><<<n, 128, 0, st>>>(a); else prefix_codes<D, 4><<<n, 256, 0, st>>>(a); }
+      if (wg > n) prefix_few<T, BITS, D, 1><<<wg - n, 256, 0, st>>>(a, n);
       return;
     }
   }
-  if (s.R == 1) prefix_few<T, BITS, D, 1><<<wg, 256, 0, st>>>(a);
-  else prefix_few<T, BITS, D, 2><<<wg, 256, 0, st>>>(a);
+  if (s.R == 1) prefix_few<T, BITS, D, 1><<<wg, 256, 0, st>>>(a, 0);
+  else prefix_few<T, BITS, D, 2><<<wg, 256, 0, st>>>(a, 0);
 }
 
 }  // namespace

@@ -297,19 +297,19 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
 //   values   weights times step_g, rounded to bfloat16, times c - 8 (a rounding weighs codes about their middle), and the sum of weights
 //            times low_g + 8 step_g, unrounded.
 // Steps are applied to 16 keys a lane, which reads them from LDS: with them LDS is what bounds it (24 of 48 wide reads a tile).
-// WK of the four waves share rows, each with 32 keys of a tile of its own, and are joined at the end.
-template <int D, int WK> struct CodesLds {
-  static constexpr int TK = 32 * WK, NG = D / 64, TILEB = TK * D * 2;
+template <int D, int NW> struct CodesLds {
+  static constexpr int TK = 32, NG = D / 64, TILEB = TK * D * 2;
   __align__(16) char lds[4 * TILEB];
   __align__(16) float kstep_l[2][NG][TK], vstep_l[2][NG][TK], vlow_l[2][NG][TK];
   uint32_t klow_l[2][TK][NG];
   int2 pages_l[LIST];
-  int32_t counts[4];
+  int32_t counts[NW];
 };
-template <int D, int WK>
-__device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, WK>& sh) {
-  constexpr int NT = 256, KS = D / 16, DB = D / 32, NG = D / 64, ROWB = D * 2, WORDS = D / 8;      // words of eight codes a row
-  constexpr int TK = 32 * WK, SUBS = 2 * WK, PT = TK * WORDS / NT, TILEB = TK * ROWB, PAIRS = (2 * TK * NG + NT - 1) / NT;      // SUBS: sixteenths of a tile
+template <int D, int NW>
+__device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, NW>& sh) {
+  constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, NG = D / 64, ROWB = D * 2, WORDS = D / 8;      // words of eight codes a row
+  constexpr int TK = 32, PT = TK * WORDS / NT, TILEB = TK * ROWB;
+  static_assert(2 * TK * NG <= NT, "a thread has one pair of a key or value and group");
   char* const lds = sh.lds;
   auto &kstep_l = sh.kstep_l, &vstep_l = sh.vstep_l, &vlow_l = sh.vlow_l;
   auto& klow_l = sh.klow_l;
@@ -322,7 +322,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, WK>&
   const int hk = part.hk, b = part.b, rows = part.rows, base_row = part.base_row, from = part.from, to = part.to;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
 
-  const int rw = wave / WK, kw = wave % WK, row = base_row + rw * 32 + c, tok = part.t0 + row / m.G, head = hk * m.G + row % m.G;
+  const int row = base_row + wave * 32 + c, tok = part.t0 + row / m.G, head = hk * m.G + row % m.G;
   const int part_lim = row < rows ? part_limit(m, part, tok) : -1;
   const bool there = part_lim >= 0;
   const int lim = there ? part_lim : INT32_MAX;
@@ -351,7 +351,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, WK>&
     if (hb) u.w[0] = u.w[1] = u.w[2] = 0;
     qsum = u.v;
   }
-  const bool wave_has_rows = base_row + rw * 32 < rows;
+  const bool wave_has_rows = base_row + wave * 32 < rows;
   int minlim = lim;
 #pragma unroll
   for (int x = 1; x < 32; x *= 2) minlim = min(minlim, __shfl_xor(minlim, x));
@@ -367,41 +367,38 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, WK>&
 
   int kaddr[KS], vaddr[DB][2];
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) kaddr[ks] = kw * 32 * ROWB + row_operand<D>(lane, ks);
+  for (int ks = 0; ks < KS; ++ks) kaddr[ks] = row_operand<D>(lane, ks);
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int x = 0; x < 2; ++x) vaddr[db][x] = kw * 32 * ROWB + col_operand<D>(lane, db, x);
+    for (int x = 0; x < 2; ++x) vaddr[db][x] = col_operand<D>(lane, db, x);
 
   const int lsub = m.lpage - 4;
   for (int e0 = from; e0 < to; e0 += LIST) {
     const int n = fill_list<NT>(m, b, nullptr, e0, 1, to, to, pages_l, counts);
-    const int parts = n << lsub, count = (parts + SUBS - 1) / SUBS;
+    const int parts = n << lsub, count = (parts + 1) / 2;
     if (!count) continue;
-    struct Raw { uint32_t kc[PT], vc[PT], pair[PAIRS]; } next, later;      // one and two tiles ahead
+    struct Raw { uint32_t kc[PT], vc[PT], pair; } next, later;      // one and two tiles ahead
     const auto fetch = [&](Raw& f, int t) __attribute__((always_inline)) {      // (past the last: that one again, masked; behind the end lies
                                                       // anything: its weight of 0 must meet a number)
-      long long at[SUBS];                             // the rows of the pool where the sixteenths start
+      long long at[2];                                // the rows of the pool where the sixteenths start
 #pragma unroll
-      for (int x = 0; x < SUBS; ++x) {
-        const int part = min(t * SUBS + x, parts - 1);
+      for (int x = 0; x < 2; ++x) {
+        const int part = min(t * 2 + x, parts - 1);
         at[x] = (((long long)uniform(pages_l[part >> lsub].y) * m.Hkv + hk) << m.lpage) + (part & ((1 << lsub) - 1)) * 16;
       }
 #pragma unroll
       for (int x = 0; x < PT; ++x) {
-        const int item = tid + x * NT;
+        const int item = tid + x * NT, half = ((wave * 64 + x * NT) / WORDS) >> 4;
         const uint32_t off = ((item / WORDS & 15) * WORDS + item % WORDS) * 4;
-        const long long row = WORDS == 16 ? at[x] : wave & 2 ? at[(2 * x + 1) % SUBS] : at[2 * x % SUBS];      // (256 threads take 16 or 32 rows)
-        f.kc[x] = *(const uint32_t*)((const char*)a.k + row * (WORDS * 4) + off);
-        f.vc[x] = *(const uint32_t*)((const char*)a.v + row * (WORDS * 4) + off);
+        f.kc[x] = *(const uint32_t*)((const char*)a.k + (half ? at[1] : at[0]) * (WORDS * 4) + off);
+        f.vc[x] = *(const uint32_t*)((const char*)a.v + (half ? at[1] : at[0]) * (WORDS * 4) + off);
       }
-#pragma unroll
-      for (int x = 0; x < PAIRS; ++x) {               // a pair of a key or value and group a thread
-        const int item = tid + x * NT, r = item / NG % TK, part = min(t * SUBS + (r >> 4), parts - 1);
-        if (item >= 2 * TK * NG) break;
+      if (tid < 2 * TK * NG) {
+        const int r = tid / NG % TK, part = min(t * 2 + (r >> 4), parts - 1);
         const int2 pp = pages_l[part >> lsub];
         const int in = (part & ((1 << lsub) - 1)) * 16 + (r & 15);
-        f.pair[x] = (pp.x << m.lpage) + in < s.n ? (item < TK * NG ? a.km : a.vm)[((((long long)pp.y * m.Hkv + hk) << m.lpage) + in) * NG + item % NG] : 0;
+        f.pair = (pp.x << m.lpage) + in < s.n ? (tid < TK * NG ? a.km : a.vm)[((((long long)pp.y * m.Hkv + hk) << m.lpage) + in) * NG + tid % NG] : 0;
       }
     };
     const auto expand = [&](const Raw& f, int stage) __attribute__((always_inline)) {
@@ -418,12 +415,10 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, WK>&
         *(u32x4_t*)(lds + stage * 2 * TILEB + at) = k;
         *(u32x4_t*)(lds + stage * 2 * TILEB + TILEB + at) = v;
       }
-#pragma unroll
-      for (int x = 0; x < PAIRS; ++x) {
-        const int item = tid + x * NT, r = item / NG % TK, gr = item % NG;
-        if (item >= 2 * TK * NG) break;
-        const float step = __uint_as_float(f.pair[x] << 16), low = __uint_as_float(f.pair[x] & 0xFFFF0000u);
-        if (item < TK * NG) { kstep_l[stage][gr][r] = step * sc; klow_l[stage][r][gr] = f.pair[x] >> 16; }
+      if (tid < 2 * TK * NG) {
+        const int r = tid / NG % TK, gr = tid % NG;
+        const float step = __uint_as_float(f.pair << 16), low = __uint_as_float(f.pair & 0xFFFF0000u);
+        if (tid < TK * NG) { kstep_l[stage][gr][r] = step * sc; klow_l[stage][r][gr] = f.pair >> 16; }
         else { vstep_l[stage][gr][r] = step; vlow_l[stage][gr][r] = fmaf(8.f, step, low); }
       }
     };
@@ -439,7 +434,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, WK>&
         const char* const vt = kt + TILEB;
         f32x16_t sacc;
         {
-          const uint32_t l0 = klow_l[stage][32 * kw + c][0], l1 = NG == 2 ? klow_l[stage][32 * kw + c][NG - 1] : 0;
+          const uint32_t l0 = klow_l[stage][c][0], l1 = NG == 2 ? klow_l[stage][c][NG - 1] : 0;
           union { uint32_t w[4]; bf16x8_t v; } u{{l0 | l0 << 16, l0 | l1 << 16, l1 | l1 << 16, 0}};
           sacc = mfma32(u.v, qsum, zero16());
           f32x16_t y[NG];
@@ -453,7 +448,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, WK>&
           for (int x = 0; x < NG; ++x)
 #pragma unroll
             for (int z = 0; z < 4; ++z) {
-              const f32x4_t step = *(const f32x4_t*)&kstep_l[stage][x][32 * kw + 8 * z + 4 * hb];
+              const f32x4_t step = *(const f32x4_t*)&kstep_l[stage][x][8 * z + 4 * hb];
 #pragma unroll
               for (int j = 0; j < 4; ++j) sacc[4 * z + j] = fmaf(step[j], y[x][4 * z + j], sacc[4 * z + j]);
             }
@@ -462,7 +457,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, WK>&
         bool whole = true;
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const int part = t * SUBS + 2 * kw + x, pg = uniform(pages_l[min(part, parts - 1) >> lsub].x);
+          const int part = t * 2 + x, pg = uniform(pages_l[min(part, parts - 1) >> lsub].x);
           key0[x] = part < parts ? (pg << m.lpage) + (part & ((1 << lsub) - 1)) * 16 : INT32_MAX - 64;
           whole = whole && key0[x] + 16 <= minlim;
         }
@@ -502,7 +497,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, WK>&
             union { uint32_t w[4]; bf16x8_t v; } u;
 #pragma unroll
             for (int z = 0; z < 2; ++z) {
-              const int at = 32 * kw + 16 * s2 + 8 * z + 4 * hb, v0 = 8 * s2 + 4 * z;
+              const int at = 16 * s2 + 8 * z + 4 * hb, v0 = 8 * s2 + 4 * z;
               const f32x4_t step = *(const f32x4_t*)&vstep_l[stage][x][at], low = *(const f32x4_t*)&vlow_l[stage][x][at];
 #pragma unroll
               for (int j = 0; j < 2; ++j) u.w[2 * z + j] = pack_bf16x2(p[v0 + 2 * j] * step[2 * j], p[v0 + 2 * j + 1] * step[2 * j + 1]);
@@ -524,45 +519,20 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, WK>&
     }
   }
 
-  float all = lrun + __shfl_xor(lrun, 32);
+  if (!there) return;
+  const float all = lrun + __shfl_xor(lrun, 32);
 #pragma unroll
   for (int x = 0; x < NG; ++x) corr[x] += __shfl_xor(corr[x], 32);
+  const long long rec = part.rec + wave * 32 + c;
 #pragma unroll
   for (int db = 0; db < DB; ++db)
 #pragma unroll
-    for (int x = 0; x < 16; ++x) oacc[db][x] += corr[db / 2];
-  if constexpr (WK == 2) {                            // the second wave's result to the first, a lane's values side by side
-    f32x4_t* const jo = (f32x4_t*)lds + rw * (DB * 4 * 64);
-    float2* const jm = (float2*)((f32x4_t*)lds + 2 * (DB * 4 * 64)) + rw * 64;
-    if (kw == 1) {
+    for (int x = 0; x < 4; ++x) {
+      f32x4_t o;
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) jo[(db * 4 + x) * 64 + lane] = f32x4_t{oacc[db][4 * x], oacc[db][4 * x + 1], oacc[db][4 * x + 2], oacc[db][4 * x + 3]};
-      jm[lane] = float2{mref, all};
+      for (int j = 0; j < 4; ++j) o[j] = oacc[db][4 * x + j] + corr[db / 2];
+      *(f32x4_t*)(part.o + rec * D + db * 32 + 8 * x + 4 * hb) = o;
     }
-    __syncthreads();
-    if (kw == 1) return;
-    const float2 other = jm[lane];
-    const float next = fmaxf(mref, other.x), f0 = __builtin_amdgcn_exp2f(mref - next), f1 = __builtin_amdgcn_exp2f(other.x - next);
-    mref = next;
-    all = fmaf(f1, other.y, all * f0);
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const f32x4_t v = jo[(db * 4 + x) * 64 + lane];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) oacc[db][4 * x + j] = fmaf(f1, v[j], oacc[db][4 * x + j] * f0);
-      }
-  }
-  if (!there) return;
-  const long long rec = part.rec + rw * 32 + c;
-#pragma unroll
-  for (int db = 0; db < DB; ++db)
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-      *(f32x4_t*)(part.o + rec * D + db * 32 + 8 * x + 4 * hb) = f32x4_t{oacc[db][4 * x], oacc[db][4 * x + 1], oacc[db][4 * x + 2], oacc[db][4 * x + 3]};
   if (hb == 0) { part.ml[rec * 2] = mref; part.ml[rec * 2 + 1] = all; }
 }
 
