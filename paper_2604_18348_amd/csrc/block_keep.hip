@@ -9,18 +9,19 @@ namespace {
 // ---- weights of keys --------------------------------------------------------------------------------------------------------
 //
 // w_j = decay w_j + sum over the rows r that see key j of 2^(scale log2(e) q_r . k_j - log2(e) lse_r): lse is the logarithm of the row's sum, so
-// no maximum runs along.  A workgroup owns 128 keys of one head of a sequence, 32 a wave, whose operands stay in registers while the
-// rows go by, 16 at a time: no two workgroups add to a weight, and a call repeats bit for bit.
+// no maximum runs along.  No two workgroups add to a weight, and a call repeats bit for bit.
+//
+// Few rows: bound by the keys' bytes.  A wave has H sixteens of keys a turn, the next turn's on their way, and 16 rows at a time; a result
+// tile holds in a lane one key and four rows, so that a key's step and lowest value, its sum and its weight are one lane's.
 //
 // 4 bits, bf16: a code c enters as the bfloat16 16 + c (0x4180 | c << 3: exact), which leaves the dimensions of a word of eight in the
-// order of code_order; the accumulator starts at -16 sum q, and steps and lowest values come behind the product, a group of 64.  (The
-// 128 + c of attention needs a shift less and is off by five times as much, which the weights of many rows average out there.)
-template <typename T, int BITS, int D> struct Keys {
-  static constexpr bool CODES = BITS == 4 && sizeof(T) == 2;
-  static constexpr int NG = D / 64;
-  RowFrag<T, D> f;
-  float step[CODES ? 4 : 1][NG], low[CODES ? 4 : 1][NG];      // of keys 4 quarter + j
-  int end;                                                    // keys from here on do not exist
+// order 0 4 1 5 2 6 3 7; the accumulator starts at -16 sum q, and steps and lowest values come behind the product, a group of 64.  (Attention
+// takes 128 + c, a shift less; that is off by five times as much, which its sums over keys average out.)
+template <typename T, int BITS, int D> struct RawKeys {      // of one row
+  static constexpr int NF = D * sizeof(T) / 64, NG = D / 64;
+  u32x4_t f[BITS ? 1 : NF];
+  uint2 c[BITS ? NG : 1];
+  uint32_t pair[BITS ? NG : 1];
 };
 // piece x of a lane's row: its place in a row of D elements
 template <typename T, int BITS> __device__ __forceinline__ int piece_of(int x, int quarter) {
@@ -28,137 +29,161 @@ template <typename T, int BITS> __device__ __forceinline__ int piece_of(int x, i
   else if constexpr (sizeof(T) == 2) return 8 * (x >> 1) + 2 * quarter + (x & 1);
   else return 16 * (x >> 2) + 4 * quarter + (x & 3);
 }
-
-// 16 keys from position key0 on (a page holds them all); those that do not exist are zero.
 template <typename T, int BITS, int D>
-__device__ __forceinline__ void load_keys(Keys<T, BITS, D>& k, const WeightsArgs& a, int n, int b, int hk, int key0, int n16, int quarter) {
-  constexpr int NF = D * sizeof(T) / 64, NG = D / 64;
-  const BlockDims& m = a.m;
-  const int phys = key0 < n ? pool_page(m, b, key0 >> m.lpage) : -1, in = key0 & (m.page - 1);
-  const bool there = phys >= 0 && key0 + n16 < n;
-  k.end = phys >= 0 ? n : 0;
-  if constexpr (BITS == 0) {
-    load_frag<T, D>(k.f, (const T*)a.k + (there ? phys * a.ks.page + (in + n16) * a.ks.token + hk * a.ks.head : 0), quarter, there);
-  } else {
-    const long long row = ((long long)max(phys, 0) * m.Hkv + hk) * m.page + in;
-    uint32_t c[NG][2];
+__device__ __forceinline__ void expand_keys(RowFrag<T, D>& f, const RawKeys<T, BITS, D>& r) {
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const uint2 w = there ? ((const uint2*)((const char*)a.k + (row + n16) * (D / 2)))[quarter + 4 * g] : uint2{0, 0};
-      c[g][0] = w.x; c[g][1] = w.y;
-    }
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-      for (int x = 0; x < NF; ++x) {
-        const uint32_t w = c[x >> 1][x & 1];
-        k.f.p[x] = u32x4_t{(w << 3 & 0x00780078u) | 0x41804180u, (w >> 1 & 0x00780078u) | 0x41804180u, (w >> 5 & 0x00780078u) | 0x41804180u,
-                           (w >> 9 & 0x00780078u) | 0x41804180u};
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int g = 0; g < NG; ++g) {
-          const uint32_t pair = phys >= 0 && key0 + 4 * quarter + j < n ? a.km[(row + 4 * quarter + j) * NG + g] : 0;
-          k.step[j][g] = __uint_as_float(pair << 16);
-          k.low[j][g] = __uint_as_float(pair & 0xFFFF0000u);
-        }
+  for (int x = 0; x < RawKeys<T, BITS, D>::NF; ++x) {
+    if constexpr (BITS == 0) f.p[x] = r.f[x];
+    else if constexpr (sizeof(T) == 2) {
+      const uint32_t w = x & 1 ? r.c[x >> 1].y : r.c[x >> 1].x;
+      f.p[x] = u32x4_t{(w << 3 & 0x00780078u) | 0x41804180u, (w >> 1 & 0x00780078u) | 0x41804180u, (w >> 5 & 0x00780078u) | 0x41804180u,
+                       (w >> 9 & 0x00780078u) | 0x41804180u};
     } else {
+      const uint32_t pair = r.pair[x >> 2], w = ((x >> 1) & 1 ? r.c[x >> 2].y : r.c[x >> 2].x) >> (16 * (x & 1));
+      const float step = __uint_as_float(pair << 16), low = __uint_as_float(pair & 0xFFFF0000u);
 #pragma unroll
-      for (int x = 0; x < NF; ++x) {
-        const uint32_t pair = there ? a.km[(row + n16) * NG + (x >> 2)] : 0, w = c[x >> 2][(x >> 1) & 1] >> (16 * (x & 1));
-        const float step = __uint_as_float(pair << 16), low = __uint_as_float(pair & 0xFFFF0000u);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) k.f.p[x][j] = there ? __float_as_uint(fmaf((float)(w >> (4 * j) & 15), step, low)) : 0u;
-      }
+      for (int j = 0; j < 4; ++j) f.p[x][j] = __float_as_uint(fmaf((float)(w >> (4 * j) & 15), step, low));
     }
   }
 }
 
+constexpr int KEY_TILES = 2;                          // of 16 keys a wave and turn
 template <typename T, int BITS, int D>
-__global__ __launch_bounds__(256) void cache_weights(WeightsArgs a, int chunks) {
-  using K = Keys<T, BITS, D>;
-  constexpr int NF = D * sizeof(T) / 64, NG = K::NG;
+__global__ __launch_bounds__(256, D == 128 && sizeof(T) == 4 ? 2 : 4) void cache_weights(WeightsArgs a, int chunks, int items) {
+  constexpr int NF = D * sizeof(T) / 64, NG = D / 64, H = KEY_TILES, CHUNK = 64 * H;
+  constexpr bool CODES = BITS == 4 && sizeof(T) == 2;
   const BlockDims& m = a.m;
-  const int chunk = blockIdx.x % chunks, hk = blockIdx.x / chunks % m.Hkv, b = blockIdx.x / chunks / m.Hkv;
+  const int chunk0 = blockIdx.x % items, hk = blockIdx.x / items % m.Hkv, b = blockIdx.x / items / m.Hkv;
   const BlockSeq s = block_seq(m, b);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n16 = lane & 15, quarter = lane >> 4;
-  const int key0 = chunk * 128 + wave * 32, most = m.max_pages << m.lpage;
-  if (key0 >= most) return;
-  f32x4_t w[2];
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), n16 = lane & 15, quarter = lane >> 4, most = m.max_pages << m.lpage;
+  const int rows = s.nq * m.G;
+
+  // 16 rows: their operand, and of the lane's four what is taken off a score, the keys they see, sums of q
+  RowFrag<T, D> q;
+  float off[4];
+  int lim[4];
+  f32x4_t qsum[CODES ? NG : 1];
+  const auto load_rows = [&](int row0) __attribute__((always_inline)) {
+    const int row = row0 + n16, t = row / m.G;
+    const T* const p = (const T*)a.q + (long long)(s.q0 + t) * a.qs.token + (long long)(hk * m.G + row % m.G) * a.qs.head;
 #pragma unroll
-  for (int h = 0; h < 2; ++h) w[h] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-  if (key0 < s.n) {
-    K k[2];
+    for (int f = 0; f < NF; ++f) q.p[f] = row < rows ? *(const u32x4_t*)(p + piece_of<T, BITS>(f, quarter) * Vec<T>::N) : u32x4_t{0, 0, 0, 0};
+    const float lse = row < rows ? a.lse[(long long)(s.q0 + t) * m.Hq + hk * m.G + row % m.G] : -INFINITY;
+    const float o = lse == -INFINITY ? INFINITY : lse * LOG2E;      // (a row without keys weighs none)
+    const int l = row < rows ? (m.causal ? min(s.n, s.first + t + 1) : s.n) : 0;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) load_keys<T, BITS, D>(k[h], a, s.n, b, hk, key0 + 16 * h, n16, quarter);
-    // causal: the first query that sees key0
-    const int t0 = m.causal ? max(0, key0 - s.first) : 0, rows = s.nq * m.G;
-    for (int row0 = t0 * m.G; row0 < rows; row0 += 16) {
-      const int row = row0 + n16, t = row / m.G;
-      const bool there = row < rows;
-      RowFrag<T, D> q;
-      const T* const p = (const T*)a.q + (long long)(s.q0 + t) * a.qs.token + (long long)(hk * m.G + row % m.G) * a.qs.head;
+    for (int j = 0; j < 4; ++j) { off[j] = __shfl(o, 4 * quarter + j); lim[j] = __shfl(l, 4 * quarter + j); }
+    if constexpr (CODES) {
 #pragma unroll
-      for (int f = 0; f < NF; ++f) q.p[f] = there ? *(const u32x4_t*)(p + piece_of<T, BITS>(f, quarter) * Vec<T>::N) : u32x4_t{0, 0, 0, 0};
-      const float lse = there ? a.lse[(long long)(s.q0 + t) * m.Hq + hk * m.G + row % m.G] : INFINITY;
-      const float off = lse == -INFINITY ? INFINITY : lse * LOG2E;      // (a row without keys weighs none)
-      const int lim = there ? (m.causal ? min(s.n, s.first + t + 1) : s.n) : 0;
-      float qsum[NG];
-      if constexpr (K::CODES) {
+      for (int g = 0; g < NG; ++g) {
+        float sum = 0.f;
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          u32x4_t& x = q.p[2 * g + c];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sum += __uint_as_float(x[j] << 16) + __uint_as_float(x[j] & 0xFFFF0000u);
+          // dimensions 0..7 -> 0 4 1 5 2 6 3 7
+          x = u32x4_t{(x[0] & 0xFFFFu) | x[2] << 16, x[0] >> 16 | (x[2] & 0xFFFF0000u), (x[1] & 0xFFFFu) | x[3] << 16, x[1] >> 16 | (x[3] & 0xFFFF0000u)};
+        }
+        sum = quarters_sum(sum);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) qsum[g][j] = __shfl(sum, 4 * quarter + j);
+      }
+    }
+  };
+
+  // A turn's keys are loaded one turn ahead, their places in the pool two.
+  struct Turn { RawKeys<T, BITS, D> k[H]; int end[H]; };      // end: keys from here on do not exist
+  int place[H];
+  const auto places = [&](int chunk) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int key = chunk * CHUNK + (wave * H + h) * 16;
+      place[h] = chunk < chunks && key < s.n ? pool_page(m, b, key >> m.lpage) : -1;
+    }
+  };
+  const auto fetch = [&](Turn& t, int chunk) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int key = chunk * CHUNK + (wave * H + h) * 16, in = key & (m.page - 1), phys = uniform(place[h]);
+      const bool there = phys >= 0 && key + n16 < s.n;
+      t.end[h] = phys >= 0 ? s.n : 0;
+      if constexpr (BITS == 0) {
+        const T* const p = (const T*)a.k + max(phys, 0) * a.ks.page + (there ? in + n16 : 0) * a.ks.token + hk * a.ks.head;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) t.k[h].f[f] = there ? *(const u32x4_t*)(p + (4 * f + quarter) * Vec<T>::N) : u32x4_t{0, 0, 0, 0};
+      } else {
+        const long long row = ((long long)max(phys, 0) * m.Hkv + hk) * m.page + in + n16;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-          float sum = 0.f;
-#pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            u32x4_t& x = q.p[2 * g + c];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sum += __uint_as_float(x[j] << 16) + __uint_as_float(x[j] & 0xFFFF0000u);
-            // dimensions 0..7 -> 0 4 1 5 2 6 3 7
-            x = u32x4_t{(x[0] & 0xFFFFu) | x[2] << 16, x[0] >> 16 | (x[2] & 0xFFFF0000u), (x[1] & 0xFFFFu) | x[3] << 16, x[1] >> 16 | (x[3] & 0xFFFF0000u)};
-          }
-          qsum[g] = quarters_sum(sum);
-        }
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        f32x4_t sc;
-        if constexpr (K::CODES) {
-          sc = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int g = 0; g < NG; ++g) {
-            const float start = -16.f * qsum[g];
-            f32x4_t x{start, start, start, start};
-            x = mma(T{}, k[h].f.p[2 * g], q.p[2 * g], x);
-            x = mma(T{}, k[h].f.p[2 * g + 1], q.p[2 * g + 1], x);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sc[j] = fmaf(k[h].step[j][g], x[j], fmaf(k[h].low[j][g], qsum[g], sc[j]));
-          }
-        } else {
-          sc = dots(k[h].f, q);
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float p = __builtin_amdgcn_exp2f(fmaf(sc[j], a.scale_log2e, -off));
-          w[h][j] += key0 + 16 * h + 4 * quarter + j < min(lim, k[h].end) ? p : 0.f;
+          t.k[h].c[g] = there ? ((const uint2*)((const char*)a.k + row * (D / 2)))[quarter + 4 * g] : uint2{0, 0};
+          t.k[h].pair[g] = there ? a.km[row * NG + g] : 0;
         }
       }
     }
-  }
-  // over the lanes of a quarter: they hold different rows
+  };
+  Turn next;
+  places(chunk0);
+  fetch(next, chunk0);
+  places(chunk0 + items);
+  const bool once = rows <= 16;
+  if (once) load_rows(0);
+  for (int chunk = chunk0; chunk < chunks; chunk += items) {
+    const int key0 = chunk * CHUNK + wave * H * 16;
+    float w[H], before[H];
+    RowFrag<T, D> k[H];
+    float step[H][NG], low[H][NG];
+    int end[H];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < H; ++h) {
+      w[h] = 0.f;
+      const int at = key0 + 16 * h + n16;
+      before[h] = a.w && at < s.n ? a.w[((long long)b * m.Hkv + hk) * most + at] : 0.f;
+      expand_keys<T, BITS, D>(k[h], next.k[h]);
+      end[h] = next.end[h];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+      for (int g = 0; g < NG; ++g) {
+        step[h][g] = CODES ? __uint_as_float(next.k[h].pair[BITS ? g : 0] << 16) : 0.f;
+        low[h][g] = CODES ? __uint_as_float(next.k[h].pair[BITS ? g : 0] & 0xFFFF0000u) : 0.f;
+      }
+    }
+    fetch(next, chunk + items);
+    places(chunk + 2 * items);
+    // causal: from the first query that sees key0
+    const long long first = m.causal ? (long long)max(0, key0 - s.first) * m.G : 0;
+    if (key0 < s.n)
+      for (int row0 = (int)min(first, (long long)rows) & ~15; row0 < rows; row0 += 16) {
+        if (!once) load_rows(row0);
 #pragma unroll
-      for (int x = 1; x < 16; x *= 2) w[h][j] += __shfl_xor(w[h][j], x);
-    const int at = key0 + 16 * h + 4 * quarter;
-    if (n16 || at >= most) continue;                  // (a page holds 16 keys at least)
-    const long long to = ((long long)b * m.Hkv + hk) * most + at;
-    const f32x4_t before = a.w && at < s.n ? *(const f32x4_t*)(a.w + to) : f32x4_t{0.f, 0.f, 0.f, 0.f};
-    f32x4_t x;
+        for (int h = 0; h < H; ++h) {
+          f32x4_t sc;
+          if constexpr (CODES) {
+            sc = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = at + j < s.n ? (a.w ? fmaf(a.decay, before[j], w[h][j]) : w[h][j]) : 0.f;
-    *(f32x4_t*)(a.out + to) = x;
+            for (int g = 0; g < NG; ++g) {
+              f32x4_t x = qsum[g] * -16.f;
+              x = mma(T{}, q.p[2 * g], k[h].p[2 * g], x);
+              x = mma(T{}, q.p[2 * g + 1], k[h].p[2 * g + 1], x);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) sc[j] = fmaf(step[h][g], x[j], fmaf(low[h][g], qsum[g][j], sc[j]));
+            }
+          } else {
+            sc = dots(q, k[h]);
+          }
+          const int at = key0 + 16 * h + n16;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float p = __builtin_amdgcn_exp2f(fmaf(sc[j], a.scale_log2e, -off[j]));
+            w[h] += at < min(lim[j], end[h]) ? p : 0.f;
+          }
+        }
+      }
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const float sum = quarters_sum(w[h]);
+      const int at = key0 + 16 * h + n16;
+      if (quarter == 0 && at < most) a.out[((long long)b * m.Hkv + hk) * most + at] = at >= s.n ? 0.f : a.w ? fmaf(a.decay, before[h], sum) : sum;
+    }
   }
 }
 
@@ -833,10 +858,13 @@ int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, WeightsArgs 
     if (sh.nsplit > 1) weights_join<<<(int)((heads * ((long long)a.m.max_pages << a.m.lpage) / 4 + 255) / 256), 256, 0, s>>>(a);
     return launched();
   }
-  const int chunks = (int)((((long long)a.m.max_pages << a.m.lpage) + 127) / 128);
-  const long long wg = (long long)chunks * a.m.Hkv * a.m.B;
+  // four workgroups a CU in all, which take a head's keys in turns
+  const int chunk = 64 * KEY_TILES, chunks = (int)((((long long)a.m.max_pages << a.m.lpage) + chunk - 1) / chunk);
+  const long long heads = (long long)a.m.Hkv * a.m.B, most = (1024 + heads - 1) / heads;
+  const int items = (int)(most < chunks ? most : chunks);
+  const long long wg = heads * items;
   if (!grid_fits(wg)) return ADACLUSTER_E_UNSUPPORTED;
-#define CALL(T, D) if (bits == 4) cache_weights<T, 4, D><<<(int)wg, 256, 0, s>>>(a, chunks); else cache_weights<T, 0, D><<<(int)wg, 256, 0, s>>>(a, chunks)
+#define CALL(T, D) if (bits == 4) cache_weights<T, 4, D><<<(int)wg, 256, 0, s>>>(a, chunks, items); else cache_weights<T, 0, D><<<(int)wg, 256, 0, s>>>(a, chunks, items)
   if (dtype == ADACLUSTER_BF16) { if (d == 64) { CALL(bf16raw, 64); } else { CALL(bf16raw, 128); } }
   else { if (d == 64) { CALL(float, 64); } else { CALL(float, 128); } }
 #undef CALL
