@@ -10,8 +10,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_lib")
 LIB_PATH = os.path.join(OUT_DIR, "libadacluster.so")
-SOURCES = ["sort.hip", "cluster.hip", "select.hip", "quest.hip", "attn.hip", "block_cache.hip", "block_attn.hip", "block_wide.hip", "block_prefix.hip", "block_keep.hip", "block_grad.hip",
-           "block_api.hip", "api.hip"]
+SOURCES = ["sort.hip", "cluster.hip", "select.hip", "quest.hip", "attn.hip", "block_cache.hip", "block_attn.hip", "block_wide.hip", "block_prefix.hip",
+           "block_weights.hip", "block_evict.hip", "block_grad.hip", "block_api.hip", "api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fgpu-rdc" if False else "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

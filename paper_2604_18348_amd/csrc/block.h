@@ -257,7 +257,7 @@ struct PrefixArgs : BlockAttnArgs {
 size_t prefix_attn_bytes(int dtype, int bits, int d, const PrefixArgs& a);
 int launch_prefix_attn(hipStream_t s, int dtype, int bits, int d, PrefixArgs a, void* ws);
 
-// (block_keep.hip)
+// (block_weights.hip)
 struct WeightsArgs {
   BlockDims m;
   const void *q, *k;
@@ -272,6 +272,7 @@ struct WeightsArgs {
 };
 size_t cache_weights_bytes(int dtype, int bits, const BlockDims& m, const KeyStride& qs);
 int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, WeightsArgs a, void* ws);
+// (block_evict.hip)
 struct EvictArgs {
   BlockDims m;
   const float* w;
