@@ -215,6 +215,7 @@ __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int pages) {
   const int32_t* const kept = a.kept + ((long long)b * m.Hkv + hk) * a.keep;
   const int last = kept[p1 - 1], here = m.table[(long long)b * m.max_pages + pg];
   const bool stays = m.seq_lens[b] <= a.keep;
+  if (last == p1 - 1 && to == here && (p1 - p0 == m.page || stays)) return;      // a page that stays as it is, in its place
   float mx[VEC], mn[VEC];
 #pragma unroll
   for (int i = 0; i < VEC; ++i) { mx[i] = -INFINITY; mn[i] = INFINITY; }
@@ -225,8 +226,6 @@ __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int pages) {
     for (int u = 0; u < U; ++u) src[u] = q0 + u * RPI < p1 ? kept[q0 + u * RPI] : -1;
 #pragma unroll
     for (int u = 0; u < U; ++u) from[u] = src[u] >= 0 ? pool_page(m, b, src[u] >> m.lpage) : -1;
-    // a page that stays as it is, in its place
-    if (last == p1 - 1 && to == here && (p1 - p0 == m.page || stays)) return;
     if constexpr (BITS == 4) {
       uint32_t kc[U], vc[U], kp[U], vp[U];
 #pragma unroll

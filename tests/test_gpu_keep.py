@@ -62,6 +62,8 @@ LAYOUTS = [  # d, page, Hq, Hkv, lens, news
     (128, 128, 12, 4, [1000, 999], [257, 129]),
     (64, 16, 8, 1, [300], [290]),                                 # (16 bits: few keys for many rows, which are shared out)
     (128, 32, 15, 3, [200, 7, 90], [200, 1, 90]),
+    (64, 16, 96, 1, [130, 40], [3, 2]),                           # more heads a key than rows a stage
+    (128, 16, 200, 2, [100], [7]),
 ]
 
 
@@ -97,6 +99,48 @@ def test_weights(layout, dtype, bits, causal):
         for h in range(Hkv):
             count = int((rows[:, h * (Hq // Hkv):(h + 1) * (Hq // Hkv)] > -math.inf).sum())
             assert abs(float(ones[b, h].double().sum()) - count) <= 1e-3 * max(1, count)
+
+
+@pytest.mark.parametrize("bits,news", [(0, 1), (4, 1), (0, 40), (4, 40)])
+def test_weights_in_a_graph_and_on_two_streams(bits, news):
+    x = Batch(BF, bits, 64, 16, 8, 2, [300, 200], [news, news], 6)
+    p, q, cu = x.params(), x.q.cuda(), x.cu_q.cuda()
+    _, lse = B.adacluster_block_attn(p, q, cu, cache=x.cache, **x.where())
+    w = torch.rand((2, 2, x.max_pages * 16), device="cuda")
+    where = x.where()
+    base = B.adacluster_cache_weights(p, q, cu, lse, x.cache, weights=w, decay=0.5, **where)
+    torch.cuda.synchronize()
+    side, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for st in side:
+        with torch.cuda.stream(st):
+            got.append(B.adacluster_cache_weights(p, q, cu, lse, x.cache, weights=w, decay=0.5, **where))
+    torch.cuda.synchronize()
+    assert all(torch.equal(base, y) for y in got)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = B.adacluster_cache_weights(p, q, cu, lse, x.cache, weights=w, decay=0.5, **where)
+    for turn in range(3):
+        w.copy_(torch.rand(w.shape, generator=torch.Generator().manual_seed(turn)))
+        q.copy_(x.q * (1 + turn))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        want = B.adacluster_cache_weights(p, q, cu, lse, x.cache, weights=w, decay=0.5, **where)
+        assert torch.equal(out, want)
+
+
+def test_weights_of_heads_far_apart():
+    """Heads of a query too far apart for the offsets of the kernel for many rows (and near enough): the same weights."""
+    x = Batch(BF, 0, 64, 16, 4, 1, [100], [12], 6)
+    p, q, cu = x.params(), x.q.cuda(), x.cu_q.cuda()
+    _, lse = B.adacluster_block_attn(p, q, cu, cache=x.cache, **x.where())
+    want, tol = _weights(x, 0, lse.cpu(), 1 / 8, 1, None)
+    for stride in (1 << 20, 1 << 29):
+        far = torch.empty(3 * stride + q.shape[0] * 64, dtype=BF, device="cuda")
+        view = far.as_strided(q.shape, (64, stride, 1))
+        view.copy_(q)
+        got = B.adacluster_cache_weights(p, view, cu, lse, x.cache, **x.where())
+        _within(got[0, :, :100], want, tol, "weights, heads %d apart" % stride)
 
 
 def test_weights_of_many_rows_in_place_equal_those_apart():
@@ -253,6 +297,8 @@ EVICT = [  # d, page, Hq, Hkv, lens, keep, recent, first
     (64, 16, 1, 1, [5000, 4097], 1000, 100, 1),                   # more positions than a workgroup takes at a time
     (128, 32, 2, 2, [9000], 8999, 3, 0),
     (64, 16, 2, 1, [300], 5000, 20, 3),                           # more room than there is
+    (64, 64, 1, 1, [70001], 40000, 500, 2),                       # three times as many as fit the registers
+    (64, 128, 1, 1, [66000, 32768], 32768, 0, 0),
 ]
 
 
@@ -287,6 +333,15 @@ def test_moves_of_every_kind_of_cache(layout, dtype, bits):
     x = Batch(dtype, bits, d, page, Hq, Hkv, lens, [0] * len(lens), 8)
     e = Evicted(x, _random_weights(x, "plain", 2), keep, recent, first)
     e.check(*e.run(x.params(keep_first=first)))
+
+
+@pytest.mark.parametrize("dtype,d,bits", [(BF, 64, 0), (BF, 128, 4), (F, 64, 0)])
+def test_last_pages_of_few_tokens_that_stay(dtype, d, bits):
+    """Sequences that keep everything, in their places: pages of any number of tokens are left as they are, their boxes too."""
+    lens = [33, 17, 7, 1, 64, 45]
+    x = Batch(dtype, bits, d, 16, 2, 2, lens, [0] * 6, 8)
+    e = Evicted(x, _random_weights(x, "plain", 2), 64, 4, 1, same=tuple((b, 4) for b in range(6)))
+    e.check(*e.run(x.params(keep_first=1)))
 
 
 @pytest.mark.parametrize("bits", [0, 4])
