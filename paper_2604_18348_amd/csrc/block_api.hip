@@ -313,7 +313,7 @@ int adacluster_cache_evict(const adacluster_block_params* p, const int32_t* seq_
   if ((long long)p->keep_first * p->page + recent > keep)
     return fail(ADACLUSTER_E_BADARG, "cache_evict: keep must hold the first pages and the last tokens: %d * %d + %d > %d", p->keep_first, p->page, recent, keep);
   if (!weights || !new_table || !kept || !new_lens || !new_weights || !boxes) return fail(ADACLUSTER_E_BADARG, "cache_evict: NULL tensor pointer");
-  if (!aligned(weights, 16)) return fail(ADACLUSTER_E_BADARG, "cache_evict: weights must start at a multiple of 16 bytes");
+  if (!aligned(weights, 16) || !aligned(new_weights, 16)) return fail(ADACLUSTER_E_BADARG, "cache_evict: weights must start at multiples of 16 bytes");
   if (weights == new_weights) return fail(ADACLUSTER_E_BADARG, "cache_evict: new_weights must not be weights");
   if (int rc = check_keys(&a.m, nullptr, seq_lens, page_table)) return rc;
   a.ks = three(a.m, p->k_stride); a.vs = three(a.m, p->v_stride);

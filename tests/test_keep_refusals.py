@@ -94,7 +94,8 @@ def test_evict(lib):
     assert "first pages" in message(lib)
     assert evict(lib, params(keep_first=1 << 30), 20, 2) == -1
     assert evict(lib, params(), new_w=ONE) == -1                                  # in place
-    assert evict(lib, params(), w=ctypes.c_void_p(264)) == -1
+    for name in ("w", "new_w"):
+        assert evict(lib, params(), **{name: ctypes.c_void_p(264)}) == -1 and "16 bytes" in message(lib), name
     assert evict(lib, params(num_pages=0, k_rows=4)) == -1
     assert evict(lib, params(bits=4)) == -1
     c = params()
