@@ -765,8 +765,10 @@ def adacluster_prefix_attn(p: BlockParams, q, cu_q, cache: BlockCache, seq_lens,
     """adacluster_block_attn of q [rows,Hq,d] over all pages of a cache, for groups of sequences that share their first prefix_lens[g]
     positions: sequences cu_group[g] .. cu_group[g+1]-1, whose shared pages (the first one's) are read once -> o like q, lse float32
     [rows,Hq].  Rows that belong to no sequence are not written: without `out` and `lse` they hold anything.  Nothing is
-    recorded for autograd."""
+    recorded for autograd (queries that require gradients, with gradients enabled, warn)."""
     dev, dt = _gpu(q), _tdtype(p)
+    if torch.is_grad_enabled() and q.requires_grad:
+        warnings.warn("adacluster_prefix_attn records nothing for autograd: no gradient reaches q through its output", stacklevel=2)
     rows, groups = q.shape[0], prefix_lens.shape[0]
     _ints("cu_q", cu_q, (p.B + 1,), dev)
     _ints("cu_group", cu_group, (groups + 1,), dev)
@@ -814,8 +816,10 @@ def _weights(name, t, p, dev):
 def adacluster_cache_weights(p: BlockParams, q, cu_q, lse, cache: BlockCache, seq_lens, page_table, weights=None, decay=1.0, out=None, ws=None):
     """decay * weights + what every cached key gets from the queries q [rows,Hq,d] whose attention over all keys left lse [rows,Hq], summed
     over queries and the heads that share the key -> float32 [B,Hkv,max_pages*page], 0 from a sequence's last key on.  weights None: from
-    nothing.  out: may be weights."""
+    nothing.  out: may be weights.  Nothing is recorded for autograd (as in adacluster_prefix_attn)."""
     dev, dt = _gpu(q), _tdtype(p)
+    if torch.is_grad_enabled() and (q.requires_grad or lse.requires_grad or weights is not None and weights.requires_grad):
+        warnings.warn("adacluster_cache_weights records nothing for autograd: no gradient reaches q, lse or weights through its output", stacklevel=2)
     rows = q.shape[0]
     _ints("cu_q", cu_q, (p.B + 1,), dev)
     _keys_of(p, None, seq_lens, page_table, dev, True)

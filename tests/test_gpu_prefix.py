@@ -70,6 +70,7 @@ LAYOUTS = [  # d, page, Hq, Hkv, lens, news, cu_group, prefix
     (128, 64, 16, 2, [3000, 2900], [1, 1], [0, 0, 2], [7, 2890]),
     (64, 16, 4, 2, [100, 90], [1, 1], [0], []),                                                     # no groups
     (64, 16, 64, 1, [300, 280], [1, 1], [0, 2], [270]),                                             # 64 heads a head of keys
+    (128, 16, 150, 1, [150, 140, 20], [2, 1, 1], [0, 3], [130]),                                    # and 150
 ]
 WIDE = [  # launches of the kernel for many rows (16 bits), sequences of any number of queries behind them
     (64, 16, 8, 1, [500 + i for i in range(12)], [1] * 12, [0, 5, 12], [480, 333]),
@@ -179,6 +180,26 @@ def test_pages_that_name_nothing_and_wild_device_data():
     for cu in ([0, 1 << 30, -3, 2], [9, 9, 9, 9], [3, 2, 1, 0]):
         B.adacluster_prefix_attn(x.params(), x.q.cuda(), torch.tensor(cu, dtype=torch.int32).cuda(), x.cache, **wild)
     torch.cuda.synchronize()
+
+
+def test_rows_behind_the_last_sequence_by_far():
+    """A buffer of queries for far more than the call's: its size bounds the shares, not the results."""
+    x = Batch(BF, 0, 64, 16, 8, 2, [300, 290], [1, 1], 4, spare=200000)
+    s = Shared(x, [0, 2], [280])
+    out = torch.full_like(x.q, 7.0, device="cuda")
+    o, lse = B.adacluster_prefix_attn(x.params(), x.q.cuda(), x.cu_q.cuda(), x.cache, **s.ints(), out=out)
+    s.check(x.params(), o, lse)
+    assert bool((o[2:] == 7).all())
+
+
+def test_a_call_on_tensors_that_require_gradients_warns():
+    x = Batch(BF, 0, 64, 16, 2, 2, [40, 40], [1, 1], 4)
+    s = Shared(x, [0, 2], [32])
+    with pytest.warns(UserWarning, match="records nothing"):
+        _, lse = B.adacluster_prefix_attn(x.params(), x.q.cuda().requires_grad_(), x.cu_q.cuda(), x.cache, **s.ints())
+    with pytest.warns(UserWarning, match="records nothing"):
+        w = B.adacluster_cache_weights(x.params(), x.q.cuda().requires_grad_(), x.cu_q.cuda(), lse, x.cache, **x.where())
+    assert not lse.requires_grad and not w.requires_grad
 
 
 @pytest.mark.parametrize("rows_heads", [(4, 2), (64, 2)])
