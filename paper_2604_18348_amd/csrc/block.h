@@ -252,6 +252,7 @@ struct PrefixArgs : BlockAttnArgs {
   int grid, split;                           // workgroups of the former, which come first, and their division among the XCDs
   int tiles, TR, shares;                     // tiles of all groups at most, rows of a tile, workgroups that share a group's pages at most
   int rts, TT, tshares;                      // of the latter: tiles of a block of queries, their rows, shares
+  int gkeys, tkeys;                          // keys of a share at least
   float *group_o, *group_ml, *tail_o, *tail_ml;
 };
 size_t prefix_attn_bytes(int dtype, int bits, int d, const PrefixArgs& a);

@@ -52,9 +52,9 @@ __global__ __launch_bounds__(256) void prefix_join(PrefixArgs a, int per) {
       group = group_at(m, a.gr, g);
       const int x = (t - group.q0) * m.G + head % m.G;
       rec = ((long long)(first_tile(m, group.q0, g, a.TR) + x / a.TR) * m.Hkv + hk) * a.shares * a.TR + x % a.TR;
-      parts = group.pages && t >= group.q0 && t < group.q1 ? splits_of(m, group.pages, a.shares, a.TR) : 0;      // (else rows do not ascend)
+      parts = group.pages && t >= group.q0 && t < group.q1 ? splits_of(m, group.pages, a.shares, a.gkeys) : 0;      // (else rows do not ascend)
     }
-    own = splits_of(m, ((s.n + m.page - 1) >> m.lpage) - group.pages, a.tshares, a.TT);
+    own = splits_of(m, ((s.n + m.page - 1) >> m.lpage) - group.pages, a.tshares, a.tkeys);
     const int blk = i / m.qblock, row = (i - blk * m.qblock) * m.G + head % m.G, rt = row / a.TT;
     trec = (((((long long)b * m.Hkv + hk) * m.nb + blk) * a.rts + rt) * a.tshares) * a.TT + row % a.TT;
   }
@@ -120,24 +120,31 @@ PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
   const long long most = (long long)m.B * m.max_q, queries = m.q_rows < most ? m.q_rows : most;
   const int groups = a->gr.groups, block = m.qblock * m.G;
   const long long rows = groups ? (queries * m.G + groups - 1) / groups : block;      // of a group, on average
-  s.wide = dtype == ADACLUSTER_BF16 && (rows > 16 || block > 16) && (bits || (a->ks.token < (1 << 25) && a->vs.token < (1 << 25)));
+  const long long keys = (long long)m.max_pages << m.lpage;
+  // Tiles of 128 rows staged for four waves (d = 128, 8 heads of keys, with the join): 16 rows over 16 384 keys 36 us (52 by prefix_few), over 2 048 and
+  // 1 024 (d = 64) 21 and 14 (20, 16); 8 rows 34 (38); 8 groups of 4 rows over 8 192 68 (62).  4 bits need a second launch for the rows' own keys
+  // and spread 32 KB of bfloat16 a tile: 32 rows over 16 384 keys 51 (70), over 2 048 34 (34), over 1 024 (d = 64) 25 (19); 16 rows over 4 096 33 (28).
+  s.wide = dtype == ADACLUSTER_BF16 && (bits ? block > 16 || (rows > 16 && rows * keys > (1 << 16)) : (block > 16 || rows > 4) && a->ks.token < (1 << 25) && a->vs.token < (1 << 25));
   s.R = rows > 16 || block > 16 ? 2 : 1;
   a->TR = s.wide ? (bits && rows <= 64 && block <= 64 ? 64 : 128) : 16 * s.R;
   a->TT = s.wide ? (bits && block <= 16 ? 16 : bits ? a->TR : block > 32 ? 128 : 32) : 16 * s.R;
   a->tiles = groups ? (int)((long long)m.q_rows * m.G / a->TR) + groups : 0;
   a->rts = (block + a->TT - 1) / a->TT;
   const long long items = (long long)a->rts * m.nb * m.Hkv * m.B, busy = (rows + a->TR - 1) / a->TR * groups * m.Hkv;
-  // Few tiles: the pages are split among the workgroups that the GPU holds at a time.
-  const long long keys = (long long)m.max_pages << m.lpage;
+  // Few tiles: the pages are split among the workgroups that the GPU holds at a time (three a CU; 128 own rows of up to 1 616 keys beside 32 768 x 128 rows
+  // and 32 beside 16 384: 134 and 62 us; for two a CU 134 and 64, four 138 and 60, but 35 -> 41 for 16).  A share has four times as many keys as rows,
+  // so that a partial result (four bytes a value) stays a quarter of what it is made of (128 rows over 16 384 keys: 43 us with 256 keys each, 36 with
+  // 512), or 256; if that leaves CUs without one, as few as 128 (128 rows over 1 024 keys, d = 64: 26 -> 21 us, over 4 096 33 -> 30).
   const int places = s.wide ? (bits ? 512 : 768) : s.R == 1 ? 512 : 256;
-  const auto share = [&](long long items, int tile) {
-    const int least = share_keys(tile);
+  const auto share = [&](long long items, int rows, int* least) {
+    const long long most = rows > 64 ? 4 * rows : 256, fill = keys * items / 256;
+    *least = (int)(!s.wide || rows == 16 || fill > most ? most : fill < 128 ? 128 : fill);      // (few rows: a quarter for each wave of the 256)
     long long n = items > 0 ? places / items : 1;
-    if (n > (keys + least - 1) / least) n = (keys + least - 1) / least;
+    if (n > (keys + *least - 1) / *least) n = (keys + *least - 1) / *least;
     return (int)(n < 1 ? 1 : n);
   };
-  a->shares = share(busy, a->TR);
-  a->tshares = share(items, a->TT);
+  a->shares = share(busy, a->TR, &a->gkeys);
+  a->tshares = share(items, a->TT, &a->tkeys);
   a->split = xcd_split(m.Hkv);
   s.rows = (size_t)a->tiles * m.Hkv * a->shares * a->TR;
   s.trows = (size_t)items * a->tshares * a->TT;

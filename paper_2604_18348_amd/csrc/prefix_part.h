@@ -47,15 +47,10 @@ __device__ __forceinline__ int row_limit(const BlockDims& m, const Group& g, int
   if (i < 0 || i >= s.nq) return -1;
   return m.causal ? max(0, min(s.n, s.first + i + 1)) : s.n;
 }
-// How many of `nsplit` workgroups with `rows` rows each share `pages` pages: 256 keys each at least, and four times as many as rows, so that
-// a partial result (four bytes a value) stays a quarter of what it is made of (128 rows over 16 384 keys of 8 heads, d = 128: 43 us with
-// 256 keys each, 36 with 512).
-__host__ __device__ constexpr int share_keys(int rows) { return rows > 64 ? 4 * rows : 256; }
-__device__ __forceinline__ int splits_of(const BlockDims& m, int pages, int nsplit, int rows) {
-  const int keys = share_keys(rows);
+// How many of `nsplit` workgroups share `pages` pages, `keys` keys each at least.
+__device__ __forceinline__ int splits_of(const BlockDims& m, int pages, int nsplit, int keys) {
   return min(nsplit, max(1, ((pages << m.lpage) + keys - 1) / keys));
 }
-
 
 // What a workgroup walks: rows of a group over a share of the pages that it shares, or rows of a block of queries of a sequence over a
 // share of the pages behind them.
@@ -88,7 +83,7 @@ __device__ __forceinline__ bool part_of(const PrefixArgs& a, int id, Part& p) {
     p.rows = (p.group.q1 - p.group.q0) * m.G;
     p.from = 0; p.to = pages = p.group.pages;
     p.s = BlockSeq{p.group.q0, p.group.q1 - p.group.q0, 0, pages << m.lpage, 0};
-    shares = splits_of(m, pages, a.shares, a.TR);
+    shares = splits_of(m, pages, a.shares, a.gkeys);
     p.rec = (((long long)tile * m.Hkv + p.hk) * a.shares + share) * a.TR;
     p.o = a.group_o; p.ml = a.group_ml;
   } else {
@@ -108,7 +103,7 @@ __device__ __forceinline__ bool part_of(const PrefixArgs& a, int id, Part& p) {
     const int last = min(p.base_row + a.TT, p.rows) - 1, lim = m.causal ? min(p.s.n, p.s.first + p.t0 + last / m.G + 1) : p.s.n;      // (no row sees further)
     p.to = lim > 0 ? (lim + m.page - 1) >> m.lpage : 0;
     pages = ((p.s.n + m.page - 1) >> m.lpage) - p.from;
-    shares = splits_of(m, pages, a.tshares, a.TT);
+    shares = splits_of(m, pages, a.tshares, a.tkeys);
     p.rec = ((long long)item * a.tshares + share) * a.TT;
     p.o = a.tail_o; p.ml = a.tail_ml;
   }

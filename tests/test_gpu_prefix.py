@@ -80,6 +80,8 @@ WIDE = [  # launches of the kernel for many rows (16 bits), sequences of any num
     (128, 32, 8, 2, [400, 380, 401], [60, 80, 33], [0, 3], [352]),                                  # queries that the prefix cuts
     (64, 64, 2, 1, [520, 530], [200, 300], [0, 2], [320]),
     (128, 16, 8, 8, [9000, 8990] + [8900] * 40, [1] * 42, [0, 42], [8880]),                         # more than 512 pages a share and few
+    (64, 16, 8, 1, [1500 + 7 * i for i in range(12)], [1] * 12, [0, 5, 12], [1480, 1333]),          # 4 bits: tiles of 64 rows
+    (64, 64, 12, 1, [1400 + i for i in range(12)], [1] * 12, [0, 12], [1399]),                      # and of 128, own rows few
 ]
 
 
@@ -152,6 +154,20 @@ def test_strides(dtype):
         s.check(p, o, lse)
         n = int(x.cu_q[-1])
         assert torch.equal(o[:n], base[0][:n]) and torch.equal(lse[:n], base[1][:n])
+
+
+@pytest.mark.parametrize("news", [[1] * 12, [7] * 12])
+def test_tokens_of_a_page_far_apart(news):
+    """Strides of a pool past what 32 bits of an offset hold: the kernel for few rows takes any number of them."""
+    x = Batch(BF, 0, 64, 16, 8, 2, [200 + i for i in range(12)], news, 4)
+    s = Shared(x, [0, 7, 12], [190, 100])
+    n = x.cache.k.shape[0]
+    far = torch.empty(16 << 25, dtype=BF, device="cuda")
+    pool = [far.as_strided((n, 2, 16, 64), (128, 64, 1 << 25, 1), at) for at in (0, 1 << 24)]
+    for to, of in zip(pool, (x.cache.k, x.cache.v)):
+        to.copy_(of)
+    o, lse = B.adacluster_prefix_attn(x.params(), x.q.cuda(), x.cu_q.cuda(), replace(x.cache, k=pool[0], v=pool[1]), **s.ints())
+    s.check(x.params(), o, lse)
 
 
 def test_pages_that_name_nothing_and_wild_device_data():
