@@ -520,7 +520,9 @@ struct WeightsShape { bool wide; int chunks, items, nsplit; size_t sums, part; }
 WeightsShape weights_shape(int dtype, int bits, const BlockDims& m, const KeyStride& qs) {
   WeightsShape s{};
   const long long rows = (long long)m.max_q * m.G, keys = (long long)m.max_pages << m.lpage;
-  s.wide = dtype == ADACLUSTER_BF16 && rows > 32 && qs.token < (1 << 24) && qs.head < (1 << 24);      // (offsets of 64 rows in 32 bits)
+  // (8 heads of keys, 8 sequences up to 16 384, d = 128, few against many: 32 rows 61 and 67 us, 48 rows 68 and 68, 64 rows 83 and 72; 4 bits: 48 rows 56 and
+  // 70, 64 rows 69 and 74, 96 rows 91 and 86)
+  s.wide = dtype == ADACLUSTER_BF16 && rows > (bits ? 64 : 32) && qs.token < (1 << 24) && qs.head < (1 << 24);      // (offsets of 64 rows in 32 bits)
   s.nsplit = 1;
   if (!s.wide) return s;
   s.chunks = (int)((keys + (bits ? 127 : 255)) / (bits ? 128 : 256));
