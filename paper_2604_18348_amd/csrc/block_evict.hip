@@ -34,20 +34,20 @@ __device__ __forceinline__ uint32_t scan64(uint32_t v) {
 }
 
 constexpr int DIGIT = 11, BINS = 1 << DIGIT, COPIES = 4, FOURS = 8;
-constexpr int segment(int nt) { return nt * 4 * FOURS; }      // positions that a workgroup holds at a time
+constexpr int NT = 1024, SEGMENT = NT * 4 * FOURS;     // positions that a workgroup holds at a time
 
 // A workgroup chooses for one head of a sequence: the weight at the border by a radix search (three digits of 11, 11 and 10 bits from the
 // top), then the positions that stay are numbered: those above it, those at it as long as there is room, and the ones that stay whatever
 // they weigh.  Weights are read once, into registers, up to 32 768 positions (else once a digit).  Bound by its chain of steps: loads,
-// counts in LDS and barriers, one workgroup a head; up to 8 192 positions four waves do it sooner than sixteen.
-template <int NT>
+// counts in LDS and barriers, one workgroup a head: 128 heads of 32 768 positions 27 us (56 with one
+// count a bin, weights read anew for every digit and branches for the protected ones), of 8 192 13 (17 with four waves), of 1 100 10.5.
 __global__ __launch_bounds__(NT) void evict_pick(EvictArgs a) {
-  constexpr int SEGMENT = segment(NT), WAVES = NT / 64, PER = BINS / NT, COUNTS = FOURS * WAVES;
+  constexpr int WAVES = NT / 64, PER = BINS / NT, COUNTS = FOURS * WAVES;
   // Counts in four copies, a quarter of the lanes each (weights of one size meet in few bins), and a bin a lane for what is not counted:
   // no branch then.
   constexpr int COPY = BINS + 16;                       // (the copies of a bin lie in different banks)
   __shared__ __align__(16) uint32_t bins[COPIES * COPY + 64];
-  __shared__ uint32_t sums[COUNTS > 64 ? COUNTS : 64];
+  __shared__ uint32_t sums[COUNTS];
   __shared__ uint32_t found[2];
   const BlockDims& m = a.m;
   const int hk = blockIdx.x % m.Hkv, b = blockIdx.x / m.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -161,10 +161,10 @@ __global__ __launch_bounds__(NT) void evict_pick(EvictArgs a) {
     }
     __syncthreads();
     if (wave == 0) {
-      constexpr int EACH = COUNTS > 64 ? COUNTS / 64 : 1;
+      constexpr int EACH = COUNTS / 64;
       uint32_t c[EACH], mine = 0;
 #pragma unroll
-      for (int y = 0; y < EACH; ++y) { c[y] = EACH * lane + y < COUNTS ? sums[EACH * lane + y] : 0; mine += c[y]; }
+      for (int y = 0; y < EACH; ++y) { c[y] = sums[EACH * lane + y]; mine += c[y]; }
       const uint32_t run = scan64(mine);
       uint32_t before = run - mine;
 #pragma unroll
@@ -293,8 +293,7 @@ int launch_cache_evict(hipStream_t s, int dtype, int bits, int d, const EvictArg
   const int pages = (a.keep + a.m.page - 1) >> a.m.lpage;
   const long long wg = (long long)pages * a.m.Hkv * a.m.B;
   if (!grid_fits(wg) || !grid_fits(4ll * a.m.Hkv * a.m.B)) return ADACLUSTER_E_UNSUPPORTED;
-  if (((long long)a.m.max_pages << a.m.lpage) <= segment(256)) evict_pick<256><<<a.m.B * a.m.Hkv, 256, 0, s>>>(a);
-  else evict_pick<1024><<<a.m.B * a.m.Hkv, 1024, 0, s>>>(a);
+  evict_pick<<<a.m.B * a.m.Hkv, NT, 0, s>>>(a);
   if (int rc = launched()) return rc;
   const int lanes = a.m.page * d / (dtype == ADACLUSTER_BF16 ? 8 : 4), nt = lanes < 256 ? lanes : 256;      // (128 for the smallest page)
 #define CALL(T, D) if (bits == 4) evict_move<T, 4, D><<<(int)wg, nt, 0, s>>>(a, pages); else evict_move<T, 0, D><<<(int)wg, nt, 0, s>>>(a, pages)
