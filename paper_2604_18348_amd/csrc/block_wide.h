@@ -291,12 +291,15 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
   if (hb == 0 && a.lse) a.lse[(long long)(s.q0 + tok) * m.Hq + head] = all == 0.f ? -INFINITY : fmaf(mref, sc, __builtin_amdgcn_logf(all)) * LN2;
 }
 
-// The same walk over 4-bit pages, for parts.  A tile's codes come one tile ahead into registers and go to LDS as bfloat16: those
+// The same walk over 4-bit pages, for parts.  A tile's codes come two tiles ahead into registers and go to LDS as bfloat16: those
 // of keys by themselves, those of values less 8.  Per group g of 64 dimensions
 //   scores   sum of step_g (c . q) + low_g sum q, scaled: the latter one more product, of (low, low, low) with three bfloat16 parts of sum q;
 //   values   weights times step_g, rounded to bfloat16, times c - 8 (a rounding weighs codes about their middle), and the sum of weights
 //            times low_g + 8 step_g, unrounded.
-// Steps are applied to 16 keys a lane, which reads them from LDS: with them LDS is what bounds it (24 of 48 wide reads a tile).
+// Steps are applied to 16 keys a lane, which reads them from LDS (24 of 48 wide reads a tile).  No unit is full: vector arithmetic, most of it
+// from codes to bfloat16, has half of the cycles, LDS a quarter, the matrix cores an eighth; each tile ends at a barrier, and a wave waits 40 % of its
+// time.  128 rows over 16 384 keys of 8 heads, d = 128, with the rows' own keys: 94 us by the kernel for few rows, 48 staged and 20 for the latter.
+// Two waves a workgroup, 64 rows, where no more are there: 64 sequences in 4 groups over 8 192 keys 66 -> 52 us.
 template <int D, int NW> struct CodesLds {
   static constexpr int TK = 32, NG = D / 64, TILEB = TK * D * 2;
   __align__(16) char lds[4 * TILEB];
