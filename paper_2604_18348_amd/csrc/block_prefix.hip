@@ -37,11 +37,12 @@ __global__ __launch_bounds__(256) void prefix_join(PrefixArgs a, int per) {
   __shared__ float jm[SLOTS][2];
   const BlockDims& m = a.m;
   const int slot = threadIdx.x / LPR, d0 = threadIdx.x % LPR * 4, part = slot % per;
-  long long id = (long long)blockIdx.x * (SLOTS / per) + slot / per;
-  const int head = (int)(id % m.Hq); id /= m.Hq;
-  const int i = (int)(id % m.max_q), b = (int)min(id / m.max_q, (long long)m.B - 1), hk = head / m.G;
+  uint32_t id = blockIdx.x * (SLOTS / per) + slot / per;      // (a launch has below 2^24 workgroups)
+  const int head = id % (uint32_t)m.Hq; id /= (uint32_t)m.Hq;
+  const int i = id % (uint32_t)m.max_q; id /= (uint32_t)m.max_q;
+  const int b = min((int)id, m.B - 1), hk = head / m.G;
   const BlockSeq s = block_seq(m, b);
-  const bool there = id / m.max_q < m.B && i < s.nq;
+  const bool there = (int)id < m.B && i < s.nq;
   const int t = s.q0 + i;
   int parts = 0, own = 0;
   long long rec = 0, trec = 0;
@@ -63,36 +64,37 @@ __global__ __launch_bounds__(256) void prefix_join(PrefixArgs a, int per) {
     const int blk = i / m.qblock, row = (i - blk * m.qblock) * m.G + head % m.G, rt = row / a.TT;
     trec = (((((long long)b * m.Hkv + hk) * m.nb + blk) * a.rts + rt) * a.tshares) * a.TT + row % a.TT;
   }
-  const auto at = [&](int z, const float*& ml) __attribute__((always_inline)) {
-    const bool sh = z < parts;
-    const long long x = sh ? rec + (long long)z * a.TR : trec + (long long)(z - parts) * a.TT;
-    ml = (sh ? a.group_ml : a.tail_ml) + x * 2;
-    return (sh ? a.group_o : a.tail_o) + x * D + d0;
-  };
   float top = -INFINITY, all = 0.f;
   f32x4_t o{0.f, 0.f, 0.f, 0.f};
-  const int count = parts + own;
-  for (int z0 = part; z0 < count; z0 += 4 * per) {
-    float mx[4], sum[4];
-    f32x4_t v[4];
+  // every per-th of `count` results, `rows` rows apart, from the z-th on
+  const auto add = [&](const float* po, const float* pml, int z, int count, int rows) __attribute__((always_inline)) {
+    for (; z < count; z += 2 * per) {
+      float mx[2], sum[2];
+      f32x4_t v[2];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int z = z0 + u * per;
-      mx[u] = -INFINITY; sum[u] = 0.f; v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      if (z < count) { const float* ml; v[u] = *(const f32x4_t*)at(z, ml); mx[u] = ml[0]; sum[u] = ml[1]; }
+      for (int u = 0; u < 2; ++u) {
+        mx[u] = -INFINITY; sum[u] = 0.f; v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (z + u * per < count) {
+          const uint32_t x = (uint32_t)(z + u * per) * rows;      // (below 2^32 / 4 D: a launch has no more workgroups than places)
+          v[u] = *(const f32x4_t*)(po + x * D);
+          mx[u] = pml[x * 2]; sum[u] = pml[x * 2 + 1];
+        }
+      }
+      const float next = fmaxf(fmaxf(mx[0], mx[1]), top);      // (finite: a result's reference is)
+      const float f0 = __builtin_amdgcn_exp2f(top - next);
+      all *= f0; o *= f0;
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const float f = __builtin_amdgcn_exp2f(mx[u] - next);
+        all = fmaf(f, sum[u], all);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = fmaf(f, v[u][j], o[j]);
+      }
+      top = next;
     }
-    const float next = fmaxf(fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])), top);      // (finite: a result's reference is)
-    const float f0 = __builtin_amdgcn_exp2f(top - next);
-    all *= f0; o *= f0;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const float f = __builtin_amdgcn_exp2f(mx[u] - next);
-      all = fmaf(f, sum[u], all);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = fmaf(f, v[u][j], o[j]);
-    }
-    top = next;
-  }
+  };
+  add(a.group_o + rec * D + d0, a.group_ml + rec * 2, part, parts, a.TR);
+  add(a.tail_o + trec * D + d0, a.tail_ml + trec * 2, (part - parts) & (per - 1), own, a.TT);
   if (per > 1) {
     *(f32x4_t*)&jo[slot][d0] = o;
     if (d0 == 0) { jm[slot][0] = top; jm[slot][1] = all; }
