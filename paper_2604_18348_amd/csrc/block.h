@@ -271,7 +271,7 @@ struct WeightsArgs {
   float* part;                               // [nsplit] like out: sums over a share of the rows
   int nsplit;
 };
-size_t cache_weights_bytes(int dtype, int bits, const BlockDims& m, const KeyStride& qs);
+size_t cache_weights_bytes(int dtype, int bits, int d, const BlockDims& m, const KeyStride& qs);
 int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, WeightsArgs a, void* ws);
 // (block_evict.hip)
 struct EvictArgs {

@@ -278,7 +278,7 @@ int adacluster_weights_workspace_bytes(const adacluster_block_params* p, size_t*
   if (int rc = check(p, &m)) return rc;
   if (!p->num_pages) return fail(ADACLUSTER_E_BADARG, "cache_weights: num_pages must be >= 1");
   if (!bytes) return fail(ADACLUSTER_E_BADARG, "bytes is NULL");
-  *bytes = cache_weights_bytes(p->dtype, p->bits, m, two(p->q_stride));
+  *bytes = cache_weights_bytes(p->dtype, p->bits, p->d, m, two(p->q_stride));
   return 0;
 }
 
@@ -297,7 +297,7 @@ int adacluster_cache_weights(const adacluster_block_params* p, const void* q, co
   if (int rc = check_rows("q", q, p->dtype, a.qs)) return rc;
   if (int rc = check_pool(p, k_pool, k_pool, k_meta, k_meta, a.ks, a.ks)) return rc;
   if ((long long)p->max_q * a.m.G > INT32_MAX) return fail(ADACLUSTER_E_UNSUPPORTED, "cache_weights: max_q * Hq / Hkv must be below 2^31");
-  if (int rc = check_ws(ws, ws_bytes, cache_weights_bytes(p->dtype, p->bits, a.m, a.qs))) return rc;
+  if (int rc = check_ws(ws, ws_bytes, cache_weights_bytes(p->dtype, p->bits, p->d, a.m, a.qs))) return rc;
   a.q = q; a.k = k_pool; a.km = k_meta; a.lse = lse; a.w = decay == 0.f ? nullptr : weights; a.out = new_weights;
   a.scale_log2e = log2_scale(p); a.decay = decay;
   return done(launch_cache_weights((hipStream_t)stream, p->dtype, p->bits, p->d, a, ws));

@@ -232,14 +232,15 @@ __global__ __launch_bounds__(256) void weights_sums(WeightsArgs a, u32x4_t* __re
 }
 
 constexpr int STAGE_ROWS = 64, STAGES = 4;      // of q in LDS: all rows of a share stay there if they fit
+constexpr int key_tiles(int bits, int d) { return bits && d == 128 ? 1 : 2; }      // of 32 keys a wave (4 bits, d = 128: steps take the registers of the second)
 
 template <int BITS, int D>
 __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int chunks, int items, int split) {
-  constexpr int KT = BITS ? 1 : 2, KS = D / 16, CH = D / 8, ROWB = D * 2, NG = D / 64;
+  constexpr int KT = key_tiles(BITS, D), KS = D / 16, CH = D / 8, ROWB = D * 2, NG = D / 64;
   constexpr int PT = STAGE_ROWS * CH / 256, STAGEB = STAGE_ROWS * ROWB;
   __shared__ __align__(16) char lds[STAGES * STAGEB];
   __shared__ __align__(16) u32x4_t sums_l[BITS ? STAGES : 1][2][BITS ? STAGE_ROWS : 1];      // (of both halves of the lanes)
-  __shared__ __align__(16) float step_l[BITS ? 4 : 1][NG][BITS ? 32 : 1];
+  __shared__ __align__(16) float step_l[BITS ? 4 : 1][KT][NG][BITS ? 32 : 1];
   __shared__ float lse_l[BITS ? 1 : STAGES][STAGE_ROWS];
   const BlockDims& m = a.m;
   const HeadItem it = xcd_item(blockIdx.x, m.B * m.Hkv, items * a.nsplit, split);
@@ -309,22 +310,32 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
   };
 
   // 4 bits: a chunk's codes and pairs are loaded one chunk ahead, its places in the pool two.
-  struct Raw { uint32_t code[KS], pair[NG], named; };
-  const auto place = [&](int chunk) __attribute__((always_inline)) {      // of the lane's key, as a row of the pool; -1: no such key
-    const int key = chunk * 128 * KT + wave * 32 * KT + c;
-    const int phys = key < s.n ? pool_page(m, b, key >> m.lpage) : -1;
-    return phys < 0 ? -1ll : ((long long)phys * m.Hkv + hk) * m.page + (key & (m.page - 1));
+  struct Raw { uint32_t code[KT][KS], pair[KT][NG], named[KT]; };
+  struct Place { long long row[KT]; };
+  const auto place = [&](int chunk) __attribute__((always_inline)) {      // of the lane's keys, as rows of the pool; -1: no such key
+    Place p;
+#pragma unroll
+    for (int x = 0; x < KT; ++x) {
+      const int key = chunk * 128 * KT + wave * 32 * KT + 32 * x + c;
+      const int phys = key < s.n ? pool_page(m, b, key >> m.lpage) : -1;
+      p.row[x] = phys < 0 ? -1ll : ((long long)phys * m.Hkv + hk) * m.page + (key & (m.page - 1));
+    }
+    return p;
   };
-  const auto fetch = [&](Raw& r, long long row) __attribute__((always_inline)) {
-    r.named = (uint32_t)__ballot(row >= 0);
+  const auto fetch = [&](Raw& r, const Place& p) __attribute__((always_inline)) {
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) r.code[ks] = row >= 0 ? ((const uint32_t*)a.k)[row * (D / 8) + ks * 2 + hb] : 0;
+    for (int x = 0; x < KT; ++x) {
+      const long long row = p.row[x];
+      r.named[x] = (uint32_t)__ballot(row >= 0);
 #pragma unroll
-    for (int g = 0; g < NG; ++g) r.pair[g] = row >= 0 ? a.km[row * NG + g] : 0;
+      for (int ks = 0; ks < KS; ++ks) r.code[x][ks] = row >= 0 ? ((const uint32_t*)a.k)[row * (D / 8) + ks * 2 + hb] : 0;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) r.pair[x][g] = row >= 0 ? a.km[row * NG + g] : 0;
+    }
   };
   const int chunk0 = it.item / a.nsplit, mine = 8 * (c / 8) + 4 * hb + (c >> 1) % 4;      // the key of 32 that the lane is left with at the end
   Raw next;
-  long long after = -1;
+  Place after;
   if constexpr (BITS == 4) { fetch(next, place(chunk0)); if (chunk0 + items < chunks) after = place(chunk0 + items); }
 
   int qrow[KS];
@@ -350,8 +361,8 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
 #pragma unroll
         for (int x = 0; x < KT; ++x) if (mine + 32 * x < s.n - key0) before[x] = a.w[((long long)b * m.Hkv + hk) * most + key0 + 32 * x + mine];
       }
-      bf16x8_t k[KT][KS], low;
-      float step[NG][BITS ? 16 : 1];
+      bf16x8_t k[KT][KS], low[BITS ? KT : 1];
+      float step[KT][NG][BITS ? 16 : 1];
       if constexpr (BITS == 0) {
 #pragma unroll
         for (int x = 0; x < KT; ++x) {
@@ -365,31 +376,36 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
           }
         }
       } else {
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          union { uint32_t w[4]; bf16x8_t v; } u;
-          const uint32_t even = next.code[ks] & 0x0F0F0F0Fu, odd = next.code[ks] >> 4 & 0x0F0F0F0Fu;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) u.w[j] = __float_as_uint((float)(even >> (8 * j) & 255)) >> 16 | __float_as_uint((float)(odd >> (8 * j) & 255));
-          k[0][ks] = u.v;
-        }
-        named[0] = next.named;
-        const uint32_t l0 = next.pair[0] >> 16, l1 = NG == 2 ? next.pair[NG - 1] >> 16 : 0;
-        union { uint32_t w[4]; bf16x8_t v; } u{{l0 | l0 << 16, l0 | l1 << 16, l1 | l1 << 16, 0}};
-        if (hb) { u.w[0] = 0xBF80BF80u; u.w[1] = 0xBF80u; u.w[2] = 0; }
-        low = u.v;
         compiler_fence();
 #pragma unroll
-        for (int g = 0; g < NG; ++g) step_l[wave][g][c] = __uint_as_float(next.pair[g] << 16) * a.scale_log2e;
-        compiler_fence();
+        for (int x = 0; x < KT; ++x) {
 #pragma unroll
-        for (int g = 0; g < NG; ++g)
+          for (int ks = 0; ks < KS; ++ks) {
+            union { uint32_t w[4]; bf16x8_t v; } u;
+            const uint32_t even = next.code[x][ks] & 0x0F0F0F0Fu, odd = next.code[x][ks] >> 4 & 0x0F0F0F0Fu;
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const f32x4_t z = *(const f32x4_t*)&step_l[wave][g][8 * y + 4 * hb];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) step[g][4 * y + j] = z[j];
+            for (int j = 0; j < 4; ++j) u.w[j] = __float_as_uint((float)(even >> (8 * j) & 255)) >> 16 | __float_as_uint((float)(odd >> (8 * j) & 255));
+            k[x][ks] = u.v;
           }
+          named[x] = next.named[x];
+          const uint32_t l0 = next.pair[x][0] >> 16, l1 = NG == 2 ? next.pair[x][NG - 1] >> 16 : 0;
+          union { uint32_t w[4]; bf16x8_t v; } u{{l0 | l0 << 16, l0 | l1 << 16, l1 | l1 << 16, 0}};
+          if (hb) { u.w[0] = 0xBF80BF80u; u.w[1] = 0xBF80u; u.w[2] = 0; }
+          low[x] = u.v;
+#pragma unroll
+          for (int g = 0; g < NG; ++g) step_l[wave][x][g][c] = __uint_as_float(next.pair[x][g] << 16) * a.scale_log2e;
+        }
+        compiler_fence();
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+          for (int g = 0; g < NG; ++g)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const f32x4_t z = *(const f32x4_t*)&step_l[wave][x][g][8 * y + 4 * hb];
+#pragma unroll
+              for (int j = 0; j < 4; ++j) step[x][g][4 * y + j] = z[j];
+            }
         compiler_fence();
         if (chunk + items < chunks) { fetch(next, after); if (chunk + 2 * items < chunks) after = place(chunk + 2 * items); }
       }
@@ -420,16 +436,16 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
             for (int g = 0; g < NG; ++g) {
               y[g] = zero16();
 #pragma unroll
-              for (int ks = 0; ks < 4; ++ks) y[g] = mfma32(k[0][4 * g + ks], q[4 * g + ks], y[g]);
+              for (int ks = 0; ks < 4; ++ks) y[g] = mfma32(k[x][4 * g + ks], q[4 * g + ks], y[g]);
             }
-            y[NG] = mfma32(low, *(const bf16x8_t*)&sums_l[slot][hb][half * 32 + c], zero16());
+            y[NG] = mfma32(low[BITS ? x : 0], *(const bf16x8_t*)&sums_l[slot][hb][half * 32 + c], zero16());
           }
         };
-        const auto weight = [&](const f32x16_t* y, float off, int v) __attribute__((always_inline)) {
+        const auto weight = [&](int x, const f32x16_t* y, float off, int v) __attribute__((always_inline)) {
           if constexpr (BITS == 0) return __builtin_amdgcn_exp2f(fmaf(y[0][v], a.scale_log2e, -off));
           float e = y[NG][v];
 #pragma unroll
-          for (int g = 0; g < NG; ++g) e = fmaf(step[g][v], y[g][v], e);
+          for (int g = 0; g < NG; ++g) e = fmaf(step[x][g][v], y[g][v], e);
           return __builtin_amdgcn_exp2f(e);
         };
         constexpr int NY = BITS ? NG + 1 : 1, MT = KS + (BITS ? 1 : 0);
@@ -450,13 +466,13 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
 #pragma unroll
             for (int j = 0; j < MT; ++j) {
               if (more) {
-                if (j == KS) z[NY - 1] = mfma32(low, *(const bf16x8_t*)&sums_l[slot][hb][half * 32 + c], zero16());
+                if (j == KS) z[NY - 1] = mfma32(low[BITS ? x : 0], *(const bf16x8_t*)&sums_l[slot][hb][half * 32 + c], zero16());
                 else if (BITS == 0) z[0] = mfma32(k[x][j], q[j], j ? z[0] : zero16());
-                else z[j / 4] = mfma32(k[0][j], q[j], j % 4 ? z[j / 4] : zero16());
+                else z[j / 4] = mfma32(k[x][j], q[j], j % 4 ? z[j / 4] : zero16());
                 if (x == KT - 1 && half == 0 && j < KS) q[j] = *(const bf16x8_t*)(qt + qrow[j] + 32 * ROWB);      // (KT 2: the second half's)
               }
 #pragma unroll
-              for (int v = 16 * max(0, j - 1) / (MT - 1); v < 16 * j / (MT - 1); ++v) w[px][v] += weight(y[(i - 1) & 1], off[ph], v);
+              for (int v = 16 * max(0, j - 1) / (MT - 1); v < 16 * j / (MT - 1); ++v) w[px][v] += weight(px, y[(i - 1) & 1], off[ph], v);
               if (more) __builtin_amdgcn_sched_barrier(0);
             }
           }
@@ -474,7 +490,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
               scores(x, half, q, y);
 #pragma unroll
               for (int v = 0; v < 16; ++v) {
-                const float p = weight(y, off, v);
+                const float p = weight(x, y, off, v);
                 w[x][v] += 32 * x + 8 * (v / 4) + v % 4 < lim ? p : 0.f;
               }
             }
@@ -523,7 +539,7 @@ __global__ __launch_bounds__(256) void weights_join(WeightsArgs a) {
 }
 
 struct WeightsShape { bool wide; int chunks, items, nsplit; size_t sums, part; };      // items: workgroups that share a head's chunks of keys
-WeightsShape weights_shape(int dtype, int bits, const BlockDims& m, const KeyStride& qs) {
+WeightsShape weights_shape(int dtype, int bits, int d, const BlockDims& m, const KeyStride& qs) {
   WeightsShape s{};
   const long long rows = (long long)m.max_q * m.G, keys = (long long)m.max_pages << m.lpage;
   // (8 heads of keys, 8 sequences up to 16 384, d = 128, few against many: 32 rows 61 and 67 us, 48 rows 68 and 68, 64 rows 83 and 72; 4 bits: 48 rows 56 and
@@ -531,7 +547,8 @@ WeightsShape weights_shape(int dtype, int bits, const BlockDims& m, const KeyStr
   s.wide = dtype == ADACLUSTER_BF16 && rows > (bits ? 64 : 32) && qs.token < (1 << 24) && qs.head < (1 << 24);      // (offsets of 64 rows in 32 bits)
   s.nsplit = 1;
   if (!s.wide) return s;
-  s.chunks = (int)((keys + (bits ? 127 : 255)) / (bits ? 128 : 256));
+  const int chunk = 128 * key_tiles(bits, d);
+  s.chunks = (int)((keys + chunk - 1) / chunk);
   // Few keys for many rows: the rows are shared until the launch has the two workgroups a CU that it holds, 512 rows each at least.
   const long long wg = (long long)s.chunks * m.Hkv * m.B;
   long long n = 512 / wg;
@@ -551,13 +568,13 @@ WeightsShape weights_shape(int dtype, int bits, const BlockDims& m, const KeyStr
 }
 }  // namespace
 
-size_t cache_weights_bytes(int dtype, int bits, const BlockDims& m, const KeyStride& qs) {
-  const WeightsShape s = weights_shape(dtype, bits, m, qs);
+size_t cache_weights_bytes(int dtype, int bits, int d, const BlockDims& m, const KeyStride& qs) {
+  const WeightsShape s = weights_shape(dtype, bits, d, m, qs);
   return s.sums + s.part;
 }
 
 int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, WeightsArgs a, void* ws) {
-  const WeightsShape sh = weights_shape(dtype, bits, a.m, a.qs);
+  const WeightsShape sh = weights_shape(dtype, bits, d, a.m, a.qs);
   if (sh.wide) {
     const long long heads = (long long)a.m.Hkv * a.m.B, grid = xcd_grid(heads, (long long)sh.items * sh.nsplit);
     const long long pre = ((long long)a.m.q_rows * a.m.Hq + 63) / 64;
