@@ -231,6 +231,17 @@ __global__ __launch_bounds__(256) void weights_sums(WeightsArgs a, u32x4_t* __re
   if (l == 1) parts[2 * id + 1] = u32x4_t{h[6] | h[7] << 16, h[8], 0, 0};
 }
 
+template <int CTRL> __device__ __forceinline__ float of_lane(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, false)); }
+// Of 2 n sums a lane keeps n, the upper ones where `bit` is set, and adds those of the lane CTRL names, whose bit is the other one.
+template <int CTRL, int BIT, int N> __device__ __forceinline__ void halve(float* w, int lane) {
+  const bool up = lane & BIT;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float give = up ? w[i] : w[i + N], mine = up ? w[i + N] : w[i];
+    w[i] = mine + of_lane<CTRL>(give);
+  }
+}
+
 constexpr int STAGE_ROWS = 64, STAGES = 4;      // of q in LDS: all rows of a share stay there if they fit
 constexpr int key_tiles(int bits, int d) { return bits && d == 128 ? 1 : 2; }      // of 32 keys a wave (4 bits, d = 128: steps take the registers of the second)
 
@@ -500,19 +511,19 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
       }
       loaded = stages <= STAGES;
     }
-    // Over the 32 rows that the lanes hold: at every step a lane passes on half of its keys, and is left with one of the 16.
+    // Over the 32 rows that the lanes hold: at every step a lane passes on half of its keys, and is left with one of the 16.  (Lanes 16, 8, then 7 and
+    // 2 numbers apart by exclusive or, without a way through LDS.)
 #pragma unroll
     for (int x = 0; x < KT; ++x) {
 #pragma unroll
-      for (int bit = 16, n = 8; bit >= 2; bit >>= 1, n >>= 1) {
-        const bool up = lane & bit;
-#pragma unroll
-        for (int i = 0; i < n; ++i) {
-          const float give = up ? w[x][i] : w[x][i + n], mine = up ? w[x][i + n] : w[x][i];
-          w[x][i] = mine + __shfl_xor(give, bit);
-        }
+      for (int i = 0; i < 8; ++i) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(w[x][i]), __float_as_uint(w[x][i + 8]), false, false);
+        w[x][i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
       }
-      w[x][0] += __shfl_xor(w[x][0], 1);
+      halve<0x128, 8, 4>(w[x], lane);
+      halve<0x141, 4, 2>(w[x], lane);
+      halve<0x4E, 2, 1>(w[x], lane);
+      w[x][0] += of_lane<0xB1>(w[x][0]);
       const int at = key0 + 32 * x + mine;
       if ((c & 1) || at >= most) continue;
       const long long to = ((long long)b * m.Hkv + hk) * most + at;
