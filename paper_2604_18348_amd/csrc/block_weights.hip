@@ -434,7 +434,12 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
         };
         const auto offset = [&](int half) __attribute__((always_inline)) {
           const float lse = lse_l[BITS ? 0 : slot][half * 32 + c];
-          return lse == -INFINITY ? INFINITY : lse * LOG2E;      // (a row without keys weighs none)
+          return lse == -INFINITY || r0 + half * 32 + c >= rows ? INFINITY : lse * LOG2E;      // (a row without keys, or behind the last, weighs none)
+        };
+        const auto sums = [&](int half) __attribute__((always_inline)) {
+          u32x4_t u = sums_l[slot][BITS ? hb : 0][BITS ? half * 32 + c : 0];
+          if (hb && r0 + half * 32 + c >= rows) u[0] = 0x7E80;      // (2^126, beside whatever else is there: nor does it here)
+          return *(const bf16x8_t*)&u;
         };
         // exponents of 32 keys and 32 rows
         const auto scores = [&](int x, int half, const bf16x8_t* q, f32x16_t* y) __attribute__((always_inline)) {
@@ -449,7 +454,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
 #pragma unroll
               for (int ks = 0; ks < 4; ++ks) y[g] = mfma32(k[x][4 * g + ks], q[4 * g + ks], y[g]);
             }
-            y[NG] = mfma32(low[BITS ? x : 0], *(const bf16x8_t*)&sums_l[slot][hb][half * 32 + c], zero16());
+            y[NG] = mfma32(low[BITS ? x : 0], sums(half), zero16());
           }
         };
         const auto weight = [&](int x, const f32x16_t* y, float off, int v) __attribute__((always_inline)) {
@@ -460,7 +465,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
           return __builtin_amdgcn_exp2f(e);
         };
         constexpr int NY = BITS ? NG + 1 : 1, MT = KS + (BITS ? 1 : 0);
-        if (r0 >= free_row && r0 + STAGE_ROWS <= rows) {
+        if (r0 >= free_row) {
           // The products of a tile in turn with the weights of the one before, as written: left to itself the compiler puts all products
           // first, and a wave's matrix core waits for its exponentials.
           f32x16_t y[2][NY];
@@ -477,7 +482,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
 #pragma unroll
             for (int j = 0; j < MT; ++j) {
               if (more) {
-                if (j == KS) z[NY - 1] = mfma32(low[BITS ? x : 0], *(const bf16x8_t*)&sums_l[slot][hb][half * 32 + c], zero16());
+                if (j == KS) z[NY - 1] = mfma32(low[BITS ? x : 0], sums(half), zero16());
                 else if (BITS == 0) z[0] = mfma32(k[x][j], q[j], j ? z[0] : zero16());
                 else z[j / 4] = mfma32(k[x][j], q[j], j % 4 ? z[j / 4] : zero16());
                 if (x == KT - 1 && half == 0 && j < KS) q[j] = *(const bf16x8_t*)(qt + qrow[j] + 32 * ROWB);      // (KT 2: the second half's)
