@@ -29,7 +29,7 @@ __global__ __launch_bounds__(NW * 64, 2) void prefix_codes(PrefixArgs a) {
 
 // Joins a row's partial results: those of the pages its group shares, then those of its own.  D / 4 lanes read a result; `per` such
 // slots share a row's results, each every per-th with a running maximum, and are joined through LDS.  Bound by waiting: 35 results of 1 024 rows,
-// d = 128, 11 us (24 with one slot a row).
+// d = 128, 8.7 us (24 with one slot a row, 11 with an address a result in 64 bits).
 template <typename T, int D>
 __global__ __launch_bounds__(256) void prefix_join(PrefixArgs a, int per) {
   constexpr int LPR = D / 4, SLOTS = 256 / LPR;
@@ -128,9 +128,9 @@ PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
   const int groups = a->gr.groups, block = m.qblock * m.G;
   const long long rows = groups ? (queries * m.G + groups - 1) / groups : block;      // of a group, on average
   const long long keys = (long long)m.max_pages << m.lpage;
-  // Tiles of 128 rows staged for four waves (d = 128, 8 heads of keys, with the join): 16 rows over 16 384 keys 36 us (52 by prefix_few), over 2 048 and
-  // 1 024 (d = 64) 21 and 14 (20, 16); 8 rows 34 (38); 8 groups of 4 rows over 8 192 68 (62).  4 bits need a second launch for the rows' own keys
-  // and spread 32 KB of bfloat16 a tile: 32 rows over 16 384 keys 51 (70), over 2 048 34 (34), over 1 024 (d = 64) 25 (19); 16 rows over 4 096 33 (28).
+  // Tiles of 128 rows staged for four waves (d = 128, 8 heads of keys, before the join): 16 rows over 16 384 keys 27 us (42 by prefix_few), over 2 048 and
+  // 1 024 (d = 64) 16 and 9 (15, 10); 8 rows 26 (28); 8 groups of 4 rows over 8 192 61 (55).  4 bits need a second launch for the rows' own keys
+  // and spread 32 KB of bfloat16 a tile: 32 rows over 16 384 keys 41 (62), over 2 048 28 (28), over 1 024 (d = 64) 19 (14); 16 rows over 4 096 26 (22).
   s.wide = dtype == ADACLUSTER_BF16 && (bits ? block > 16 || (rows > 16 && rows * keys > (1 << 16)) : (block > 16 || rows > 4) && a->ks.token < (1 << 25) && a->vs.token < (1 << 25));
   s.R = rows > 16 || block > 16 ? 2 : 1;
   a->TR = s.wide ? (bits && rows <= 64 && block <= 64 ? 64 : 128) : 16 * s.R;
@@ -141,7 +141,7 @@ PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
   // Few tiles: the pages are split among the workgroups that the GPU holds at a time (three a CU; 128 own rows of up to 1 616 keys beside 32 768 x 128 rows
   // and 32 beside 16 384: 134 and 62 us; for two a CU 134 and 64, four 138 and 60, but 35 -> 41 for 16).  A share has four times as many keys as rows,
   // so that a partial result (four bytes a value) stays a quarter of what it is made of (128 rows over 16 384 keys: 43 us with 256 keys each, 36 with
-  // 512), or 256; if that leaves CUs without one, as few as 128 (128 rows over 1 024 keys, d = 64: 26 -> 21 us, over 4 096 33 -> 30).
+  // 512), or 256; if that leaves CUs without one, as few as 128 (128 rows over 1 024 keys, d = 64: 21 -> 14 us; 64 over 4 096, d = 128: 27 -> 22).
   const int places = s.wide ? (bits ? 512 : 768) : s.R == 1 ? 512 : 256;
   const auto share = [&](long long items, int rows, int* least) {
     const long long most = rows > 64 ? 4 * rows : 256, fill = keys * items / 256;

@@ -196,7 +196,7 @@ __global__ __launch_bounds__(256, D == 128 && sizeof(T) == 4 ? 2 : 4) void cache
 // 4 bits: a code c is a bfloat16 by itself.  Per group g of 64 dimensions x_g = c . q, and score = sum over g of step_g x_g + low_g sum_g q.
 // The latter, scaled, less the row's log2(e) lse is one more product, of (low, low, low, .., -1, -1, -1) with three bfloat16 parts (24 bits) of every
 // factor, which weights_sums has left: what remains is two multiplications, the exponential and an addition (64 tokens of 4 sequences up to 32 768:
-// 214 us a step and lowest value a weight, 106 so, with a chunk's codes loaded a chunk ahead).
+// 214 us a step and lowest value a weight, 108 so, with a chunk's codes loaded a chunk ahead, 104 with its sums over the lanes in registers).
 
 // 32 bytes a row and head: the sums of q over 64 dimensions, times scale log2(e), in three parts each, for the lanes below 32, and log2(e) lse
 // in three parts for the others, which meet -1.
@@ -558,9 +558,9 @@ struct WeightsShape { bool wide; int chunks, items, nsplit; size_t sums, part; }
 WeightsShape weights_shape(int dtype, int bits, int d, const BlockDims& m, const KeyStride& qs) {
   WeightsShape s{};
   const long long rows = (long long)m.max_q * m.G, keys = (long long)m.max_pages << m.lpage;
-  // (8 heads of keys, 8 sequences up to 16 384, d = 128, few against many: 32 rows 61 and 67 us, 48 rows 68 and 68, 64 rows 83 and 72; 4 bits: 48 rows 56 and
-  // 70, 64 rows 69 and 74, 96 rows 91 and 86)
-  s.wide = dtype == ADACLUSTER_BF16 && rows > (bits ? 64 : 32) && qs.token < (1 << 24) && qs.head < (1 << 24);      // (offsets of 64 rows in 32 bits)
+  // (8 heads of keys, 8 sequences up to 16 384, d = 128, few against many: 32 rows 61 and 62 us, 40 rows 72 and 67, 64 rows 82 and 67; 4 bits: 32 rows 46 and
+  // 63, 48 rows 56 and 64, 64 rows 69 and 67, 96 rows 92 and 81)
+  s.wide = dtype == ADACLUSTER_BF16 && rows > (bits ? 48 : 32) && qs.token < (1 << 24) && qs.head < (1 << 24);      // (offsets of 64 rows in 32 bits)
   s.nsplit = 1;
   if (!s.wide) return s;
   const int chunk = 128 * key_tiles(bits, d);
@@ -570,9 +570,9 @@ WeightsShape weights_shape(int dtype, int bits, int d, const BlockDims& m, const
   long long n = 512 / wg;
   if (n > rows / 512) n = rows / 512;
   if (n > 1) s.nsplit = (int)n;
-  // (one sequence of 2 048 tokens over as many keys, d = 128: 176 us, in shares 48 and 5 for their sum)
+  // (one sequence of 2 048 tokens over as many keys, d = 128: 176 us by one share, 48 and 5 for their sum by eight)
   // Where the rows stay in LDS a workgroup takes several chunks of keys, four workgroups a CU in all (32 and 64 tokens of 8 sequences up to 16 384, 16
-  // bits: 74 and 101 us; two a CU 79 and 101, three 90 and 121).
+  // bits: 68 and 96 us; two a CU 74 and 93, three 72 and 107; of 2 sequences up to 32 768 46 and 59; 43 and 52, 49 and 65).
   s.items = s.chunks;
   if (rows <= STAGES * STAGE_ROWS) {
     const long long most = (1024 + (long long)m.Hkv * m.B - 1) / ((long long)m.Hkv * m.B);
