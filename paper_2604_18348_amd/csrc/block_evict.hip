@@ -288,7 +288,7 @@ __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int pages) {
 }  // namespace
 
 int launch_cache_evict(hipStream_t s, int dtype, int bits, int d, const EvictArgs& a) {
-  const int pages = (a.keep + a.m.page - 1) >> a.m.lpage;
+  const int all = (a.keep + a.m.page - 1) >> a.m.lpage, pages = all < a.m.max_pages ? all : a.m.max_pages;
   const long long wg = (long long)pages * a.m.Hkv * a.m.B;
   if (!grid_fits(wg) || !grid_fits(4ll * a.m.Hkv * a.m.B)) return ADACLUSTER_E_UNSUPPORTED;
   evict_pick<<<a.m.B * a.m.Hkv, NT, 0, s>>>(a);

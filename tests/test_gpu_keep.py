@@ -387,6 +387,32 @@ def test_evict_with_strides_a_graph_and_wild_lengths():
         assert new.tolist() == [min(max(0, min(n, x.max_pages * 16)), 100) for n in lens] and int(kept.max()) < x.max_pages * 16
 
 
+@pytest.mark.parametrize("news", [1, 40])
+@pytest.mark.parametrize("dtype,bits,far", [(BF, 0, 66000), (F, 0, 66000), (BF, 4, 265000)])
+def test_pools_past_32_bits(dtype, bits, far, news):
+    """All calls over a pool whose named pages lie behind 2^32 bytes of others give what they give over the same pages alone."""
+    x = Batch(dtype, bits, 128, 128, 4, 2, [300, 290, 140], [news] * 3, 4)
+    s, e = Shared(x, [0, 2], [256]), Evicted(x, _random_weights(x, "plain", 2), 150, 20, 1)
+    p, q, cu, n = x.params(keep_first=1), x.q.cuda(), x.cu_q.cuda(), 3 * news
+
+    def behind(t):
+        if t is not None:
+            y = torch.empty((far + t.shape[0], *t.shape[1:]), dtype=t.dtype, device="cuda")
+            y[far:] = t
+            return y
+
+    def calls(cache, at):
+        table = lambda t: torch.where(t >= 0, t + at, t).cuda()  # noqa: E731
+        o, lse = B.adacluster_prefix_attn(p, q, cu, cache, **{**s.ints(), "page_table": table(s.table)})
+        w = B.adacluster_cache_weights(p, q, cu, lse, cache, x.lens_t.cuda(), table(x.table), e.w.cuda(), 0.5)
+        got = B.adacluster_cache_evict(p, cache, x.lens_t.cuda(), table(x.table), w, 150, 20, table(e.new_table))
+        return [o[:n], lse[:n], w, *got] + [t[at:] for t in (cache.k, cache.v, cache.k_meta, cache.v_meta, cache.boxes) if t is not None]
+
+    big = calls(B.BlockCache(*[behind(t) for t in (e.cache.k, e.cache.v, e.cache.k_meta, e.cache.v_meta, e.cache.boxes)]), far)
+    for i, (a, b) in enumerate(zip(calls(e.cache, 0), big)):
+        assert torch.equal(a.contiguous().view(torch.uint8), b.contiguous().view(torch.uint8)), i
+
+
 # ---- together -----------------------------------------------------------------------------------------------------------
 
 
