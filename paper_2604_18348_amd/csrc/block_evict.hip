@@ -196,8 +196,8 @@ __global__ __launch_bounds__(NT) void evict_pick(EvictArgs a) {
 }
 
 // A workgroup fills one page of one head: rows as they are, 16 bytes a lane (4 bits: codes), and the page's box of them.  Bound by memory: rows of 256
-// bytes from anywhere, read and written: 16 x 8 heads x 4 096 rows of d = 128 104 us, 5.2 TB/s (106 with four on their way a lane); 4 bits, 32 x 8
-// heads x 2 001 rows of 64 bytes and 8 of steps 55 us with four on their way, 60 with one.
+// bytes from anywhere, read and written: 16 x 8 heads x 4 096 rows of d = 128 115 us, 4.7 TB/s (118 with four on their way a lane); 4 bits, 32 x 8
+// heads x 2 001 rows of 64 bytes and 8 of steps, each out of a line of 128, 70 us with four on their way, 72 with one.
 template <typename T, int BITS, int D>
 __global__ __launch_bounds__(256) void evict_move(EvictArgs a, int pages) {
   constexpr int VEC = Vec<T>::N, LPR = D / VEC;         // lanes a row
