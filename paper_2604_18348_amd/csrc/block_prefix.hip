@@ -120,6 +120,7 @@ __global__ __launch_bounds__(256) void prefix_join(PrefixArgs a, int per) {
 }
 
 // Which kernel, what it is given: fills a's shape.  `rows`, `trows`: of partial results.
+constexpr long long FAR = 1 << 25;                    // tokens this far apart: offsets inside a page pass 32 bits
 struct PrefixShape { bool wide; int R; size_t rows, trows; };
 PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
   const BlockDims& m = a->m;
@@ -131,7 +132,8 @@ PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
   // Tiles of 128 rows staged for four waves (d = 128, 8 heads of keys, before the join): 16 rows over 16 384 keys 27 us (42 by prefix_few), over 2 048 and
   // 1 024 (d = 64) 16 and 9 (15, 10); 8 rows 26 (28); 8 groups of 4 rows over 8 192 61 (55).  4 bits need a second launch for the rows' own keys
   // and spread 32 KB of bfloat16 a tile: 32 rows over 16 384 keys 41 (62), over 2 048 28 (28), over 1 024 (d = 64) 19 (14); 16 rows over 4 096 26 (22).
-  s.wide = dtype == ADACLUSTER_BF16 && (bits ? block > 16 || (rows > 16 && rows * keys > (1 << 16)) : (block > 16 || rows > 4) && a->ks.token < (1 << 25) && a->vs.token < (1 << 25));
+  s.wide = dtype == ADACLUSTER_BF16 && (block > 16 || (bits ? rows > 16 && rows * keys > (1 << 16) : rows > 4)) &&
+           (bits || (a->ks.token < FAR && a->vs.token < FAR));
   s.R = rows > 16 || block > 16 ? 2 : 1;
   a->TR = s.wide ? (bits && rows <= 64 && block <= 64 ? 64 : 128) : 16 * s.R;
   a->TT = s.wide ? (bits && block <= 16 ? 16 : bits ? a->TR : block > 32 ? 128 : 32) : 16 * s.R;
@@ -179,9 +181,15 @@ void go(hipStream_t st, const PrefixShape& s, int wg, const PrefixArgs& a) {
 }  // namespace
 
 size_t prefix_attn_bytes(int dtype, int bits, int d, const PrefixArgs& a) {
-  PrefixArgs x = a;
-  const PrefixShape s = shape_of(dtype, bits, &x);
-  return align_up(s.rows * d * 4, 256) + align_up(s.rows * 8, 256) + align_up(s.trows * d * 4, 256) + align_up(s.trows * 8, 256);
+  size_t most = 0;
+  for (const long long token : {0ll, FAR}) {            // (of any strides: who asks may not have them yet)
+    PrefixArgs x = a;
+    x.ks.token = x.vs.token = token;
+    const PrefixShape s = shape_of(dtype, bits, &x);
+    const size_t n = align_up(s.rows * d * 4, 256) + align_up(s.rows * 8, 256) + align_up(s.trows * d * 4, 256) + align_up(s.trows * 8, 256);
+    if (n > most) most = n;
+  }
+  return most;
 }
 
 int launch_prefix_attn(hipStream_t st, int dtype, int bits, int d, PrefixArgs a, void* ws) {

@@ -46,6 +46,9 @@ def test_prefix(lib):
         c = params()
         getattr(c, name)[1] = 12
         assert prefix(lib, c) == -1, name
+    far = params()
+    far.k_stride[1] = 1 << 25                                                     # tokens of a page far apart: another kernel, the same workspace
+    assert size(lib, far) == size(lib, params())
     need = size(lib, params())[1]
     assert prefix(lib, params(), ws=Z) == -4 and prefix(lib, params(), ws=ctypes.c_void_p(272)) == -4 and prefix(lib, params(), n=need - 1) == -4
 
