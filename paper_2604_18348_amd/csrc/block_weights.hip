@@ -322,32 +322,34 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
 
   // 4 bits: a chunk's codes and pairs are loaded one chunk ahead, its places in the pool two.
   struct Raw { uint32_t code[KT][KS], pair[KT][NG], named[KT]; };
-  struct Place { long long row[KT]; };
-  const auto place = [&](int chunk) __attribute__((always_inline)) {      // of the lane's keys, as rows of the pool; -1: no such key
+  struct Place { int entry[KT]; };
+  const auto place = [&](int chunk) __attribute__((always_inline)) {      // the table's entries of the lane's keys, as they are: nothing waits for them here
     Place p;
 #pragma unroll
     for (int x = 0; x < KT; ++x) {
       const int key = chunk * 128 * KT + wave * 32 * KT + 32 * x + c;
-      const int phys = key < s.n ? pool_page(m, b, key >> m.lpage) : -1;
-      p.row[x] = phys < 0 ? -1ll : ((long long)phys * m.Hkv + hk) * m.page + (key & (m.page - 1));
+      p.entry[x] = -1;
+      if (key < s.n) p.entry[x] = m.table[(long long)b * m.max_pages + (key >> m.lpage)];
     }
     return p;
   };
-  const auto fetch = [&](Raw& r, const Place& p) __attribute__((always_inline)) {
+  const auto fetch = [&](Raw& r, int chunk, const Place& p) __attribute__((always_inline)) {
 #pragma unroll
     for (int x = 0; x < KT; ++x) {
-      const long long row = p.row[x];
-      r.named[x] = (uint32_t)__ballot(row >= 0);
+      const int key = chunk * 128 * KT + wave * 32 * KT + 32 * x + c;
+      const bool there = (unsigned)p.entry[x] < (unsigned)m.num_pages;
+      const long long row = ((long long)p.entry[x] * m.Hkv + hk) * m.page + (key & (m.page - 1));
+      r.named[x] = (uint32_t)__ballot(there);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) r.code[x][ks] = row >= 0 ? ((const uint32_t*)a.k)[row * (D / 8) + ks * 2 + hb] : 0;
+      for (int ks = 0; ks < KS; ++ks) r.code[x][ks] = there ? ((const uint32_t*)a.k)[row * (D / 8) + ks * 2 + hb] : 0;
 #pragma unroll
-      for (int g = 0; g < NG; ++g) r.pair[x][g] = row >= 0 ? a.km[row * NG + g] : 0;
+      for (int g = 0; g < NG; ++g) r.pair[x][g] = there ? a.km[row * NG + g] : 0;
     }
   };
   const int chunk0 = it.item / a.nsplit, mine = 8 * (c / 8) + 4 * hb + (c >> 1) % 4;      // the key of 32 that the lane is left with at the end
   Raw next;
   Place after;
-  if constexpr (BITS == 4) { fetch(next, place(chunk0)); if (chunk0 + items < chunks) after = place(chunk0 + items); }
+  if constexpr (BITS == 4) { after = place(chunk0); fetch(next, chunk0, after); after = place(chunk0 + items); }
 
   int qrow[KS];
 #pragma unroll
@@ -418,7 +420,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
               for (int j = 0; j < 4; ++j) step[x][g][4 * y + j] = z[j];
             }
         compiler_fence();
-        if (chunk + items < chunks) { fetch(next, after); if (chunk + 2 * items < chunks) after = place(chunk + 2 * items); }
+        if (chunk + items < chunks) { fetch(next, chunk + items, after); after = place(chunk + 2 * items); }
       }
       // Rows from which on all keys of the wave are seen.  (Keys that do not exist are left out at the end.)
       const int last = min(key0 + 32 * KT, s.n) - 1;
