@@ -12,6 +12,7 @@ import functools
 import os
 import operator
 import struct
+import threading
 import warnings
 from dataclasses import dataclass, replace
 
@@ -244,17 +245,18 @@ def adacluster_workspace_bytes(p: Params) -> int:
     return out.value
 
 
-_ws_cache = {}
+_ws_cache = threading.local()
 
 
 def workspace(p: Params, device="cuda"):
-    """A torch uint8 workspace of the required size (cached per size and device)."""
+    """A torch uint8 workspace of the required size (cached per size and device, for every host thread by itself: calls of two threads
+    at once must not share scratch)."""
     n = adacluster_workspace_bytes(p)
     key = (str(device), n)
-    if key not in _ws_cache:
-        _ws_cache.clear()
-        _ws_cache[key] = torch.empty(n + 256, dtype=torch.uint8, device=device)
-    t = _ws_cache[key]
+    if getattr(_ws_cache, "key", None) != key:
+        _ws_cache.t = _ws_cache.key = None               # (the old one goes before the new one comes)
+        _ws_cache.t, _ws_cache.key = torch.empty(n + 256, dtype=torch.uint8, device=device), key
+    t = _ws_cache.t
     off = (-t.data_ptr()) % 256
     return t[off:off + n]
 
