@@ -264,7 +264,7 @@ __global__ __launch_bounds__(256, 2) void cache_weights_wide(WeightsArgs a, int 
   const int all_rows = s.nq * m.G, from = (int)((long long)all_rows * share / a.nsplit), rows = (int)((long long)all_rows * (share + 1) / a.nsplit);
   const int stages = (rows - from + STAGE_ROWS - 1) / STAGE_ROWS;
 
-  // Where this thread's pieces of a stage lie, in bytes from the token of the stage's first row (below 2^32: the host sees to it); if the
+  // Where this thread's pieces of a stage lie, in bytes from the token of the stage's first row (below 2^32: near() sees to it); if the
   // heads of a key do not divide 64 they change from stage to stage, without a division.
   const int ht = STAGE_ROWS / m.G, hr = STAGE_ROWS % m.G;
   const uint32_t token = (uint32_t)(a.qs.token * 2), head = (uint32_t)(a.qs.head * 2);
@@ -556,13 +556,19 @@ __global__ __launch_bounds__(256) void weights_join(WeightsArgs a) {
   *(f32x4_t*)(a.out + to) = sum;
 }
 
+// Whether 32 bits hold every offset (in bytes, from a stage's first token) of the kernel for many rows: the stage's first row may be any head of
+// its token, so its 64 rows reach (G + 62) / G tokens further, and any of the G heads.
+bool near(const KeyStride& qs, int G, int d) {
+  if (qs.token >= (1 << 24) || qs.head >= (1 << 24)) return false;
+  return 2 * ((long long)((G + STAGE_ROWS - 2) / G) * qs.token + (long long)(G - 1) * qs.head + d) <= 1ll << 32;
+}
 struct WeightsShape { bool wide; int chunks, items, nsplit; size_t sums, part; };      // items: workgroups that share a head's chunks of keys
 WeightsShape weights_shape(int dtype, int bits, int d, const BlockDims& m, const KeyStride& qs) {
   WeightsShape s{};
   const long long rows = (long long)m.max_q * m.G, keys = (long long)m.max_pages << m.lpage;
   // (8 heads of keys, 8 sequences up to 16 384, d = 128, few against many: 32 rows 61 and 62 us, 40 rows 72 and 67, 64 rows 82 and 67; 4 bits: 32 rows 46 and
   // 63, 48 rows 56 and 64, 64 rows 69 and 67, 96 rows 92 and 81)
-  s.wide = dtype == ADACLUSTER_BF16 && rows > (bits ? 48 : 32) && qs.token < (1 << 24) && qs.head < (1 << 24);      // (offsets of 64 rows in 32 bits)
+  s.wide = dtype == ADACLUSTER_BF16 && rows > (bits ? 48 : 32) && near(qs, m.G, d);
   s.nsplit = 1;
   if (!s.wide) return s;
   const int chunk = 128 * key_tiles(bits, d);
