@@ -245,18 +245,27 @@ def adacluster_workspace_bytes(p: Params) -> int:
     return out.value
 
 
-_ws_cache = threading.local()
+_ws_cache = threading.local()      # .of: {(device, stream): (size, tensor)}
 
 
 def workspace(p: Params, device="cuda"):
-    """A torch uint8 workspace of the required size (cached per size and device, for every host thread by itself: calls of two threads
-    at once must not share scratch)."""
+    """A torch uint8 workspace of the required size for calls on the current stream: kept from call to call, for every host thread, device
+    and stream by itself (calls of two threads or streams at once must not share scratch), until one of another size is asked for there.
+    While the stream is being captured it is a tensor of its own instead, which torch takes from the graph's pool and which therefore lives as
+    long as the graph.  Whoever captures without torch, or goes on with it on another stream, holds a workspace and passes it as `ws`."""
     n = adacluster_workspace_bytes(p)
-    key = (str(device), n)
-    if getattr(_ws_cache, "key", None) != key:
-        _ws_cache.t = _ws_cache.key = None               # (the old one goes before the new one comes)
-        _ws_cache.t, _ws_cache.key = torch.empty(n + 256, dtype=torch.uint8, device=device), key
-    t = _ws_cache.t
+    device, at = torch.device(device), "host"
+    if device.type == "cuda":
+        i = torch.cuda.current_device() if device.index is None else device.index
+        device, at = torch.device("cuda", i), (i, _raw_stream(i))
+    if at != "host" and torch.cuda.is_current_stream_capturing():
+        t = torch.empty(n + 256, dtype=torch.uint8, device=device)
+    else:
+        kept = _ws_cache.__dict__.setdefault("of", {})
+        if at not in kept or kept[at][0] != n:
+            kept.pop(at, None)                           # (the old one goes before the new one comes)
+            kept[at] = n, torch.empty(n + 256, dtype=torch.uint8, device=device)
+        t = kept[at][1]
     off = (-t.data_ptr()) % 256
     return t[off:off + n]
 
