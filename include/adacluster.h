@@ -433,7 +433,7 @@ int adacluster_cache_weights(const adacluster_block_params* p, const void* q, co
  * less than any number); one of n <= keep keeps all.  They become its positions 0 .. in their order, in the pages that new_table
  * [B][max_pages] names: keys and values (codes) as they are, weights along with them, and the boxes of those pages anew, over what
  * the tokens are read as (adacluster_cache_read).  keep >= keep_first * page + recent.
- *   kept [B][Hkv][keep] out: the positions that stay, ascending, -1 behind the end.  new_lens [B] out: min(n, keep).
+ *   kept [B][Hkv][keep] out: the positions that stay, ascending, -1 behind the end.  new_lens [B] out: min(n, keep); not in place of seq_lens.
  *   weights [B][Hkv][max_pages * page] in; new_weights the same shape out (another tensor), fully overwritten, 0 behind the end
  *   (a weight of -0 becomes 0, a NaN some NaN).
  * A page of new_table must belong to one sequence of the call and must not be one that page_table names, but for a page whose tokens all

@@ -61,6 +61,8 @@ int check_keys(BlockDims* m, const int32_t* cu_k, const int32_t* seq_lens, const
   return 0;
 }
 
+bool apart(const void* a, size_t na, const void* b, size_t nb) { return (uintptr_t)a + na <= (uintptr_t)b || (uintptr_t)b + nb <= (uintptr_t)a; }
+
 bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 
 // 16-byte rows: the base and every stride that is used
@@ -318,6 +320,8 @@ int adacluster_cache_evict(const adacluster_block_params* p, const int32_t* seq_
   if (int rc = check_keys(&a.m, nullptr, seq_lens, page_table)) return rc;
   a.ks = three(a.m, p->k_stride); a.vs = three(a.m, p->v_stride);
   if (int rc = check_pool(p, k_pool, v_pool, k_meta, v_meta, a.ks, a.vs)) return rc;
+  // (the workgroup of a sequence's first head writes new_lens while those of the others read seq_lens, and the move reads it again)
+  if (!apart(seq_lens, p->B * sizeof(int32_t), new_lens, p->B * sizeof(int32_t))) return fail(ADACLUSTER_E_BADARG, "cache_evict: new_lens must not overlap seq_lens");
   a.w = weights; a.new_table = new_table; a.keep = keep; a.recent = recent; a.kept = kept; a.new_lens = new_lens; a.new_w = new_weights;
   a.kp = k_pool; a.vp = v_pool; a.km = k_meta; a.vm = v_meta; a.boxes = boxes;
   return done(launch_cache_evict((hipStream_t)stream, p->dtype, p->bits, p->d, a));
