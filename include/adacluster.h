@@ -418,7 +418,7 @@ int adacluster_prefix_attn(const adacluster_block_params* p, int32_t groups, con
  *   new_weights[b][g][j] = decay weights[b][g][j] + sum over the queries t that see j and the query heads h of g of exp(scale q_th . k_j - lse_th)
  * with lse [q_rows][Hq] of attention over the same queries and ALL keys (adacluster_block_attn without lists, adacluster_prefix_attn);
  * rows whose lse is -inf add nothing.  0 from the sequence's last key on.  decay in [0,1]; 0, or weights NULL: what was there is not
- * read.  Both [B][Hkv][max_pages * page] fp32; new_weights may be weights.  Sums are fp32 in a fixed order.
+ * read.  Both [B][Hkv][max_pages * page] fp32; new_weights may be weights, and overlaps them in no other way.  Sums are fp32 in a fixed order.
  * Queries, positions and pages are those of adacluster_block_attn over a paged cache (a page that is not named: no weight).
  * max_q * Hq / Hkv must be below 2^31.
  */
@@ -434,7 +434,7 @@ int adacluster_cache_weights(const adacluster_block_params* p, const void* q, co
  * [B][max_pages] names: keys and values (codes) as they are, weights along with them, and the boxes of those pages anew, over what
  * the tokens are read as (adacluster_cache_read).  keep >= keep_first * page + recent.
  *   kept [B][Hkv][keep] out: the positions that stay, ascending, -1 behind the end.  new_lens [B] out: min(n, keep); not in place of seq_lens.
- *   weights [B][Hkv][max_pages * page] in; new_weights the same shape out (another tensor), fully overwritten, 0 behind the end
+ *   weights [B][Hkv][max_pages * page] in; new_weights the same shape out (apart from them), fully overwritten, 0 behind the end
  *   (a weight of -0 becomes 0, a NaN some NaN).
  * A page of new_table must belong to one sequence of the call and must not be one that page_table names, but for a page whose tokens all
  * stay in their place (keep_first; a sequence that keeps everything): its entry may name the page itself, which is then left as

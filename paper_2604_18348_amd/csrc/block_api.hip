@@ -293,6 +293,8 @@ int adacluster_cache_weights(const adacluster_block_params* p, const void* q, co
   if (!(decay >= 0.f && decay <= 1.f)) return fail(ADACLUSTER_E_BADARG, "cache_weights: decay must be in [0,1]");
   if (!cu_q || !lse || !new_weights) return fail(ADACLUSTER_E_BADARG, "cache_weights: NULL tensor pointer");
   if (!aligned(weights, 16) || !aligned(new_weights, 16)) return fail(ADACLUSTER_E_BADARG, "cache_weights: weights must start at multiples of 16 bytes");
+  const size_t all = (size_t)p->B * p->Hkv * p->max_pages * p->page * sizeof(float);
+  if (weights && decay > 0.f && weights != new_weights && !apart(weights, all, new_weights, all)) return fail(ADACLUSTER_E_BADARG, "cache_weights: new_weights must be weights or lie apart from them");
   if (int rc = check_keys(&a.m, nullptr, seq_lens, page_table)) return rc;
   a.m.cu_q = cu_q;
   a.qs = two(p->q_stride); a.ks = three(a.m, p->k_stride);
@@ -316,7 +318,8 @@ int adacluster_cache_evict(const adacluster_block_params* p, const int32_t* seq_
     return fail(ADACLUSTER_E_BADARG, "cache_evict: keep must hold the first pages and the last tokens: %d * %d + %d > %d", p->keep_first, p->page, recent, keep);
   if (!weights || !new_table || !kept || !new_lens || !new_weights || !boxes) return fail(ADACLUSTER_E_BADARG, "cache_evict: NULL tensor pointer");
   if (!aligned(weights, 16) || !aligned(new_weights, 16)) return fail(ADACLUSTER_E_BADARG, "cache_evict: weights must start at multiples of 16 bytes");
-  if (weights == new_weights) return fail(ADACLUSTER_E_BADARG, "cache_evict: new_weights must not be weights");
+  const size_t all = (size_t)p->B * p->Hkv * p->max_pages * p->page * sizeof(float);
+  if (!apart(weights, all, new_weights, all)) return fail(ADACLUSTER_E_BADARG, "cache_evict: new_weights must not overlap weights");
   if (int rc = check_keys(&a.m, nullptr, seq_lens, page_table)) return rc;
   a.ks = three(a.m, p->k_stride); a.vs = three(a.m, p->v_stride);
   if (int rc = check_pool(p, k_pool, v_pool, k_meta, v_meta, a.ks, a.vs)) return rc;

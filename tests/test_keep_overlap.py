@@ -36,3 +36,13 @@ def test_new_lens_in_place_of_seq_lens(lib):
     here = PLACES["lens"].value
     for to in (here, here + 4, here + 12, here - 4, here - 12):      # (four lengths each)
         assert evict(lib, c, new_lens=at(to)) == -1 and "new_lens" in message(lib), to - here
+
+
+def test_new_weights_over_part_of_weights(lib):
+    c = params(B=2, Hkv=2, max_pages=8)                          # 2 x 2 x 8 x 16 weights: 2048 bytes
+    here = PLACES["w"].value
+    for off in (0, 16, 512, 2032, -16, -2032):
+        assert evict(lib, c, new_w=at(here + off)) == -1 and "new_weights" in message(lib), off
+        if off:                                                  # (the weights of keys may be added to in place)
+            assert lib.adacluster_cache_weights(ctypes.byref(c), PLACES["k"], PLACES["lens"], PLACES["boxes"], PLACES["k"], Z, PLACES["lens"], PLACES["table"],
+                                                PLACES["w"], 0.5, at(here + off), Z, 0, Z) == -1 and "new_weights" in message(lib), off
