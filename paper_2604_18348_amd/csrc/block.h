@@ -57,8 +57,9 @@ __device__ __forceinline__ int pool_page(const BlockDims& m, int b, int pg) {
   return (unsigned)t < (unsigned)m.num_pages ? t : -1;
 }
 
-// Groups of sequences that share their first pages (prefix_part.h); groups 0: none.
-struct BlockGroups { int groups; const int32_t *cu_group, *prefix; };
+// Groups of sequences that share their first pages (prefix_part.h); groups 0: none.  slots: 0, or how many places every sequence has among its
+// group's queries (Group).
+struct BlockGroups { int groups, slots; const int32_t *cu_group, *prefix; };
 
 // Entry e of a list of pages (NULL: all pages in order), or -1: past the pages, or not above the entry before it.
 __device__ __forceinline__ int list_page(const int32_t* __restrict__ list, int e, int pages) {

@@ -125,15 +125,17 @@ __device__ __forceinline__ void few_rows(const Args& a, int rts, int id, FewLds<
   for (int r = 0; r < R; ++r) {
     const int row = base_row + r * 16 + n16, t = t0 + row / m.G;
     bool there = row < rows;
+    int at = s.q0 + t;                                   // its row in the tensor
     if constexpr (PART) {
-      const int l = there ? part_limit(m, part, t) : -1;
-      there = l >= 0;
-      lim[r] = there ? l : INT32_MAX;
+      const QueryRow query = there ? part_query(a, part, t) : QueryRow{0, -1};
+      at = query.t;
+      there = query.lim >= 0;
+      lim[r] = there ? query.lim : INT32_MAX;
       part_min = min(part_min, lim[r]);
     } else {
       lim[r] = there ? (m.causal ? min(s.n, s.first + t + 1) : s.n) : INT32_MAX;      // (a row that is not there needs no mask)
     }
-    const T* const p = (const T*)a.q + (long long)(s.q0 + t) * a.qs.token + (long long)(hk * m.G + row % m.G) * a.qs.head;
+    const T* const p = (const T*)a.q + (long long)at * a.qs.token + (long long)(hk * m.G + row % m.G) * a.qs.head;
 #pragma unroll
     for (int f = 0; f < NF; ++f) q[r].p[f] = there ? *(const u32x4_t*)(p + piece_at<T, BITS>(f, quarter) * Vec<T>::N) : u32x4_t{0, 0, 0, 0};
     if constexpr (CODES) {

@@ -56,9 +56,9 @@ __global__ __launch_bounds__(256) void prefix_join(PrefixArgs a, int per) {
     Group group{0, 0, 0, 0, 0};
     if (g >= 0) {
       group = group_at(m, a.gr, g);
-      const int x = (t - group.q0) * m.G + head % m.G;
+      const int query = a.gr.slots ? b * a.gr.slots + i : t, x = (query - group.q0) * m.G + head % m.G;
       rec = ((long long)(first_tile(m, group.q0, g, a.TR) + x / a.TR) * m.Hkv + hk) * a.shares * a.TR + x % a.TR;
-      parts = group.pages && t >= group.q0 && t < group.q1 ? splits_of(m, group.pages, a.shares, a.gkeys) : 0;      // (else rows do not ascend)
+      parts = group.pages && query >= group.q0 && query < group.q1 ? splits_of(m, group.pages, a.shares, a.gkeys) : 0;      // (else rows do not ascend)
     }
     own = splits_of(m, ((s.n + m.page - 1) >> m.lpage) - group.pages, a.tshares, a.tkeys);
     const int blk = i / m.qblock, row = (i - blk * m.qblock) * m.G + head % m.G, rt = row / a.TT;
@@ -137,7 +137,8 @@ PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
   s.R = rows > 16 || block > 16 ? 2 : 1;
   a->TR = s.wide ? (bits && rows <= 64 && block <= 64 ? 64 : 128) : 16 * s.R;
   a->TT = s.wide ? (bits && block <= 16 ? 16 : bits ? a->TR : block > 32 ? 128 : 32) : 16 * s.R;
-  a->tiles = groups ? (int)((long long)m.q_rows * m.G / a->TR) + groups : 0;
+  a->gr.slots = m.q_rows > most ? m.max_q : 0;
+  a->tiles = groups ? (int)(queries * m.G / a->TR) + groups : 0;
   a->rts = (block + a->TT - 1) / a->TT;
   const long long items = (long long)a->rts * m.nb * m.Hkv * m.B, busy = (rows + a->TR - 1) / a->TR * groups * m.Hkv;
   // Few tiles: the pages are split among the workgroups that the GPU holds at a time (three a CU; 128 own rows of up to 1 616 keys beside 32 768 x 128 rows

@@ -108,19 +108,19 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
 
   const int row = base_row + wave * 32 + c, tok = t0 + row / m.G, head = hk * m.G + row % m.G;
-  int part_lim = -1;
-  if constexpr (PART) { if (row < rows) part_lim = part_limit(m, part, tok); }
-  const bool there = PART ? part_lim >= 0 : row < rows;
+  QueryRow query{s.q0 + tok, -1};
+  if constexpr (PART) { if (row < rows) query = part_query(a, part, tok); }
+  const bool there = PART ? query.lim >= 0 : row < rows;
   bf16x8_t qf[KS];
   {
-    const bf16raw* const p = (const bf16raw*)a.q + (long long)(s.q0 + tok) * a.qs.token + (long long)head * a.qs.head + hb * 8;
+    const bf16raw* const p = (const bf16raw*)a.q + (long long)query.t * a.qs.token + (long long)head * a.qs.head + hb * 8;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       const u32x4_t w = there ? *(const u32x4_t*)(p + ks * 16) : u32x4_t{0, 0, 0, 0};
       qf[ks] = *(const bf16x8_t*)&w;
     }
   }
-  const int lim = there ? (PART ? part_lim : m.causal ? min(s.n, s.first + tok + 1) : s.n) : INT32_MAX;      // (a row that is not there needs no mask)
+  const int lim = there ? (PART ? query.lim : m.causal ? min(s.n, s.first + tok + 1) : s.n) : INT32_MAX;      // (a row that is not there needs no mask)
   const int wave_first = base_row + wave * 32;
   const bool wave_has_rows = wave_first < rows;
   int minlim = m.causal ? min(s.n, s.first + t0 + wave_first / m.G + 1) : s.n;       // keys below: seen by all rows of the wave
@@ -326,13 +326,13 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, NW>&
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 31, hb = lane >> 5;
 
   const int row = base_row + wave * 32 + c, tok = part.t0 + row / m.G, head = hk * m.G + row % m.G;
-  const int part_lim = row < rows ? part_limit(m, part, tok) : -1;
-  const bool there = part_lim >= 0;
-  const int lim = there ? part_lim : INT32_MAX;
+  const QueryRow query = row < rows ? part_query(a, part, tok) : QueryRow{0, -1};
+  const bool there = query.lim >= 0;
+  const int lim = there ? query.lim : INT32_MAX;
   const float sc = a.scale_log2e;
   bf16x8_t qf[KS], qsum;
   {
-    const bf16raw* const p = (const bf16raw*)a.q + (long long)(s.q0 + tok) * a.qs.token + (long long)head * a.qs.head + hb * 8;
+    const bf16raw* const p = (const bf16raw*)a.q + (long long)query.t * a.qs.token + (long long)head * a.qs.head + hb * 8;
     float sum[NG];
 #pragma unroll
     for (int x = 0; x < NG; ++x) sum[x] = 0.f;

@@ -5,14 +5,21 @@
 
 namespace adac {
 
-// Sequences [b0, b1) of group g, their query rows [q0, q1), and the whole pages of what they share (of what the first one holds).
+// Sequences [b0, b1) of group g, its queries [q0, q1), and the whole pages of what they share (of what the first one holds).  Queries are counted
+// as their rows lie in the tensor; where that has more rows than the call can have queries, B * max_q, in places instead, max_q for every
+// sequence: tiles and partial results are as many as either count may need.
 struct Group { int b0, b1, q0, q1, pages; };
 __device__ __forceinline__ Group group_at(const BlockDims& m, const BlockGroups& gr, int g) {
   Group x{0, 0, 0, 0, 0};
   x.b0 = min(max(gr.cu_group[g], 0), m.B);
   x.b1 = min(max(gr.cu_group[g + 1], x.b0), m.B);
-  x.q0 = min(max(m.cu_q[x.b0], 0), m.q_rows);
-  x.q1 = min(max(m.cu_q[x.b1], x.q0), m.q_rows);
+  if (gr.slots) {
+    x.q0 = x.b0 * gr.slots;
+    x.q1 = x.b1 * gr.slots;
+  } else {
+    x.q0 = min(max(m.cu_q[x.b0], 0), m.q_rows);
+    x.q1 = min(max(m.cu_q[x.b1], x.q0), m.q_rows);
+  }
   if (x.b0 < x.b1) x.pages = min(max(gr.prefix[g], 0), min(max(m.seq_lens[x.b0], 0), m.max_pages << m.lpage)) >> m.lpage;
   return x;
 }
@@ -30,22 +37,32 @@ __device__ __forceinline__ int group_of(const BlockGroups& gr, int b) {
   const int g = last_group(gr.groups, [&](int x) { return gr.cu_group[x] <= b; });
   return g >= 0 && b < gr.cu_group[g + 1] ? g : -1;
 }
-// Tiles of TR rows (a query of a head each) start anew at every group: the first tile of a group whose rows start at q0.  Groups
-// that follow each other have different ones, and all lie below q_rows * G / TR + groups.
+// Tiles of TR rows (a query of a head each) start anew at every group: the first tile of a group whose queries start at q0.  Groups
+// that follow each other have different ones, and all lie below min(q_rows, B * max_q) * G / TR + groups.
 __device__ __forceinline__ int first_tile(const BlockDims& m, int q0, int g, int TR) { return q0 * m.G / TR + g; }
 
-// The key below which query row t of the group sees, or -1 (a row of no sequence).
-__device__ __forceinline__ int row_limit(const BlockDims& m, const Group& g, int t) {
-  int b = g.b0 + (t - g.q0);                           // (one query a sequence)
-  if (m.max_q > 1 || b >= g.b1 || m.cu_q[b] > t || m.cu_q[b + 1] <= t) {
-    int lo = g.b0, hi = g.b1;                          // cu_q[lo] <= t < cu_q[hi]
-    while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (m.cu_q[mid] <= t) lo = mid; else hi = mid; }
-    b = lo;
+// Query x of the group, counted as above: its row in the tensor, and the key below which it sees, or -1 (a row of no sequence).
+struct QueryRow { int t, lim; };
+__device__ __forceinline__ QueryRow group_query(const BlockDims& m, const BlockGroups& gr, const Group& g, int x) {
+  int b, t;
+  BlockSeq s;
+  if (gr.slots) {
+    b = min(x / gr.slots, m.B - 1);
+    s = block_seq(m, b);
+    t = s.q0 + x % gr.slots;
+  } else {
+    t = x;
+    b = g.b0 + (t - g.q0);                             // (one query a sequence)
+    if (m.max_q > 1 || b >= g.b1 || m.cu_q[b] > t || m.cu_q[b + 1] <= t) {
+      int lo = g.b0, hi = g.b1;                        // cu_q[lo] <= t < cu_q[hi]
+      while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (m.cu_q[mid] <= t) lo = mid; else hi = mid; }
+      b = lo;
+    }
+    s = block_seq(m, b);
   }
-  const BlockSeq s = block_seq(m, b);
   const int i = t - s.q0;
-  if (i < 0 || i >= s.nq) return -1;
-  return m.causal ? max(0, min(s.n, s.first + i + 1)) : s.n;
+  if (i < 0 || i >= s.nq) return {0, -1};
+  return {t, m.causal ? max(0, min(s.n, s.first + i + 1)) : s.n};
 }
 // How many of `nsplit` workgroups share `pages` pages, `keys` keys each at least.
 __device__ __forceinline__ int splits_of(const BlockDims& m, int pages, int nsplit, int keys) {
@@ -55,7 +72,7 @@ __device__ __forceinline__ int splits_of(const BlockDims& m, int pages, int nspl
 // What a workgroup walks: rows of a group over a share of the pages that it shares, or rows of a block of queries of a sequence over a
 // share of the pages behind them.
 struct Part {
-  BlockSeq s;                      // shared: the group's rows, and as keys the pages that it shares
+  BlockSeq s;                      // shared: the group's queries, as Group counts them, and as keys the pages that it shares
   Group group;
   int hk, b, t0, rows, base_row;   // rows from base_row on below `rows`; row r is query t0 + r / G
   int from, to;                    // pages
@@ -113,9 +130,11 @@ __device__ __forceinline__ bool part_of(const PrefixArgs& a, int id, Part& p) {
   p.to = uniform(first + (int)((long long)n * (share + 1) / shares));
   return true;
 }
-// The key below which the row of its query t (from the first of p.s) sees, or -1: no such row.
-__device__ __forceinline__ int part_limit(const BlockDims& m, const Part& p, int t) {
-  return p.shared ? row_limit(m, p.group, p.s.q0 + t) : max(0, m.causal ? min(p.s.n, p.s.first + t + 1) : p.s.n);
+// Its query x, from the first of p.s: the row in the tensor, and the key below which it sees, or -1 (no such row).
+__device__ __forceinline__ QueryRow part_query(const PrefixArgs& a, const Part& p, int x) {
+  const BlockDims& m = a.m;
+  if (p.shared) return group_query(m, a.gr, p.group, p.s.q0 + x);
+  return {p.s.q0 + x, max(0, m.causal ? min(p.s.n, p.s.first + x + 1) : p.s.n)};
 }
 
 }  // namespace adac
