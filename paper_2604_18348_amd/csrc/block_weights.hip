@@ -601,8 +601,8 @@ int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, WeightsArgs 
   const WeightsShape sh = weights_shape(dtype, bits, d, a.m, a.qs);
   if (sh.wide) {
     const long long heads = (long long)a.m.Hkv * a.m.B, grid = xcd_grid(heads, (long long)sh.items * sh.nsplit);
-    const long long pre = ((long long)a.m.q_rows * a.m.Hq + 63) / 64;
-    if (!grid_fits(grid) || !grid_fits(pre)) return ADACLUSTER_E_UNSUPPORTED;
+    const long long pre = ((long long)a.m.q_rows * a.m.Hq + 63) / 64;      // of weights_sums (4 bits)
+    if (!grid_fits(grid) || (bits && !grid_fits(pre))) return ADACLUSTER_E_UNSUPPORTED;
     a.sums = (const u32x4_t*)ws;
     a.part = (float*)((char*)ws + sh.sums);
     a.nsplit = sh.nsplit;
