@@ -405,7 +405,7 @@ int adacluster_block_attn_backward(const adacluster_block_params* p, const void*
  *     at.  Positions behind them are every sequence's own.
  * Everything else is as in adacluster_block_attn (a query sees positions up to its own if causal; empty rows, range, layout), in the
  * same workspace rules: adacluster_prefix_workspace_bytes.  topk, qblock and keep_first are not used.  lse may be NULL.
- * q_rows * Hq / Hkv must be below 2^31.  cu_group that does not ascend: results are unspecified, no access is out of bounds.
+ * q_rows * Hq / Hkv must be at most 2^31 - 1024.  cu_group that does not ascend: results are unspecified, no access is out of bounds.
  */
 int adacluster_prefix_workspace_bytes(const adacluster_block_params* p, int32_t groups, size_t* bytes /* host */);
 int adacluster_prefix_attn(const adacluster_block_params* p, int32_t groups, const void* q, const int32_t* cu_q,
@@ -420,7 +420,7 @@ int adacluster_prefix_attn(const adacluster_block_params* p, int32_t groups, con
  * rows whose lse is -inf add nothing.  0 from the sequence's last key on.  decay in [0,1]; 0, or weights NULL: what was there is not
  * read.  Both [B][Hkv][max_pages * page] fp32; new_weights may be weights, and overlaps them in no other way.  Sums are fp32 in a fixed order.
  * Queries, positions and pages are those of adacluster_block_attn over a paged cache (a page that is not named: no weight).
- * max_q * Hq / Hkv must be below 2^31.
+ * max_q * Hq / Hkv must be at most 2^31 - 1024.
  */
 int adacluster_weights_workspace_bytes(const adacluster_block_params* p, size_t* bytes /* host; may be 0, and ws NULL then */);
 int adacluster_cache_weights(const adacluster_block_params* p, const void* q, const int32_t* cu_q, const float* lse,

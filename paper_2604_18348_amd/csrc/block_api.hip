@@ -115,12 +115,15 @@ BlockDims unlisted(BlockDims m) {
 double scale_of(const adacluster_block_params* p) { return p->softmax_scale > 0.f ? p->softmax_scale : 1.0 / sqrt((double)p->d); }
 float log2_scale(const adacluster_block_params* p) { return (float)(scale_of(p) * 1.4426950408889634); }      // (rounded once: logits of 20 feel it)
 
+// rows of a head of keys: their numbers, and those of the rows past the last that its tile or stage goes on with, are 32 bits
+constexpr long long MOST_ROWS = (1ll << 31) - 1024;
+
 // what the shape of a call of prefix_attn follows from
 int prefix_args(const adacluster_block_params* p, int32_t groups, PrefixArgs* a) {
   if (int rc = check(p, &a->m)) return rc;
   if (!p->num_pages) return fail(ADACLUSTER_E_BADARG, "prefix_attn: num_pages must be >= 1 (a paged cache)");
   if (groups < 0 || groups > p->B) return fail(ADACLUSTER_E_BADSHAPE, "groups must be in [0,B] (groups=%d)", groups);
-  if ((long long)p->q_rows * a->m.G > INT32_MAX) return fail(ADACLUSTER_E_UNSUPPORTED, "prefix_attn: q_rows * Hq / Hkv must be below 2^31");
+  if ((long long)p->q_rows * a->m.G > MOST_ROWS) return fail(ADACLUSTER_E_UNSUPPORTED, "prefix_attn: q_rows * Hq / Hkv must be at most 2^31 - 1024");
   a->m = unlisted(a->m);
   a->gr.groups = groups;
   a->qs = two(p->q_stride); a->os = two(p->o_stride); a->ks = three(a->m, p->k_stride); a->vs = three(a->m, p->v_stride);
@@ -300,7 +303,7 @@ int adacluster_cache_weights(const adacluster_block_params* p, const void* q, co
   a.qs = two(p->q_stride); a.ks = three(a.m, p->k_stride);
   if (int rc = check_rows("q", q, p->dtype, a.qs)) return rc;
   if (int rc = check_pool(p, k_pool, k_pool, k_meta, k_meta, a.ks, a.ks)) return rc;
-  if ((long long)p->max_q * a.m.G > INT32_MAX) return fail(ADACLUSTER_E_UNSUPPORTED, "cache_weights: max_q * Hq / Hkv must be below 2^31");
+  if ((long long)p->max_q * a.m.G > MOST_ROWS) return fail(ADACLUSTER_E_UNSUPPORTED, "cache_weights: max_q * Hq / Hkv must be at most 2^31 - 1024");
   if (int rc = check_ws(ws, ws_bytes, cache_weights_bytes(p->dtype, p->bits, p->d, a.m, a.qs))) return rc;
   a.q = q; a.k = k_pool; a.km = k_meta; a.lse = lse; a.w = decay == 0.f ? nullptr : weights; a.out = new_weights;
   a.scale_log2e = log2_scale(p); a.decay = decay;
