@@ -197,6 +197,11 @@ __device__ __forceinline__ void store_frag(char* lds, int row, int quarter, cons
   for (int x = 0; x < (int)(D * sizeof(T) / 64); ++x) *(u32x4_t*)(lds + lds_piece<T, D>(row, 4 * x + quarter)) = f.p[x];
 }
 
+// What the rounding of x, y to `packed` (pack_bf16x2) leaves of them, rounded: up to 2^-8 of a value, off by up to 2^-16 of it.
+__device__ __forceinline__ uint32_t rounding_rest(float x, float y, uint32_t packed) {
+  return pack_bf16x2(x - __uint_as_float(packed << 16), y - __uint_as_float(packed & 0xFFFF0000u));
+}
+
 __device__ __forceinline__ void compiler_fence() { asm volatile("" ::: "memory"); }
 
 __device__ __forceinline__ float quarters_sum(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }

@@ -72,6 +72,7 @@ __device__ __forceinline__ void expand(RowFrag<T, D>& f, const Raw<T, BITS, D>& 
 // rounding of O.  With more rows it is rounded (an error of half a step of bfloat16 of each weight); with 4-bit values the weights
 // are multiplied by the steps of their keys first, and then rounded (in two parts 32 sequences over whole caches of up to 16 384 tokens
 // 132.7 -> 140.7 us, for values that are off by half a step of 4 bits as it is).
+// Parts of attention over shared prefixes have them in two parts whatever the rows and bits (block_prefix.hip).
 template <typename T, int BITS, int D> struct FewLds {
   static constexpr int VBYTES = 32 * D * sizeof(T), JBYTES = 4 * 16 * D * 4 + 4 * 16 * 2 * 4;
   static constexpr bool CODES = BITS == 4 && sizeof(T) == 2;
@@ -315,32 +316,38 @@ __device__ __forceinline__ void few_rows(const Args& a, int rts, int id, FewLds<
             // weights times steps, rounded here: what is taken off for the 128 has to be what the product adds.  8 more are taken off
             // and come back unrounded: the rounding then weighs codes about their middle, not from 0 up.
             const bf16x2_t one = {(__bf16)1.0f, (__bf16)1.0f};
-            union { uint32_t w[4]; bf16x2_t b[4]; bf16x8_t v; } u;
+            union { uint32_t w[4]; bf16x2_t b[4]; bf16x8_t v; } u, rest;
             float c = 0.f, back = corr[r][g];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
               const int h = x >> 1, j = 2 * (x & 1);
-              u.w[x] = pack_bf16x2(p[h][j] * vp[h][j][2 * g], p[h][j + 1] * vp[h][j + 1][2 * g]);
+              const float p0 = p[h][j] * vp[h][j][2 * g], p1 = p[h][j + 1] * vp[h][j + 1][2 * g];
+              u.w[x] = pack_bf16x2(p0, p1);
               c = __builtin_amdgcn_fdot2_f32_bf16(u.b[x], one, c, false);
+              if constexpr (PART) {
+                rest.w[x] = rounding_rest(p0, p1, u.w[x]);
+                c = __builtin_amdgcn_fdot2_f32_bf16(rest.b[x], one, c, false);
+              }
               back = fmaf(p[h][j + 1], vp[h][j + 1][2 * g + 1], fmaf(p[h][j], vp[h][j][2 * g + 1], back));
             }
             corr[r][g] = fmaf(-136.f, c, back);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) acc[r][4 * g + x] = mma_cols<D>(vl, 64 * g + 16 * x, lane, u.v, acc[r][4 * g + x]);
+            for (int x = 0; x < 4; ++x) {
+              if constexpr (PART) acc[r][4 * g + x] = mma_cols<D>(vl, 64 * g + 16 * x, lane, u.v, rest.v, acc[r][4 * g + x]);
+              else acc[r][4 * g + x] = mma_cols<D>(vl, 64 * g + 16 * x, lane, u.v, acc[r][4 * g + x]);
+            }
           }
         } else if constexpr (sizeof(T) == 2) {
           union { uint32_t w[4]; bf16x8_t v; } u{{pack_bf16x2(p[0][0], p[0][1]), pack_bf16x2(p[0][2], p[0][3]), pack_bf16x2(p[1][0], p[1][1]), pack_bf16x2(p[1][2], p[1][3])}};
           union { uint32_t w[4]; bf16x8_t v; } rest;
-          if constexpr (R == 1) {
+          constexpr bool TWO = PART || R == 1;
+          if constexpr (TWO) {
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const int h = x >> 1, j = 2 * (x & 1);
-              rest.w[x] = pack_bf16x2(p[h][j] - __uint_as_float(u.w[x] << 16), p[h][j + 1] - __uint_as_float(u.w[x] & 0xFFFF0000u));
-            }
+            for (int x = 0; x < 4; ++x) rest.w[x] = rounding_rest(p[x >> 1][2 * (x & 1)], p[x >> 1][2 * (x & 1) + 1], u.w[x]);
           }
 #pragma unroll
           for (int x = 0; x < ND; ++x) {
-            if constexpr (R == 1) acc[r][x] = mma_cols<D>(vl, 16 * x, lane, u.v, rest.v, acc[r][x]);
+            if constexpr (TWO) acc[r][x] = mma_cols<D>(vl, 16 * x, lane, u.v, rest.v, acc[r][x]);
             else acc[r][x] = mma_cols<D>(vl, 16 * x, lane, u.v, acc[r][x]);
           }
         } else {
