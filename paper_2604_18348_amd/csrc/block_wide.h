@@ -184,7 +184,8 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
       wait_vmcnt<0>();
       lds_barrier();
     } else {
-      for (int x = 1; x < STAGES - 1 && x < tiles; ++x) issue(x, x);
+      static_assert(STAGES == 3, "the waits below count the loads of one tile behind the present one");
+      if (tiles > 1) issue(1, 1);
     }
     int stage = 0;
     for (int t = 0; t < tiles; ++t) {
@@ -192,12 +193,11 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
         if (t + 1 < tiles) issue((t + 1) & 1, t + 1);
         stage = t & 1;
       } else {                                      // two tiles on their way: the prefix of one group waits for memory, not for products
-        if (STAGES > 3 && t + 2 < tiles) wait_vmcnt<4 * PT>();
-        else if (t + 1 < tiles) wait_vmcnt<2 * PT>();
+        if (t + 1 < tiles) wait_vmcnt<2 * PT>();
         else wait_vmcnt<0>();
         lds_barrier();
-        if (t) stage = stage == STAGES - 1 ? 0 : stage + 1;
-        if (t + STAGES - 1 < tiles) issue(stage == 0 ? STAGES - 1 : stage - 1, t + STAGES - 1);
+        if (t) stage = stage == 2 ? 0 : stage + 1;
+        if (t + 2 < tiles) issue(stage == 0 ? 2 : stage - 1, t + 2);
       }
       if (wave_has_rows) {
         const char* const kt = lds + stage * 2 * TILEB;
