@@ -72,7 +72,7 @@ __device__ __forceinline__ void expand(RowFrag<T, D>& f, const Raw<T, BITS, D>& 
 // rounding of O.  With more rows it is rounded (an error of half a step of bfloat16 of each weight); with 4-bit values the weights
 // are multiplied by the steps of their keys first, and then rounded (in two parts 32 sequences over whole caches of up to 16 384 tokens
 // 132.7 -> 140.7 us, for values that are off by half a step of 4 bits as it is).
-// Parts of attention over shared prefixes have them in two parts whatever the rows and bits (block_prefix.hip).
+// Attention over shared prefixes has them in two parts here, whatever the rows and bits (block_prefix.hip).
 template <typename T, int BITS, int D> struct FewLds {
   static constexpr int VBYTES = 32 * D * sizeof(T), JBYTES = 4 * 16 * D * 4 + 4 * 16 * 2 * 4;
   static constexpr bool CODES = BITS == 4 && sizeof(T) == 2;

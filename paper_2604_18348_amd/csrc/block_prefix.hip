@@ -8,7 +8,8 @@
 // Weights of 16-bit and 4-bit calls enter the product with V in two parts, their rounding to bfloat16 and the rounding of what that leaves (up to 2^-16 of
 // a weight): results are then off by their own rounding alone, 0.00166 relative to 64 bits, however many rows share the keys.  Rounded once they
 // are off by 0.0020 to 0.0023, and take (two parts -> one) 75 -> 71 us in the first call above, 161 -> 140 in the second, 36 -> 33.5 for 16 rows over 16 384
-// keys, 185 -> 157 for 16 sequences of up to 64 queries over 8 192, 4 bits 316 -> 266 and 88 -> 80 for 64 sequences in 4 groups over 8 192.
+// keys, 88 -> 80 for 64 sequences in 4 groups over 8 192 of 4 bits.  Blocks of 128 rows, chunks of a prompt, are rounded once, as by block_attn_wide: they
+// are bound by products (16 sequences of up to 64 queries over 8 192 keys 185 -> 157 us, 4 bits 316 -> 266).
 #include "block_few.h"
 #include "block_wide.h"
 
@@ -21,15 +22,15 @@ __global__ __launch_bounds__(256, (few_waves<T, BITS, D, R>())) void prefix_few(
   __shared__ FewLds<T, BITS, D> sh;
   few_rows<T, BITS, D, R, true>(a, 1, first + blockIdx.x, sh);
 }
-template <int D>
+template <int D, bool TWO>
 __global__ __launch_bounds__(256, 3) void prefix_wide(PrefixArgs a) {
   __shared__ WideLds<D, 4, true> sh;
-  wide_rows<D, 4, true>(a, 1, 1, sh);
+  wide_rows<D, 4, true, TWO>(a, 1, 1, sh);
 }
-template <int D, int NW>
+template <int D, int NW, bool TWO>
 __global__ __launch_bounds__(NW * 64, 2) void prefix_codes(PrefixArgs a) {
   __shared__ CodesLds<D, NW> sh;
-  wide_codes<D, NW>(a, sh);
+  wide_codes<D, NW, TWO>(a, sh);
 }
 
 // Joins a row's partial results: those of the pages its group shares, then those of its own.  D / 4 lanes read a result; `per` such
@@ -126,7 +127,7 @@ __global__ __launch_bounds__(256) void prefix_join(PrefixArgs a, int per) {
 
 // Which kernel, what it is given: fills a's shape.  `rows`, `trows`: of partial results.
 constexpr long long FAR = 1 << 25;                    // tokens this far apart: offsets inside a page pass 32 bits
-struct PrefixShape { bool wide; int R; size_t rows, trows; };
+struct PrefixShape { bool wide, two; int R; size_t rows, trows; };      // two: weights in two parts
 PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
   const BlockDims& m = a->m;
   PrefixShape s;
@@ -139,6 +140,7 @@ PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
   // and spread 32 KB of bfloat16 a tile: 32 rows over 16 384 keys 41 (62), over 2 048 28 (28), over 1 024 (d = 64) 19 (14); 16 rows over 4 096 26 (22).
   s.wide = dtype == ADACLUSTER_BF16 && (block > 16 || (bits ? rows > 16 && rows * keys > (1 << 16) : rows > 4)) &&
            (bits || (a->ks.token < FAR && a->vs.token < FAR));
+  s.two = block < 128;
   s.R = rows > 16 || block > 16 ? 2 : 1;
   a->TR = s.wide ? (bits && rows <= 64 && block <= 64 ? 64 : 128) : 16 * s.R;
   a->TT = s.wide ? (bits && block <= 16 ? 16 : bits ? a->TR : block > 32 ? 128 : 32) : 16 * s.R;
@@ -169,13 +171,17 @@ PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
 template <typename T, int BITS, int D>
 void go(hipStream_t st, const PrefixShape& s, int wg, const PrefixArgs& a) {
   if constexpr (sizeof(T) == 2 && BITS == 0) {
-    if (s.wide) { prefix_wide<D><<<wg, 256, 0, st>>>(a); return; }
+    if (s.wide) { if (s.two) prefix_wide<D, true><<<wg, 256, 0, st>>>(a); else prefix_wide<D, false><<<wg, 256, 0, st>>>(a); return; }
   }
   if constexpr (sizeof(T) == 2 && BITS == 4) {
     if (s.wide) {
       // a sequence's own few rows take codes straight into their products, in a launch of their own
       const int n = a.TT == 16 ? a.grid : wg;
-      if (n) { if (a.TR == 64) prefix_codes<D, 2><<<n, 128, 0, st>>>(a); else prefix_codes<D, 4><<<n, 256, 0, st>>>(a); }
+      if (n) {
+        if (a.TR == 64) prefix_codes<D, 2, true><<<n, 128, 0, st>>>(a);      // (blocks of 64 rows at most)
+        else if (s.two) prefix_codes<D, 4, true><<<n, 256, 0, st>>>(a);
+        else prefix_codes<D, 4, false><<<n, 256, 0, st>>>(a);
+      }
       if (wg > n) prefix_few<T, BITS, D, 1><<<wg - n, 256, 0, st>>>(a, n);
       return;
     }

@@ -79,8 +79,8 @@ template <int D, int NW, bool PART> struct WideLds {
   int2 pages_l[LIST];
   int32_t counts[NW];
 };
-// PART: a share of a group's or a sequence's pages (prefix_part.h), whose result is left as a partial one; weights in two parts (block_prefix.hip).
-template <int D, int NW, bool PART, typename Args>
+// PART: a share of a group's or a sequence's pages (prefix_part.h), whose result is left as a partial one.  TWO: weights in two parts (block_prefix.hip).
+template <int D, int NW, bool PART, bool TWO, typename Args>
 __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, WideLds<D, NW, PART>& sh) {
   constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, CH = D / 8, ROWB = D * 2;
   constexpr int TK = 32, PARTS = TK / 16;      // keys a tile: one product's rows
@@ -221,7 +221,7 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
         // p = 2^((s - reference) scale): any reference gives the same result as long as nothing overflows.  The row sum of the tile
         // tells (on the first tile with a score above -inf it is infinite): only then is the tile's maximum taken, the reference
         // moved up to it and the accumulator scaled.
-        bf16x8_t pf[2], rest[2];                      // weights, and PART: what their rounding leaves
+        bf16x8_t pf[2], rest[2];                      // weights, and TWO: what their rounding leaves
         float rsum;
         auto weights = [&]() __attribute__((always_inline)) {
           const float off = mref * sc;
@@ -234,12 +234,12 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
             for (int j = 0; j < 4; ++j) {
               const float p0 = __builtin_amdgcn_exp2f(fmaf(sacc[8 * s2 + 2 * j], sc, -off)), p1 = __builtin_amdgcn_exp2f(fmaf(sacc[8 * s2 + 2 * j + 1], sc, -off));
               u.w[j] = pack_bf16x2(p0, p1);
-              if constexpr (PART) r.w[j] = rounding_rest(p0, p1, u.w[j]);
+              if constexpr (TWO) r.w[j] = rounding_rest(p0, p1, u.w[j]);
               part[s2] += p0;                       // (not the rounded ones: the sum's logarithm is an output)
               part[s2] += p1;
             }
             pf[s2] = u.v;
-            if constexpr (PART) rest[s2] = r.v;
+            if constexpr (TWO) rest[s2] = r.v;
           }
           rsum = part[0] + part[1];
         };
@@ -263,7 +263,7 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
 #pragma unroll
           for (int db = 0; db < DB; ++db) {
             const bf16x8_t cols = join_tr(read_tr(p + vaddr[db][0]), read_tr(p + vaddr[db][1]));
-            if constexpr (PART) oacc[db] = mfma32(cols, rest[s2], oacc[db]);
+            if constexpr (TWO) oacc[db] = mfma32(cols, rest[s2], oacc[db]);
             oacc[db] = mfma32(cols, pf[s2], oacc[db]);
           }
         }
@@ -300,7 +300,8 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
 // The same walk over 4-bit pages, for parts.  A tile's codes come two tiles ahead into registers and go to LDS as bfloat16: those
 // of keys by themselves, those of values less 8.  Per group g of 64 dimensions
 //   scores   sum of step_g (c . q) + low_g sum q, scaled: the latter one more product, of (low, low, low) with three bfloat16 parts of sum q;
-//   values   weights times step_g, in two bfloat16 parts, times c - 8, and the sum of weights times low_g + 8 step_g, unrounded.
+//   values   weights times step_g, in two bfloat16 parts or rounded to one (it weighs codes about their middle), times c - 8, and the sum of
+//            weights times low_g + 8 step_g, unrounded.
 // Steps are applied to 16 keys a lane, which reads them from LDS (24 of 48 wide reads a tile).  No unit is full: vector arithmetic, most of it
 // from codes to bfloat16, has half of the cycles, LDS a quarter, the matrix cores an eighth; each tile ends at a barrier, and a wave waits 40 % of its
 // time.  128 rows over 16 384 keys of 8 heads, d = 128, with the rows' own keys: 94 us by the kernel for few rows, 48 staged and 20 for the latter.
@@ -313,7 +314,7 @@ template <int D, int NW> struct CodesLds {
   int2 pages_l[LIST];
   int32_t counts[NW];
 };
-template <int D, int NW>
+template <int D, int NW, bool TWO>
 __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, NW>& sh) {
   constexpr int NT = NW * 64, KS = D / 16, DB = D / 32, NG = D / 64, ROWB = D * 2, WORDS = D / 8;      // words of eight codes a row
   constexpr int TK = 32, PT = TK * WORDS / NT, TILEB = TK * ROWB;
@@ -511,13 +512,13 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, NW>&
               for (int j = 0; j < 2; ++j) {
                 const float p0 = p[v0 + 2 * j] * step[2 * j], p1 = p[v0 + 2 * j + 1] * step[2 * j + 1];
                 u.w[2 * z + j] = pack_bf16x2(p0, p1);
-                r.w[2 * z + j] = rounding_rest(p0, p1, u.w[2 * z + j]);
+                if constexpr (TWO) r.w[2 * z + j] = rounding_rest(p0, p1, u.w[2 * z + j]);
               }
 #pragma unroll
               for (int j = 0; j < 4; ++j) corr[x] = fmaf(p[v0 + j], low[j], corr[x]);
             }
             pf[s2] = u.v;
-            rest[s2] = r.v;
+            if constexpr (TWO) rest[s2] = r.v;
           }
 #pragma unroll
           for (int s2 = 0; s2 < 2; ++s2) {
@@ -525,7 +526,7 @@ __device__ __forceinline__ void wide_codes(const PrefixArgs& a, CodesLds<D, NW>&
 #pragma unroll
             for (int db = 2 * x; db < 2 * x + 2; ++db) {
               const bf16x8_t cols = join_tr(read_tr(q + vaddr[db][0]), read_tr(q + vaddr[db][1]));
-              oacc[db] = mfma32(cols, rest[s2], oacc[db]);
+              if constexpr (TWO) oacc[db] = mfma32(cols, rest[s2], oacc[db]);
               oacc[db] = mfma32(cols, pf[s2], oacc[db]);
             }
           }

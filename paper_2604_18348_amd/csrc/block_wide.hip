@@ -8,7 +8,7 @@ namespace {
 template <int D, int NW>
 __global__ __launch_bounds__(NW * 64, NW == 4 ? 3 : 2) void block_attn_wide(BlockAttnArgs a, int rts, int split) {
   __shared__ WideLds<D, NW, false> sh;
-  wide_rows<D, NW, false>(a, rts, split, sh);
+  wide_rows<D, NW, false, false>(a, rts, split, sh);
 }
 
 }  // namespace
