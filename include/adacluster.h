@@ -405,6 +405,10 @@ int adacluster_block_attn_backward(const adacluster_block_params* p, const void*
  *     at.  Positions behind them are every sequence's own.
  * Everything else is as in adacluster_block_attn (a query sees positions up to its own if causal; empty rows, range, layout), in the
  * same workspace rules: adacluster_prefix_workspace_bytes.  topk, qblock and keep_first are not used.  lse may be NULL.
+ * It is the faster call where many rows share many keys and a sequence has few new tokens (steps of generation, drafts, chunks of a hundred
+ * tokens).  Every row leaves an fp32 partial result of the shared keys, and at least one of its sequence's own, in the workspace
+ * (8 * Hq * (d + 2) bytes a query and more): for long chunks adacluster_block_attn takes less time and no workspace.  It is also the call for prefixes
+ * that are a small part of the keys; over a thousand keys the two are alike.
  * q_rows * Hq / Hkv must be at most 2^31 - 1024.  cu_group that does not ascend: results are unspecified, no access is out of bounds.
  */
 int adacluster_prefix_workspace_bytes(const adacluster_block_params* p, int32_t groups, size_t* bytes /* host */);

@@ -2,13 +2,13 @@
 // at once, every sequence's rows its own pages behind them, both in one launch; then a row's partial results are joined.
 //   o = sum_z 2^(m_z - m) o_z / sum_z 2^(m_z - m) l_z,  m = max_z m_z: every part z leaves o_z unnormalised, l_z and m_z, in fp32.
 // Bound by the pages' bytes as long as a group has few hundred rows (one token of 32 sequences, 16 384 shared keys and up to 1 616 own, 32 / 8 heads, d = 128:
-// 61 us for 176 MB and 25 MB of partial results, 3.3 TB/s; 83 by the kernel for few rows), then by what lies between the walk's products (128 sequences,
-// 32 768 shared keys, 4 heads of keys: 126 us, 0.55 PFLOP/s, matrix cores 30 % of the cycles, vector arithmetic 36 %; 307).
+// 66 us for 176 MB and 25 MB of partial results, 3.0 TB/s; 89 by the kernel for few rows), then by what lies between the walk's products (128 sequences,
+// 32 768 shared keys, 4 heads of keys: 141 us, 0.49 PFLOP/s, matrix cores 40 % of the cycles, vector arithmetic 42 %; 334).
 //
 // Weights of 16-bit and 4-bit calls enter the product with V in two parts, their rounding to bfloat16 and the rounding of what that leaves (up to 2^-16 of
 // a weight): results are then off by their own rounding alone, 0.00166 relative to 64 bits, however many rows share the keys.  Rounded once they
-// are off by 0.0020 to 0.0023, and take (two parts -> one) 75 -> 71 us in the first call above, 161 -> 140 in the second, 36 -> 33.5 for 16 rows over 16 384
-// keys, 88 -> 80 for 64 sequences in 4 groups over 8 192 of 4 bits.  Blocks of 128 rows, chunks of a prompt, are rounded once, as by block_attn_wide: they
+// are off by 0.0020 to 0.0023, and take (whole calls, two parts -> one) 75 -> 71 us in the first call above, 159 -> 140 in the second, 36 -> 33.5 for 16 rows
+// over 16 384 keys, 87 -> 80 for 64 sequences in 4 groups over 8 192 of 4 bits.  Blocks of 128 rows, chunks of a prompt, are rounded once, as by block_attn_wide: they
 // are bound by products (16 sequences of up to 64 queries over 8 192 keys 185 -> 157 us, 4 bits 316 -> 266).
 #include "block_few.h"
 #include "block_wide.h"
@@ -135,9 +135,9 @@ PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
   const int groups = a->gr.groups, block = m.qblock * m.G;
   const long long rows = groups ? (queries * m.G + groups - 1) / groups : block;      // of a group, on average
   const long long keys = (long long)m.max_pages << m.lpage;
-  // Tiles of 128 rows staged for four waves (d = 128, 8 heads of keys, before the join): 16 rows over 16 384 keys 27 us (42 by prefix_few), over 2 048 and
-  // 1 024 (d = 64) 16 and 9 (15, 10); 8 rows 26 (28); 8 groups of 4 rows over 8 192 61 (55).  4 bits need a second launch for the rows' own keys
-  // and spread 32 KB of bfloat16 a tile: 32 rows over 16 384 keys 41 (62), over 2 048 28 (28), over 1 024 (d = 64) 19 (14); 16 rows over 4 096 26 (22).
+  // Tiles of 128 rows staged for four waves (d = 128, 8 heads of keys, before the join): 16 rows over 16 384 keys 30 us (41 by prefix_few), over 2 048 and
+  // 1 024 (d = 64) 17 and 9 (15, 10); 8 rows 29 (28); 8 groups of 4 rows over 8 192 62 (54).  4 bits need a second launch for the rows' own keys
+  // and spread 32 KB of bfloat16 a tile: 32 rows over 16 384 keys 43 (64), over 2 048 28 (29), over 1 024 (d = 64) 19 (13); 16 rows over 4 096 30 (22).
   s.wide = dtype == ADACLUSTER_BF16 && (block > 16 || (bits ? rows > 16 && rows * keys > (1 << 16) : rows > 4)) &&
            (bits || (a->ks.token < FAR && a->vs.token < FAR));
   s.two = block < 128;
@@ -152,6 +152,7 @@ PrefixShape shape_of(int dtype, int bits, PrefixArgs* a) {
   // and 32 beside 16 384: 134 and 62 us; for two a CU 134 and 64, four 138 and 60, but 35 -> 41 for 16).  A share has four times as many keys as rows,
   // so that a partial result (four bytes a value) stays a quarter of what it is made of (128 rows over 16 384 keys: 43 us with 256 keys each, 36 with
   // 512), or 256; if that leaves CUs without one, as few as 128 (128 rows over 1 024 keys, d = 64: 21 -> 14 us; 64 over 4 096, d = 128: 27 -> 22).
+  // (Both sides measured with weights rounded once.)  Keys are counted by the width of page_table, which the host knows, not by the sequences.
   const int places = s.wide ? (bits ? 512 : 768) : s.R == 1 ? 512 : 256;
   const auto share = [&](long long items, int rows, int* least) {
     const long long most = rows > 64 ? 4 * rows : 256, fill = keys * items / 256;

@@ -8,9 +8,9 @@ namespace {
 // w_j = decay w_j + sum over the rows r that see key j of 2^(scale log2(e) q_r . k_j - log2(e) lse_r): lse is the logarithm of the row's sum, so
 // no maximum runs along.  No two workgroups add to a weight, and a call repeats bit for bit.
 //
-// Few rows: bound by the keys' bytes (one token of 32 sequences up to 16 384, 8 heads, d = 128: 171 us, 4.9 TB/s).  A wave has H sixteens of keys a
+// Few rows: bound by the keys' bytes (one token of 32 sequences up to 16 384, 8 heads, d = 128: 173 us, 4.9 TB/s).  A wave has H sixteens of keys a
 // turn, the next turn's on their way, and 16 rows at a time; a result tile holds in a lane one key and four rows, so that a key's step and
-// lowest value, its sum and its weight are one lane's (4 bits, the same call: 256 us with a lane's four keys and one row, 94 so, bound by what
+// lowest value, its sum and its weight are one lane's (4 bits, the same call: 256 us with a lane's four keys and one row, 93 so, bound by what
 // becomes of a code).
 //
 // 4 bits, bf16: a code c enters as the bfloat16 16 + c (0x4180 | c << 3: exact), which leaves the dimensions of a word of eight in the
@@ -191,12 +191,13 @@ __global__ __launch_bounds__(256, D == 128 && sizeof(T) == 4 ? 2 : 4) void cache
 // once: for a wave's 64 weights an exponential (8 cycles of a SIMD), a multiply-add and an addition (4 each) beside 16 of the product at
 // d = 128; of the cycles the matrix cores have 44 %, the vector units 64 %, at the 1.8 GHz that the power limit leaves.  Chunks of 2 x 1 024
 // tokens, 32 / 8 heads, up to 16 384 keys: 1 048 us by 16 x 16 products without stages, 352 staged, 305 with a tile's products in turn with
-// the weights of the one before.
+// the weights of the one before (each in its first twenty calls; call after call the last one takes 273).
 //
 // 4 bits: a code c is a bfloat16 by itself.  Per group g of 64 dimensions x_g = c . q, and score = sum over g of step_g x_g + low_g sum_g q.
 // The latter, scaled, less the row's log2(e) lse is one more product, of (low, low, low, .., -1, -1, -1) with three bfloat16 parts (24 bits) of every
 // factor, which weights_sums has left: what remains is two multiplications, the exponential and an addition (64 tokens of 4 sequences up to 32 768:
-// 214 us a step and lowest value a weight, 108 so, with a chunk's codes loaded a chunk ahead, 104 with its sums over the lanes in registers).
+// 214 us a step and lowest value a weight, 108 so, with a chunk's codes loaded a chunk ahead, 104 with its sums over the lanes in registers; call after
+// call 93).
 
 // 32 bytes a row and head: the sums of q over 64 dimensions, times scale log2(e), in three parts each, for the lanes below 32, and log2(e) lse
 // in three parts for the others, which meet -1.
@@ -620,7 +621,7 @@ int launch_cache_weights(hipStream_t s, int dtype, int bits, int d, WeightsArgs 
     if (sh.nsplit > 1) weights_join<<<(int)((heads * ((long long)a.m.max_pages << a.m.lpage) / 4 + 255) / 256), 256, 0, s>>>(a);
     return launched();
   }
-  // four workgroups a CU in all, which take a head's keys in turns (one token of 32 sequences up to 16 384: 177 us; two a CU 210, eight 178)
+  // four workgroups a CU in all, which take a head's keys in turns (one token of 32 sequences up to 16 384: two a CU take 1.19 of the time, eight as long)
   const int chunk = 64 * KEY_TILES, chunks = (int)((((long long)a.m.max_pages << a.m.lpage) + chunk - 1) / chunk);
   const long long heads = (long long)a.m.Hkv * a.m.B, most = (1024 + heads - 1) / heads;
   const int items = (int)(most < chunks ? most : chunks);

@@ -303,9 +303,9 @@ __device__ __forceinline__ void wide_rows(const Args& a, int rts, int split, Wid
 //   values   weights times step_g, in two bfloat16 parts or rounded to one (it weighs codes about their middle), times c - 8, and the sum of
 //            weights times low_g + 8 step_g, unrounded.
 // Steps are applied to 16 keys a lane, which reads them from LDS (24 of 48 wide reads a tile).  No unit is full: vector arithmetic, most of it
-// from codes to bfloat16, has half of the cycles, LDS a quarter, the matrix cores an eighth; each tile ends at a barrier, and a wave waits 40 % of its
-// time.  128 rows over 16 384 keys of 8 heads, d = 128, with the rows' own keys: 94 us by the kernel for few rows, 48 staged and 20 for the latter.
-// Two waves a workgroup, 64 rows, where no more are there: 64 sequences in 4 groups over 8 192 keys 66 -> 52 us.
+// from codes to bfloat16, has half of the cycles, LDS a quarter, the matrix cores a sixth; each tile ends at a barrier, and a wave waits 40 % of its
+// time.  128 rows over 16 384 keys of 8 heads, d = 128, with the rows' own keys: 100 us by the kernel for few rows, 53 staged and 20 for the latter.
+// Two waves a workgroup, 64 rows, where no more are there: 64 sequences in 4 groups over 8 192 keys 66 -> 52 us (weights rounded once; 55 in two parts).
 template <int D, int NW> struct CodesLds {
   static constexpr int TK = 32, NG = D / 64, TILEB = TK * D * 2;
   __align__(16) char lds[4 * TILEB];
